@@ -374,6 +374,64 @@ hq_status hq_conv2d_direct(const void* x, hq_dtype xdt, const float* w, const fl
 hq_status hq_attention(const void* qkv, int64_t Nb, int64_t L, int64_t C, int heads, void* out, int32_t* dev_status,
                        void* stream);
 
+/* ---- A transformer block's attention in training: the norm of queries and keys with the position rotation, attention that keeps
+ * the statistic its gradient needs, and both gradients (no counterpart in the paper's equations; its training differentiates the
+ * network around the quantized layers).  Matrices are [rows][ld] with the heads side by side (head h at columns h*dh ..), so that the
+ * thirds of a fused QKV projection are passed in place: q, q + heads*dh, q + (heads + kv_heads)*dh with one pitch.  Query head h
+ * uses key head h / (heads / kv_heads).  dh: a multiple of 8 up to 128.  Base pointers 16-byte aligned, pitches multiples of 16
+ * bytes.  Outputs may not overlap inputs, except where said. ----------------------------------------------------------------------
+ *
+ * hq_qk_norm_rope: per row and head y = x / sqrt(mean(x^2) + eps) * gamma, then the rotation of the first `rot` channels (even, <= dh;
+ *   0: none): pairs (j, j + rot/2), or (2j, 2j + 1) when interleaved != 0, become (a c_j - b s_j, b c_j + a s_j).
+ *   q, q_out   device [rows] x heads heads, fp32 or bf16 (xdt); k, k_out [rows] x kv_heads heads of the same type, or NULL with
+ *              kv_heads 0 (queries only; keys of another length take a call of their own as `q`).  q_out may be q, k_out may be k.
+ *   gamma_q, gamma_k   device fp32 [dh], or NULL (1).
+ *   cos, sin   device fp32 [npos][rot/2]; positions device int32 [rows], the table row of each token (clamped to the table), or
+ *              NULL: token r takes row r mod npos (samples of npos tokens).
+ * hq_qk_norm_rope_bwd: dq, dk from dq_out, dk_out and the inputs q, k of the forward call; dgamma_q, dgamma_k (device fp32 [dh],
+ *   NULL: not wanted) are sums over all rows and heads, taken in a fixed order (the same bits on every run).
+ *   dq may be dq_out or q, dk may be dk_out or k.  workspace: hq_qk_norm_rope_bwd_workspace_size bytes, 4-byte aligned; not needed
+ *   (NULL) where neither dgamma is wanted. */
+hq_status hq_qk_norm_rope(const void* q, int64_t ldq, const void* k, int64_t ldk, hq_dtype xdt, int64_t rows, int heads, int kv_heads,
+                          int dh, const float* gamma_q, const float* gamma_k, float eps, const float* cos, const float* sin,
+                          int64_t npos, int rot, const int32_t* positions, int interleaved, void* q_out, int64_t ldq_out, void* k_out,
+                          int64_t ldk_out, void* stream);
+hq_status hq_qk_norm_rope_bwd_workspace_size(int64_t rows, int heads, int kv_heads, int dh, size_t* bytes);
+hq_status hq_qk_norm_rope_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, hq_dtype xdt, int64_t rows, int heads,
+                              int kv_heads, int dh, const float* gamma_q, const float* gamma_k, float eps, const float* cos,
+                              const float* sin, int64_t npos, int rot, const int32_t* positions, int interleaved,
+                              const void* dq_out, int64_t lddq_out, const void* dk_out, int64_t lddk_out, void* dq, int64_t lddq,
+                              void* dk, int64_t lddk, float* dgamma_q, float* dgamma_k, void* workspace, size_t ws_bytes,
+                              void* stream);
+
+/* hq_attention_fwd: out[i] = sum_j softmax_j(scale q_i . k_j) v_j over the keys j that query i sees, lse[i] = log sum_j exp(scale q_i . k_j).
+ *   q, out     device bf16 [Nb*Lq] x heads heads; k, v [Nb*Lk] x kv_heads heads; lse device fp32 [Nb][heads][Lq].
+ *   q_lens, k_lens   device int32 [Nb], or NULL (Lq, Lk): queries and keys of sample n that are there (values are clamped to
+ *              0 .. L).  Rows behind them are never part of a result, whatever they hold.
+ *   causal     != 0: query i sees keys j <= i + k_len - q_len (the last query sees every key).
+ *   A query that sees no key, and one behind its sample's length: out = 0, lse = -infinity.
+ *   scale      positive and finite.  bf16 operands on the tensor cores, fp32 accumulation and softmax; the weights are rounded to
+ *              bf16 before they multiply the values.
+ *   workspace  hq_attention_fwd_workspace_size bytes, 16-byte aligned (NULL where that is 0).
+ * hq_attention_bwd: the gradients dq, dk, dv of the same call from dout, its inputs and its results out and lse:
+ *   P = exp(scale q k^T - lse), dS = P o (dout v^T - rowsum(dout o out)), dq = scale dS k, dk = scale dS^T q, dv = P^T dout, the last
+ *   two summed over the heads that share k and v.  P and dS are rounded to bf16 before they enter the second products.
+ *   Every sum runs in a fixed order: the same inputs give the same bits.  Rows behind the lengths, and of queries that see no key: zeros.
+ *   dq, dk, dv  device bf16, laid out as q, k, v with pitches of their own.
+ *   workspace  hq_attention_bwd_workspace_size bytes, 16-byte aligned; it need not be cleared, and calls that may overlap on the GPU
+ *              (other streams, captured graphs that run side by side) need one each. */
+hq_status hq_attention_fwd_workspace_size(int64_t Nb, int64_t Lq, int64_t Lk, int heads, int kv_heads, int dh, size_t* bytes);
+hq_status hq_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int64_t Nb, int64_t Lq,
+                           int64_t Lk, int heads, int kv_heads, int dh, float scale, int causal, const int32_t* q_lens,
+                           const int32_t* k_lens, void* out, int64_t ldo, float* lse, void* workspace, size_t ws_bytes,
+                           int32_t* dev_status, void* stream);
+hq_status hq_attention_bwd_workspace_size(int64_t Nb, int64_t Lq, int64_t Lk, int heads, int kv_heads, int dh, size_t* bytes);
+hq_status hq_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* out,
+                           int64_t ldo, const float* lse, const void* dout, int64_t lddo, int64_t Nb, int64_t Lq, int64_t Lk, int heads,
+                           int kv_heads, int dh, float scale, int causal, const int32_t* q_lens, const int32_t* k_lens, void* dq,
+                           int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv, void* workspace, size_t ws_bytes,
+                           int32_t* dev_status, void* stream);
+
 /* ---- Fused linear layer that allocates nothing and takes no workspace (the paper has no counterpart: this is a
  * packaging of hq_qlinear for a particular kind of caller, not another operation). ---------------------------------
  * Who it is for: code that must not, or cannot, obtain device memory at the moment it runs a layer -- an inference

@@ -15,6 +15,7 @@
 
 #include "hq_common.cuh"
 #include "hq_fwht.cuh"
+#include "hq_mma_bf16.cuh"
 
 namespace hq {
 // hq_gemm.cu: bf16 [rows][cols] with a row pitch, boxes of box_rows x 64 columns in the 128-byte swizzle
@@ -36,54 +37,6 @@ struct AttnParams {
     float scale_log2;            // log2(e) / sqrt(dh)
     int32_t* dev_status;
 };
-
-// Shared-memory matrix descriptor without swizzle: 8 x 16-byte core matrices; `lbo` / `sbo` are the byte distances between
-// core matrices along K and along M/N for a K-major operand, and along K and along N (groups of 8) for an MN-major one.
-__device__ __forceinline__ uint64_t make_desc_noswizzle(uint32_t smem_addr, uint32_t lbo, uint32_t sbo) {
-    uint64_t d = 0;
-    d |= uint64_t((smem_addr & 0x3FFFFu) >> 4);
-    d |= uint64_t((lbo >> 4) & 0x3FFFu) << 16;
-    d |= uint64_t((sbo >> 4) & 0x3FFFu) << 32;
-    d |= uint64_t(1) << 46;
-    return d;
-}
-
-// Instruction descriptor for kind::f16 with bf16 operands and an fp32 accumulator, tile M x N; B MN-major when asked.
-__host__ __device__ constexpr uint32_t make_idesc_bf16(int M, int N, bool b_mn_major) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn_major ? (1u << 16) : 0u) | (uint32_t(N >> 3) << 17) |
-           (uint32_t(M >> 4) << 24);
-}
-
-__device__ __forceinline__ void mma_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                         uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-
-__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
-}
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<uint32_t*>(&h);
-}
 
 // Copies `rows_valid` rows (of 128) x DH bf16 from global memory (row pitch `pitch` elements) into the canonical
 // core-matrix layout: the 16-byte piece (row, v) lands at (row / 8) * group_stride + v * 128 + (row % 8) * 16.  Rows beyond
@@ -316,16 +269,6 @@ __global__ void __launch_bounds__(128, (DH <= 64 ? 4 : 2)) attention_kernel(cons
 // weights then stay below 2^8 (exact in bf16's range), the normalisation by the row sum at the end is unchanged, and
 // the read-modify-write of the output accumulator in tensor memory is almost never needed after the first block.
 constexpr int32_t kStatusAttnTma = 0x601;
-
-__device__ __forceinline__ uint64_t make_sw128_mnmajor_desc(uint32_t smem_addr, uint32_t atom_stride_bytes) {
-    uint64_t d = 0;
-    d |= uint64_t((smem_addr & 0x3FFFFu) >> 4);
-    d |= uint64_t((atom_stride_bytes >> 4) & 0x3FFFu) << 16;   // between 64-element groups along N
-    d |= uint64_t(1024 >> 4) << 32;                            // between 8-row groups along K
-    d |= uint64_t(1) << 46;
-    d |= uint64_t(2) << 61;
-    return d;
-}
 
 // Warps 0-3 do the softmax, thread t the row t of the tile; one lane of warp 4 issues every load and product, so that no softmax
 // warp waits for its own instruction issue.  The S columns are free as soon as the four warps hold block j's scores in registers:

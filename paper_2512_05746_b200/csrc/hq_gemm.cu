@@ -179,6 +179,19 @@ bool encode_2d_bf16_sw128(CUtensorMap* tm, const void* base, uint64_t cols, uint
     });
 }
 
+bool encode_heads_bf16(CUtensorMap* tm, const void* base, uint64_t dh, uint64_t heads, uint64_t rows, uint64_t batch, uint64_t pitch,
+                       uint32_t box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (fn == nullptr) return false;
+    cuuint64_t dims[4] = {dh, heads, rows, batch};
+    cuuint64_t strides[3] = {dh * 2, pitch * 2, rows * pitch * 2};
+    cuuint32_t box[4] = {64, 1, box_rows, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Output tensor map for the epilogue's bulk stores: bf16 [rows][N] with pitch ldy, boxes of 32 rows x 32 columns
 // in the 64-byte swizzle the staging buffers are written in.
 bool encode_y(CUtensorMap* tm, const void* y, uint64_t N, uint64_t rows, uint64_t ldy) {

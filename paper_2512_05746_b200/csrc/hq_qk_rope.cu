@@ -1,0 +1,316 @@
+// The norm of queries and keys for each head with the position rotation in the same pass, and its gradient: what stands between the
+// QKV projection of a transformer block and its attention.
+//
+//   y = x / sqrt(mean(x^2) + eps) * gamma          over the dh channels of one head (gamma [dh], shared by the heads)
+//   (a, b) -> (a c - b s, b c + a s)               for the pairs of the first `rot` channels; c, s: the table row of the token
+//
+// Gradient, with u = the rotation's transpose applied to the output's gradient, xh = x / sqrt(mean(x^2) + eps):
+//   dx = (gamma u - xh mean(gamma u xh)) / sqrt(mean(x^2) + eps),     dgamma = sum over rows and heads of u xh
+//
+// Memory-bound: every value is read and written once, tables and gamma come from the caches.  A group of dh / 8 lanes holds one head of
+// one row, 8 channels a lane (16 bytes of bf16), so that the row's sums are a few shuffles; 32 / (dh / 8) heads a warp.  Sums and
+// the rotation in fp32, one rounding at the end.
+#include "hq_common.cuh"
+
+namespace hq {
+namespace {
+
+struct RopeSide { const void* x; const void* g; void* out; int64_t ldx, ldg, ldo; const float* gamma; float* dgamma; int heads; };
+struct RopeParams {
+    RopeSide q, k;
+    int64_t rows;
+    int dh, rot;
+    const float *cos, *sin;                        // [npos][rot / 2]
+    const int32_t* positions;                      // [rows], or NULL: row % npos
+    int64_t npos;
+    float eps;
+    float* partial;                                // gradient of gamma: [2][blocks][dh]
+};
+constexpr int kRopeThreads = 256;
+constexpr int kRopeMaxBlocks = 1184;               // CTAs whose partial sums of gamma's gradient the workspace holds (148 SMs x 8)
+
+template <typename T> struct Vec8;
+template <> struct Vec8<__nv_bfloat16> {
+    uint4 w;
+    __device__ __forceinline__ void load(const void* base, int64_t at) { w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) + at); }
+    __device__ __forceinline__ void get(float (&f)[8]) const {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { f[2 * e] = __uint_as_float(u[e] << 16); f[2 * e + 1] = __uint_as_float(u[e] & 0xFFFF0000u); }
+    }
+    static __device__ __forceinline__ void store(void* base, int64_t at, const float (&f)[8]) {
+        uint32_t u[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+            u[e] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(base) + at) = make_uint4(u[0], u[1], u[2], u[3]);
+    }
+};
+template <> struct Vec8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const void* base, int64_t at) {
+        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
+        a = p[0]; b = p[1];
+    }
+    __device__ __forceinline__ void get(float (&f)[8]) const {
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    }
+    static __device__ __forceinline__ void store(void* base, int64_t at, const float (&f)[8]) {
+        float4* p = reinterpret_cast<float4*>(static_cast<float*>(base) + at);
+        p[0] = make_float4(f[0], f[1], f[2], f[3]); p[1] = make_float4(f[4], f[5], f[6], f[7]);
+    }
+};
+
+// Sum over the `v` lanes of a group, in every lane of it.
+__device__ __forceinline__ float group_sum(float x, int pos, int v, int base) {
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) {
+        const float o = __shfl_down_sync(0xffffffffu, x, off);
+        if (pos < off && pos + off < v) x += o;
+    }
+    return __shfl_sync(0xffffffffu, x, base);
+}
+
+enum RopePairs { kInterleaved = 0, kHalvesByLane = 1, kHalvesAny = 2 };
+
+// The rotation (SIGN 1) or its transpose (-1) of the 8 channels of each lane.  Halves whose distance rot / 2 is a multiple of 8
+// channels meet in another lane at the same place (shuffles); at other distances through `line`, the warp's 256 floats of shared memory.
+template <int PAIRS, int SIGN>
+__device__ __forceinline__ void rotate(float (&y)[8], const RopeParams& p, int64_t at, int pos, int base, int lane, float* line) {
+    const int half = p.rot >> 1, c0 = pos * 8;
+    const float *cs = p.cos + at * half, *sn = p.sin + at * half;
+    if (PAIRS == kInterleaved) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2)
+            if (c0 + e < p.rot) {
+                const float c = __ldg(cs + (c0 + e) / 2), s = SIGN * __ldg(sn + (c0 + e) / 2), a = y[e], b = y[e + 1];
+                y[e] = a * c - b * s;
+                y[e + 1] = b * c + a * s;
+            }
+    } else if (PAIRS == kHalvesByLane) {
+        const bool hi = c0 >= half;
+        const int step = half >> 3, other = c0 < p.rot ? (hi ? lane - step : lane + step) : lane, t0 = hi ? c0 - half : c0;
+        const float sign = hi ? float(SIGN) : float(-SIGN);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float o = __shfl_sync(0xffffffffu, y[e], other);
+            if (c0 < p.rot) y[e] = y[e] * __ldg(cs + t0 + e) + sign * o * __ldg(sn + t0 + e);
+        }
+    } else {
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) line[lane * 8 + e] = y[e];
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int c = c0 + e;
+            if (c < p.rot) {
+                const bool hi = c >= half;
+                const float o = line[base * 8 + (hi ? c - half : c + half)];
+                const int t = hi ? c - half : c;
+                y[e] = y[e] * __ldg(cs + t) + (hi ? float(SIGN) : float(-SIGN)) * o * __ldg(sn + t);
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ int64_t table_row(const RopeParams& p, int64_t row) {
+    if (p.positions == nullptr) return p.npos == p.rows ? row : row % p.npos;
+    return min(max(int64_t(__ldg(p.positions + row)), int64_t(0)), p.npos - 1);
+}
+
+// blockIdx.y: 0 queries, 1 keys.  GRAD: `g` is the output's gradient and `out` the input's.
+template <typename T, int PAIRS, bool GRAD>
+__global__ void __launch_bounds__(kRopeThreads) qk_rope_kernel(const RopeParams p) {
+    __shared__ float lines[GRAD || PAIRS == kHalvesAny ? kRopeThreads * 8 : 1];
+    const RopeSide& s = blockIdx.y == 0 ? p.q : p.k;
+    const int v = p.dh / 8, per_warp = 32 / v, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // lanes left over (32 no multiple of v) stand behind a head's last channel
+    const int sub = lane / v, pos = sub < per_warp ? lane - sub * v : v, base = sub < per_warp ? sub * v : 0;
+    const int64_t items = p.rows * s.heads;
+    float* line = lines + (PAIRS == kHalvesAny ? warp * 256 : 0);
+    float gamma[8], dgamma[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { gamma[e] = s.gamma != nullptr && pos < v ? __ldg(s.gamma + pos * 8 + e) : 1.0f; dgamma[e] = 0.f; }
+    for (int64_t i0 = (int64_t(blockIdx.x) * (kRopeThreads / 32) + warp) * per_warp; i0 < items; i0 += int64_t(gridDim.x) * (kRopeThreads / 32) * per_warp) {
+        const int64_t item = i0 + sub;
+        const bool mine = pos < v && item < items;
+        const int64_t row = mine ? item / s.heads : 0;
+        const int64_t c = (mine ? item - row * s.heads : 0) * p.dh + (mine ? pos : 0) * 8;
+        const int64_t at = table_row(p, row);
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        Vec8<T> in;
+        if (mine) { in.load(s.x, row * s.ldx + c); in.get(x); }
+        float sq = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sq = fmaf(x[e], x[e], sq);
+        if (!GRAD) {
+            const float inv = rsqrtf(group_sum(sq, pos, v, base) / float(p.dh) + p.eps);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * gamma[e];
+            rotate<PAIRS, 1>(x, p, at, pos, base, lane, line);
+            if (mine) Vec8<T>::store(s.out, row * s.ldo + c, x);
+        } else {
+            float u[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (mine) { in.load(s.g, row * s.ldg + c); in.get(u); }
+            rotate<PAIRS, -1>(u, p, at, pos, base, lane, line);
+            float dot = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot = fmaf(gamma[e] * u[e], x[e], dot);
+            const float inv = rsqrtf(group_sum(sq, pos, v, base) / float(p.dh) + p.eps);
+            const float mean = group_sum(dot, pos, v, base) / float(p.dh) * inv;             // of gamma u xh
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float xh = x[e] * inv;
+                if (mine) dgamma[e] = fmaf(u[e], xh, dgamma[e]);
+                x[e] = inv * (gamma[e] * u[e] - xh * mean);
+            }
+            if (mine) Vec8<T>::store(s.out, row * s.ldo + c, x);
+        }
+    }
+    if (GRAD && s.dgamma != nullptr) {
+        // the CTA's share: lanes of the same place in a head, in a fixed order
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) lines[threadIdx.x * 8 + e] = dgamma[e];
+        __syncthreads();
+        if (int(threadIdx.x) < p.dh) {
+            float sum = 0.f;
+            for (int w = 0; w < kRopeThreads / 32; ++w)
+                for (int g = 0; g < per_warp; ++g) sum += lines[w * 256 + g * p.dh + threadIdx.x];
+            p.partial[(int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * p.dh + threadIdx.x] = sum;
+        }
+    }
+}
+
+// gamma's gradient from the CTAs' shares: one CTA for queries and one for keys, thread = (channel, every so-many-th share)
+__global__ void __launch_bounds__(1024) qk_rope_gamma_kernel(const RopeParams p, int blocks) {
+    __shared__ float sums[1024];
+    const RopeSide& s = blockIdx.x == 0 ? p.q : p.k;
+    if (s.dgamma == nullptr) return;
+    const int ways = 1024 / p.dh, way = threadIdx.x / p.dh, c = threadIdx.x - way * p.dh;
+    float sum = 0.f;
+    if (way < ways)
+        for (int b = way; b < blocks; b += ways) sum += p.partial[(int64_t(blockIdx.x) * blocks + b) * p.dh + c];
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    if (int(threadIdx.x) < p.dh) {
+        float total = 0.f;
+        for (int w = 0; w < ways; ++w) total += sums[w * p.dh + threadIdx.x];
+        s.dgamma[threadIdx.x] = total;
+    }
+}
+
+template <typename T, bool GRAD>
+hq_status launch_pairs(const RopeParams& p, int pairs, dim3 grid, cudaStream_t st) {
+    if (pairs == kInterleaved) qk_rope_kernel<T, kInterleaved, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
+    else if (pairs == kHalvesByLane) qk_rope_kernel<T, kHalvesByLane, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
+    else qk_rope_kernel<T, kHalvesAny, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
+    return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+}
+
+int rope_blocks(int64_t rows, int heads, int dh, bool grad) {
+    const int64_t per_cta = (kRopeThreads / 32) * (32 / (dh / 8));
+    int64_t blocks = (rows * heads + per_cta - 1) / per_cta;
+    const int64_t most = grad ? kRopeMaxBlocks : 1 << 20;
+    return int(blocks < most ? blocks : most);
+}
+
+hq_status check_matrix(const void* x, int64_t ld, int heads, int dh, hq_dtype dt) {
+    if (x == nullptr) return HQ_ERR_INVALID_ARG;
+    if (ld < int64_t(heads) * dh) return HQ_ERR_SHAPE;
+    if (!aligned16(x) || (ld * (dt == HQ_BF16 ? 2 : 4)) % 16 != 0) return HQ_ERR_ALIGNMENT;
+    return HQ_OK;
+}
+
+hq_status check_call(hq_dtype dt, int64_t rows, int heads, int kv_heads, int dh, const void* cos, const void* sin, int64_t npos, int rot, float eps) {
+    if (dt != HQ_F32 && dt != HQ_BF16) return HQ_ERR_INVALID_ARG;
+    if (rows < 0 || heads <= 0 || kv_heads < 0 || dh <= 0 || rot < 0 || rot > dh || rot % 2 != 0) return HQ_ERR_SHAPE;
+    if (dh % 8 != 0 || dh > 128 || heads > 65535 || kv_heads > 65535 || rows > 0x7fffffff) return HQ_ERR_UNSUPPORTED;
+    if (rot > 0 && (cos == nullptr || sin == nullptr)) return HQ_ERR_INVALID_ARG;
+    if (rot > 0 && npos <= 0) return HQ_ERR_SHAPE;
+    if (!(eps >= 0.f)) return HQ_ERR_INVALID_ARG;
+    return HQ_OK;
+}
+
+hq_status run(RopeParams p, hq_dtype dt, int interleaved, bool grad, cudaStream_t st) {
+    if (p.rot == 0) { p.npos = 1; p.positions = nullptr; }
+    const int pairs = interleaved || p.rot == 0 ? kInterleaved : (p.rot / 2) % 8 == 0 ? kHalvesByLane : kHalvesAny;
+    const int blocks = rope_blocks(p.rows, p.q.heads > p.k.heads ? p.q.heads : p.k.heads, p.dh, grad);
+    const dim3 grid(unsigned(blocks), p.k.heads > 0 ? 2u : 1u);
+    hq_status e;
+    if (grad) e = dt == HQ_BF16 ? launch_pairs<__nv_bfloat16, true>(p, pairs, grid, st) : launch_pairs<float, true>(p, pairs, grid, st);
+    else e = dt == HQ_BF16 ? launch_pairs<__nv_bfloat16, false>(p, pairs, grid, st) : launch_pairs<float, false>(p, pairs, grid, st);
+    if (e != HQ_OK || (p.q.dgamma == nullptr && p.k.dgamma == nullptr)) return e;
+    qk_rope_gamma_kernel<<<grid.y, 1024, 0, st>>>(p, blocks);
+    return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace hq
+
+extern "C" hq_status hq_qk_norm_rope(const void* q, int64_t ldq, const void* k, int64_t ldk, hq_dtype xdt, int64_t rows, int heads, int kv_heads,
+                                     int dh, const float* gamma_q, const float* gamma_k, float eps, const float* cos, const float* sin,
+                                     int64_t npos, int rot, const int32_t* positions, int interleaved, void* q_out, int64_t ldq_out, void* k_out,
+                                     int64_t ldk_out, void* stream) {
+    using namespace hq;
+    hq_status e = check_call(xdt, rows, heads, kv_heads, dh, cos, sin, npos, rot, eps);
+    if (e != HQ_OK) return e;
+    if (rows == 0) return HQ_OK;
+    if ((e = check_matrix(q, ldq, heads, dh, xdt)) != HQ_OK || (e = check_matrix(q_out, ldq_out, heads, dh, xdt)) != HQ_OK) return e;
+    if (kv_heads > 0 && ((e = check_matrix(k, ldk, kv_heads, dh, xdt)) != HQ_OK || (e = check_matrix(k_out, ldk_out, kv_heads, dh, xdt)) != HQ_OK)) return e;
+    RopeParams p{};
+    p.q = RopeSide{q, nullptr, q_out, ldq, 0, ldq_out, gamma_q, nullptr, heads};
+    p.k = RopeSide{k, nullptr, k_out, ldk, 0, ldk_out, gamma_k, nullptr, kv_heads};
+    p.rows = rows; p.dh = dh; p.rot = rot; p.cos = cos; p.sin = sin; p.positions = positions; p.npos = npos; p.eps = eps;
+    return run(p, xdt, interleaved, false, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" hq_status hq_qk_norm_rope_bwd_workspace_size(int64_t rows, int heads, int kv_heads, int dh, size_t* bytes) {
+    using namespace hq;
+    if (bytes == nullptr) return HQ_ERR_INVALID_ARG;
+    const hq_status e = check_call(HQ_BF16, rows, heads, kv_heads, dh, nullptr, nullptr, 1, 0, 0.f);
+    if (e != HQ_OK) return e;
+    *bytes = size_t(2) * rope_blocks(rows, heads > kv_heads ? heads : kv_heads, dh, true) * dh * sizeof(float);
+    return HQ_OK;
+}
+
+extern "C" hq_status hq_qk_norm_rope_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, hq_dtype xdt, int64_t rows, int heads,
+                                         int kv_heads, int dh, const float* gamma_q, const float* gamma_k, float eps, const float* cos,
+                                         const float* sin, int64_t npos, int rot, const int32_t* positions, int interleaved,
+                                         const void* dq_out, int64_t lddq_out, const void* dk_out, int64_t lddk_out, void* dq, int64_t lddq,
+                                         void* dk, int64_t lddk, float* dgamma_q, float* dgamma_k, void* workspace, size_t ws_bytes,
+                                         void* stream) {
+    using namespace hq;
+    hq_status e = check_call(xdt, rows, heads, kv_heads, dh, cos, sin, npos, rot, eps);
+    if (e != HQ_OK) return e;
+    if (kv_heads == 0 && dgamma_k != nullptr) return HQ_ERR_INVALID_ARG;
+    const bool sums = dgamma_q != nullptr || dgamma_k != nullptr;
+    if (rows == 0) {
+        cudaStream_t st = static_cast<cudaStream_t>(stream);
+        if (dgamma_q != nullptr) HQ_CUDA_OK(cudaMemsetAsync(dgamma_q, 0, dh * sizeof(float), st));
+        if (dgamma_k != nullptr) HQ_CUDA_OK(cudaMemsetAsync(dgamma_k, 0, dh * sizeof(float), st));
+        return HQ_OK;
+    }
+    if ((e = check_matrix(q, ldq, heads, dh, xdt)) != HQ_OK || (e = check_matrix(dq_out, lddq_out, heads, dh, xdt)) != HQ_OK ||
+        (e = check_matrix(dq, lddq, heads, dh, xdt)) != HQ_OK)
+        return e;
+    if (kv_heads > 0 && ((e = check_matrix(k, ldk, kv_heads, dh, xdt)) != HQ_OK || (e = check_matrix(dk_out, lddk_out, kv_heads, dh, xdt)) != HQ_OK ||
+                         (e = check_matrix(dk, lddk, kv_heads, dh, xdt)) != HQ_OK))
+        return e;
+    if (sums) {
+        size_t need = 0;
+        if (workspace == nullptr) return HQ_ERR_INVALID_ARG;
+        if ((reinterpret_cast<uintptr_t>(workspace) & 3u) != 0) return HQ_ERR_ALIGNMENT;
+        hq_qk_norm_rope_bwd_workspace_size(rows, heads, kv_heads, dh, &need);
+        if (ws_bytes < need) return HQ_ERR_WORKSPACE;
+    }
+    RopeParams p{};
+    p.q = RopeSide{q, dq_out, dq, ldq, lddq_out, lddq, gamma_q, dgamma_q, heads};
+    p.k = RopeSide{k, dk_out, dk, ldk, lddk_out, lddk, gamma_k, dgamma_k, kv_heads};
+    p.rows = rows; p.dh = dh; p.rot = rot; p.cos = cos; p.sin = sin; p.positions = positions; p.npos = npos; p.eps = eps;
+    p.partial = static_cast<float*>(workspace);
+    return run(p, xdt, interleaved, true, static_cast<cudaStream_t>(stream));
+}
