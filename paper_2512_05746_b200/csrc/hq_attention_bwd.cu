@@ -13,15 +13,16 @@
 // tensor memory (as operands of the second products they are read where they were written), no fp32 partial dq in memory and no
 // order of additions that changes from run to run.
 //
-// Warps 0-7: thread = lane, four warps per half of the 128 columns; warp 8 loads, warp 9 issues.  The tile a CTA keeps (K and V, or Q
-// and dout) stays in shared memory; pairs of the other side's tiles come through a ring of two.
+// Warps 0-15: thread = lane, four warps per quarter of the 128 columns; warp 16 loads, warp 17 issues.  The tile a CTA keeps (K and V,
+// or Q and dout) stays in shared memory; pairs of the other side's tiles come through a ring of two.
 #include "hq_attention_tile.cuh"
 
 namespace hq {
 namespace {
 
 constexpr int32_t kStatusBwdWait = 0x710, kStatusBwdTma = 0x711;
-constexpr int kBwdThreads = 320;
+constexpr int kBwdWarps = 16;                                  // of the probabilities
+constexpr int kBwdThreads = (kBwdWarps + 2) * 32;
 constexpr int kBwdStages = 2;
 constexpr uint32_t kStatBytes = 2 * kAttnTile * 4;             // per query tile: lse * log2(e) of 128 rows, then D of 128 rows
 template <int NH> constexpr size_t bwd_smem() { return size_t(2 + 2 * kBwdStages) * NH * kAttnPart + kBwdStages * kStatBytes + 1024; }
@@ -76,7 +77,7 @@ __device__ __forceinline__ void bwd_run(const CUtensorMap* tmA0, const CUtensorM
         return;
     }
 
-    if (warp == 8) {
+    if (warp == kBwdWarps) {
         if (elect_one()) {
             bool ok = true;
             int loads = 0;
@@ -104,7 +105,7 @@ __device__ __forceinline__ void bwd_run(const CUtensorMap* tmA0, const CUtensorM
             for (int i = max(0, loads - kBwdStages); i < loads; ++i) mbar_wait(&bar.full[i % kBwdStages], uint32_t(i / kBwdStages) & 1u, nullptr, 0);
         }
         __syncwarp();
-    } else if (warp == 9) {
+    } else if (warp == kBwdWarps + 1) {
         const uint32_t idesc_s = make_idesc_bf16(kAttnTile, kAttnTile, false);
         const uint32_t idesc_acc = make_idesc_bf16(kAttnTile, (s.dh + 15) & ~15, true);
         const int ksteps = (s.dh + 15) / 16;
@@ -135,12 +136,12 @@ __device__ __forceinline__ void bwd_run(const CUtensorMap* tmA0, const CUtensorM
             }
             mma_commit(done);
         };
-        // 64 columns of bf16 for each half of the 128: elements 0..63 at `column`, 64..127 at column + 64
+        // bf16 elements of each quarter in the first half of its 32 columns
         auto acc_product = [&](int i, int which, uint32_t column, uint32_t acc) {
             const uint64_t db = make_sw128_mnmajor_desc(smem_u32(stage_of(i) + which * kTile), kAttnPart);
 #pragma unroll
             for (int k = 0; k < kAttnTile / 16; ++k)
-                mma_bf16_ts(tmem_base + acc, tmem_base + column + uint32_t((k >> 2) * 64 + (k & 3) * 8), db + uint64_t(k * 128), idesc_acc,
+                mma_bf16_ts(tmem_base + acc, tmem_base + column + uint32_t((k >> 1) * 32 + (k & 1) * 8), db + uint64_t(k * 128), idesc_acc,
                             (i | k) != 0 ? 1u : 0u);
         };
         auto wait = [&](uint64_t* b, int i) { return __all_sync(0xffffffffu, mbar_wait(b, uint32_t(i) & 1u, p.dev_status, kStatusBwdWait)); };
@@ -201,10 +202,10 @@ __device__ __forceinline__ void bwd_run(const CUtensorMap* tmA0, const CUtensorM
             __syncwarp();
         }
     } else {
-        const int half = warp >> 2;                            // columns half * 64 ..
+        const int quarter = warp >> 2;                         // columns quarter * 32 ..
         const int lane_row = (warp & 3) * 32 + lane, r = row0 + lane_row;
         const uint32_t t_lane = tmem_base + (uint32_t((warp & 3) * 32) << 16);
-        const uint32_t t_s = t_lane + uint32_t(half * 64);
+        const uint32_t t_s = t_lane + uint32_t(quarter * 32);
         const float sc = s.scale_log2;
         bool ok = true;
         int b_tile = first;
@@ -218,27 +219,25 @@ __device__ __forceinline__ void bwd_run(const CUtensorMap* tmA0, const CUtensorM
         }
         for (int i = 0; i < total && ok; ++i) {
             const uint32_t par = uint32_t(i) & 1u;
-            const int c0 = b_tile * kAttnTile + half * 64;     // the first column's query or key
+            const int c0 = b_tile * kAttnTile + quarter * 32;  // the first column's query or key
             if (++b_tile == last) b_tile = first;
-            const float* stat = sStat + (i % kBwdStages) * 2 * kAttnTile + half * 64;
+            const float* stat = sStat + (i % kBwdStages) * 2 * kAttnTile + quarter * 32;
             if (KEYS) ok = mbar_wait(&bar.full[i % kBwdStages], uint32_t(i / kBwdStages) & 1u, p.dev_status, kStatusBwdTma);
             ok = __all_sync(0xffffffffu, ok && mbar_wait(&bar.s, par, p.dev_status, kStatusBwdWait));
             if (!ok) break;
             tc_fence_after();
-            uint32_t sr[64];
-#pragma unroll
-            for (int c = 0; c < 2; ++c) tmem_ld_32x32(t_s + uint32_t(c * 32), *reinterpret_cast<uint32_t (*)[32]>(&sr[32 * c]));
-#pragma unroll
-            for (int c = 0; c < 2; ++c) tmem_ld_wait_32(*reinterpret_cast<uint32_t (*)[32]>(&sr[32 * c]));
+            uint32_t sr[32], w[16];
+            tmem_ld_32x32(t_s, sr);
+            tmem_ld_wait_32(sr);
             if (!KEYS) {
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bar.read);
             }
-            float pr[64];
+            float pr[32];
             const f32x2 sc2 = pk2(sc, sc);
 #pragma unroll
-            for (int e = 0; e < 64; e += 4) {
+            for (int e = 0; e < 32; e += 4) {
                 float4 l = make_float4(row_lse, row_lse, row_lse, row_lse);
                 if (KEYS) l = *reinterpret_cast<const float4*>(stat + e);
                 float z[4];
@@ -252,52 +251,42 @@ __device__ __forceinline__ void bwd_run(const CUtensorMap* tmA0, const CUtensorM
                 const int from = s.causal ? r - sm.shift - c0 : 0;
                 if (__any_sync(0xffffffffu, from > 0)) {
 #pragma unroll
-                    for (int e = 0; e < 64; ++e)
+                    for (int e = 0; e < 32; ++e)
                         if (e < from) pr[e] = 0.f;
                 }
-            }
-            const int valid = KEYS ? 64 : limit - c0;
-            const bool cut = !KEYS && __any_sync(0xffffffffu, valid < 64);
-            if (KEYS) {
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(pr[32 * c + 2 * e], pr[32 * c + 2 * e + 1]);
-                    tmem_st_32x16(t_s + uint32_t(c * 16), w);
-                }
+                for (int e = 0; e < 16; ++e) w[e] = pack_bf16(pr[2 * e], pr[2 * e + 1]);
+                tmem_st_32x16(t_s, w);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bar.p);
             }
+            const int valid = KEYS ? 32 : limit - c0;
+            const bool cut = !KEYS && __any_sync(0xffffffffu, valid < 32);
             ok = __all_sync(0xffffffffu, mbar_wait(&bar.dp, par, p.dev_status, kStatusBwdWait));
             if (!ok) break;
             tc_fence_after();
             const uint32_t t_dp = t_s + (KEYS ? 128u : 128u + 128u * par);
+            uint32_t dp[32];
+            tmem_ld_32x32(t_dp, dp);
+            tmem_ld_wait_32(dp);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t dp[32], w[16];
-                tmem_ld_32x32(t_dp + uint32_t(c * 32), dp);
-                tmem_ld_wait_32(dp);
+            for (int e = 0; e < 32; e += 4) {
+                float4 d = make_float4(row_d, row_d, row_d, row_d);
+                if (KEYS) d = *reinterpret_cast<const float4*>(stat + kAttnTile + e);
+                float g[4];
+                upk2(mul2(pk2(pr[e], pr[e + 1]), sub2(pk2(__uint_as_float(dp[e]), __uint_as_float(dp[e + 1])), pk2(d.x, d.y))), g[0], g[1]);
+                upk2(mul2(pk2(pr[e + 2], pr[e + 3]), sub2(pk2(__uint_as_float(dp[e + 2]), __uint_as_float(dp[e + 3])), pk2(d.z, d.w))), g[2], g[3]);
+                if (cut) {
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    float4 d = make_float4(row_d, row_d, row_d, row_d);
-                    if (KEYS) d = *reinterpret_cast<const float4*>(stat + kAttnTile + 32 * c + e);
-                    float g[4];
-                    upk2(mul2(pk2(pr[32 * c + e], pr[32 * c + e + 1]), sub2(pk2(__uint_as_float(dp[e]), __uint_as_float(dp[e + 1])), pk2(d.x, d.y))), g[0], g[1]);
-                    upk2(mul2(pk2(pr[32 * c + e + 2], pr[32 * c + e + 3]), sub2(pk2(__uint_as_float(dp[e + 2]), __uint_as_float(dp[e + 3])), pk2(d.z, d.w))), g[2], g[3]);
-                    if (cut) {
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            if (32 * c + e + x >= valid) g[x] = 0.f;
-                    }
-                    w[e / 2] = pack_bf16(g[0], g[1]);
-                    w[e / 2 + 1] = pack_bf16(g[2], g[3]);
+                    for (int x = 0; x < 4; ++x)
+                        if (e + x >= valid) g[x] = 0.f;
                 }
-                // the second half's dP is still to be read: dS goes over the columns of the first 32 only
-                tmem_st_32x16(t_dp + uint32_t(c * 16), w);
+                w[e / 2] = pack_bf16(g[0], g[1]);
+                w[e / 2 + 1] = pack_bf16(g[2], g[3]);
             }
+            tmem_st_32x16(t_dp, w);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
@@ -306,15 +295,16 @@ __device__ __forceinline__ void bwd_run(const CUtensorMap* tmA0, const CUtensorM
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&bar.acc, 0, p.dev_status, kStatusBwdWait));
         if (ok) {
             tc_fence_after();
+            const uint32_t c = uint32_t(quarter * 32);
             if (KEYS) {
                 const bool row_ok = r < s.Lk, keep = r < sm.kl;
                 const int64_t at = int64_t(n) * s.Lk + (row_ok ? r : 0);
-                store_rows(t_lane + 256u + uint32_t(half * 64), p.dv + at * p.lddv + head * s.dh, half * 64, s.dh, row_ok, keep, 1.0f);
-                store_rows(t_lane + 384u + uint32_t(half * 64), p.dk + at * p.lddk + head * s.dh, half * 64, s.dh, row_ok, keep, s.scale);
+                store_rows(t_lane + 256u + c, p.dv + at * p.lddv + head * s.dh, int(c), s.dh, row_ok, keep, 1.0f);
+                store_rows(t_lane + 384u + c, p.dk + at * p.lddk + head * s.dh, int(c), s.dh, row_ok, keep, s.scale);
             } else {
                 const bool row_ok = r < s.Lq, keep = limit > 0;
                 const int64_t at = int64_t(n) * s.Lq + (row_ok ? r : 0);
-                store_rows(t_lane + 384u + uint32_t(half * 64), p.dq + at * p.lddq + head * s.dh, half * 64, s.dh, row_ok, keep, s.scale);
+                store_rows(t_lane + 384u + c, p.dq + at * p.lddq + head * s.dh, int(c), s.dh, row_ok, keep, s.scale);
             }
         }
     }
@@ -334,10 +324,10 @@ attention_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         mbar_init(&bar.keep, 1);
         for (int i = 0; i < kBwdStages; ++i) { mbar_init(&bar.full[i], 1); mbar_init(&bar.empty[i], 1); }
         mbar_init(&bar.s, 1); mbar_init(&bar.dp, 1); mbar_init(&bar.acc, 1);
-        mbar_init(&bar.read, 8); mbar_init(&bar.p, 8); mbar_init(&bar.ds, 8);
+        mbar_init(&bar.read, kBwdWarps); mbar_init(&bar.p, kBwdWarps); mbar_init(&bar.ds, kBwdWarps);
         fence_barrier_init();
     }
-    if (warp == 9) { __syncwarp(); tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
+    if (warp == kBwdWarps + 1) { __syncwarp(); tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -355,7 +345,7 @@ attention_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) tmem_dealloc(tmem_base, 512);
+    if (warp == kBwdWarps + 1) tmem_dealloc(tmem_base, 512);
 }
 
 // Per query and head: D = dout . out in fp32, and lse * log2(e), in tiles of 128 rows as the gradient kernel loads them.  Rows without

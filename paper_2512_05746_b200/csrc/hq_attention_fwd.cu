@@ -230,8 +230,7 @@ attention_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             const bool row_ok = i < s.Lq, keep = limit > 0 && blocks > 0;
             __nv_bfloat16* dst = p.out + (int64_t(n) * s.Lq + (row_ok ? i : 0)) * p.ldo + head * s.dh;
             const float inv = keep ? 1.0f / l_run : 0.f;
-            store_rows(t_o, dst, 0, s.dh, row_ok, keep, inv);
-            store_rows(t_o + 64u, dst, 64, s.dh, row_ok, keep, inv);
+            for (int c = 0; c < s.dh; c += 32) store_rows(t_o + uint32_t(c), dst, c, s.dh, row_ok, keep, inv);
             if (row_ok) p.lse[(int64_t(n) * s.heads + head) * s.Lq + i] = keep ? m_run * s.scale + logf(l_run) : -INFINITY;
         }
     }

@@ -54,10 +54,10 @@ __device__ __forceinline__ void clear_rows(unsigned char* tile, int lo, int hi, 
         }
 }
 
-// 64 accumulator columns of this warp's lanes as scaled bf16 into rows of global memory: `dst` is the row's first channel of the
-// head, `c0` the first channel of the 64.  A row that is not kept gets zeros; one that does not exist (row_ok false) nothing.
+// 32 accumulator columns of this warp's lanes as scaled bf16 into rows of global memory: `dst` is the row's first channel of the
+// head, `c0` the first channel of the 32.  A row that is not kept gets zeros; one that does not exist (row_ok false) nothing.
 __device__ __forceinline__ void store_rows(uint32_t taddr, __nv_bfloat16* dst, int c0, int dh, bool row_ok, bool keep, float mul) {
-    for (int c = 0; c < 64 && c0 + c < dh; c += 16) {
+    for (int c = 0; c < 32 && c0 + c < dh; c += 16) {
         uint32_t r[16];
         tmem_ld_32x16(taddr + uint32_t(c), r);
         tmem_ld_wait_16(r);
