@@ -13,346 +13,512 @@
 // tensor memory (as operands of the second products they are read where they were written), no fp32 partial dq in memory and no
 // order of additions that changes from run to run.
 //
-// Warps 0-15: thread = lane, four warps per quarter of the 128 columns; warp 16 loads, warp 17 issues.  The tile a CTA keeps (K and V,
-// or Q and dout) stays in shared memory; pairs of the other side's tiles come through a ring of two.
+// The kernel is persistent: a CTA takes an item (a tile of one kind), then the next that no other has taken.  Warps 0-15: thread =
+// lane, four warps per quarter of the 128 columns; warp 16 takes items and loads, warp 17 issues, warp 18 stores.  The tile an item keeps
+// (K and V, or Q and dout) stays in shared memory, where its gradient is staged at the end; the other side's two kinds of tiles come
+// through a ring each.
 #include "hq_attention_tile.cuh"
 
 namespace hq {
 namespace {
 
-constexpr int32_t kStatusBwdWait = 0x710, kStatusBwdTma = 0x711;
+constexpr int32_t kStatusBwdWait = 0x710, kStatusBwdTma = 0x711, kStatusBwdSmem = 0x712;
 constexpr int kBwdWarps = 16;                                  // of the probabilities
-constexpr int kBwdThreads = (kBwdWarps + 2) * 32;
-constexpr int kBwdStages = 2;
-constexpr uint32_t kStatBytes = 2 * kAttnTile * 4;             // per query tile: lse * log2(e) of 128 rows, then D of 128 rows
-template <int NH> constexpr size_t bwd_smem() { return size_t(2 + 2 * kBwdStages) * NH * kAttnPart + kBwdStages * kStatBytes + 1024; }
+constexpr int kBwdThreads = (kBwdWarps + 3) * 32;
+constexpr uint32_t kStatBytes = kAttnTile * 4;                 // of one query tile: -lse * log2(e), and as many for -D
+
+// Rings: tiles of 16 KB up to 64 channels, 32 KB above, where two kept tiles, three and two take all but 2 KB of the shared memory.
+template <int NH> struct BwdRings {
+    static constexpr int kKeep = NH == 1 ? 2 : 1;              // kept pairs: the next item's loads begin under this one's last steps
+    static constexpr int kB0 = NH == 1 ? 4 : 3, kB1 = NH == 1 ? 4 : 2;
+    static constexpr int kTile = NH * kAttnPart;
+    static constexpr int kTiles = (2 * kKeep + kB0 + kB1) * kTile, kStats = (kB0 + kB1) * int(kStatBytes);
+};
 
 struct BwdParams {
     AttnShape s;
     const float* stats;                            // [Nb * heads][q_tiles][2][128]
+    unsigned* taken;                               // items taken beyond the first of every CTA
     __nv_bfloat16 *dq, *dk, *dv;
     int64_t lddq, lddk, lddv;
     int q_tiles;
-    unsigned key_ctas;
+    unsigned key_items, items;
     int32_t* dev_status;
 };
+struct BwdMaps { CUtensorMap q, k, v, dout, dq, dk, dv; };
 
-struct BwdBars { uint64_t keep, full[kBwdStages], empty[kBwdStages], s, dp, read, p, ds, acc; };
+template <int NH> struct BwdBars {
+    using R = BwdRings<NH>;
+    uint64_t keep_full[R::kKeep], keep_empty[R::kKeep], b0_full[R::kB0], b0_empty[R::kB0], b1_full[R::kB1], b1_empty[R::kB1];
+    // dP and dS of a step alternate between two barriers: where the next dP does not wait for this dS, one could come round twice
+    // before a slow warp has looked at it
+    uint64_t s, p, dp[2], ds[2], acc, staged[R::kKeep], item_full[2], item_empty[2];
+    uint32_t item[2], tmem_slot;
+};
+template <int NH> constexpr size_t bwd_smem() { return size_t(BwdRings<NH>::kTiles + BwdRings<NH>::kStats) + sizeof(BwdBars<NH>); }
 
-// KEYS: the CTA keeps a tile of keys and values (A0 = K, A1 = V; B0 = Q, B1 = dout), else one of queries (A0 = Q, A1 = dout; B0 = K,
-// B1 = V).  Tensor memory: S at columns 0, dP at 128; KEYS: dv at 256, dk at 384; else dP's second buffer at 256, dq at 384.
-template <int NH, bool KEYS>
-__device__ __forceinline__ void bwd_run(const CUtensorMap* tmA0, const CUtensorMap* tmA1, const CUtensorMap* tmB0, const CUtensorMap* tmB1,
-                                        const BwdParams& p, unsigned char* smem, BwdBars& bar, uint32_t tmem_base, int n, int head, int tile,
-                                        const AttnSample& sm) {
-    constexpr int kTile = NH * kAttnPart;
+// A place in a ring and how often it has come round.
+template <int N> struct RingAt {
+    int slot = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next() { if (++slot == N) { slot = 0; phase ^= 1u; } }
+};
+
+// What an item is: a tile of keys of one (sample, key head) or of queries of one (sample, head), and the other side's tiles it walks.
+struct BwdItem {
+    bool keys;
+    int n, head, tile, row0;
+    AttnSample sm;
+    int first, last, total;                        // tiles [first, last) of each of its heads; steps over all of them
+};
+__device__ __forceinline__ BwdItem bwd_item(const BwdParams& p, unsigned index) {
     const AttnShape& s = p.s;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    unsigned char* sA = smem;
-    unsigned char* sB = smem + 2 * kTile;
-    float* sStat = reinterpret_cast<float*>(sB + kBwdStages * 2 * kTile);
-    const int row0 = tile * kAttnTile;
-    const int group = s.heads / s.kv_heads;
-    // the other side's tiles [first, last) of each head
-    int first, last;
-    if (KEYS) {
-        first = max(sm.q_lo, s.causal ? row0 - sm.shift : 0) / kAttnTile;
-        last = row0 < sm.kl ? (sm.q_hi + kAttnTile - 1) / kAttnTile : 0;
+    BwdItem t;
+    // tiles of keys first (they walk every head of their group); under the causal mask the first keys and the last queries walk the most
+    t.keys = index < p.key_items;
+    const unsigned at = t.keys ? index : index - p.key_items, heads = unsigned(t.keys ? s.kv_heads : s.heads), per = unsigned(s.Nb) * heads;
+    const unsigned block = at / per, bh = at - block * per;
+    t.n = int(bh / heads);
+    t.head = int(bh - unsigned(t.n) * heads);
+    t.tile = !t.keys && s.causal ? p.q_tiles - 1 - int(block) : int(block);
+    t.row0 = t.tile * kAttnTile;
+    t.sm = attn_sample(s, t.n);
+    if (t.keys) {
+        t.first = max(t.sm.q_lo, s.causal ? t.row0 - t.sm.shift : 0) / kAttnTile;
+        t.last = t.row0 < t.sm.kl ? (t.sm.q_hi + kAttnTile - 1) / kAttnTile : 0;
     } else {
-        const int end = min(row0 + kAttnTile, sm.q_hi) - 1;
-        first = 0;
-        last = row0 > end || end < sm.q_lo ? 0 : (attn_key_limit(s, sm, end) + kAttnTile - 1) / kAttnTile;
+        const int end = min(t.row0 + kAttnTile, t.sm.q_hi) - 1;
+        t.first = 0;
+        t.last = t.row0 > end || end < t.sm.q_lo ? 0 : (attn_key_limit(s, t.sm, end) + kAttnTile - 1) / kAttnTile;
     }
-    const int per_head = max(0, last - first);
-    const int total = KEYS ? per_head * group : per_head;
-    if (total == 0) {                              // nothing seen: the gradient is zero
-        if (KEYS) {
-            const int rows = min(kAttnTile, s.Lk - row0);
-            const int64_t r = int64_t(n) * s.Lk + row0;
-            zero_rows(p.dk + r * p.lddk + head * s.dh, p.lddk, rows, s.dh);
-            zero_rows(p.dv + r * p.lddv + head * s.dh, p.lddv, rows, s.dh);
-        } else {
-            zero_rows(p.dq + (int64_t(n) * s.Lq + row0) * p.lddq + head * s.dh, p.lddq, min(kAttnTile, s.Lq - row0), s.dh);
-        }
-        return;
-    }
+    t.total = max(0, t.last - t.first) * (t.keys ? s.heads / s.kv_heads : 1);
+    return t;
+}
 
-    if (warp == kBwdWarps) {
-        if (elect_one()) {
-            bool ok = true;
-            int loads = 0;
-            mbar_expect_tx(&bar.keep, 2 * kTile + (KEYS ? 0 : kStatBytes));
-            load_tile<NH>(sA, tmA0, &bar.keep, head, row0, n);
-            load_tile<NH>(sA + kTile, tmA1, &bar.keep, head, row0, n);
-            if (!KEYS) bulk_load(sStat, p.stats + (int64_t(n * s.heads + head) * p.q_tiles + tile) * (2 * kAttnTile), kStatBytes, &bar.keep);
-            int b_head = KEYS ? head * group : head / group, b_tile = first;
-            for (int i = 0; i < total && ok; ++i) {
-                const int stage = i % kBwdStages, use = i / kBwdStages;
-                if (use > 0) ok = mbar_wait(&bar.empty[stage], uint32_t(use - 1) & 1u, p.dev_status, kStatusBwdWait);
-                if (!ok) break;
-                unsigned char* to = sB + stage * 2 * kTile;
-                mbar_expect_tx(&bar.full[stage], 2 * kTile + (KEYS ? kStatBytes : 0));
-                load_tile<NH>(to, tmB0, &bar.full[stage], b_head, b_tile * kAttnTile, n);
-                load_tile<NH>(to + kTile, tmB1, &bar.full[stage], b_head, b_tile * kAttnTile, n);
-                if (KEYS)
-                    bulk_load(sStat + stage * 2 * kAttnTile, p.stats + (int64_t(n * s.heads + b_head) * p.q_tiles + b_tile) * (2 * kAttnTile),
-                              kStatBytes, &bar.full[stage]);
-                ++loads;
-                if (++b_tile == last) { b_tile = first; ++b_head; }
-            }
-            // what was requested lands before the CTA's shared memory is given up, on every way out
-            mbar_wait(&bar.keep, 0, nullptr, 0);
-            for (int i = max(0, loads - kBwdStages); i < loads; ++i) mbar_wait(&bar.full[i % kBwdStages], uint32_t(i / kBwdStages) & 1u, nullptr, 0);
+// ---- warp 16, one lane: takes items, tells the others, loads their tiles
+template <int NH>
+__device__ __forceinline__ void bwd_load(const BwdMaps& m, const BwdParams& p, unsigned char* smem, float* stat0, float* stat1, BwdBars<NH>& bar) {
+    using R = BwdRings<NH>;
+    unsigned char *sB0 = smem + 2 * R::kKeep * R::kTile, *sB1 = sB0 + R::kB0 * R::kTile;
+    const int group = p.s.heads / p.s.kv_heads;
+    RingAt<R::kKeep> keep;
+    RingAt<R::kB0> b0;
+    RingAt<R::kB1> b1;
+    RingAt<2> told;
+    int keeps = 0, n0 = 0, n1 = 0;                 // begun so far
+    bool ok = true;
+    unsigned index = blockIdx.x;
+    while (ok) {
+        ok = mbar_wait(&bar.item_empty[told.slot], told.phase ^ 1u, p.dev_status, kStatusBwdWait);
+        if (!ok) break;
+        bar.item[told.slot] = index;
+        mbar_arrive(&bar.item_full[told.slot]);
+        told.next();
+        if (index >= p.items) break;
+        const unsigned following = gridDim.x + atomicAdd(p.taken, 1u);
+        const BwdItem t = bwd_item(p, index);
+        index = following;
+        if (t.total == 0) continue;
+        ok = mbar_wait(&bar.keep_empty[keep.slot], keep.phase ^ 1u, p.dev_status, kStatusBwdWait);
+        if (!ok) break;
+        unsigned char* to = smem + 2 * keep.slot * R::kTile;
+        mbar_expect_tx(&bar.keep_full[keep.slot], 2 * R::kTile);
+        load_tile<NH>(to, t.keys ? &m.k : &m.q, &bar.keep_full[keep.slot], t.head, t.row0, t.n);
+        load_tile<NH>(to + R::kTile, t.keys ? &m.v : &m.dout, &bar.keep_full[keep.slot], t.head, t.row0, t.n);
+        keep.next();
+        ++keeps;
+        int head = t.keys ? t.head * group : t.head / group, tile = t.first;
+        for (int i = 0; i < t.total; ++i) {
+            const float* stats = p.stats + (int64_t(t.n * p.s.heads + head) * p.q_tiles + tile) * (2 * kAttnTile);
+            ok = mbar_wait(&bar.b0_empty[b0.slot], b0.phase ^ 1u, p.dev_status, kStatusBwdWait);
+            if (!ok) break;
+            mbar_expect_tx(&bar.b0_full[b0.slot], R::kTile + (t.keys ? kStatBytes : 0));
+            load_tile<NH>(sB0 + b0.slot * R::kTile, t.keys ? &m.q : &m.k, &bar.b0_full[b0.slot], head, tile * kAttnTile, t.n);
+            if (t.keys) bulk_load(stat0 + b0.slot * kAttnTile, stats, kStatBytes, &bar.b0_full[b0.slot]);
+            b0.next();
+            ++n0;
+            ok = mbar_wait(&bar.b1_empty[b1.slot], b1.phase ^ 1u, p.dev_status, kStatusBwdWait);
+            if (!ok) break;
+            mbar_expect_tx(&bar.b1_full[b1.slot], R::kTile + (t.keys ? kStatBytes : 0));
+            load_tile<NH>(sB1 + b1.slot * R::kTile, t.keys ? &m.dout : &m.v, &bar.b1_full[b1.slot], head, tile * kAttnTile, t.n);
+            if (t.keys) bulk_load(stat1 + b1.slot * kAttnTile, stats + kAttnTile, kStatBytes, &bar.b1_full[b1.slot]);
+            b1.next();
+            ++n1;
+            if (++tile == t.last) { tile = t.first; ++head; }
         }
-        __syncwarp();
-    } else if (warp == kBwdWarps + 1) {
-        const uint32_t idesc_s = make_idesc_bf16(kAttnTile, kAttnTile, false);
-        const uint32_t idesc_acc = make_idesc_bf16(kAttnTile, (s.dh + 15) & ~15, true);
-        const int ksteps = (s.dh + 15) / 16;
-        const uint64_t dA = make_sw128_kmajor_desc(smem_u32(sA));
-        auto stage_of = [&](int i) { return sB + (i % kBwdStages) * 2 * kTile; };
-        // the stage's tiles have landed, and rows of tokens outside the lengths are zero
-        int b_tile = first;
-        auto landed = [&](int i) {
-            if (!__all_sync(0xffffffffu, mbar_wait(&bar.full[i % kBwdStages], uint32_t(i / kBwdStages) & 1u, p.dev_status, kStatusBwdTma))) return false;
-            const int r0 = b_tile * kAttnTile;
-            const int lo = KEYS ? sm.q_lo - r0 : 0, hi = (KEYS ? sm.q_hi : sm.kl) - r0;
-            const int exist = (KEYS ? s.Lq : s.Lk) - r0;       // rows behind these are zero as they come
-            if (lo > 0 || hi < min(kAttnTile, exist)) {
-                clear_rows<NH>(stage_of(i), lo, hi, lane);
-                if (KEYS) clear_rows<NH>(stage_of(i) + kTile, lo, hi, lane);
+    }
+    // what was requested lands before the CTA's shared memory is given up, on every way out
+    for (int i = max(0, keeps - R::kKeep); i < keeps; ++i) mbar_wait(&bar.keep_full[i % R::kKeep], uint32_t(i / R::kKeep) & 1u, nullptr, 0);
+    for (int i = max(0, n0 - R::kB0); i < n0; ++i) mbar_wait(&bar.b0_full[i % R::kB0], uint32_t(i / R::kB0) & 1u, nullptr, 0);
+    for (int i = max(0, n1 - R::kB1); i < n1; ++i) mbar_wait(&bar.b1_full[i % R::kB1], uint32_t(i / R::kB1) & 1u, nullptr, 0);
+}
+
+// The next item's number (p.items and beyond: none, or a wait ran out), the same in every lane.
+template <int NH>
+__device__ __forceinline__ unsigned bwd_next(const BwdParams& p, BwdBars<NH>& bar, RingAt<2>& told, int lane) {
+    if (!__all_sync(0xffffffffu, mbar_wait(&bar.item_full[told.slot], told.phase, p.dev_status, kStatusBwdWait))) return 0xffffffffu;
+    const unsigned index = *const_cast<volatile uint32_t*>(&bar.item[told.slot]);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&bar.item_empty[told.slot]);
+    told.next();
+    return index;
+}
+
+// ---- warp 17: products.  Tensor memory: S at columns 0, dP at 128; keys: dv at 256, dk at 384; queries: dP's second buffer at 256,
+// dq at 384.  Products run in the order of their issue: one that overwrites another's operand or result in tensor memory, or an
+// accumulator that the other warps have read before they handed over the operand it waits for, is issued behind it.
+template <int NH>
+__device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* smem, BwdBars<NH>& bar, uint32_t tmem_base, int lane) {
+    using R = BwdRings<NH>;
+    const AttnShape& s = p.s;
+    unsigned char *sB0 = smem + 2 * R::kKeep * R::kTile, *sB1 = sB0 + R::kB0 * R::kTile;
+    const uint32_t idesc_s = make_idesc_bf16(kAttnTile, kAttnTile, false);
+    const uint32_t idesc_acc = make_idesc_bf16(kAttnTile, (s.dh + 15) & ~15, true);
+    const int ksteps = (s.dh + 15) / 16;
+    const uint64_t dA = make_sw128_kmajor_desc(smem_u32(smem));
+    const uint64_t dB0 = make_sw128_kmajor_desc(smem_u32(sB0)), dB1 = make_sw128_kmajor_desc(smem_u32(sB1));
+    const uint64_t dB0t = make_sw128_mnmajor_desc(smem_u32(sB0), kAttnPart), dB1t = make_sw128_mnmajor_desc(smem_u32(sB1), kAttnPart);
+    constexpr uint64_t kTileUnits = R::kTile >> 4;
+    auto score_product = [&](uint64_t a, uint64_t b, uint32_t column) {
+        for (int k = 0; k < ksteps; ++k) {
+            const uint64_t step = uint64_t((k >> 2) * (kAttnPart >> 4) + 2 * (k & 3));
+            mma_bf16(tmem_base + column, a + step, b + step, idesc_s, k != 0 ? 1u : 0u);
+        }
+    };
+    // bf16 operand of each quarter in the first half of its 32 columns
+    auto acc_product = [&](uint32_t column, uint64_t b, uint32_t acc, bool add) {
+#pragma unroll
+        for (int k = 0; k < kAttnTile / 16; ++k)
+            mma_bf16_ts(tmem_base + acc, tmem_base + column + uint32_t((k >> 1) * 32 + (k & 1) * 8), b + uint64_t(k * 128), idesc_acc,
+                        add || k != 0 ? 1u : 0u);
+    };
+    auto wait = [&](uint64_t* b, uint32_t parity, int32_t code) { return __all_sync(0xffffffffu, mbar_wait(b, parity, p.dev_status, code)); };
+    RingAt<R::kKeep> keep;
+    RingAt<R::kB0> s0, a0;                         // B0's tile of the next score product / of the next sum
+    RingAt<R::kB1> s1, a1;
+    RingAt<2> told;
+    uint32_t step = 0;                             // over all items
+    for (;;) {
+        const unsigned index = bwd_next<NH>(p, bar, told, lane);
+        if (index >= p.items) return;
+        const BwdItem t = bwd_item(p, index);
+        if (t.total == 0) continue;
+        // rows of tokens outside the lengths (zero as they come behind the last row of the matrix) are made zero where they would
+        // meet zero probabilities in a sum: queries and their gradients, or keys
+        int tile = t.first;
+        const int outer_lo = t.keys ? t.sm.q_lo : 0, outer_hi = t.keys ? t.sm.q_hi : t.sm.kl, exist = t.keys ? s.Lq : s.Lk;
+        auto clear = [&](unsigned char* at, int which_tile) {
+            const int r0 = which_tile * kAttnTile;
+            if (outer_lo > r0 || outer_hi < min(r0 + kAttnTile, exist)) {
+                clear_rows<NH>(at, outer_lo - r0, outer_hi - r0, lane);
                 fence_proxy_async_smem();
                 __syncwarp();
             }
-            if (++b_tile == last) b_tile = first;
-            return true;
         };
-        auto score_product = [&](int i, int which, uint32_t column, uint64_t* done) {          // which: 0 scores, 1 dP
-            const uint64_t da = dA + uint64_t(which * (kTile >> 4));
-            const uint64_t db = make_sw128_kmajor_desc(smem_u32(stage_of(i) + which * kTile));
-            for (int k = 0; k < ksteps; ++k) {
-                const uint64_t step = uint64_t((k >> 2) * (kAttnPart >> 4) + 2 * (k & 3));
-                mma_bf16(tmem_base + column, da + step, db + step, idesc_s, k != 0 ? 1u : 0u);
-            }
-            mma_commit(done);
-        };
-        // bf16 elements of each quarter in the first half of its 32 columns
-        auto acc_product = [&](int i, int which, uint32_t column, uint32_t acc) {
-            const uint64_t db = make_sw128_mnmajor_desc(smem_u32(stage_of(i) + which * kTile), kAttnPart);
-#pragma unroll
-            for (int k = 0; k < kAttnTile / 16; ++k)
-                mma_bf16_ts(tmem_base + acc, tmem_base + column + uint32_t((k >> 1) * 32 + (k & 1) * 8), db + uint64_t(k * 128), idesc_acc,
-                            (i | k) != 0 ? 1u : 0u);
-        };
-        auto wait = [&](uint64_t* b, int i) { return __all_sync(0xffffffffu, mbar_wait(b, uint32_t(i) & 1u, p.dev_status, kStatusBwdWait)); };
-        bool ok = __all_sync(0xffffffffu, mbar_wait(&bar.keep, 0, p.dev_status, kStatusBwdTma)) && landed(0);
-        if (ok) {
+        const uint64_t a = dA + uint64_t(keep.slot) * (2 * kTileUnits);
+        if (!wait(&bar.keep_full[keep.slot], keep.phase, kStatusBwdTma)) return;
+        keep.next();
+        auto scores = [&](int which_tile) {        // S of the next tile
+            if (!wait(&bar.b0_full[s0.slot], s0.phase, kStatusBwdTma)) return false;
+            clear(sB0 + s0.slot * R::kTile, which_tile);
             if (elect_one()) {
                 tc_fence_after();
-                score_product(0, 0, 0u, &bar.s);
-                score_product(0, 1, 128u, &bar.dp);
+                score_product(a, dB0 + uint64_t(s0.slot) * kTileUnits, 0u);
+                mma_commit(&bar.s);
             }
             __syncwarp();
-        }
-        // Products run in the order of their issue: one that overwrites another's operand in tensor memory is issued behind it.
-        for (int i = 0; i < total && ok; ++i) {
-            if (KEYS) {
-                ok = wait(&bar.p, i);
-                if (!ok) break;
-                if (elect_one()) { tc_fence_after(); acc_product(i, 1, 0u, 256u); }
-                __syncwarp();
-                if (i + 1 < total) {
-                    ok = landed(i + 1);
-                    if (!ok) break;
-                    if (elect_one()) { tc_fence_after(); score_product(i + 1, 0, 0u, &bar.s); }
-                    __syncwarp();
-                }
-                ok = wait(&bar.ds, i);
-                if (!ok) break;
+            s0.next();
+            return true;
+        };
+        auto dprobs = [&](int which_tile, uint32_t column, uint32_t of) {  // dP of the next tile, step `of`
+            if (!wait(&bar.b1_full[s1.slot], s1.phase, kStatusBwdTma)) return false;
+            if (t.keys) clear(sB1 + s1.slot * R::kTile, which_tile);
+            if (elect_one()) {
+                tc_fence_after();
+                score_product(a + kTileUnits, dB1 + uint64_t(s1.slot) * kTileUnits, column);
+                mma_commit(&bar.dp[of & 1u]);
+                if (!t.keys) mma_commit(&bar.b1_empty[s1.slot]);
+            }
+            __syncwarp();
+            s1.next();
+            return true;
+        };
+        if (!scores(tile) || !dprobs(tile, 128u, step)) return;
+        for (int i = 0; i < t.total; ++i) {
+            const bool more = i + 1 < t.total;
+            if (++tile == t.last) tile = t.first;
+            if (!wait(&bar.p, step & 1u, kStatusBwdWait)) return;
+            if (t.keys) {
                 if (elect_one()) {
                     tc_fence_after();
-                    acc_product(i, 0, 128u, 384u);
-                    mma_commit(&bar.empty[i % kBwdStages]);
-                    if (i + 1 < total) score_product(i + 1, 1, 128u, &bar.dp);
+                    acc_product(0u, dB1t + uint64_t(a1.slot) * kTileUnits, 256u, i != 0);
                 }
                 __syncwarp();
-            } else {
-                if (i + 1 < total) {
-                    ok = landed(i + 1) && wait(&bar.read, i);
-                    if (!ok) break;
-                    if (elect_one()) {
-                        tc_fence_after();
-                        score_product(i + 1, 0, 0u, &bar.s);
-                        score_product(i + 1, 1, 128u + 128u * uint32_t((i + 1) & 1), &bar.dp);
-                    }
-                    __syncwarp();
-                }
-                ok = wait(&bar.ds, i);
-                if (!ok) break;
-                if (elect_one()) {
-                    tc_fence_after();
-                    acc_product(i, 0, 128u + 128u * uint32_t(i & 1), 384u);
-                    mma_commit(&bar.empty[i % kBwdStages]);
-                }
-                __syncwarp();
+                if (more && !scores(tile)) return;
+            } else if (more) {
+                if (!scores(tile) || !dprobs(tile, 128u + 128u * uint32_t((i + 1) & 1), step + 1u)) return;
             }
-        }
-        if (ok) {
-            if (elect_one()) mma_commit(&bar.acc);
+            if (!wait(&bar.ds[step & 1u], (step >> 1) & 1u, kStatusBwdWait)) return;
+            if (elect_one()) {
+                tc_fence_after();
+                acc_product(t.keys || !(i & 1) ? 128u : 256u, dB0t + uint64_t(a0.slot) * kTileUnits, 384u, i != 0);
+                mma_commit(&bar.b0_empty[a0.slot]);
+                if (t.keys) mma_commit(&bar.b1_empty[a1.slot]);        // its statistics have been read by now
+                if (!more) mma_commit(&bar.acc);
+            }
             __syncwarp();
-        }
-    } else {
-        const int quarter = warp >> 2;                         // columns quarter * 32 ..
-        const int lane_row = (warp & 3) * 32 + lane, r = row0 + lane_row;
-        const uint32_t t_lane = tmem_base + (uint32_t((warp & 3) * 32) << 16);
-        const uint32_t t_s = t_lane + uint32_t(quarter * 32);
-        const float sc = s.scale_log2;
-        bool ok = true;
-        int b_tile = first;
-        float row_lse = 0.f, row_d = 0.f;
-        int limit = 0;                                         // queries: keys the row sees
-        if (!KEYS) {
-            ok = __all_sync(0xffffffffu, mbar_wait(&bar.keep, 0, p.dev_status, kStatusBwdTma));
-            row_lse = sStat[lane_row];
-            row_d = sStat[kAttnTile + lane_row];
-            limit = r < sm.q_hi ? attn_key_limit(s, sm, r) : 0;
-        }
-        for (int i = 0; i < total && ok; ++i) {
-            const uint32_t par = uint32_t(i) & 1u;
-            const int c0 = b_tile * kAttnTile + quarter * 32;  // the first column's query or key
-            if (++b_tile == last) b_tile = first;
-            const float* stat = sStat + (i % kBwdStages) * 2 * kAttnTile + quarter * 32;
-            if (KEYS) ok = mbar_wait(&bar.full[i % kBwdStages], uint32_t(i / kBwdStages) & 1u, p.dev_status, kStatusBwdTma);
-            ok = __all_sync(0xffffffffu, ok && mbar_wait(&bar.s, par, p.dev_status, kStatusBwdWait));
-            if (!ok) break;
-            tc_fence_after();
-            uint32_t sr[32], w[16];
-            tmem_ld_32x32(t_s, sr);
-            tmem_ld_wait_32(sr);
-            if (!KEYS) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bar.read);
-            }
-            float pr[32];
-            const f32x2 sc2 = pk2(sc, sc);
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-                float4 l = make_float4(row_lse, row_lse, row_lse, row_lse);
-                if (KEYS) l = *reinterpret_cast<const float4*>(stat + e);
-                float z[4];
-                upk2(fma2(pk2(__uint_as_float(sr[e]), __uint_as_float(sr[e + 1])), sc2, pk2(-l.x, -l.y)), z[0], z[1]);
-                upk2(fma2(pk2(__uint_as_float(sr[e + 2]), __uint_as_float(sr[e + 3])), sc2, pk2(-l.z, -l.w)), z[2], z[3]);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) pr[e + c] = ex2(z[c]);
-            }
-            // what the row does not see: keys behind its limit, or queries in front of the first that sees it
-            if (KEYS) {
-                const int from = s.causal ? r - sm.shift - c0 : 0;
-                if (__any_sync(0xffffffffu, from > 0)) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (e < from) pr[e] = 0.f;
-                }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) w[e] = pack_bf16(pr[2 * e], pr[2 * e + 1]);
-                tmem_st_32x16(t_s, w);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bar.p);
-            }
-            const int valid = KEYS ? 32 : limit - c0;
-            const bool cut = !KEYS && __any_sync(0xffffffffu, valid < 32);
-            ok = __all_sync(0xffffffffu, mbar_wait(&bar.dp, par, p.dev_status, kStatusBwdWait));
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t t_dp = t_s + (KEYS ? 128u : 128u + 128u * par);
-            uint32_t dp[32];
-            tmem_ld_32x32(t_dp, dp);
-            tmem_ld_wait_32(dp);
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-                float4 d = make_float4(row_d, row_d, row_d, row_d);
-                if (KEYS) d = *reinterpret_cast<const float4*>(stat + kAttnTile + e);
-                float g[4];
-                upk2(mul2(pk2(pr[e], pr[e + 1]), sub2(pk2(__uint_as_float(dp[e]), __uint_as_float(dp[e + 1])), pk2(d.x, d.y))), g[0], g[1]);
-                upk2(mul2(pk2(pr[e + 2], pr[e + 3]), sub2(pk2(__uint_as_float(dp[e + 2]), __uint_as_float(dp[e + 3])), pk2(d.z, d.w))), g[2], g[3]);
-                if (cut) {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        if (e + x >= valid) g[x] = 0.f;
-                }
-                w[e / 2] = pack_bf16(g[0], g[1]);
-                w[e / 2 + 1] = pack_bf16(g[2], g[3]);
-            }
-            tmem_st_32x16(t_dp, w);
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bar.ds);
-        }
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&bar.acc, 0, p.dev_status, kStatusBwdWait));
-        if (ok) {
-            tc_fence_after();
-            const uint32_t c = uint32_t(quarter * 32);
-            if (KEYS) {
-                const bool row_ok = r < s.Lk, keep = r < sm.kl;
-                const int64_t at = int64_t(n) * s.Lk + (row_ok ? r : 0);
-                store_rows(t_lane + 256u + c, p.dv + at * p.lddv + head * s.dh, int(c), s.dh, row_ok, keep, 1.0f);
-                store_rows(t_lane + 384u + c, p.dk + at * p.lddk + head * s.dh, int(c), s.dh, row_ok, keep, s.scale);
-            } else {
-                const bool row_ok = r < s.Lq, keep = limit > 0;
-                const int64_t at = int64_t(n) * s.Lq + (row_ok ? r : 0);
-                store_rows(t_lane + 384u + c, p.dq + at * p.lddq + head * s.dh, int(c), s.dh, row_ok, keep, s.scale);
-            }
+            a0.next();
+            a1.next();
+            if (t.keys && more && !dprobs(tile, 128u, step + 1u)) return;
+            ++step;
         }
     }
 }
 
-template <int NH>
-__global__ void __launch_bounds__(kBwdThreads, 1)
-attention_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                     const __grid_constant__ CUtensorMap tmDo, const BwdParams p) {
-    extern __shared__ __align__(1024) unsigned char smem_bwd[];
-    __shared__ BwdBars bar;
-    __shared__ uint32_t tmem_slot;
-    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_bwd) + 1023) & ~uintptr_t(1023));
+// ---- warps 0-15: probabilities and their gradients
+template <int NH, bool KEYS>
+__device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdItem& t, const float* stat0, const float* stat1, BwdBars<NH>& bar,
+                                                  RingAt<BwdRings<NH>::kB0>& b0, RingAt<BwdRings<NH>::kB1>& b1, uint32_t& step,
+                                                  uint32_t t_s, int r, int quarter, int lane) {
     const AttnShape& s = p.s;
-    const int warp = threadIdx.x >> 5;
+    const f32x2 sc2 = pk2(s.scale_log2, s.scale_log2);
+    f32x2 row_lse = 0, row_d = 0;
+    int limit = 0;                                             // queries: keys the row sees
+    if (!KEYS) {
+        const float* stats = p.stats + (int64_t(t.n * s.heads + t.head) * p.q_tiles + t.tile) * (2 * kAttnTile) + (r - t.row0);
+        const float l = __ldg(stats), d = __ldg(stats + kAttnTile);
+        row_lse = pk2(l, l);
+        row_d = pk2(d, d);
+        limit = r < t.sm.q_hi ? attn_key_limit(s, t.sm, r) : 0;
+        if (limit == 1) limit = 0;                             // a weight of 1, whatever its score: no gradient
+    }
+    int tile = t.first;
+    for (int i = 0; i < t.total; ++i) {
+        const int c0 = tile * kAttnTile + quarter * 32;        // the first column's query or key
+        if (++tile == t.last) tile = t.first;
+        bool ok = mbar_wait(&bar.s, step & 1u, p.dev_status, kStatusBwdWait);
+        if (KEYS) ok = ok && mbar_wait(&bar.b0_full[b0.slot], b0.phase, p.dev_status, kStatusBwdTma) &&
+                       mbar_wait(&bar.b1_full[b1.slot], b1.phase, p.dev_status, kStatusBwdTma);
+        if (!__all_sync(0xffffffffu, ok)) return false;
+        tc_fence_after();
+        uint32_t sr[32], w[16];
+        tmem_ld_32x32(t_s, sr);
+        tmem_ld_wait_32(sr);
+        if (!KEYS) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.p);
+        }
+        const float* nl = stat0 + b0.slot * kAttnTile + quarter * 32;
+        f32x2 pr[16];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            f32x2 l0 = row_lse, l1 = row_lse;
+            if (KEYS) {
+                const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(nl + 2 * e);
+                l0 = l.x; l1 = l.y;
+            }
+            float z[4];
+            upk2(fma2(pk2(__uint_as_float(sr[2 * e]), __uint_as_float(sr[2 * e + 1])), sc2, l0), z[0], z[1]);
+            upk2(fma2(pk2(__uint_as_float(sr[2 * e + 2]), __uint_as_float(sr[2 * e + 3])), sc2, l1), z[2], z[3]);
+            pr[e] = pk2(ex2(z[0]), ex2(z[1]));
+            pr[e + 1] = pk2(ex2(z[2]), ex2(z[3]));
+        }
+        if (KEYS) {
+            // queries in front of the first that sees the row's key
+            const int from = s.causal ? r - t.sm.shift - c0 : 0;
+            if (__any_sync(0xffffffffu, from > 0)) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    float a, b;
+                    upk2(pr[e], a, b);
+                    pr[e] = pk2(2 * e < from ? 0.f : a, 2 * e + 1 < from ? 0.f : b);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                float a, b;
+                upk2(pr[e], a, b);
+                w[e] = pack_bf16(a, b);
+            }
+            tmem_st_32x16(t_s, w);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.p);
+        }
+        if (!__all_sync(0xffffffffu, mbar_wait(&bar.dp[step & 1u], (step >> 1) & 1u, p.dev_status, kStatusBwdWait))) return false;
+        tc_fence_after();
+        const uint32_t t_dp = t_s + (KEYS || !(i & 1) ? 128u : 256u);
+        const float* nd = stat1 + b1.slot * kAttnTile + quarter * 32;
+        tmem_ld_32x32(t_dp, sr);
+        tmem_ld_wait_32(sr);
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            f32x2 d0 = row_d, d1 = row_d;
+            if (KEYS) {
+                const ulonglong2 d = *reinterpret_cast<const ulonglong2*>(nd + 2 * e);
+                d0 = d.x; d1 = d.y;
+            }
+            float a, b;
+            upk2(mul2(pr[e], add2(pk2(__uint_as_float(sr[2 * e]), __uint_as_float(sr[2 * e + 1])), d0)), a, b);
+            w[e] = pack_bf16(a, b);
+            upk2(mul2(pr[e + 1], add2(pk2(__uint_as_float(sr[2 * e + 2]), __uint_as_float(sr[2 * e + 3])), d1)), a, b);
+            w[e + 1] = pack_bf16(a, b);
+        }
+        if (KEYS) {
+            if (t.sm.kl == 1) {                                // every query sees one key only
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] = 0u;
+            }
+        } else {
+            const int valid = limit - c0;                      // what lies behind may be anything
+            if (__any_sync(0xffffffffu, valid < 32)) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] &= 2 * e + 1 < valid ? 0xFFFFFFFFu : 2 * e < valid ? 0xFFFFu : 0u;
+            }
+        }
+        tmem_st_32x16(t_dp, w);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar.ds[step & 1u]);
+        b0.next();
+        b1.next();
+        ++step;
+    }
+    return true;
+}
+
+// 32 columns of an accumulator as scaled bf16 into the staging tile (rows of 128 bytes, 128-byte swizzle); rows not kept become zeros.
+template <int NH>
+__device__ __forceinline__ void stage_rows(uint32_t taddr, unsigned char* tile, int row, int quarter, int dh, bool keep, float mul) {
+    if (quarter * 32 >= dh) return;
+    uint32_t r[32];
+    tmem_ld_32x32(taddr, r);
+    tmem_ld_wait_32(r);
+    unsigned char* line = tile + (quarter >> 1) * kAttnPart + row * 128;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        uint4 w;
+        w.x = pack_bf16(__uint_as_float(r[8 * c]) * mul, __uint_as_float(r[8 * c + 1]) * mul);
+        w.y = pack_bf16(__uint_as_float(r[8 * c + 2]) * mul, __uint_as_float(r[8 * c + 3]) * mul);
+        w.z = pack_bf16(__uint_as_float(r[8 * c + 4]) * mul, __uint_as_float(r[8 * c + 5]) * mul);
+        w.w = pack_bf16(__uint_as_float(r[8 * c + 6]) * mul, __uint_as_float(r[8 * c + 7]) * mul);
+        if (!keep) w = make_uint4(0u, 0u, 0u, 0u);
+        *reinterpret_cast<uint4*>(line + ((((quarter & 1) * 4 + c) ^ (row & 7)) * 16)) = w;
+    }
+}
+
+template <int NH>
+__global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __grid_constant__ BwdMaps m, const BwdParams p) {
+    using R = BwdRings<NH>;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    float *stat0 = reinterpret_cast<float*>(smem + R::kTiles), *stat1 = stat0 + R::kB0 * kAttnTile;
+    BwdBars<NH>& bar = *reinterpret_cast<BwdBars<NH>*>(smem + R::kTiles + R::kStats);
+    const AttnShape& s = p.s;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if ((smem_u32(smem) & 1023u) != 0) {                       // the tiles' swizzle needs it; dynamic shared memory begins there
+        if (threadIdx.x == 0 && p.dev_status != nullptr) atomicExch(p.dev_status, kStatusBwdSmem);
+        return;
+    }
     if (threadIdx.x == 0) {
-        mbar_init(&bar.keep, 1);
-        for (int i = 0; i < kBwdStages; ++i) { mbar_init(&bar.full[i], 1); mbar_init(&bar.empty[i], 1); }
-        mbar_init(&bar.s, 1); mbar_init(&bar.dp, 1); mbar_init(&bar.acc, 1);
-        mbar_init(&bar.read, kBwdWarps); mbar_init(&bar.p, kBwdWarps); mbar_init(&bar.ds, kBwdWarps);
+        for (int i = 0; i < R::kKeep; ++i) { mbar_init(&bar.keep_full[i], 1); mbar_init(&bar.keep_empty[i], 1); }
+        for (int i = 0; i < R::kB0; ++i) { mbar_init(&bar.b0_full[i], 1); mbar_init(&bar.b0_empty[i], 1); }
+        for (int i = 0; i < R::kB1; ++i) { mbar_init(&bar.b1_full[i], 1); mbar_init(&bar.b1_empty[i], 1); }
+        mbar_init(&bar.s, 1); mbar_init(&bar.p, kBwdWarps); mbar_init(&bar.acc, 1);
+        for (int i = 0; i < R::kKeep; ++i) mbar_init(&bar.staged[i], kBwdWarps);
+        for (int i = 0; i < 2; ++i) { mbar_init(&bar.dp[i], 1); mbar_init(&bar.ds[i], kBwdWarps); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&bar.item_full[i], 1); mbar_init(&bar.item_empty[i], kBwdWarps + 2); }
         fence_barrier_init();
     }
-    if (warp == kBwdWarps + 1) { __syncwarp(); tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
+    if (warp == kBwdWarps && lane < 7) tma_prefetch_desc(&m.q + lane);
+    if (warp == kBwdWarps + 1) { __syncwarp(); tmem_alloc(&bar.tmem_slot, 512); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem_base = tmem_slot;
-    // tiles of keys first (they walk every head of their group), then tiles of queries; under the causal mask the first keys and
-    // the last queries walk the most
-    if (blockIdx.x < p.key_ctas) {
-        const unsigned per = unsigned(s.Nb) * unsigned(s.kv_heads), tile = blockIdx.x / per, bh = blockIdx.x - tile * per;
-        const int n = int(bh / s.kv_heads);
-        bwd_run<NH, true>(&tmK, &tmV, &tmQ, &tmDo, p, smem, bar, tmem_base, n, int(bh) - n * s.kv_heads, int(tile), attn_sample(s, n));
+    const uint32_t tmem_base = bar.tmem_slot;
+
+    if (warp == kBwdWarps) {
+        if (elect_one()) bwd_load<NH>(m, p, smem, stat0, stat1, bar);
+        __syncwarp();
+    } else if (warp == kBwdWarps + 1) {
+        bwd_issue<NH>(p, smem, bar, tmem_base, lane);
+    } else if (warp == kBwdWarps + 2) {
+        RingAt<2> told;
+        RingAt<R::kKeep> keep;
+        for (;;) {
+            const unsigned index = bwd_next<NH>(p, bar, told, lane);
+            if (index >= p.items) break;
+            const BwdItem t = bwd_item(p, index);
+            if (t.total == 0) continue;
+            if (!__all_sync(0xffffffffu, mbar_wait(&bar.staged[keep.slot], keep.phase, p.dev_status, kStatusBwdWait))) break;
+            if (elect_one()) {
+                const unsigned char* from = smem + 2 * keep.slot * R::kTile;
+#pragma unroll
+                for (int h = 0; h < NH; ++h) tma_store_4d(t.keys ? &m.dk : &m.dq, from + h * kAttnPart, 64 * h, t.head, t.row0, t.n);
+                if (t.keys) {
+#pragma unroll
+                    for (int h = 0; h < NH; ++h) tma_store_4d(&m.dv, from + R::kTile + h * kAttnPart, 64 * h, t.head, t.row0, t.n);
+                }
+                bulk_commit_group();
+                bulk_wait_read_all();
+                mbar_arrive(&bar.keep_empty[keep.slot]);
+            }
+            __syncwarp();
+            keep.next();
+        }
     } else {
-        const unsigned b = blockIdx.x - p.key_ctas, per = unsigned(s.Nb) * unsigned(s.heads), block = b / per, bh = b - block * per;
-        const int n = int(bh / s.heads), tile = s.causal ? p.q_tiles - 1 - int(block) : int(block);
-        bwd_run<NH, false>(&tmQ, &tmDo, &tmK, &tmV, p, smem, bar, tmem_base, n, int(bh) - n * s.heads, tile, attn_sample(s, n));
+        const int quarter = warp >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t t_lane = tmem_base + (uint32_t((warp & 3) * 32) << 16), t_s = t_lane + uint32_t(quarter * 32);
+        RingAt<2> told;
+        RingAt<R::kKeep> keep;
+        RingAt<R::kB0> b0;
+        RingAt<R::kB1> b1;
+        uint32_t step = 0, item_par = 0;
+        for (;;) {
+            const unsigned index = bwd_next<NH>(p, bar, told, lane);
+            if (index >= p.items) break;
+            const BwdItem t = bwd_item(p, index);
+            if (t.total == 0) {                                // nothing seen: the gradient is zero
+                if (t.keys) {
+                    const int rows = min(kAttnTile, s.Lk - t.row0);
+                    const int64_t at = int64_t(t.n) * s.Lk + t.row0;
+                    zero_rows(p.dk + at * p.lddk + t.head * s.dh, p.lddk, rows, s.dh, kBwdWarps * 32);
+                    zero_rows(p.dv + at * p.lddv + t.head * s.dh, p.lddv, rows, s.dh, kBwdWarps * 32);
+                } else {
+                    zero_rows(p.dq + (int64_t(t.n) * s.Lq + t.row0) * p.lddq + t.head * s.dh, p.lddq, min(kAttnTile, s.Lq - t.row0), s.dh, kBwdWarps * 32);
+                }
+                continue;
+            }
+            const int r = t.row0 + row;
+            const bool done = t.keys ? bwd_probabilities<NH, true>(p, t, stat0, stat1, bar, b0, b1, step, t_s, r, quarter, lane)
+                                     : bwd_probabilities<NH, false>(p, t, stat0, stat1, bar, b0, b1, step, t_s, r, quarter, lane);
+            if (!done || !__all_sync(0xffffffffu, mbar_wait(&bar.acc, item_par, p.dev_status, kStatusBwdWait))) break;
+            tc_fence_after();
+            unsigned char* stage = smem + 2 * keep.slot * R::kTile;
+            const bool kept = t.keys ? r < t.sm.kl : r >= t.sm.q_lo && r < t.sm.q_hi;
+            stage_rows<NH>(t_s + 384u, stage, row, quarter, s.dh, kept, s.scale);
+            if (t.keys) stage_rows<NH>(t_s + 256u, stage + R::kTile, row, quarter, s.dh, kept, 1.0f);
+            tc_fence_before();
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.staged[keep.slot]);
+            keep.next();
+            item_par ^= 1u;
+        }
     }
     tc_fence_before();
     __syncthreads();
     if (warp == kBwdWarps + 1) tmem_dealloc(tmem_base, 512);
 }
 
-// Per query and head: D = dout . out in fp32, and lse * log2(e), in tiles of 128 rows as the gradient kernel loads them.  Rows without
-// a key, outside the lengths or behind the last get lse = +inf and D = 0: their probabilities are exp2(-inf) = 0.  A group of
-// dh / 8 lanes takes a row; memory-bound, two reads.
+// Per query and head: -D, D = dout . out in fp32, and -lse * log2(e), in tiles of 128 rows as the gradient kernel loads them.  Rows
+// without a key, outside the lengths or behind the last get lse = +inf and D = 0: their probabilities are exp2(-inf) = 0.  A group of
+// dh / 8 lanes takes a row; memory-bound, two reads.  Also clears the count of items taken.
 __global__ void __launch_bounds__(256) attention_stats_kernel(const __nv_bfloat16* out, int64_t ldo, const __nv_bfloat16* dout, int64_t lddo,
-                                                              const float* lse, const AttnShape s, int q_tiles, float* stats) {
+                                                              const float* lse, const AttnShape s, int q_tiles, float* stats, unsigned* taken) {
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *taken = 0u;
     const int v = s.dh / 8, per_warp = 32 / v, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int sub = lane / v, pos = lane - sub * v;
     const int bh = blockIdx.y, n = bh / s.heads, head = bh - n * s.heads;
@@ -380,34 +546,39 @@ __global__ void __launch_bounds__(256) attention_stats_kernel(const __nv_bfloat1
         }
         if (mine && pos == 0) {
             float* to = stats + (int64_t(bh) * q_tiles + i / kAttnTile) * (2 * kAttnTile) + i % kAttnTile;
-            float l = INFINITY;
+            float l = -INFINITY;
             if (live) {
                 const float given = __ldg(lse + int64_t(bh) * s.Lq + i);
-                if (given != -INFINITY) l = given * 1.4426950408889634f;
+                if (given != -INFINITY) l = given * -1.4426950408889634f;
             }
             to[0] = l;
-            to[kAttnTile] = d;
+            to[kAttnTile] = -d;
         }
     }
 }
 
 template <int NH>
 hq_status launch_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* dout, int64_t lddo,
-                     const BwdParams& p, unsigned grid, cudaStream_t st) {
+                     const BwdParams& p, cudaStream_t st) {
     const AttnShape& s = p.s;
-    CUtensorMap tmQ, tmK, tmV, tmDo;
-    if (!encode_heads_bf16(&tmQ, q, s.dh, s.heads, s.Lq, s.Nb, ldq, kAttnTile) ||
-        !encode_heads_bf16(&tmK, k, s.dh, s.kv_heads, s.Lk, s.Nb, ldk, kAttnTile) ||
-        !encode_heads_bf16(&tmV, v, s.dh, s.kv_heads, s.Lk, s.Nb, ldv, kAttnTile) ||
-        !encode_heads_bf16(&tmDo, dout, s.dh, s.heads, s.Lq, s.Nb, lddo, kAttnTile))
+    BwdMaps m;
+    if (!encode_heads_bf16(&m.q, q, s.dh, s.heads, s.Lq, s.Nb, ldq, kAttnTile) ||
+        !encode_heads_bf16(&m.k, k, s.dh, s.kv_heads, s.Lk, s.Nb, ldk, kAttnTile) ||
+        !encode_heads_bf16(&m.v, v, s.dh, s.kv_heads, s.Lk, s.Nb, ldv, kAttnTile) ||
+        !encode_heads_bf16(&m.dout, dout, s.dh, s.heads, s.Lq, s.Nb, lddo, kAttnTile) ||
+        !encode_heads_bf16(&m.dq, p.dq, s.dh, s.heads, s.Lq, s.Nb, p.lddq, kAttnTile) ||
+        !encode_heads_bf16(&m.dk, p.dk, s.dh, s.kv_heads, s.Lk, s.Nb, p.lddk, kAttnTile) ||
+        !encode_heads_bf16(&m.dv, p.dv, s.dh, s.kv_heads, s.Lk, s.Nb, p.lddv, kAttnTile))
         return HQ_ERR_CUDA;
     if (cudaFuncSetAttribute(attention_bwd_kernel<NH>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bwd_smem<NH>())) != cudaSuccess)
         return HQ_ERR_CUDA;
-    attention_bwd_kernel<NH><<<grid, kBwdThreads, bwd_smem<NH>(), st>>>(tmQ, tmK, tmV, tmDo, p);
+    const unsigned sms = unsigned(sm_count()), grid = p.items < sms ? p.items : sms;
+    attention_bwd_kernel<NH><<<grid, kBwdThreads, bwd_smem<NH>(), st>>>(m, p);
     return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }
 
-int64_t stats_bytes(int64_t Nb, int64_t Lq, int heads) { return Nb * heads * ((Lq + kAttnTile - 1) / kAttnTile) * kStatBytes; }
+// statistics, then the count of items taken
+int64_t stats_bytes(int64_t Nb, int64_t Lq, int heads) { return Nb * heads * ((Lq + kAttnTile - 1) / kAttnTile) * 2 * kStatBytes; }
 
 }  // namespace
 }  // namespace hq
@@ -417,7 +588,7 @@ extern "C" hq_status hq_attention_bwd_workspace_size(int64_t Nb, int64_t Lq, int
     if (bytes == nullptr) return HQ_ERR_INVALID_ARG;
     const hq_status e = attn_check(Nb, Lq, Lk, heads, kv_heads, dh, 1.0f);
     if (e != HQ_OK) return e;
-    *bytes = size_t(stats_bytes(Nb, Lq, heads));
+    *bytes = size_t(stats_bytes(Nb, Lq, heads)) + 16;
     return HQ_OK;
 }
 
@@ -437,23 +608,25 @@ extern "C" hq_status hq_attention_bwd(const void* q, int64_t ldq, const void* k,
         return e;
     if (lse == nullptr || workspace == nullptr) return HQ_ERR_INVALID_ARG;
     if (!aligned16(workspace)) return HQ_ERR_ALIGNMENT;
-    if (int64_t(ws_bytes) < stats_bytes(Nb, Lq, heads)) return HQ_ERR_WORKSPACE;
+    const int64_t stat_bytes = stats_bytes(Nb, Lq, heads);
+    if (int64_t(ws_bytes) < stat_bytes + 16) return HQ_ERR_WORKSPACE;
     const int64_t q_tiles = (Lq + kAttnTile - 1) / kAttnTile, k_tiles = (Lk + kAttnTile - 1) / kAttnTile;
-    const int64_t key_ctas = Nb * kv_heads * k_tiles, grid = key_ctas + Nb * heads * q_tiles;
-    if (grid > 0x7fffffff) return HQ_ERR_UNSUPPORTED;
+    const int64_t key_items = Nb * kv_heads * k_tiles, items = key_items + Nb * heads * q_tiles;
+    if (items > 0x3fffffff) return HQ_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     BwdParams p{};
     p.s = AttnShape{q_lens, k_lens, int(Nb), int(Lq), int(Lk), heads, kv_heads, dh, causal != 0, scale, float(double(scale) * 1.4426950408889634)};
     p.stats = static_cast<const float*>(workspace);
+    p.taken = reinterpret_cast<unsigned*>(static_cast<unsigned char*>(workspace) + stat_bytes);
     p.dq = static_cast<__nv_bfloat16*>(dq); p.dk = static_cast<__nv_bfloat16*>(dk); p.dv = static_cast<__nv_bfloat16*>(dv);
     p.lddq = lddq; p.lddk = lddk; p.lddv = lddv;
-    p.q_tiles = int(q_tiles); p.key_ctas = unsigned(key_ctas); p.dev_status = dev_status;
+    p.q_tiles = int(q_tiles); p.key_items = unsigned(key_items); p.items = unsigned(items); p.dev_status = dev_status;
     const int rows_per_cta = 8 * (32 / (dh / 8));
     int64_t stat_ctas = (q_tiles * kAttnTile + rows_per_cta - 1) / rows_per_cta;
     if (stat_ctas > 64) stat_ctas = 64;
     attention_stats_kernel<<<dim3(unsigned(stat_ctas), unsigned(Nb * heads)), 256, 0, st>>>(
-        static_cast<const __nv_bfloat16*>(out), ldo, static_cast<const __nv_bfloat16*>(dout), lddo, lse, p.s, p.q_tiles, static_cast<float*>(workspace));
+        static_cast<const __nv_bfloat16*>(out), ldo, static_cast<const __nv_bfloat16*>(dout), lddo, lse, p.s, p.q_tiles,
+        static_cast<float*>(workspace), p.taken);
     if (cudaGetLastError() != cudaSuccess) return HQ_ERR_CUDA;
-    return dh <= 64 ? launch_bwd<1>(q, ldq, k, ldk, v, ldv, dout, lddo, p, unsigned(grid), st)
-                    : launch_bwd<2>(q, ldq, k, ldk, v, ldv, dout, lddo, p, unsigned(grid), st);
+    return dh <= 64 ? launch_bwd<1>(q, ldq, k, ldk, v, ldv, dout, lddo, p, st) : launch_bwd<2>(q, ldq, k, ldk, v, ldv, dout, lddo, p, st);
 }
