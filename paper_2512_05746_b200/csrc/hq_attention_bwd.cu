@@ -13,8 +13,8 @@
 // tensor memory (as operands of the second products they are read where they were written), no fp32 partial dq in memory and no
 // order of additions that changes from run to run.
 //
-// The kernel is persistent: a CTA takes an item (a tile of one kind), then the next that no other has taken.  Warps 0-15: thread =
-// lane, four warps per quarter of the 128 columns; warp 16 takes items and loads, warp 17 issues, warp 18 stores.  The tile an item keeps
+// The kernel is persistent: a CTA takes an item (a tile of one kind), then the next that no other has taken.  Warp 0 issues, warp 1
+// takes items and loads, warp 2 stores; warps 4-19: thread = lane, four warps per quarter of the 128 columns.  The tile an item keeps
 // (K and V, or Q and dout) stays in shared memory, where its gradient is staged at the end; the other side's two kinds of tiles come
 // through a ring each.
 #include "hq_attention_tile.cuh"
@@ -23,8 +23,9 @@ namespace hq {
 namespace {
 
 constexpr int32_t kStatusBwdWait = 0x710, kStatusBwdTma = 0x711, kStatusBwdSmem = 0x712;
-constexpr int kBwdWarps = 16;                                  // of the probabilities
-constexpr int kBwdThreads = (kBwdWarps + 3) * 32;
+constexpr int kBwdWarps = 16, kBwdFirst = 4;                   // of the probabilities; in front of them the others (the issuing warp
+                                                               // is the oldest of its scheduler's)
+constexpr int kBwdThreads = (kBwdFirst + kBwdWarps) * 32;
 constexpr uint32_t kStatBytes = kAttnTile * 4;                 // of one query tile: -lse * log2(e), and as many for -D
 
 // Rings: tiles of 16 KB up to 64 channels, 32 KB above, where two kept tiles, three and two take all but 2 KB of the shared memory.
@@ -95,7 +96,7 @@ __device__ __forceinline__ BwdItem bwd_item(const BwdParams& p, unsigned index) 
     return t;
 }
 
-// ---- warp 16, one lane: takes items, tells the others, loads their tiles
+// ---- warp 1, one lane: takes items, tells the others, loads their tiles
 template <int NH>
 __device__ __forceinline__ void bwd_load(const BwdMaps& m, const BwdParams& p, unsigned char* smem, float* stat0, float* stat1, BwdBars<NH>& bar) {
     using R = BwdRings<NH>;
@@ -109,7 +110,7 @@ __device__ __forceinline__ void bwd_load(const BwdMaps& m, const BwdParams& p, u
     bool ok = true;
     unsigned index = blockIdx.x;
     while (ok) {
-        ok = mbar_wait(&bar.item_empty[told.slot], told.phase ^ 1u, p.dev_status, kStatusBwdWait);
+        ok = mbar_wait_lane(&bar.item_empty[told.slot], told.phase ^ 1u, p.dev_status, kStatusBwdWait);
         if (!ok) break;
         bar.item[told.slot] = index;
         mbar_arrive(&bar.item_full[told.slot]);
@@ -119,7 +120,7 @@ __device__ __forceinline__ void bwd_load(const BwdMaps& m, const BwdParams& p, u
         const BwdItem t = bwd_item(p, index);
         index = following;
         if (t.total == 0) continue;
-        ok = mbar_wait(&bar.keep_empty[keep.slot], keep.phase ^ 1u, p.dev_status, kStatusBwdWait);
+        ok = mbar_wait_lane(&bar.keep_empty[keep.slot], keep.phase ^ 1u, p.dev_status, kStatusBwdWait);
         if (!ok) break;
         unsigned char* to = smem + 2 * keep.slot * R::kTile;
         mbar_expect_tx(&bar.keep_full[keep.slot], 2 * R::kTile);
@@ -130,14 +131,14 @@ __device__ __forceinline__ void bwd_load(const BwdMaps& m, const BwdParams& p, u
         int head = t.keys ? t.head * group : t.head / group, tile = t.first;
         for (int i = 0; i < t.total; ++i) {
             const float* stats = p.stats + (int64_t(t.n * p.s.heads + head) * p.q_tiles + tile) * (2 * kAttnTile);
-            ok = mbar_wait(&bar.b0_empty[b0.slot], b0.phase ^ 1u, p.dev_status, kStatusBwdWait);
+            ok = mbar_wait_lane(&bar.b0_empty[b0.slot], b0.phase ^ 1u, p.dev_status, kStatusBwdWait);
             if (!ok) break;
             mbar_expect_tx(&bar.b0_full[b0.slot], R::kTile + (t.keys ? kStatBytes : 0));
             load_tile<NH>(sB0 + b0.slot * R::kTile, t.keys ? &m.q : &m.k, &bar.b0_full[b0.slot], head, tile * kAttnTile, t.n);
             if (t.keys) bulk_load(stat0 + b0.slot * kAttnTile, stats, kStatBytes, &bar.b0_full[b0.slot]);
             b0.next();
             ++n0;
-            ok = mbar_wait(&bar.b1_empty[b1.slot], b1.phase ^ 1u, p.dev_status, kStatusBwdWait);
+            ok = mbar_wait_lane(&bar.b1_empty[b1.slot], b1.phase ^ 1u, p.dev_status, kStatusBwdWait);
             if (!ok) break;
             mbar_expect_tx(&bar.b1_full[b1.slot], R::kTile + (t.keys ? kStatBytes : 0));
             load_tile<NH>(sB1 + b1.slot * R::kTile, t.keys ? &m.dout : &m.v, &bar.b1_full[b1.slot], head, tile * kAttnTile, t.n);
@@ -148,15 +149,15 @@ __device__ __forceinline__ void bwd_load(const BwdMaps& m, const BwdParams& p, u
         }
     }
     // what was requested lands before the CTA's shared memory is given up, on every way out
-    for (int i = max(0, keeps - R::kKeep); i < keeps; ++i) mbar_wait(&bar.keep_full[i % R::kKeep], uint32_t(i / R::kKeep) & 1u, nullptr, 0);
-    for (int i = max(0, n0 - R::kB0); i < n0; ++i) mbar_wait(&bar.b0_full[i % R::kB0], uint32_t(i / R::kB0) & 1u, nullptr, 0);
-    for (int i = max(0, n1 - R::kB1); i < n1; ++i) mbar_wait(&bar.b1_full[i % R::kB1], uint32_t(i / R::kB1) & 1u, nullptr, 0);
+    for (int i = max(0, keeps - R::kKeep); i < keeps; ++i) mbar_wait_lane(&bar.keep_full[i % R::kKeep], uint32_t(i / R::kKeep) & 1u, nullptr, 0);
+    for (int i = max(0, n0 - R::kB0); i < n0; ++i) mbar_wait_lane(&bar.b0_full[i % R::kB0], uint32_t(i / R::kB0) & 1u, nullptr, 0);
+    for (int i = max(0, n1 - R::kB1); i < n1; ++i) mbar_wait_lane(&bar.b1_full[i % R::kB1], uint32_t(i / R::kB1) & 1u, nullptr, 0);
 }
 
 // The next item's number (p.items and beyond: none, or a wait ran out), the same in every lane.
 template <int NH>
 __device__ __forceinline__ unsigned bwd_next(const BwdParams& p, BwdBars<NH>& bar, RingAt<2>& told, int lane) {
-    if (!__all_sync(0xffffffffu, mbar_wait(&bar.item_full[told.slot], told.phase, p.dev_status, kStatusBwdWait))) return 0xffffffffu;
+    if (!mbar_wait_warp(&bar.item_full[told.slot], told.phase, p.dev_status, kStatusBwdWait)) return 0xffffffffu;
     const unsigned index = *const_cast<volatile uint32_t*>(&bar.item[told.slot]);
     __syncwarp();
     if (lane == 0) mbar_arrive(&bar.item_empty[told.slot]);
@@ -164,7 +165,7 @@ __device__ __forceinline__ unsigned bwd_next(const BwdParams& p, BwdBars<NH>& ba
     return index;
 }
 
-// ---- warp 17: products.  Tensor memory: S at columns 0, dP at 128; keys: dv at 256, dk at 384; queries: dP's second buffer at 256,
+// ---- warp 0: products.  Tensor memory: S at columns 0, dP at 128; keys: dv at 256, dk at 384; queries: dP's second buffer at 256,
 // dq at 384.  Products run in the order of their issue: one that overwrites another's operand or result in tensor memory, or an
 // accumulator that the other warps have read before they handed over the operand it waits for, is issued behind it.
 template <int NH>
@@ -180,9 +181,10 @@ __device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* sme
     const uint64_t dB0t = make_sw128_mnmajor_desc(smem_u32(sB0), kAttnPart), dB1t = make_sw128_mnmajor_desc(smem_u32(sB1), kAttnPart);
     constexpr uint64_t kTileUnits = R::kTile >> 4;
     auto score_product = [&](uint64_t a, uint64_t b, uint32_t column) {
-        for (int k = 0; k < ksteps; ++k) {
+#pragma unroll
+        for (int k = 0; k < 4 * NH; ++k) {
             const uint64_t step = uint64_t((k >> 2) * (kAttnPart >> 4) + 2 * (k & 3));
-            mma_bf16(tmem_base + column, a + step, b + step, idesc_s, k != 0 ? 1u : 0u);
+            if (k < ksteps) mma_bf16(tmem_base + column, a + step, b + step, idesc_s, k != 0 ? 1u : 0u);
         }
     };
     // bf16 operand of each quarter in the first half of its 32 columns
@@ -192,7 +194,7 @@ __device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* sme
             mma_bf16_ts(tmem_base + acc, tmem_base + column + uint32_t((k >> 1) * 32 + (k & 1) * 8), b + uint64_t(k * 128), idesc_acc,
                         add || k != 0 ? 1u : 0u);
     };
-    auto wait = [&](uint64_t* b, uint32_t parity, int32_t code) { return __all_sync(0xffffffffu, mbar_wait(b, parity, p.dev_status, code)); };
+    auto wait = [&](uint64_t* b, uint32_t parity, int32_t code) { return mbar_wait_warp(b, parity, p.dev_status, code); };
     RingAt<R::kKeep> keep;
     RingAt<R::kB0> s0, a0;                         // B0's tile of the next score product / of the next sum
     RingAt<R::kB1> s1, a1;
@@ -275,7 +277,7 @@ __device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* sme
     }
 }
 
-// ---- warps 0-15: probabilities and their gradients
+// ---- warps 4-19: probabilities and their gradients
 template <int NH, bool KEYS>
 __device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdItem& t, const float* stat0, const float* stat1, BwdBars<NH>& bar,
                                                   RingAt<BwdRings<NH>::kB0>& b0, RingAt<BwdRings<NH>::kB1>& b1, uint32_t& step,
@@ -296,10 +298,8 @@ __device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdI
     for (int i = 0; i < t.total; ++i) {
         const int c0 = tile * kAttnTile + quarter * 32;        // the first column's query or key
         if (++tile == t.last) tile = t.first;
-        bool ok = mbar_wait(&bar.s, step & 1u, p.dev_status, kStatusBwdWait);
-        if (KEYS) ok = ok && mbar_wait(&bar.b0_full[b0.slot], b0.phase, p.dev_status, kStatusBwdTma) &&
-                       mbar_wait(&bar.b1_full[b1.slot], b1.phase, p.dev_status, kStatusBwdTma);
-        if (!__all_sync(0xffffffffu, ok)) return false;
+        if (!mbar_wait_warp(&bar.s, step & 1u, p.dev_status, kStatusBwdWait)) return false;
+        if (KEYS && !mbar_wait_warp(&bar.b0_full[b0.slot], b0.phase, p.dev_status, kStatusBwdTma)) return false;
         tc_fence_after();
         uint32_t sr[32], w[16];
         tmem_ld_32x32(t_s, sr);
@@ -347,7 +347,8 @@ __device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdI
             __syncwarp();
             if (lane == 0) mbar_arrive(&bar.p);
         }
-        if (!__all_sync(0xffffffffu, mbar_wait(&bar.dp[step & 1u], (step >> 1) & 1u, p.dev_status, kStatusBwdWait))) return false;
+        if (!mbar_wait_warp(&bar.dp[step & 1u], (step >> 1) & 1u, p.dev_status, kStatusBwdWait)) return false;
+        if (KEYS && !mbar_wait_warp(&bar.b1_full[b1.slot], b1.phase, p.dev_status, kStatusBwdTma)) return false;
         tc_fence_after();
         const uint32_t t_dp = t_s + (KEYS || !(i & 1) ? 128u : 256u);
         const float* nd = stat1 + b1.slot * kAttnTile + quarter * 32;
@@ -432,19 +433,19 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
         for (int i = 0; i < 2; ++i) { mbar_init(&bar.item_full[i], 1); mbar_init(&bar.item_empty[i], kBwdWarps + 2); }
         fence_barrier_init();
     }
-    if (warp == kBwdWarps && lane < 7) tma_prefetch_desc(&m.q + lane);
-    if (warp == kBwdWarps + 1) { __syncwarp(); tmem_alloc(&bar.tmem_slot, 512); tmem_relinquish(); }
+    if (warp == 1 && lane < 7) tma_prefetch_desc(&m.q + lane);
+    if (warp == 0) { __syncwarp(); tmem_alloc(&bar.tmem_slot, 512); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = bar.tmem_slot;
 
-    if (warp == kBwdWarps) {
+    if (warp == 1) {
         if (elect_one()) bwd_load<NH>(m, p, smem, stat0, stat1, bar);
         __syncwarp();
-    } else if (warp == kBwdWarps + 1) {
+    } else if (warp == 0) {
         bwd_issue<NH>(p, smem, bar, tmem_base, lane);
-    } else if (warp == kBwdWarps + 2) {
+    } else if (warp == 2) {
         RingAt<2> told;
         RingAt<R::kKeep> keep;
         for (;;) {
@@ -452,7 +453,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
             if (index >= p.items) break;
             const BwdItem t = bwd_item(p, index);
             if (t.total == 0) continue;
-            if (!__all_sync(0xffffffffu, mbar_wait(&bar.staged[keep.slot], keep.phase, p.dev_status, kStatusBwdWait))) break;
+            if (!mbar_wait_warp(&bar.staged[keep.slot], keep.phase, p.dev_status, kStatusBwdWait)) break;
             if (elect_one()) {
                 const unsigned char* from = smem + 2 * keep.slot * R::kTile;
 #pragma unroll
@@ -468,8 +469,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
             __syncwarp();
             keep.next();
         }
-    } else {
-        const int quarter = warp >> 2, row = (warp & 3) * 32 + lane;
+    } else if (warp >= kBwdFirst) {
+        const int quarter = (warp - kBwdFirst) >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t t_lane = tmem_base + (uint32_t((warp & 3) * 32) << 16), t_s = t_lane + uint32_t(quarter * 32);
         RingAt<2> told;
         RingAt<R::kKeep> keep;
@@ -484,17 +485,17 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
                 if (t.keys) {
                     const int rows = min(kAttnTile, s.Lk - t.row0);
                     const int64_t at = int64_t(t.n) * s.Lk + t.row0;
-                    zero_rows(p.dk + at * p.lddk + t.head * s.dh, p.lddk, rows, s.dh, kBwdWarps * 32);
-                    zero_rows(p.dv + at * p.lddv + t.head * s.dh, p.lddv, rows, s.dh, kBwdWarps * 32);
+                    zero_rows(p.dk + at * p.lddk + t.head * s.dh, p.lddk, rows, s.dh, int(threadIdx.x) - kBwdFirst * 32, kBwdWarps * 32);
+                    zero_rows(p.dv + at * p.lddv + t.head * s.dh, p.lddv, rows, s.dh, int(threadIdx.x) - kBwdFirst * 32, kBwdWarps * 32);
                 } else {
-                    zero_rows(p.dq + (int64_t(t.n) * s.Lq + t.row0) * p.lddq + t.head * s.dh, p.lddq, min(kAttnTile, s.Lq - t.row0), s.dh, kBwdWarps * 32);
+                    zero_rows(p.dq + (int64_t(t.n) * s.Lq + t.row0) * p.lddq + t.head * s.dh, p.lddq, min(kAttnTile, s.Lq - t.row0), s.dh, int(threadIdx.x) - kBwdFirst * 32, kBwdWarps * 32);
                 }
                 continue;
             }
             const int r = t.row0 + row;
             const bool done = t.keys ? bwd_probabilities<NH, true>(p, t, stat0, stat1, bar, b0, b1, step, t_s, r, quarter, lane)
                                      : bwd_probabilities<NH, false>(p, t, stat0, stat1, bar, b0, b1, step, t_s, r, quarter, lane);
-            if (!done || !__all_sync(0xffffffffu, mbar_wait(&bar.acc, item_par, p.dev_status, kStatusBwdWait))) break;
+            if (!done || !mbar_wait_warp(&bar.acc, item_par, p.dev_status, kStatusBwdWait)) break;
             tc_fence_after();
             unsigned char* stage = smem + 2 * keep.slot * R::kTile;
             const bool kept = t.keys ? r < t.sm.kl : r >= t.sm.q_lo && r < t.sm.q_hi;
@@ -510,7 +511,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == kBwdWarps + 1) tmem_dealloc(tmem_base, 512);
+    if (warp == 0) tmem_dealloc(tmem_base, 512);
 }
 
 // Per query and head: -D, D = dout . out in fp32, and -lse * log2(e), in tiles of 128 rows as the gradient kernel loads them.  Rows

@@ -73,10 +73,10 @@ __device__ __forceinline__ void store_rows(uint32_t taddr, __nv_bfloat16* dst, i
         }
     }
 }
-// Zeros for `rows` rows of one head: the CTA's first `threads` threads.
-__device__ __forceinline__ void zero_rows(__nv_bfloat16* base, int64_t ld, int rows, int dh, int threads) {
+// Zeros for `rows` rows of one head, by `threads` threads.
+__device__ __forceinline__ void zero_rows(__nv_bfloat16* base, int64_t ld, int rows, int dh, int thread, int threads) {
     const int v = dh / 8;
-    for (int f = threadIdx.x; f < rows * v; f += threads) {
+    for (int f = thread; f < rows * v; f += threads) {
         const int row = f / v;
         *reinterpret_cast<uint4*>(base + int64_t(row) * ld + (f - row * v) * 8) = make_uint4(0u, 0u, 0u, 0u);
     }
