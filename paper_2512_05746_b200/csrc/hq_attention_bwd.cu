@@ -14,7 +14,7 @@
 // order of additions that changes from run to run.
 //
 // The kernel is persistent: a CTA takes an item (a tile of one kind), then the next that no other has taken.  Warp 0 issues, warp 1
-// takes items and loads, warp 2 stores, warp 3 clears rows outside the lengths; warps 4-19: thread = lane, four warps per quarter of the 128 columns.  The tile an item keeps
+// takes items and loads, warp 2 stores; warps 4-19: thread = lane, four warps per quarter of the 128 columns.  The tile an item keeps
 // (K and V, or Q and dout) stays in shared memory, where its gradient is staged at the end; the other side's two kinds of tiles come
 // through a ring each.
 #include "hq_attention_tile.cuh"
@@ -44,7 +44,6 @@ struct BwdParams {
     int64_t lddq, lddk, lddv;
     int q_tiles;
     unsigned key_items, items;
-    int ragged;                                    // rows outside the lengths may lie in a tile
     int32_t* dev_status;
 };
 struct BwdMaps { CUtensorMap q, k, v, dout, dq, dk, dv; };
@@ -52,8 +51,9 @@ struct BwdMaps { CUtensorMap q, k, v, dout, dq, dk, dv; };
 template <int NH> struct BwdBars {
     using R = BwdRings<NH>;
     uint64_t keep_full[R::kKeep], keep_empty[R::kKeep], b0_full[R::kB0], b0_empty[R::kB0], b1_full[R::kB1], b1_empty[R::kB1];
-    uint64_t b0_ready[R::kB0], b1_ready[R::kB1];               // landed, and cleared of rows outside the lengths
-    uint64_t s[2], p, dp, ds, acc, staged[R::kKeep], item_full[2], item_empty[2];
+    // dP and dS of a step alternate between two barriers: where the next dP does not wait for this dS, one could come round twice
+    // before a slow warp has looked at it
+    uint64_t s, p, dp[2], ds[2], acc, staged[R::kKeep], item_full[2], item_empty[2];
     uint32_t item[2], tmem_slot;
 };
 template <int NH> constexpr size_t bwd_smem() { return size_t(BwdRings<NH>::kTiles + BwdRings<NH>::kStats) + sizeof(BwdBars<NH>); }
@@ -165,56 +165,12 @@ __device__ __forceinline__ unsigned bwd_next(const BwdParams& p, BwdBars<NH>& ba
     return index;
 }
 
-// ---- warp 3: rows of tokens outside the lengths (zero as they come behind the last row of the matrix) are made zero where they would
-// meet zero probabilities in a sum: queries and their gradients, or keys
+// ---- warp 0: products.  Tensor memory: S at columns 0, dP at 128; keys: dv at 256, dk at 384; queries: dP's second buffer at 256,
+// dq at 384.  Products run in the order of their issue: one that overwrites another's operand or result in tensor memory, or an
+// accumulator that the other warps have read before they handed over the operand it waits for, is issued behind it.
 template <int NH>
-__device__ __forceinline__ void bwd_clear(const BwdParams& p, unsigned char* smem, BwdBars<NH>& bar, int lane) {
+__device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* smem, BwdBars<NH>& bar, uint32_t tmem_base, int lane) {
     using R = BwdRings<NH>;
-    unsigned char *sB0 = smem + 2 * R::kKeep * R::kTile, *sB1 = sB0 + R::kB0 * R::kTile;
-    RingAt<R::kB0> b0;
-    RingAt<R::kB1> b1;
-    RingAt<2> told;
-    for (;;) {
-        const unsigned index = bwd_next<NH>(p, bar, told, lane);
-        if (index >= p.items) return;
-        const BwdItem t = bwd_item(p, index);
-        const int lo = t.keys ? t.sm.q_lo : 0, hi = t.keys ? t.sm.q_hi : t.sm.kl, exist = t.keys ? p.s.Lq : p.s.Lk;
-        int tile = t.first;
-        for (int i = 0; i < t.total; ++i) {
-            const int r0 = tile * kAttnTile;
-            const bool partly = lo > r0 || hi < min(r0 + kAttnTile, exist);
-            if (++tile == t.last) tile = t.first;
-            if (!mbar_wait_warp(&bar.b0_full[b0.slot], b0.phase, p.dev_status, kStatusBwdTma)) return;
-            if (partly) clear_rows<NH>(sB0 + b0.slot * R::kTile, lo - r0, hi - r0, lane);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bar.b0_ready[b0.slot]);
-            if (!mbar_wait_warp(&bar.b1_full[b1.slot], b1.phase, p.dev_status, kStatusBwdTma)) return;
-            if (partly && t.keys) clear_rows<NH>(sB1 + b1.slot * R::kTile, lo - r0, hi - r0, lane);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bar.b1_ready[b1.slot]);
-            b0.next();
-            b1.next();
-        }
-    }
-}
-
-// Where a step's scores and dP stand in tensor memory, and the sums.  Two buffers of scores wherever there is room: the scores of
-// step i + 2 are then computed behind dS of step i, and no warp waits for scores.  With sums of 128 columns for keys there is not:
-// scores of step i + 1 come behind the product that reads P of step i, which stands in their place.
-template <int NH> struct BwdTmem {
-    static __device__ __forceinline__ bool two(bool keys) { return NH == 1 || !keys; }
-    static __device__ __forceinline__ uint32_t scores(bool keys, int i) { return two(keys) && (i & 1) ? (NH == 1 ? 128u : 256u) : 0u; }
-    static constexpr uint32_t kDp = NH == 1 ? 256u : 128u, kDv = NH == 1 ? 384u : 256u, kDk = NH == 1 ? 448u : 384u, kDq = kDk;
-};
-
-// ---- warp 0, one lane: products.  They run in the order of their issue: one that overwrites another's operand or result in tensor
-// memory, or an accumulator that the other warps have read before they handed over the operand it waits for, is issued behind it.
-template <int NH>
-__device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* smem, BwdBars<NH>& bar, uint32_t tmem_base) {
-    using R = BwdRings<NH>;
-    using T = BwdTmem<NH>;
     const AttnShape& s = p.s;
     unsigned char *sB0 = smem + 2 * R::kKeep * R::kTile, *sB1 = sB0 + R::kB0 * R::kTile;
     const uint32_t idesc_s = make_idesc_bf16(kAttnTile, kAttnTile, false);
@@ -225,9 +181,10 @@ __device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* sme
     const uint64_t dB0t = make_sw128_mnmajor_desc(smem_u32(sB0), kAttnPart), dB1t = make_sw128_mnmajor_desc(smem_u32(sB1), kAttnPart);
     constexpr uint64_t kTileUnits = R::kTile >> 4;
     auto score_product = [&](uint64_t a, uint64_t b, uint32_t column) {
-        for (int k = 0; k < ksteps; ++k) {         // a loop: unrolled under a condition it gave wrong products above 64 channels
+#pragma unroll
+        for (int k = 0; k < 4 * NH; ++k) {
             const uint64_t step = uint64_t((k >> 2) * (kAttnPart >> 4) + 2 * (k & 3));
-            mma_bf16(tmem_base + column, a + step, b + step, idesc_s, k != 0 ? 1u : 0u);
+            if (k < ksteps) mma_bf16(tmem_base + column, a + step, b + step, idesc_s, k != 0 ? 1u : 0u);
         }
     };
     // bf16 operand of each quarter in the first half of its 32 columns
@@ -237,69 +194,85 @@ __device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* sme
             mma_bf16_ts(tmem_base + acc, tmem_base + column + uint32_t((k >> 1) * 32 + (k & 1) * 8), b + uint64_t(k * 128), idesc_acc,
                         add || k != 0 ? 1u : 0u);
     };
-    auto wait = [&](uint64_t* b, uint32_t parity, int32_t code) { return mbar_wait_lane(b, parity, p.dev_status, code); };
-    RingAt<R::kKeep> keep, before;                 // before: the item in front of this one
+    auto wait = [&](uint64_t* b, uint32_t parity, int32_t code) { return mbar_wait_warp(b, parity, p.dev_status, code); };
+    RingAt<R::kKeep> keep;
     RingAt<R::kB0> s0, a0;                         // B0's tile of the next score product / of the next sum
     RingAt<R::kB1> s1, a1;
     RingAt<2> told;
-    uint32_t n_s = 0, n_p = 0, n_ds = 0;           // of each kind, over all items
-    bool any = false;
+    uint32_t step = 0;                             // over all items
     for (;;) {
-        if (!wait(&bar.item_full[told.slot], told.phase, kStatusBwdWait)) return;
-        const unsigned index = *const_cast<volatile uint32_t*>(&bar.item[told.slot]);
-        mbar_arrive(&bar.item_empty[told.slot]);
-        told.next();
+        const unsigned index = bwd_next<NH>(p, bar, told, lane);
         if (index >= p.items) return;
         const BwdItem t = bwd_item(p, index);
         if (t.total == 0) continue;
-        const bool keys = t.keys;
+        // rows of tokens outside the lengths (zero as they come behind the last row of the matrix) are made zero where they would
+        // meet zero probabilities in a sum: queries and their gradients, or keys
+        int tile = t.first;
+        const int outer_lo = t.keys ? t.sm.q_lo : 0, outer_hi = t.keys ? t.sm.q_hi : t.sm.kl, exist = t.keys ? s.Lq : s.Lk;
+        auto clear = [&](unsigned char* at, int which_tile) {
+            const int r0 = which_tile * kAttnTile;
+            if (outer_lo > r0 || outer_hi < min(r0 + kAttnTile, exist)) {
+                clear_rows<NH>(at, outer_lo - r0, outer_hi - r0, lane);
+                fence_proxy_async_smem();
+                __syncwarp();
+            }
+        };
         const uint64_t a = dA + uint64_t(keep.slot) * (2 * kTileUnits);
         if (!wait(&bar.keep_full[keep.slot], keep.phase, kStatusBwdTma)) return;
         keep.next();
-        auto scores = [&](int i) {                 // S of the item's step i
-            if (!wait(p.ragged ? &bar.b0_ready[s0.slot] : &bar.b0_full[s0.slot], s0.phase, kStatusBwdTma)) return false;
-            tc_fence_after();
-            score_product(a, dB0 + uint64_t(s0.slot) * kTileUnits, T::scores(keys, i));
-            mma_commit(&bar.s[n_s & 1u]);
-            ++n_s;
+        auto scores = [&](int which_tile) {        // S of the next tile
+            if (!wait(&bar.b0_full[s0.slot], s0.phase, kStatusBwdTma)) return false;
+            clear(sB0 + s0.slot * R::kTile, which_tile);
+            if (elect_one()) {
+                tc_fence_after();
+                score_product(a, dB0 + uint64_t(s0.slot) * kTileUnits, 0u);
+                mma_commit(&bar.s);
+            }
+            __syncwarp();
             s0.next();
             return true;
         };
-        auto dprobs = [&]() {                      // dP of the next step
-            if (!wait(p.ragged ? &bar.b1_ready[s1.slot] : &bar.b1_full[s1.slot], s1.phase, kStatusBwdTma)) return false;
-            tc_fence_after();
-            score_product(a + kTileUnits, dB1 + uint64_t(s1.slot) * kTileUnits, T::kDp);
-            mma_commit(&bar.dp);
-            if (!keys) mma_commit(&bar.b1_empty[s1.slot]);
+        auto dprobs = [&](int which_tile, uint32_t column, uint32_t of) {  // dP of the next tile, step `of`
+            if (!wait(&bar.b1_full[s1.slot], s1.phase, kStatusBwdTma)) return false;
+            if (t.keys) clear(sB1 + s1.slot * R::kTile, which_tile);
+            if (elect_one()) {
+                tc_fence_after();
+                score_product(a + kTileUnits, dB1 + uint64_t(s1.slot) * kTileUnits, column);
+                mma_commit(&bar.dp[of & 1u]);
+                if (!t.keys) mma_commit(&bar.b1_empty[s1.slot]);
+            }
+            __syncwarp();
             s1.next();
             return true;
         };
-        if (!scores(0) || !dprobs()) return;
-        if (T::two(keys) && t.total > 1) {
-            // above 64 channels the second buffer is where the sums of a tile of keys stand until they have been staged
-            if (NH == 2 && any && !wait(&bar.staged[before.slot], before.phase, kStatusBwdWait)) return;
-            if (!scores(1)) return;
-        }
-        if (any) before.next();
-        any = true;
+        if (!scores(tile) || !dprobs(tile, 128u, step)) return;
         for (int i = 0; i < t.total; ++i) {
             const bool more = i + 1 < t.total;
-            if (keys) {
-                if (!wait(&bar.p, n_p++ & 1u, kStatusBwdWait)) return;
-                tc_fence_after();
-                acc_product(T::scores(true, i), dB1t + uint64_t(a1.slot) * kTileUnits, T::kDv, i != 0);
-                if (!T::two(true) && more && !scores(i + 1)) return;
+            if (++tile == t.last) tile = t.first;
+            if (!wait(&bar.p, step & 1u, kStatusBwdWait)) return;
+            if (t.keys) {
+                if (elect_one()) {
+                    tc_fence_after();
+                    acc_product(0u, dB1t + uint64_t(a1.slot) * kTileUnits, 256u, i != 0);
+                }
+                __syncwarp();
+                if (more && !scores(tile)) return;
+            } else if (more) {
+                if (!scores(tile) || !dprobs(tile, 128u + 128u * uint32_t((i + 1) & 1), step + 1u)) return;
             }
-            if (!wait(&bar.ds, n_ds++ & 1u, kStatusBwdWait)) return;
-            tc_fence_after();
-            acc_product(T::kDp, dB0t + uint64_t(a0.slot) * kTileUnits, keys ? T::kDk : T::kDq, i != 0);
-            mma_commit(&bar.b0_empty[a0.slot]);
-            if (keys) mma_commit(&bar.b1_empty[a1.slot]);              // its statistics have been read by now
-            if (!more) mma_commit(&bar.acc);
+            if (!wait(&bar.ds[step & 1u], (step >> 1) & 1u, kStatusBwdWait)) return;
+            if (elect_one()) {
+                tc_fence_after();
+                acc_product(t.keys || !(i & 1) ? 128u : 256u, dB0t + uint64_t(a0.slot) * kTileUnits, 384u, i != 0);
+                mma_commit(&bar.b0_empty[a0.slot]);
+                if (t.keys) mma_commit(&bar.b1_empty[a1.slot]);        // its statistics have been read by now
+                if (!more) mma_commit(&bar.acc);
+            }
+            __syncwarp();
             a0.next();
             a1.next();
-            if (more && !dprobs()) return;
-            if (T::two(keys) && i + 2 < t.total && !scores(i + 2)) return;
+            if (t.keys && more && !dprobs(tile, 128u, step + 1u)) return;
+            ++step;
         }
     }
 }
@@ -308,7 +281,7 @@ __device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* sme
 template <int NH, bool KEYS>
 __device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdItem& t, const float* stat0, const float* stat1, BwdBars<NH>& bar,
                                                   RingAt<BwdRings<NH>::kB0>& b0, RingAt<BwdRings<NH>::kB1>& b1, uint32_t& step,
-                                                  uint32_t t_lane, int r, int quarter, int lane) {
+                                                  uint32_t t_s, int r, int quarter, int lane) {
     const AttnShape& s = p.s;
     const f32x2 sc2 = pk2(s.scale_log2, s.scale_log2);
     f32x2 row_lse = 0, row_d = 0;
@@ -325,13 +298,17 @@ __device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdI
     for (int i = 0; i < t.total; ++i) {
         const int c0 = tile * kAttnTile + quarter * 32;        // the first column's query or key
         if (++tile == t.last) tile = t.first;
-        if (!mbar_wait_warp(&bar.s[step & 1u], (step >> 1) & 1u, p.dev_status, kStatusBwdWait)) return false;
+        if (!mbar_wait_warp(&bar.s, step & 1u, p.dev_status, kStatusBwdWait)) return false;
         if (KEYS && !mbar_wait_warp(&bar.b0_full[b0.slot], b0.phase, p.dev_status, kStatusBwdTma)) return false;
         tc_fence_after();
-        const uint32_t t_s = t_lane + BwdTmem<NH>::scores(KEYS, i), t_dp = t_lane + BwdTmem<NH>::kDp;
         uint32_t sr[32], w[16];
         tmem_ld_32x32(t_s, sr);
         tmem_ld_wait_32(sr);
+        if (!KEYS) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.p);
+        }
         const float* nl = stat0 + b0.slot * kAttnTile + quarter * 32;
         f32x2 pr[16];
 #pragma unroll
@@ -370,9 +347,10 @@ __device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdI
             __syncwarp();
             if (lane == 0) mbar_arrive(&bar.p);
         }
-        if (!mbar_wait_warp(&bar.dp, step & 1u, p.dev_status, kStatusBwdWait)) return false;
+        if (!mbar_wait_warp(&bar.dp[step & 1u], (step >> 1) & 1u, p.dev_status, kStatusBwdWait)) return false;
         if (KEYS && !mbar_wait_warp(&bar.b1_full[b1.slot], b1.phase, p.dev_status, kStatusBwdTma)) return false;
         tc_fence_after();
+        const uint32_t t_dp = t_s + (KEYS || !(i & 1) ? 128u : 256u);
         const float* nd = stat1 + b1.slot * kAttnTile + quarter * 32;
         tmem_ld_32x32(t_dp, sr);
         tmem_ld_wait_32(sr);
@@ -405,7 +383,7 @@ __device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdI
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bar.ds);
+        if (lane == 0) mbar_arrive(&bar.ds[step & 1u]);
         b0.next();
         b1.next();
         ++step;
@@ -449,12 +427,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
         for (int i = 0; i < R::kKeep; ++i) { mbar_init(&bar.keep_full[i], 1); mbar_init(&bar.keep_empty[i], 1); }
         for (int i = 0; i < R::kB0; ++i) { mbar_init(&bar.b0_full[i], 1); mbar_init(&bar.b0_empty[i], 1); }
         for (int i = 0; i < R::kB1; ++i) { mbar_init(&bar.b1_full[i], 1); mbar_init(&bar.b1_empty[i], 1); }
-        for (int i = 0; i < R::kB0; ++i) mbar_init(&bar.b0_ready[i], 1);
-        for (int i = 0; i < R::kB1; ++i) mbar_init(&bar.b1_ready[i], 1);
-        mbar_init(&bar.s[0], 1); mbar_init(&bar.s[1], 1); mbar_init(&bar.dp, 1); mbar_init(&bar.acc, 1);
-        mbar_init(&bar.p, kBwdWarps); mbar_init(&bar.ds, kBwdWarps);
+        mbar_init(&bar.s, 1); mbar_init(&bar.p, kBwdWarps); mbar_init(&bar.acc, 1);
         for (int i = 0; i < R::kKeep; ++i) mbar_init(&bar.staged[i], kBwdWarps);
-        for (int i = 0; i < 2; ++i) { mbar_init(&bar.item_full[i], 1); mbar_init(&bar.item_empty[i], kBwdWarps + 2 + (p.ragged ? 1 : 0)); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&bar.dp[i], 1); mbar_init(&bar.ds[i], kBwdWarps); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&bar.item_full[i], 1); mbar_init(&bar.item_empty[i], kBwdWarps + 2); }
         fence_barrier_init();
     }
     if (warp == 1 && lane < 7) tma_prefetch_desc(&m.q + lane);
@@ -468,10 +444,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
         if (elect_one()) bwd_load<NH>(m, p, smem, stat0, stat1, bar);
         __syncwarp();
     } else if (warp == 0) {
-        if (elect_one()) bwd_issue<NH>(p, smem, bar, tmem_base);
-        __syncwarp();
-    } else if (warp == 3) {
-        if (p.ragged) bwd_clear<NH>(p, smem, bar, lane);
+        bwd_issue<NH>(p, smem, bar, tmem_base, lane);
     } else if (warp == 2) {
         RingAt<2> told;
         RingAt<R::kKeep> keep;
@@ -496,9 +469,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
             __syncwarp();
             keep.next();
         }
-    } else {
+    } else if (warp >= kBwdFirst) {
         const int quarter = (warp - kBwdFirst) >> 2, row = (warp & 3) * 32 + lane;
-        const uint32_t t_lane = tmem_base + (uint32_t((warp & 3) * 32) << 16) + uint32_t(quarter * 32);
+        const uint32_t t_lane = tmem_base + (uint32_t((warp & 3) * 32) << 16), t_s = t_lane + uint32_t(quarter * 32);
         RingAt<2> told;
         RingAt<R::kKeep> keep;
         RingAt<R::kB0> b0;
@@ -520,14 +493,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
                 continue;
             }
             const int r = t.row0 + row;
-            const bool done = t.keys ? bwd_probabilities<NH, true>(p, t, stat0, stat1, bar, b0, b1, step, t_lane, r, quarter, lane)
-                                     : bwd_probabilities<NH, false>(p, t, stat0, stat1, bar, b0, b1, step, t_lane, r, quarter, lane);
+            const bool done = t.keys ? bwd_probabilities<NH, true>(p, t, stat0, stat1, bar, b0, b1, step, t_s, r, quarter, lane)
+                                     : bwd_probabilities<NH, false>(p, t, stat0, stat1, bar, b0, b1, step, t_s, r, quarter, lane);
             if (!done || !mbar_wait_warp(&bar.acc, item_par, p.dev_status, kStatusBwdWait)) break;
             tc_fence_after();
             unsigned char* stage = smem + 2 * keep.slot * R::kTile;
             const bool kept = t.keys ? r < t.sm.kl : r >= t.sm.q_lo && r < t.sm.q_hi;
-            stage_rows<NH>(t_lane + (t.keys ? BwdTmem<NH>::kDk : BwdTmem<NH>::kDq), stage, row, quarter, s.dh, kept, s.scale);
-            if (t.keys) stage_rows<NH>(t_lane + BwdTmem<NH>::kDv, stage + R::kTile, row, quarter, s.dh, kept, 1.0f);
+            stage_rows<NH>(t_s + 384u, stage, row, quarter, s.dh, kept, s.scale);
+            if (t.keys) stage_rows<NH>(t_s + 256u, stage + R::kTile, row, quarter, s.dh, kept, 1.0f);
             tc_fence_before();
             fence_proxy_async_smem();
             __syncwarp();
@@ -648,8 +621,7 @@ extern "C" hq_status hq_attention_bwd(const void* q, int64_t ldq, const void* k,
     p.taken = reinterpret_cast<unsigned*>(static_cast<unsigned char*>(workspace) + stat_bytes);
     p.dq = static_cast<__nv_bfloat16*>(dq); p.dk = static_cast<__nv_bfloat16*>(dk); p.dv = static_cast<__nv_bfloat16*>(dv);
     p.lddq = lddq; p.lddk = lddk; p.lddv = lddv;
-    p.q_tiles = int(q_tiles); p.key_items = unsigned(key_items); p.items = unsigned(items);
-    p.ragged = q_lens != nullptr || k_lens != nullptr || (causal && Lq > Lk); p.dev_status = dev_status;
+    p.q_tiles = int(q_tiles); p.key_items = unsigned(key_items); p.items = unsigned(items); p.dev_status = dev_status;
     const int rows_per_cta = 8 * (32 / (dh / 8));
     int64_t stat_ctas = (q_tiles * kAttnTile + rows_per_cta - 1) / rows_per_cta;
     if (stat_ctas > 64) stat_ctas = 64;
