@@ -27,7 +27,7 @@ struct RopeParams {
     float* partial;                                // gradient of gamma: [2][blocks][dh]
 };
 constexpr int kRopeThreads = 256;
-constexpr int kRopeMaxBlocks = 1184;               // CTAs whose partial sums of gamma's gradient the workspace holds (148 SMs x 8)
+constexpr int kRopeMaxBlocks = 1184;               // 8 CTAs for each of 148 SMs, on every device: gamma's gradient is summed in one order
 
 template <typename T> struct Vec8;
 template <> struct Vec8<__nv_bfloat16> {
@@ -75,29 +75,57 @@ __device__ __forceinline__ float group_sum(float x, int pos, int v, int base) {
 
 enum RopePairs { kInterleaved = 0, kHalvesByLane = 1, kHalvesAny = 2 };
 
-// The rotation (SIGN 1) or its transpose (-1) of the 8 channels of each lane.  Halves whose distance rot / 2 is a multiple of 8
-// channels meet in another lane at the same place (shuffles); at other distances through `line`, the warp's 256 floats of shared memory.
+// What a lane's 8 channels meet in a row's rotation: c[e], s[e] with y'[e] = y[e] c[e] + other[e] s[e], the sign of the pair's first member
+// in s.  Interleaved pairs lie in the lane; halves whose distance rot / 2 is a multiple of 8 channels in another lane at the same place;
+// other halves anywhere in the head.  Channels that are not rotated: 1 and 0.
+template <int PAIRS, bool VEC>
+__device__ __forceinline__ void turns(float (&c)[8], float (&s)[8], const RopeParams& p, uint32_t at, int c0) {
+    const int half = p.rot >> 1;
+    const float *cs = p.cos + int64_t(at) * half, *sn = p.sin + int64_t(at) * half;
+    if (VEC && PAIRS == kInterleaved && c0 + 8 <= p.rot) {
+        const float4 a = __ldg(reinterpret_cast<const float4*>(cs + c0 / 2)), b = __ldg(reinterpret_cast<const float4*>(sn + c0 / 2));
+        c[0] = c[1] = a.x; c[2] = c[3] = a.y; c[4] = c[5] = a.z; c[6] = c[7] = a.w;
+        s[1] = b.x; s[3] = b.y; s[5] = b.z; s[7] = b.w;
+        s[0] = -b.x; s[2] = -b.y; s[4] = -b.z; s[6] = -b.w;
+        return;
+    }
+    if (VEC && PAIRS == kHalvesByLane && c0 < p.rot) {
+        const bool hi = c0 >= half;
+        const int t = hi ? c0 - half : c0;
+        const float sign = hi ? 1.f : -1.f;
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+            const float4 a = __ldg(reinterpret_cast<const float4*>(cs + t + e)), b = __ldg(reinterpret_cast<const float4*>(sn + t + e));
+            c[e] = a.x; c[e + 1] = a.y; c[e + 2] = a.z; c[e + 3] = a.w;
+            s[e] = sign * b.x; s[e + 1] = sign * b.y; s[e + 2] = sign * b.z; s[e + 3] = sign * b.w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int ch = c0 + e;
+        c[e] = 1.f; s[e] = 0.f;
+        if (ch < p.rot) {
+            const bool second = PAIRS == kInterleaved ? (ch & 1) != 0 : ch >= half;
+            const int t = PAIRS == kInterleaved ? ch >> 1 : second ? ch - half : ch;
+            c[e] = __ldg(cs + t);
+            s[e] = second ? __ldg(sn + t) : -__ldg(sn + t);
+        }
+    }
+}
+
+// The rotation (SIGN 1) or its transpose (-1) of the 8 channels of each lane.
 template <int PAIRS, int SIGN>
-__device__ __forceinline__ void rotate(float (&y)[8], const RopeParams& p, int64_t at, int pos, int base, int lane, float* line) {
-    const int half = p.rot >> 1, c0 = pos * 8;
-    const float *cs = p.cos + at * half, *sn = p.sin + at * half;
+__device__ __forceinline__ void rotate(float (&y)[8], const float (&c)[8], const float (&s)[8], int rot, int pos, int base, int lane, float* line) {
+    const int half = rot >> 1, c0 = pos * 8;
+    float o[8];
     if (PAIRS == kInterleaved) {
 #pragma unroll
-        for (int e = 0; e < 8; e += 2)
-            if (c0 + e < p.rot) {
-                const float c = __ldg(cs + (c0 + e) / 2), s = SIGN * __ldg(sn + (c0 + e) / 2), a = y[e], b = y[e + 1];
-                y[e] = a * c - b * s;
-                y[e + 1] = b * c + a * s;
-            }
+        for (int e = 0; e < 8; ++e) o[e] = y[e ^ 1];
     } else if (PAIRS == kHalvesByLane) {
-        const bool hi = c0 >= half;
-        const int step = half >> 3, other = c0 < p.rot ? (hi ? lane - step : lane + step) : lane, t0 = hi ? c0 - half : c0;
-        const float sign = hi ? float(SIGN) : float(-SIGN);
+        const int step = half >> 3, other = c0 < rot ? (c0 >= half ? lane - step : lane + step) : lane;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float o = __shfl_sync(0xffffffffu, y[e], other);
-            if (c0 < p.rot) y[e] = y[e] * __ldg(cs + t0 + e) + sign * o * __ldg(sn + t0 + e);
-        }
+        for (int e = 0; e < 8; ++e) o[e] = __shfl_sync(0xffffffffu, y[e], other);
     } else {
         __syncwarp();
 #pragma unroll
@@ -105,72 +133,91 @@ __device__ __forceinline__ void rotate(float (&y)[8], const RopeParams& p, int64
         __syncwarp();
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int c = c0 + e;
-            if (c < p.rot) {
-                const bool hi = c >= half;
-                const float o = line[base * 8 + (hi ? c - half : c + half)];
-                const int t = hi ? c - half : c;
-                y[e] = y[e] * __ldg(cs + t) + (hi ? float(SIGN) : float(-SIGN)) * o * __ldg(sn + t);
-            }
+            const int ch = c0 + e;
+            o[e] = ch < rot ? line[base * 8 + (ch >= half ? ch - half : ch + half)] : 0.f;
         }
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = fmaf(y[e], c[e], SIGN > 0 ? o[e] * s[e] : -(o[e] * s[e]));
 }
 
-__device__ __forceinline__ int64_t table_row(const RopeParams& p, int64_t row) {
-    if (p.positions == nullptr) return p.npos == p.rows ? row : row % p.npos;
-    return min(max(int64_t(__ldg(p.positions + row)), int64_t(0)), p.npos - 1);
-}
-
-// blockIdx.y: 0 queries, 1 keys.  GRAD: `g` is the output's gradient and `out` the input's.
-template <typename T, int PAIRS, bool GRAD>
-__global__ void __launch_bounds__(kRopeThreads) qk_rope_kernel(const RopeParams p) {
+// blockIdx.y: 0 queries, 1 keys.  GRAD: `g` is the output's gradient and `out` the input's.  A warp's groups of lanes take the heads of
+// one row, step by step (or, where a row has fewer heads than the warp has groups, of several rows); the row's part of the tables stays in
+// registers meanwhile.
+template <typename T, int PAIRS, bool VEC, bool GRAD>
+__global__ void __launch_bounds__(kRopeThreads, sizeof(T) == 2 && !GRAD ? 4 : 3) qk_rope_kernel(const RopeParams p) {
+    constexpr int kAhead = GRAD ? 1 : 2;                       // steps whose loads are in flight together
     __shared__ float lines[GRAD || PAIRS == kHalvesAny ? kRopeThreads * 8 : 1];
-    const RopeSide& s = blockIdx.y == 0 ? p.q : p.k;
-    const int v = p.dh / 8, per_warp = 32 / v, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const RopeSide& side = blockIdx.y == 0 ? p.q : p.k;
+    const int v = p.dh / 8, per_warp = 32 / v, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, heads = side.heads;
     // lanes left over (32 no multiple of v) stand behind a head's last channel
     const int sub = lane / v, pos = sub < per_warp ? lane - sub * v : v, base = sub < per_warp ? sub * v : 0;
-    const int64_t items = p.rows * s.heads;
+    const int together = heads < per_warp ? per_warp / heads : 1;                            // rows a warp takes at a time
+    const int row_sub = together > 1 ? sub / heads : 0, head0 = together > 1 ? sub - row_sub * heads : sub;
+    const bool group = pos < v && row_sub < together;
     float* line = lines + (PAIRS == kHalvesAny ? warp * 256 : 0);
     float gamma[8], dgamma[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { gamma[e] = s.gamma != nullptr && pos < v ? __ldg(s.gamma + pos * 8 + e) : 1.0f; dgamma[e] = 0.f; }
-    for (int64_t i0 = (int64_t(blockIdx.x) * (kRopeThreads / 32) + warp) * per_warp; i0 < items; i0 += int64_t(gridDim.x) * (kRopeThreads / 32) * per_warp) {
-        const int64_t item = i0 + sub;
-        const bool mine = pos < v && item < items;
-        const int64_t row = mine ? item / s.heads : 0;
-        const int64_t c = (mine ? item - row * s.heads : 0) * p.dh + (mine ? pos : 0) * 8;
-        const int64_t at = table_row(p, row);
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        Vec8<T> in;
-        if (mine) { in.load(s.x, row * s.ldx + c); in.get(x); }
-        float sq = 0.f;
+    for (int e = 0; e < 8; ++e) { gamma[e] = side.gamma != nullptr && pos < v ? __ldg(side.gamma + pos * 8 + e) : 1.0f; dgamma[e] = 0.f; }
+    const float inv_dh = 1.0f / float(p.dh);
+    const uint32_t rows = uint32_t(p.rows), npos = uint32_t(p.npos);
+    const uint32_t stride = gridDim.x * (kRopeThreads / 32) * uint32_t(together);
+    for (uint32_t row0 = (blockIdx.x * (kRopeThreads / 32) + uint32_t(warp)) * uint32_t(together); row0 < rows; row0 += stride) {
+        const uint32_t row = row0 + uint32_t(row_sub);
+        const bool live = group && row < rows;
+        float c[8], sn[8];
+        {
+            uint32_t at = 0;
+            if (live) at = p.positions == nullptr ? row % npos : uint32_t(min(max(int64_t(__ldg(p.positions + row)), int64_t(0)), int64_t(npos) - 1));
+            turns<PAIRS, VEC>(c, sn, p, at, pos * 8);
+        }
+        const int64_t r = live ? int64_t(row) : 0;
+        for (int h0 = 0; h0 < heads; h0 += per_warp * kAhead) {
+            Vec8<T> x_in[kAhead], g_in;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sq = fmaf(x[e], x[e], sq);
-        if (!GRAD) {
-            const float inv = rsqrtf(group_sum(sq, pos, v, base) / float(p.dh) + p.eps);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * gamma[e];
-            rotate<PAIRS, 1>(x, p, at, pos, base, lane, line);
-            if (mine) Vec8<T>::store(s.out, row * s.ldo + c, x);
-        } else {
-            float u[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (mine) { in.load(s.g, row * s.ldg + c); in.get(u); }
-            rotate<PAIRS, -1>(u, p, at, pos, base, lane, line);
-            float dot = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dot = fmaf(gamma[e] * u[e], x[e], dot);
-            const float inv = rsqrtf(group_sum(sq, pos, v, base) / float(p.dh) + p.eps);
-            const float mean = group_sum(dot, pos, v, base) / float(p.dh) * inv;             // of gamma u xh
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float xh = x[e] * inv;
-                if (mine) dgamma[e] = fmaf(u[e], xh, dgamma[e]);
-                x[e] = inv * (gamma[e] * u[e] - xh * mean);
+            for (int u = 0; u < kAhead; ++u) {
+                const int head = h0 + u * per_warp + head0;
+                if (live && head < heads) {
+                    x_in[u].load(side.x, r * side.ldx + head * p.dh + pos * 8);
+                    if (GRAD) g_in.load(side.g, r * side.ldg + head * p.dh + pos * 8);
+                }
             }
-            if (mine) Vec8<T>::store(s.out, row * s.ldo + c, x);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (u > 0 && h0 + u * per_warp >= heads) break;                              // the same in every lane
+                const int head = h0 + u * per_warp + head0;
+                const bool mine = live && head < heads;
+                float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                if (mine) x_in[u].get(x);
+                float sq = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sq = fmaf(x[e], x[e], sq);
+                if (!GRAD) {
+                    const float inv = rsqrtf(group_sum(sq, pos, v, base) * inv_dh + p.eps);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * gamma[e];
+                    rotate<PAIRS, 1>(x, c, sn, p.rot, pos, base, lane, line);
+                } else {
+                    float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    if (mine) g_in.get(w);
+                    rotate<PAIRS, -1>(w, c, sn, p.rot, pos, base, lane, line);
+                    float dot = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dot = fmaf(gamma[e] * w[e], x[e], dot);
+                    const float inv = rsqrtf(group_sum(sq, pos, v, base) * inv_dh + p.eps);
+                    const float mean = group_sum(dot, pos, v, base) * inv_dh * inv;          // of gamma u xh
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float xh = x[e] * inv;
+                        dgamma[e] = fmaf(w[e], xh, dgamma[e]);                               // zeros where there is no head
+                        x[e] = inv * (gamma[e] * w[e] - xh * mean);
+                    }
+                }
+                if (mine) Vec8<T>::store(side.out, r * side.ldo + head * p.dh + pos * 8, x);
+            }
         }
     }
-    if (GRAD && s.dgamma != nullptr) {
+    if (GRAD && side.dgamma != nullptr) {
         // the CTA's share: lanes of the same place in a head, in a fixed order
         __syncthreads();
 #pragma unroll
@@ -204,18 +251,25 @@ __global__ void __launch_bounds__(1024) qk_rope_gamma_kernel(const RopeParams p,
 }
 
 template <typename T, bool GRAD>
-hq_status launch_pairs(const RopeParams& p, int pairs, dim3 grid, cudaStream_t st) {
-    if (pairs == kInterleaved) qk_rope_kernel<T, kInterleaved, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
-    else if (pairs == kHalvesByLane) qk_rope_kernel<T, kHalvesByLane, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
-    else qk_rope_kernel<T, kHalvesAny, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
+hq_status launch_pairs(const RopeParams& p, int pairs, bool vec, dim3 grid, cudaStream_t st) {
+    if (pairs == kInterleaved) {
+        if (vec) qk_rope_kernel<T, kInterleaved, true, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
+        else qk_rope_kernel<T, kInterleaved, false, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
+    } else if (pairs == kHalvesByLane) {
+        if (vec) qk_rope_kernel<T, kHalvesByLane, true, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
+        else qk_rope_kernel<T, kHalvesByLane, false, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
+    } else {
+        qk_rope_kernel<T, kHalvesAny, false, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
+    }
     return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }
 
-int rope_blocks(int64_t rows, int heads, int dh, bool grad) {
-    const int64_t per_cta = (kRopeThreads / 32) * (32 / (dh / 8));
-    int64_t blocks = (rows * heads + per_cta - 1) / per_cta;
-    const int64_t most = grad ? kRopeMaxBlocks : 1 << 20;
-    return int(blocks < most ? blocks : most);
+// A row (or several rows of few heads) for each warp, up to kRopeMaxBlocks CTAs.
+int rope_blocks(int64_t rows, int heads, int kv_heads, int dh) {
+    const int per_warp = 32 / (dh / 8), most = kv_heads > heads ? kv_heads : heads;
+    const int64_t together = most < per_warp ? per_warp / most : 1, per_cta = (kRopeThreads / 32) * together;
+    const int64_t blocks = (rows + per_cta - 1) / per_cta;
+    return int(blocks < kRopeMaxBlocks ? blocks : kRopeMaxBlocks);
 }
 
 hq_status check_matrix(const void* x, int64_t ld, int heads, int dh, hq_dtype dt) {
@@ -237,12 +291,14 @@ hq_status check_call(hq_dtype dt, int64_t rows, int heads, int kv_heads, int dh,
 
 hq_status run(RopeParams p, hq_dtype dt, int interleaved, bool grad, cudaStream_t st) {
     if (p.rot == 0) { p.npos = 1; p.positions = nullptr; }
+    if (p.npos > 0x7fffffff) p.npos = 0x7fffffff;              // rows and positions end there
     const int pairs = interleaved || p.rot == 0 ? kInterleaved : (p.rot / 2) % 8 == 0 ? kHalvesByLane : kHalvesAny;
-    const int blocks = rope_blocks(p.rows, p.q.heads > p.k.heads ? p.q.heads : p.k.heads, p.dh, grad);
+    const int blocks = rope_blocks(p.rows, p.q.heads, p.k.heads, p.dh);
     const dim3 grid(unsigned(blocks), p.k.heads > 0 ? 2u : 1u);
     hq_status e;
-    if (grad) e = dt == HQ_BF16 ? launch_pairs<__nv_bfloat16, true>(p, pairs, grid, st) : launch_pairs<float, true>(p, pairs, grid, st);
-    else e = dt == HQ_BF16 ? launch_pairs<__nv_bfloat16, false>(p, pairs, grid, st) : launch_pairs<float, false>(p, pairs, grid, st);
+    const bool vec = p.rot % 8 == 0 && aligned16(p.cos) && aligned16(p.sin);                 // every table row 16-byte aligned
+    if (grad) e = dt == HQ_BF16 ? launch_pairs<__nv_bfloat16, true>(p, pairs, vec, grid, st) : launch_pairs<float, true>(p, pairs, vec, grid, st);
+    else e = dt == HQ_BF16 ? launch_pairs<__nv_bfloat16, false>(p, pairs, vec, grid, st) : launch_pairs<float, false>(p, pairs, vec, grid, st);
     if (e != HQ_OK || (p.q.dgamma == nullptr && p.k.dgamma == nullptr)) return e;
     qk_rope_gamma_kernel<<<grid.y, 1024, 0, st>>>(p, blocks);
     return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
@@ -273,7 +329,7 @@ extern "C" hq_status hq_qk_norm_rope_bwd_workspace_size(int64_t rows, int heads,
     if (bytes == nullptr) return HQ_ERR_INVALID_ARG;
     const hq_status e = check_call(HQ_BF16, rows, heads, kv_heads, dh, nullptr, nullptr, 1, 0, 0.f);
     if (e != HQ_OK) return e;
-    *bytes = size_t(2) * rope_blocks(rows, heads > kv_heads ? heads : kv_heads, dh, true) * dh * sizeof(float);
+    *bytes = size_t(2) * rope_blocks(rows, heads, kv_heads, dh) * dh * sizeof(float);
     return HQ_OK;
 }
 
