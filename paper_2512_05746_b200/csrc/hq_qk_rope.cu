@@ -11,6 +11,7 @@
 // one row, 8 channels a lane (16 bytes of bf16), so that the row's sums are a few shuffles; 32 / (dh / 8) heads a warp.  Sums and
 // the rotation in fp32, one rounding at the end.
 #include "hq_common.cuh"
+#include "hq_fwht.cuh"
 
 namespace hq {
 namespace {
@@ -29,20 +30,30 @@ struct RopeParams {
 constexpr int kRopeThreads = 256;
 constexpr int kRopeMaxBlocks = 1184;               // 8 CTAs for each of 148 SMs, on every device: gamma's gradient is summed in one order
 
+// 8 channels of a lane, as they lie in memory and as four pairs of floats.
 template <typename T> struct Vec8;
 template <> struct Vec8<__nv_bfloat16> {
     uint4 w;
+    __device__ __forceinline__ void clear() { w = make_uint4(0u, 0u, 0u, 0u); }
     __device__ __forceinline__ void load(const void* base, int64_t at) { w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) + at); }
-    __device__ __forceinline__ void get(float (&f)[8]) const {
+    __device__ __forceinline__ Vec8 of(int lane) const {       // the other lane's
+        Vec8 r;
+        r.w.x = __shfl_sync(0xffffffffu, w.x, lane); r.w.y = __shfl_sync(0xffffffffu, w.y, lane);
+        r.w.z = __shfl_sync(0xffffffffu, w.z, lane); r.w.w = __shfl_sync(0xffffffffu, w.w, lane);
+        return r;
+    }
+    __device__ __forceinline__ void get(f32x2 (&f)[4]) const {
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { f[2 * e] = __uint_as_float(u[e] << 16); f[2 * e + 1] = __uint_as_float(u[e] & 0xFFFF0000u); }
+        for (int e = 0; e < 4; ++e) f[e] = pk2(__uint_as_float(u[e] << 16), __uint_as_float(u[e] & 0xFFFF0000u));
     }
-    static __device__ __forceinline__ void store(void* base, int64_t at, const float (&f)[8]) {
+    static __device__ __forceinline__ void store(void* base, int64_t at, const f32x2 (&f)[4]) {
         uint32_t u[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+            float a, b;
+            upk2(f[e], a, b);
+            const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
             u[e] = *reinterpret_cast<const uint32_t*>(&h);
         }
         *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(base) + at) = make_uint4(u[0], u[1], u[2], u[3]);
@@ -50,21 +61,36 @@ template <> struct Vec8<__nv_bfloat16> {
 };
 template <> struct Vec8<float> {
     float4 a, b;
+    __device__ __forceinline__ void clear() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void load(const void* base, int64_t at) {
         const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
         a = p[0]; b = p[1];
     }
-    __device__ __forceinline__ void get(float (&f)[8]) const {
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    __device__ __forceinline__ Vec8 of(int lane) const {
+        Vec8 r;
+        r.a.x = __shfl_sync(0xffffffffu, a.x, lane); r.a.y = __shfl_sync(0xffffffffu, a.y, lane);
+        r.a.z = __shfl_sync(0xffffffffu, a.z, lane); r.a.w = __shfl_sync(0xffffffffu, a.w, lane);
+        r.b.x = __shfl_sync(0xffffffffu, b.x, lane); r.b.y = __shfl_sync(0xffffffffu, b.y, lane);
+        r.b.z = __shfl_sync(0xffffffffu, b.z, lane); r.b.w = __shfl_sync(0xffffffffu, b.w, lane);
+        return r;
     }
-    static __device__ __forceinline__ void store(void* base, int64_t at, const float (&f)[8]) {
+    __device__ __forceinline__ void get(f32x2 (&f)[4]) const { f[0] = pk2(a.x, a.y); f[1] = pk2(a.z, a.w); f[2] = pk2(b.x, b.y); f[3] = pk2(b.z, b.w); }
+    static __device__ __forceinline__ void store(void* base, int64_t at, const f32x2 (&f)[4]) {
         float4* p = reinterpret_cast<float4*>(static_cast<float*>(base) + at);
-        p[0] = make_float4(f[0], f[1], f[2], f[3]); p[1] = make_float4(f[4], f[5], f[6], f[7]);
+        float4 x, y;
+        upk2(f[0], x.x, x.y); upk2(f[1], x.z, x.w); upk2(f[2], y.x, y.y); upk2(f[3], y.z, y.w);
+        p[0] = x; p[1] = y;
     }
 };
 
-// Sum over the `v` lanes of a group, in every lane of it.
+// Sum over the lanes of a group, in every lane of it.  V: their number where it is 4, 8 or 16, else 0.
+template <int V>
 __device__ __forceinline__ float group_sum(float x, int pos, int v, int base) {
+    if (V > 0) {
+#pragma unroll
+        for (int off = V / 2; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+        return x;
+    }
 #pragma unroll
     for (int off = 8; off > 0; off >>= 1) {
         const float o = __shfl_down_sync(0xffffffffu, x, off);
@@ -72,148 +98,186 @@ __device__ __forceinline__ float group_sum(float x, int pos, int v, int base) {
     }
     return __shfl_sync(0xffffffffu, x, base);
 }
+__device__ __forceinline__ float pair_sum(f32x2 v) { float a, b; upk2(v, a, b); return a + b; }
 
 enum RopePairs { kInterleaved = 0, kHalvesByLane = 1, kHalvesAny = 2 };
 
-// What a lane's 8 channels meet in a row's rotation: c[e], s[e] with y'[e] = y[e] c[e] + other[e] s[e], the sign of the pair's first member
-// in s.  Interleaved pairs lie in the lane; halves whose distance rot / 2 is a multiple of 8 channels in another lane at the same place;
-// other halves anywhere in the head.  Channels that are not rotated: 1 and 0.
+// What a lane's 8 channels meet in a row's rotation: out = y c + other s, the sign of the pair's first member in s.  Interleaved pairs
+// lie in the lane; halves whose distance rot / 2 is a multiple of 8 channels in another lane at the same place; other halves anywhere in
+// the head.  Channels that are not rotated: 1 and 0.  VEC: every table row is 16-byte aligned.
 template <int PAIRS, bool VEC>
-__device__ __forceinline__ void turns(float (&c)[8], float (&s)[8], const RopeParams& p, uint32_t at, int c0) {
+__device__ __forceinline__ void turns(f32x2 (&c)[4], f32x2 (&s)[4], const RopeParams& p, uint32_t at, int c0) {
     const int half = p.rot >> 1;
     const float *cs = p.cos + int64_t(at) * half, *sn = p.sin + int64_t(at) * half;
     if (VEC && PAIRS == kInterleaved && c0 + 8 <= p.rot) {
         const float4 a = __ldg(reinterpret_cast<const float4*>(cs + c0 / 2)), b = __ldg(reinterpret_cast<const float4*>(sn + c0 / 2));
-        c[0] = c[1] = a.x; c[2] = c[3] = a.y; c[4] = c[5] = a.z; c[6] = c[7] = a.w;
-        s[1] = b.x; s[3] = b.y; s[5] = b.z; s[7] = b.w;
-        s[0] = -b.x; s[2] = -b.y; s[4] = -b.z; s[6] = -b.w;
+        c[0] = pk2(a.x, a.x); c[1] = pk2(a.y, a.y); c[2] = pk2(a.z, a.z); c[3] = pk2(a.w, a.w);
+        s[0] = pk2(-b.x, b.x); s[1] = pk2(-b.y, b.y); s[2] = pk2(-b.z, b.z); s[3] = pk2(-b.w, b.w);
         return;
     }
     if (VEC && PAIRS == kHalvesByLane && c0 < p.rot) {
         const bool hi = c0 >= half;
         const int t = hi ? c0 - half : c0;
-        const float sign = hi ? 1.f : -1.f;
+        const f32x2 sign = hi ? pk2(1.f, 1.f) : pk2(-1.f, -1.f);
 #pragma unroll
-        for (int e = 0; e < 8; e += 4) {
-            const float4 a = __ldg(reinterpret_cast<const float4*>(cs + t + e)), b = __ldg(reinterpret_cast<const float4*>(sn + t + e));
-            c[e] = a.x; c[e + 1] = a.y; c[e + 2] = a.z; c[e + 3] = a.w;
-            s[e] = sign * b.x; s[e + 1] = sign * b.y; s[e + 2] = sign * b.z; s[e + 3] = sign * b.w;
+        for (int e = 0; e < 2; ++e) {
+            const float4 a = __ldg(reinterpret_cast<const float4*>(cs + t) + e), b = __ldg(reinterpret_cast<const float4*>(sn + t) + e);
+            c[2 * e] = pk2(a.x, a.y); c[2 * e + 1] = pk2(a.z, a.w);
+            s[2 * e] = mul2(sign, pk2(b.x, b.y)); s[2 * e + 1] = mul2(sign, pk2(b.z, b.w));
         }
         return;
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int ch = c0 + e;
-        c[e] = 1.f; s[e] = 0.f;
-        if (ch < p.rot) {
-            const bool second = PAIRS == kInterleaved ? (ch & 1) != 0 : ch >= half;
-            const int t = PAIRS == kInterleaved ? ch >> 1 : second ? ch - half : ch;
-            c[e] = __ldg(cs + t);
-            s[e] = second ? __ldg(sn + t) : -__ldg(sn + t);
+    for (int e = 0; e < 4; ++e) {
+        float cc[2], ss[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int ch = c0 + 2 * e + x;
+            cc[x] = 1.f; ss[x] = 0.f;
+            if (ch < p.rot) {
+                const bool second = PAIRS == kInterleaved ? x == 1 : ch >= half;
+                const int t = PAIRS == kInterleaved ? ch >> 1 : second ? ch - half : ch;
+                cc[x] = __ldg(cs + t);
+                ss[x] = second ? __ldg(sn + t) : -__ldg(sn + t);
+            }
         }
+        c[e] = pk2(cc[0], cc[1]); s[e] = pk2(ss[0], ss[1]);
     }
 }
 
-// The rotation (SIGN 1) or its transpose (-1) of the 8 channels of each lane.
-template <int PAIRS, int SIGN>
-__device__ __forceinline__ void rotate(float (&y)[8], const float (&c)[8], const float (&s)[8], int rot, int pos, int base, int lane, float* line) {
+// The other members of the pairs of a lane's 8 channels, as they were loaded; at distances that are no multiple of 8 channels through
+// `line`, the warp's 256 floats of shared memory.
+template <int PAIRS, typename T>
+__device__ __forceinline__ void partners(f32x2 (&o)[4], const f32x2 (&y)[4], const Vec8<T>& raw, int rot, int pos, int base, int lane, float* line) {
     const int half = rot >> 1, c0 = pos * 8;
-    float o[8];
     if (PAIRS == kInterleaved) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = y[e ^ 1];
+        for (int e = 0; e < 4; ++e) { float a, b; upk2(y[e], a, b); o[e] = pk2(b, a); }
     } else if (PAIRS == kHalvesByLane) {
-        const int step = half >> 3, other = c0 < rot ? (c0 >= half ? lane - step : lane + step) : lane;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = __shfl_sync(0xffffffffu, y[e], other);
+        const int step = half >> 3;
+        raw.of(c0 < rot ? (c0 >= half ? lane - step : lane + step) : lane).get(o);
     } else {
         __syncwarp();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) line[lane * 8 + e] = y[e];
+        for (int e = 0; e < 4; ++e) { float a, b; upk2(y[e], a, b); line[lane * 8 + 2 * e] = a; line[lane * 8 + 2 * e + 1] = b; }
         __syncwarp();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int ch = c0 + e;
-            o[e] = ch < rot ? line[base * 8 + (ch >= half ? ch - half : ch + half)] : 0.f;
+        for (int e = 0; e < 4; ++e) {
+            float t[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int ch = c0 + 2 * e + x;
+                t[x] = ch < rot ? line[base * 8 + (ch >= half ? ch - half : ch + half)] : 0.f;
+            }
+            o[e] = pk2(t[0], t[1]);
         }
     }
+}
+// gamma of a lane's channels (1 without), and of their pairs' other members.
+template <int PAIRS>
+__device__ __forceinline__ void gammas(f32x2 (&own)[4], f32x2 (&other)[4], const float* gamma, int rot, int dh, int c0) {
+    const int half = rot >> 1;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = fmaf(y[e], c[e], SIGN > 0 ? o[e] * s[e] : -(o[e] * s[e]));
+    for (int e = 0; e < 4; ++e) {
+        float a[2] = {1.f, 1.f}, b[2] = {1.f, 1.f};
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int ch = c0 + 2 * e + x, t = ch >= rot ? ch : PAIRS == kInterleaved ? ch ^ 1 : ch >= half ? ch - half : ch + half;
+            if (gamma != nullptr && ch < dh) { a[x] = __ldg(gamma + ch); b[x] = __ldg(gamma + t); }
+        }
+        own[e] = pk2(a[0], a[1]); other[e] = pk2(b[0], b[1]);
+    }
 }
 
 // blockIdx.y: 0 queries, 1 keys.  GRAD: `g` is the output's gradient and `out` the input's.  A warp's groups of lanes take the heads of
 // one row, step by step (or, where a row has fewer heads than the warp has groups, of several rows); the row's part of the tables stays in
-// registers meanwhile.
-template <typename T, int PAIRS, bool VEC, bool GRAD>
-__global__ void __launch_bounds__(kRopeThreads, sizeof(T) == 2 && !GRAD ? 4 : 3) qk_rope_kernel(const RopeParams p) {
+// registers meanwhile.  Arithmetic on pairs of floats.
+template <typename T, int PAIRS, bool VEC, bool GRAD, int V>
+__global__ void __launch_bounds__(kRopeThreads, GRAD || sizeof(T) == 4 ? 3 : 4) qk_rope_kernel(const RopeParams p) {
     constexpr int kAhead = GRAD ? 1 : 2;                       // steps whose loads are in flight together
     __shared__ float lines[GRAD || PAIRS == kHalvesAny ? kRopeThreads * 8 : 1];
     const RopeSide& side = blockIdx.y == 0 ? p.q : p.k;
-    const int v = p.dh / 8, per_warp = 32 / v, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, heads = side.heads;
+    const int v = V > 0 ? V : p.dh / 8, dh = V > 0 ? V * 8 : p.dh;
+    const int per_warp = 32 / v, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, heads = side.heads;
     // lanes left over (32 no multiple of v) stand behind a head's last channel
     const int sub = lane / v, pos = sub < per_warp ? lane - sub * v : v, base = sub < per_warp ? sub * v : 0;
     const int together = heads < per_warp ? per_warp / heads : 1;                            // rows a warp takes at a time
     const int row_sub = together > 1 ? sub / heads : 0, head0 = together > 1 ? sub - row_sub * heads : sub;
     const bool group = pos < v && row_sub < together;
     float* line = lines + (PAIRS == kHalvesAny ? warp * 256 : 0);
-    float gamma[8], dgamma[8];
+    f32x2 gamma[4], other_gamma[4], dgamma[4];                 // without GRAD both go into the turns, where there is a gamma
+    gammas<PAIRS>(gamma, other_gamma, side.gamma, p.rot, dh, pos * 8);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { gamma[e] = side.gamma != nullptr && pos < v ? __ldg(side.gamma + pos * 8 + e) : 1.0f; dgamma[e] = 0.f; }
-    const float inv_dh = 1.0f / float(p.dh);
+    for (int e = 0; e < 4; ++e) dgamma[e] = pk2(0.f, 0.f);
+    const float inv_dh = 1.0f / float(dh);
     const uint32_t rows = uint32_t(p.rows), npos = uint32_t(p.npos);
     const uint32_t stride = gridDim.x * (kRopeThreads / 32) * uint32_t(together);
-    for (uint32_t row0 = (blockIdx.x * (kRopeThreads / 32) + uint32_t(warp)) * uint32_t(together); row0 < rows; row0 += stride) {
+    uint32_t row0 = (blockIdx.x * (kRopeThreads / 32) + uint32_t(warp)) * uint32_t(together);
+    const uint32_t cyc_on = stride % npos;
+    uint32_t cyc = (row0 + uint32_t(row_sub)) % npos;          // the row's place in its sample
+    for (; row0 < rows; row0 += stride) {
         const uint32_t row = row0 + uint32_t(row_sub);
         const bool live = group && row < rows;
-        float c[8], sn[8];
+        const int64_t r = live ? int64_t(row) : 0, c0 = r * side.ldx + pos * 8, g0 = GRAD ? r * side.ldg + pos * 8 : 0, o0 = r * side.ldo + pos * 8;
+        f32x2 c[4], sn[4];
         {
             uint32_t at = 0;
-            if (live) at = p.positions == nullptr ? row % npos : uint32_t(min(max(int64_t(__ldg(p.positions + row)), int64_t(0)), int64_t(npos) - 1));
+            if (live) at = p.positions == nullptr ? cyc : uint32_t(min(max(__ldg(p.positions + row), 0), int(npos) - 1));
             turns<PAIRS, VEC>(c, sn, p, at, pos * 8);
+            cyc += cyc_on;
+            if (cyc >= npos) cyc -= npos;
+            if (!GRAD) {                                       // out = (x gamma c + other gamma' s) / rms
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { c[e] = mul2(c[e], gamma[e]); sn[e] = mul2(sn[e], other_gamma[e]); }
+            }
         }
-        const int64_t r = live ? int64_t(row) : 0;
         for (int h0 = 0; h0 < heads; h0 += per_warp * kAhead) {
             Vec8<T> x_in[kAhead], g_in;
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int head = h0 + u * per_warp + head0;
+                x_in[u].clear();
+                if (GRAD) g_in.clear();
                 if (live && head < heads) {
-                    x_in[u].load(side.x, r * side.ldx + head * p.dh + pos * 8);
-                    if (GRAD) g_in.load(side.g, r * side.ldg + head * p.dh + pos * 8);
+                    x_in[u].load(side.x, c0 + head * dh);
+                    if (GRAD) g_in.load(side.g, g0 + head * dh);
                 }
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 if (u > 0 && h0 + u * per_warp >= heads) break;                              // the same in every lane
                 const int head = h0 + u * per_warp + head0;
-                const bool mine = live && head < heads;
-                float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                if (mine) x_in[u].get(x);
-                float sq = 0.f;
+                f32x2 x[4], o[4], sq = pk2(0.f, 0.f);
+                x_in[u].get(x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sq = fmaf(x[e], x[e], sq);
+                for (int e = 0; e < 4; ++e) sq = fma2(x[e], x[e], sq);
                 if (!GRAD) {
-                    const float inv = rsqrtf(group_sum(sq, pos, v, base) * inv_dh + p.eps);
+                    const float inv = rsqrtf(group_sum<V>(pair_sum(sq), pos, v, base) * inv_dh + p.eps);
+                    partners<PAIRS>(o, x, x_in[u], p.rot, pos, base, lane, line);
+                    const f32x2 inv2 = pk2(inv, inv);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * gamma[e];
-                    rotate<PAIRS, 1>(x, c, sn, p.rot, pos, base, lane, line);
+                    for (int e = 0; e < 4; ++e) x[e] = mul2(inv2, fma2(x[e], c[e], mul2(o[e], sn[e])));
                 } else {
-                    float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                    if (mine) g_in.get(w);
-                    rotate<PAIRS, -1>(w, c, sn, p.rot, pos, base, lane, line);
-                    float dot = 0.f;
+                    f32x2 w[4], dot = pk2(0.f, 0.f);
+                    g_in.get(w);
+                    partners<PAIRS>(o, w, g_in, p.rot, pos, base, lane, line);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) dot = fmaf(gamma[e] * w[e], x[e], dot);
-                    const float inv = rsqrtf(group_sum(sq, pos, v, base) * inv_dh + p.eps);
-                    const float mean = group_sum(dot, pos, v, base) * inv_dh * inv;          // of gamma u xh
+                    for (int e = 0; e < 4; ++e) {
+                        w[e] = sub2(mul2(w[e], c[e]), mul2(o[e], sn[e]));                    // u, the transpose's
+                        o[e] = mul2(gamma[e], w[e]);
+                        dot = fma2(o[e], x[e], dot);
+                    }
+                    const float inv = rsqrtf(group_sum<V>(pair_sum(sq), pos, v, base) * inv_dh + p.eps);
+                    const float mean = group_sum<V>(pair_sum(dot), pos, v, base) * inv_dh * inv;             // of gamma u xh
+                    const f32x2 inv2 = pk2(inv, inv), less = pk2(-mean, -mean);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float xh = x[e] * inv;
-                        dgamma[e] = fmaf(w[e], xh, dgamma[e]);                               // zeros where there is no head
-                        x[e] = inv * (gamma[e] * w[e] - xh * mean);
+                    for (int e = 0; e < 4; ++e) {
+                        const f32x2 xh = mul2(x[e], inv2);
+                        dgamma[e] = fma2(w[e], xh, dgamma[e]);                               // zeros where there is no head
+                        x[e] = mul2(inv2, fma2(xh, less, o[e]));
                     }
                 }
-                if (mine) Vec8<T>::store(side.out, r * side.ldo + head * p.dh + pos * 8, x);
+                if (live && head < heads) Vec8<T>::store(side.out, o0 + head * dh, x);
             }
         }
     }
@@ -221,13 +285,18 @@ __global__ void __launch_bounds__(kRopeThreads, sizeof(T) == 2 && !GRAD ? 4 : 3)
         // the CTA's share: lanes of the same place in a head, in a fixed order
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) lines[threadIdx.x * 8 + e] = dgamma[e];
+        for (int e = 0; e < 4; ++e) {
+            float a, b;
+            upk2(dgamma[e], a, b);
+            lines[threadIdx.x * 8 + 2 * e] = a;
+            lines[threadIdx.x * 8 + 2 * e + 1] = b;
+        }
         __syncthreads();
-        if (int(threadIdx.x) < p.dh) {
+        if (int(threadIdx.x) < dh) {
             float sum = 0.f;
             for (int w = 0; w < kRopeThreads / 32; ++w)
-                for (int g = 0; g < per_warp; ++g) sum += lines[w * 256 + g * p.dh + threadIdx.x];
-            p.partial[(int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * p.dh + threadIdx.x] = sum;
+                for (int g = 0; g < per_warp; ++g) sum += lines[w * 256 + g * dh + threadIdx.x];
+            p.partial[(int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * dh + threadIdx.x] = sum;
         }
     }
 }
@@ -250,18 +319,27 @@ __global__ void __launch_bounds__(1024) qk_rope_gamma_kernel(const RopeParams p,
     }
 }
 
-template <typename T, bool GRAD>
+template <typename T, bool GRAD, int V>
 hq_status launch_pairs(const RopeParams& p, int pairs, bool vec, dim3 grid, cudaStream_t st) {
     if (pairs == kInterleaved) {
-        if (vec) qk_rope_kernel<T, kInterleaved, true, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
-        else qk_rope_kernel<T, kInterleaved, false, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
+        if (vec) qk_rope_kernel<T, kInterleaved, true, GRAD, V><<<grid, kRopeThreads, 0, st>>>(p);
+        else qk_rope_kernel<T, kInterleaved, false, GRAD, V><<<grid, kRopeThreads, 0, st>>>(p);
     } else if (pairs == kHalvesByLane) {
-        if (vec) qk_rope_kernel<T, kHalvesByLane, true, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
-        else qk_rope_kernel<T, kHalvesByLane, false, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
+        if (vec) qk_rope_kernel<T, kHalvesByLane, true, GRAD, V><<<grid, kRopeThreads, 0, st>>>(p);
+        else qk_rope_kernel<T, kHalvesByLane, false, GRAD, V><<<grid, kRopeThreads, 0, st>>>(p);
     } else {
-        qk_rope_kernel<T, kHalvesAny, false, GRAD><<<grid, kRopeThreads, 0, st>>>(p);
+        qk_rope_kernel<T, kHalvesAny, false, GRAD, V><<<grid, kRopeThreads, 0, st>>>(p);
     }
     return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+}
+template <typename T, bool GRAD>
+hq_status launch_width(const RopeParams& p, int pairs, bool vec, dim3 grid, cudaStream_t st) {
+    switch (p.dh) {
+        case 32: return launch_pairs<T, GRAD, 4>(p, pairs, vec, grid, st);
+        case 64: return launch_pairs<T, GRAD, 8>(p, pairs, vec, grid, st);
+        case 128: return launch_pairs<T, GRAD, 16>(p, pairs, vec, grid, st);
+        default: return launch_pairs<T, GRAD, 0>(p, pairs, vec, grid, st);
+    }
 }
 
 // A row (or several rows of few heads) for each warp, up to kRopeMaxBlocks CTAs.
@@ -297,8 +375,8 @@ hq_status run(RopeParams p, hq_dtype dt, int interleaved, bool grad, cudaStream_
     const dim3 grid(unsigned(blocks), p.k.heads > 0 ? 2u : 1u);
     hq_status e;
     const bool vec = p.rot % 8 == 0 && aligned16(p.cos) && aligned16(p.sin);                 // every table row 16-byte aligned
-    if (grad) e = dt == HQ_BF16 ? launch_pairs<__nv_bfloat16, true>(p, pairs, vec, grid, st) : launch_pairs<float, true>(p, pairs, vec, grid, st);
-    else e = dt == HQ_BF16 ? launch_pairs<__nv_bfloat16, false>(p, pairs, vec, grid, st) : launch_pairs<float, false>(p, pairs, vec, grid, st);
+    if (grad) e = dt == HQ_BF16 ? launch_width<__nv_bfloat16, true>(p, pairs, vec, grid, st) : launch_width<float, true>(p, pairs, vec, grid, st);
+    else e = dt == HQ_BF16 ? launch_width<__nv_bfloat16, false>(p, pairs, vec, grid, st) : launch_width<float, false>(p, pairs, vec, grid, st);
     if (e != HQ_OK || (p.q.dgamma == nullptr && p.k.dgamma == nullptr)) return e;
     qk_rope_gamma_kernel<<<grid.y, 1024, 0, st>>>(p, blocks);
     return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
