@@ -86,17 +86,18 @@ template <> struct Vec8<float> {
 // Sum over the lanes of a group, in every lane of it.  V: their number where it is 4, 8 or 16, else 0.
 template <int V>
 __device__ __forceinline__ float group_sum(float x, int pos, int v, int base) {
-    if (V > 0) {
+    if constexpr (V > 0) {
 #pragma unroll
         for (int off = V / 2; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
         return x;
-    }
+    } else {
 #pragma unroll
-    for (int off = 8; off > 0; off >>= 1) {
-        const float o = __shfl_down_sync(0xffffffffu, x, off);
-        if (pos < off && pos + off < v) x += o;
+        for (int off = 8; off > 0; off >>= 1) {
+            const float o = __shfl_down_sync(0xffffffffu, x, off);
+            if (pos < off && pos + off < v) x += o;
+        }
+        return __shfl_sync(0xffffffffu, x, base);
     }
-    return __shfl_sync(0xffffffffu, x, base);
 }
 __device__ __forceinline__ float pair_sum(f32x2 v) { float a, b; upk2(v, a, b); return a + b; }
 
@@ -193,8 +194,8 @@ __device__ __forceinline__ void gammas(f32x2 (&own)[4], f32x2 (&other)[4], const
 // one row, step by step (or, where a row has fewer heads than the warp has groups, of several rows); the row's part of the tables stays in
 // registers meanwhile.  Arithmetic on pairs of floats.
 template <typename T, int PAIRS, bool VEC, bool GRAD, int V>
-__global__ void __launch_bounds__(kRopeThreads, GRAD || sizeof(T) == 4 ? 3 : 4) qk_rope_kernel(const RopeParams p) {
-    constexpr int kAhead = GRAD ? 1 : 2;                       // steps whose loads are in flight together
+__global__ void __launch_bounds__(kRopeThreads, GRAD ? 2 : sizeof(T) == 4 ? 3 : 4) qk_rope_kernel(const RopeParams p) {
+    constexpr int kAhead = 2;                                  // steps whose loads are in flight together
     __shared__ float lines[GRAD || PAIRS == kHalvesAny ? kRopeThreads * 8 : 1];
     const RopeSide& side = blockIdx.y == 0 ? p.q : p.k;
     const int v = V > 0 ? V : p.dh / 8, dh = V > 0 ? V * 8 : p.dh;
@@ -219,6 +220,20 @@ __global__ void __launch_bounds__(kRopeThreads, GRAD || sizeof(T) == 4 ? 3 : 4) 
         const uint32_t row = row0 + uint32_t(row_sub);
         const bool live = group && row < rows;
         const int64_t r = live ? int64_t(row) : 0, c0 = r * side.ldx + pos * 8, g0 = GRAD ? r * side.ldg + pos * 8 : 0, o0 = r * side.ldo + pos * 8;
+        Vec8<T> x_in[kAhead], g_in[kAhead];
+        auto request = [&](int h0) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int head = h0 + u * per_warp + head0;
+                x_in[u].clear();
+                if (GRAD) g_in[u].clear();
+                if (live && head < heads) {
+                    x_in[u].load(side.x, c0 + head * dh);
+                    if (GRAD) g_in[u].load(side.g, g0 + head * dh);
+                }
+            }
+        };
+        request(0);                                            // in front of the tables' loads
         f32x2 c[4], sn[4];
         {
             uint32_t at = 0;
@@ -232,17 +247,7 @@ __global__ void __launch_bounds__(kRopeThreads, GRAD || sizeof(T) == 4 ? 3 : 4) 
             }
         }
         for (int h0 = 0; h0 < heads; h0 += per_warp * kAhead) {
-            Vec8<T> x_in[kAhead], g_in;
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int head = h0 + u * per_warp + head0;
-                x_in[u].clear();
-                if (GRAD) g_in.clear();
-                if (live && head < heads) {
-                    x_in[u].load(side.x, c0 + head * dh);
-                    if (GRAD) g_in.load(side.g, g0 + head * dh);
-                }
-            }
+            if (h0 > 0) request(h0);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 if (u > 0 && h0 + u * per_warp >= heads) break;                              // the same in every lane
@@ -259,8 +264,8 @@ __global__ void __launch_bounds__(kRopeThreads, GRAD || sizeof(T) == 4 ? 3 : 4) 
                     for (int e = 0; e < 4; ++e) x[e] = mul2(inv2, fma2(x[e], c[e], mul2(o[e], sn[e])));
                 } else {
                     f32x2 w[4], dot = pk2(0.f, 0.f);
-                    g_in.get(w);
-                    partners<PAIRS>(o, w, g_in, p.rot, pos, base, lane, line);
+                    g_in[u].get(w);
+                    partners<PAIRS>(o, w, g_in[u], p.rot, pos, base, lane, line);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         w[e] = sub2(mul2(w[e], c[e]), mul2(o[e], sn[e]));                    // u, the transpose's
