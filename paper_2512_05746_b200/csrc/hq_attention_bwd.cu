@@ -58,13 +58,6 @@ template <int NH> struct BwdBars {
 };
 template <int NH> constexpr size_t bwd_smem() { return size_t(BwdRings<NH>::kTiles + BwdRings<NH>::kStats) + sizeof(BwdBars<NH>); }
 
-// A place in a ring and how often it has come round.
-template <int N> struct RingAt {
-    int slot = 0;
-    uint32_t phase = 0;
-    __device__ __forceinline__ void next() { if (++slot == N) { slot = 0; phase ^= 1u; } }
-};
-
 // What an item is: a tile of keys of one (sample, key head) or of queries of one (sample, head), and the other side's tiles it walks.
 struct BwdItem {
     bool keys;
@@ -181,10 +174,9 @@ __device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* sme
     const uint64_t dB0t = make_sw128_mnmajor_desc(smem_u32(sB0), kAttnPart), dB1t = make_sw128_mnmajor_desc(smem_u32(sB1), kAttnPart);
     constexpr uint64_t kTileUnits = R::kTile >> 4;
     auto score_product = [&](uint64_t a, uint64_t b, uint32_t column) {
-#pragma unroll
-        for (int k = 0; k < 4 * NH; ++k) {
+        for (int k = 0; k < ksteps; ++k) {
             const uint64_t step = uint64_t((k >> 2) * (kAttnPart >> 4) + 2 * (k & 3));
-            if (k < ksteps) mma_bf16(tmem_base + column, a + step, b + step, idesc_s, k != 0 ? 1u : 0u);
+            mma_bf16(tmem_base + column, a + step, b + step, idesc_s, k != 0 ? 1u : 0u);
         }
     };
     // bf16 operand of each quarter in the first half of its 32 columns
@@ -389,26 +381,6 @@ __device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdI
         ++step;
     }
     return true;
-}
-
-// 32 columns of an accumulator as scaled bf16 into the staging tile (rows of 128 bytes, 128-byte swizzle); rows not kept become zeros.
-template <int NH>
-__device__ __forceinline__ void stage_rows(uint32_t taddr, unsigned char* tile, int row, int quarter, int dh, bool keep, float mul) {
-    if (quarter * 32 >= dh) return;
-    uint32_t r[32];
-    tmem_ld_32x32(taddr, r);
-    tmem_ld_wait_32(r);
-    unsigned char* line = tile + (quarter >> 1) * kAttnPart + row * 128;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        uint4 w;
-        w.x = pack_bf16(__uint_as_float(r[8 * c]) * mul, __uint_as_float(r[8 * c + 1]) * mul);
-        w.y = pack_bf16(__uint_as_float(r[8 * c + 2]) * mul, __uint_as_float(r[8 * c + 3]) * mul);
-        w.z = pack_bf16(__uint_as_float(r[8 * c + 4]) * mul, __uint_as_float(r[8 * c + 5]) * mul);
-        w.w = pack_bf16(__uint_as_float(r[8 * c + 6]) * mul, __uint_as_float(r[8 * c + 7]) * mul);
-        if (!keep) w = make_uint4(0u, 0u, 0u, 0u);
-        *reinterpret_cast<uint4*>(line + ((((quarter & 1) * 4 + c) ^ (row & 7)) * 16)) = w;
-    }
 }
 
 template <int NH>

@@ -54,25 +54,33 @@ __device__ __forceinline__ void clear_rows(unsigned char* tile, int lo, int hi, 
         }
 }
 
-// 32 accumulator columns of this warp's lanes as scaled bf16 into rows of global memory: `dst` is the row's first channel of the
-// head, `c0` the first channel of the 32.  A row that is not kept gets zeros; one that does not exist (row_ok false) nothing.
-__device__ __forceinline__ void store_rows(uint32_t taddr, __nv_bfloat16* dst, int c0, int dh, bool row_ok, bool keep, float mul) {
-    for (int c = 0; c < 32 && c0 + c < dh; c += 16) {
-        uint32_t r[16];
-        tmem_ld_32x16(taddr + uint32_t(c), r);
-        tmem_ld_wait_16(r);
-        uint4 w[2];
-        uint32_t* u = reinterpret_cast<uint32_t*>(w);
+// A place in a ring and how often it has come round.
+template <int N> struct RingAt {
+    int slot = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next() { if (++slot == N) { slot = 0; phase ^= 1u; } }
+};
+
+// 32 columns of an accumulator as scaled bf16 into the staging tile (rows of 128 bytes, 128-byte swizzle); rows not kept become zeros.
+template <int NH>
+__device__ __forceinline__ void stage_rows(uint32_t taddr, unsigned char* tile, int row, int quarter, int dh, bool keep, float mul) {
+    if (quarter * 32 >= dh) return;
+    uint32_t r[32];
+    tmem_ld_32x32(taddr, r);
+    tmem_ld_wait_32(r);
+    unsigned char* line = tile + (quarter >> 1) * kAttnPart + row * 128;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            u[e] = keep ? pack_bf16(__uint_as_float(r[2 * e]) * mul, __uint_as_float(r[2 * e + 1]) * mul) : 0u;
-        if (row_ok) {
-            uint4* to = reinterpret_cast<uint4*>(dst + c0 + c);
-            to[0] = w[0];
-            if (c0 + c + 8 < dh) to[1] = w[1];
-        }
+    for (int c = 0; c < 4; ++c) {
+        uint4 w;
+        w.x = pack_bf16(__uint_as_float(r[8 * c]) * mul, __uint_as_float(r[8 * c + 1]) * mul);
+        w.y = pack_bf16(__uint_as_float(r[8 * c + 2]) * mul, __uint_as_float(r[8 * c + 3]) * mul);
+        w.z = pack_bf16(__uint_as_float(r[8 * c + 4]) * mul, __uint_as_float(r[8 * c + 5]) * mul);
+        w.w = pack_bf16(__uint_as_float(r[8 * c + 6]) * mul, __uint_as_float(r[8 * c + 7]) * mul);
+        if (!keep) w = make_uint4(0u, 0u, 0u, 0u);
+        *reinterpret_cast<uint4*>(line + ((((quarter & 1) * 4 + c) ^ (row & 7)) * 16)) = w;
     }
 }
+
 // Zeros for `rows` rows of one head, by `threads` threads.
 __device__ __forceinline__ void zero_rows(__nv_bfloat16* base, int64_t ld, int rows, int dh, int thread, int threads) {
     const int v = dh / 8;
