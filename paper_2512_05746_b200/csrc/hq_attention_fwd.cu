@@ -6,9 +6,9 @@
 //   S = Q K^T        both operands from shared memory (128-byte swizzle), fp32 in 128 columns of tensor memory
 //   P = exp2(c S - c m) as bf16 in tensor memory
 //   O += P V         P from tensor memory, V from shared memory, read along its keys without a transpose
-// Warp 0 issues, warp 1 takes items and loads, warp 2 stores, warp 3 clears rows outside the lengths; warps 4-7 do the softmax of the first
-// tile and warps 8-11 that of the second, thread = query row (two threads a row, with twice the warps, spend on telling each other the
-// maximum what they gain).  Up to 64 channels P has columns of its own, and the next block's S is computed under this one's exponentials; above, P
+// Warp 0 issues, warp 1 takes items and loads, warp 2 stores, warp 3 clears rows outside the lengths; warps 4-11 do the softmax of the first
+// tile and warps 12-19 that of the second: thread = query row, 64 of the block's 128 keys; the two halves of a row tell each other their
+// maximum.  Up to 64 channels P has columns of its own, and the next block's S is computed under this one's exponentials; above, P
 // stands over S, whose next block comes behind the product that reads P, and the other tile's exponentials cover that time.
 // The running maximum moves only when a block's maximum exceeds it by more than 2^8 in the exponent: the weights stay below 2^8, the
 // division by the row sum at the end is the same, and O is read and rescaled in tensor memory almost never.  P is rounded to bf16
@@ -19,19 +19,20 @@ namespace hq {
 namespace {
 
 constexpr int32_t kStatusFwdWait = 0x700, kStatusFwdTma = 0x701, kStatusFwdSmem = 0x702;
-constexpr int kFwdWarps = 8, kFwdFirst = 4;        // of the softmax; in front of them the others
+constexpr int kFwdWarps = 16, kFwdFirst = 4;       // of the softmax; in front of them the others
 constexpr int kFwdThreads = (kFwdFirst + kFwdWarps) * 32;
 
 template <int NH> struct FwdRings {
     static constexpr int kQ = NH == 1 ? 2 : 1;     // pairs of query tiles: the next item's loads begin under this one's last steps
-    static constexpr int kK = NH == 1 ? 4 : 3, kV = NH == 1 ? 4 : 2;
+    static constexpr int kK = NH == 1 ? 4 : 2, kV = NH == 1 ? 4 : 2;
     static constexpr int kTile = NH * kAttnPart;
     static constexpr int kTiles = (2 * kQ + kK + kV) * kTile;
 };
 // Columns of tensor memory: S of the tiles at 0 and 128, then
 template <int NH> struct FwdTmem {
     static __device__ __forceinline__ uint32_t o(int t) { return 256u + uint32_t(t) * (NH == 1 ? 64u : 128u); }
-    static __device__ __forceinline__ uint32_t p(int t) { return NH == 1 ? 384u + uint32_t(t * 64) : uint32_t(t * 128); }    // bf16 weights
+    // bf16 weights of keys 64 h ..: over the scores of the half where there are no columns left
+    static __device__ __forceinline__ uint32_t p(int t, int h) { return NH == 1 ? 384u + uint32_t(t * 64 + h * 32) : uint32_t(t * 128 + h * 64); }
 };
 
 struct FwdParams {
@@ -49,6 +50,8 @@ template <int NH> struct FwdBars {
     using R = FwdRings<NH>;
     uint64_t q_full[R::kQ], q_empty[R::kQ], k_full[R::kK], k_empty[R::kK], v_full[R::kV], v_ready[R::kV], v_empty[R::kV];
     uint64_t s[2], read[2], p[2], o[2], staged[R::kQ], item_full[2], item_empty[2];
+    uint64_t turn[2][8], pair[8];                  // a warp of the first tile has done its exponentials / one of the second; halves of a row
+    float most[2][2][2][kAttnTile];                // [exchange & 1][tile][half][row]: a half row's maximum, at the end its sum
     uint32_t item[2], tmem_slot;
 };
 template <int NH> constexpr size_t fwd_smem() { return size_t(FwdRings<NH>::kTiles) + sizeof(FwdBars<NH>); }
@@ -205,7 +208,7 @@ __device__ __forceinline__ void fwd_issue(const FwdParams& p, unsigned char* sme
             tc_fence_after();
 #pragma unroll
             for (int x = 0; x < kAttnTile / 16; ++x)
-                mma_bf16_ts(tmem_base + T::o(tile), tmem_base + T::p(tile) + uint32_t(8 * x), db + uint64_t(x * 128), idesc_o,
+                mma_bf16_ts(tmem_base + T::o(tile), tmem_base + T::p(tile, x >> 2) + uint32_t(8 * (x & 3)), db + uint64_t(x * 128), idesc_o,
                             (j | x) != 0 ? 1u : 0u);
             mma_commit(&bar.o[tile]);
         };
@@ -265,9 +268,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_fwd_kernel(const __g
         for (int i = 0; i < R::kV; ++i) { mbar_init(&bar.v_full[i], 1); mbar_init(&bar.v_ready[i], 1); mbar_init(&bar.v_empty[i], 1); }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bar.s[i], 1); mbar_init(&bar.o[i], 1);
+            for (int w = 0; w < 8; ++w) mbar_init(&bar.turn[i][w], 1);
             mbar_init(&bar.read[i], kFwdWarps / 2); mbar_init(&bar.p[i], kFwdWarps / 2);
             mbar_init(&bar.item_full[i], 1); mbar_init(&bar.item_empty[i], kFwdWarps + 2 + (p.ragged ? 1 : 0));
         }
+        for (int i = 0; i < 8; ++i) mbar_init(&bar.pair[i], 2);
         fence_barrier_init();
     }
     if (warp == 1 && lane < 4) tma_prefetch_desc(&m.q + lane);
@@ -310,13 +315,25 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_fwd_kernel(const __g
     } else if (warp == 3) {
         if (p.ragged) fwd_clear<NH>(p, smem, bar, lane);
     } else {
-        const int tile = (warp - kFwdFirst) >> 2, row = (warp & 3) * 32 + lane;
+        const int tile = (warp - kFwdFirst) >> 3, half = ((warp - kFwdFirst) >> 2) & 1, row = (warp & 3) * 32 + lane;
         const uint32_t t_lane = tmem_base + (uint32_t((warp & 3) * 32) << 16);
-        const uint32_t t_s = t_lane + uint32_t(tile * 128), t_p = t_lane + T::p(tile), t_o = t_lane + T::o(tile);
+        const uint32_t t_s = t_lane + uint32_t(tile * 128 + half * 64), t_p = t_lane + T::p(tile, half), t_o = t_lane + T::o(tile);
         const float sc = s.scale_log2;
         RingAt<2> told;
         RingAt<R::kQ> q;
-        uint32_t n = 0;                            // blocks over all items
+        uint64_t* pair = &bar.pair[tile * 4 + (warp & 3)];
+        const int lot = half * 4 + (warp & 3);
+        uint32_t n = 0, turns = 0, told_pair = 0;  // blocks over all items; of these where both tiles take turns; exchanges
+        // gives the row's other half a value, returns the other's
+        auto exchange = [&](float mine, float& other) {
+            bar.most[told_pair & 1u][tile][half][row] = mine;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(pair);
+            const bool told_ok = mbar_wait_warp(pair, told_pair & 1u, p.dev_status, kStatusFwdWait);
+            other = *const_cast<volatile float*>(&bar.most[told_pair & 1u][tile][half ^ 1][row]);
+            ++told_pair;
+            return told_ok;
+        };
         for (;;) {
             const unsigned index = fwd_next<NH>(p, bar, told, lane);
             if (index >= p.items) break;
@@ -326,11 +343,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_fwd_kernel(const __g
             if (t.blocks == 0) {                   // no query of the two tiles sees a key
                 const int first = t.q0 + tile * kAttnTile;
                 zero_rows(p.out + (int64_t(t.n) * s.Lq + first) * p.ldo + t.head * s.dh, p.ldo, min(kAttnTile, s.Lq - first), s.dh,
-                          int(threadIdx.x) & 127, 128);
-                if (i < s.Lq) *lse = -INFINITY;
+                          (int(threadIdx.x) - kFwdFirst * 32) & 255, 256);
+                if (half == 0 && i < s.Lq) *lse = -INFINITY;
                 continue;
             }
-            const int blocks = t.nb[tile];
+            const int blocks = t.nb[tile], both = min(t.nb[0], t.nb[1]);
             const int limit = i < t.sm.q_hi ? attn_key_limit(s, t.sm, i) : 0;
             float m_run = -INFINITY, l_run = 0.f;
             bool ok = true;
@@ -338,29 +355,32 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_fwd_kernel(const __g
                 ok = mbar_wait_warp(&bar.s[tile], n & 1u, p.dev_status, kStatusFwdWait);
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t sreg[128];
+                uint32_t sreg[64];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld_32x32(t_s + uint32_t(c * 32), *reinterpret_cast<uint32_t (*)[32]>(&sreg[32 * c]));
+                for (int c = 0; c < 2; ++c) tmem_ld_32x32(t_s + uint32_t(c * 32), *reinterpret_cast<uint32_t (*)[32]>(&sreg[32 * c]));
 #pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld_wait_32(*reinterpret_cast<uint32_t (*)[32]>(&sreg[32 * c]));
+                for (int c = 0; c < 2; ++c) tmem_ld_wait_32(*reinterpret_cast<uint32_t (*)[32]>(&sreg[32 * c]));
                 if (NH == 1) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bar.read[tile]);
                 }
-                const int valid = limit - j * kAttnTile;
-                if (__any_sync(0xffffffffu, valid < kAttnTile)) {
+                const int valid = limit - j * kAttnTile - half * 64;
+                if (__any_sync(0xffffffffu, valid < 64)) {
 #pragma unroll
-                    for (int e = 0; e < 128; ++e)
+                    for (int e = 0; e < 64; ++e)
                         if (e >= valid) sreg[e] = 0xFF800000u;
                 }
                 float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int e = 0; e < 128; e += 8) {
+                for (int e = 0; e < 64; e += 8) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) m4[c] = max3(m4[c], __uint_as_float(sreg[e + 2 * c]), __uint_as_float(sreg[e + 2 * c + 1]));
                 }
-                const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+                float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), other;
+                ok = exchange(mx, other);
+                if (!ok) break;
+                mx = fmaxf(mx, other);
                 // first block with a key: the difference is infinite; none yet: -inf - -inf compares false and -inf stays
                 const bool moved = (mx - m_run) * sc > 8.0f;
                 const float m_new = moved ? mx : m_run;
@@ -372,7 +392,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_fwd_kernel(const __g
                     if (!ok) break;
                     if (__any_sync(0xffffffffu, moved)) {
                         tc_fence_after();
-                        for (int c = 0; c < s.dh; c += 16) {
+                        for (int c = half * 32; c < s.dh; c += (c & 31) == 16 ? 48 : 16) {        // its 32 columns of each 64
                             uint32_t r[16];
                             tmem_ld_32x16(t_o + uint32_t(c), r);
                             tmem_ld_wait_16(r);
@@ -382,10 +402,17 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_fwd_kernel(const __g
                         }
                     }
                 }
+                // The two warps of a scheduler take turns at the exponentials (16 a clock in an SM): side by side both would be at them, then
+                // both at the rest.  Only the order of work hangs on this.
+                if (j < both) {
+                    if (tile == 1) ok = mbar_wait_warp(&bar.turn[0][lot], turns & 1u, p.dev_status, kStatusFwdWait);
+                    else if (turns > 0) ok = mbar_wait_warp(&bar.turn[1][lot], (turns - 1u) & 1u, p.dev_status, kStatusFwdWait);
+                    if (!ok) break;
+                }
                 const f32x2 sc2 = pk2(sc, sc), nmc2 = pk2(-mc, -mc);
                 f32x2 sum2[2] = {pk2(0.f, 0.f), pk2(0.f, 0.f)};
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 0; c < 2; ++c) {
                     uint32_t w[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
@@ -397,6 +424,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_fwd_kernel(const __g
                     }
                     tmem_st_32x16(t_p + uint32_t(c * 16), w);
                 }
+                if (j < both) {
+                    if (lane == 0) mbar_arrive(&bar.turn[tile][lot]);
+                    ++turns;
+                }
                 float s0, s1;
                 upk2(add2(sum2[0], sum2[1]), s0, s1);
                 l_run = fmaf(l_run, alpha, s0 + s1);
@@ -407,6 +438,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_fwd_kernel(const __g
                 if (lane == 0) mbar_arrive(&bar.p[tile]);
                 ++n;
             }
+            float other = 0.f;
+            ok = ok && exchange(l_run, other);
+            l_run += other;
             if (ok && blocks > 0) ok = mbar_wait_warp(&bar.o[tile], (n - 1u) & 1u, p.dev_status, kStatusFwdWait);
             else if (ok) ok = mbar_wait_warp(&bar.q_full[q.slot], q.phase, p.dev_status, kStatusFwdTma);     // zeros are staged behind the tile's load
             if (!ok) break;
@@ -415,8 +449,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_fwd_kernel(const __g
             const float inv = keep ? 1.0f / l_run : 0.f;
             unsigned char* stage = smem + (2 * q.slot + tile) * R::kTile;
 #pragma unroll
-            for (int c = 0; c < 2 * NH; ++c) stage_rows<NH>(t_o + uint32_t(c * 32), stage, row, c, s.dh, keep, inv);
-            if (i < s.Lq) *lse = keep ? m_run * s.scale + logf(l_run) : -INFINITY;
+            for (int h = 0; h < NH; ++h) stage_rows<NH>(t_o + uint32_t(h * 64 + half * 32), stage, row, h * 2 + half, s.dh, keep, inv);
+            if (half == 0 && i < s.Lq) *lse = keep ? m_run * s.scale + logf(l_run) : -INFINITY;
             tc_fence_before();
             fence_proxy_async_smem();
             __syncwarp();
