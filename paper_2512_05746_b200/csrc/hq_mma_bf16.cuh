@@ -85,21 +85,27 @@ __device__ __forceinline__ bool mbar_poll(uint64_t* bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
-static __device__ __noinline__ bool mbar_wait_longer(uint64_t* bar, uint32_t parity, int32_t* dev_status, int32_t code, uint32_t lanes) {
-    const long long t0 = clock64();
-    for (;;) {
-        if (__all_sync(lanes, mbar_poll(bar, parity))) return true;
-        if (__any_sync(lanes, clock64() - t0 >= 2000000000LL)) break;
-    }
-    if (dev_status) atomicExch(dev_status, code);
-    return false;
-}
+// In line, the loop too: a call would have the live registers moved to where the callee leaves them alone, wait or not.
+__device__ __forceinline__ uint32_t clock_lo() { uint32_t t; asm volatile("mov.u32 %0, %%clock;" : "=r"(t)); return t; }
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, int32_t* dev_status, int32_t code) {
-    if (__all_sync(0xffffffffu, mbar_poll(bar, parity))) return true;
-    return mbar_wait_longer(bar, parity, dev_status, code, 0xffffffffu);
+    bool ok = __all_sync(0xffffffffu, mbar_poll(bar, parity));
+    if (!ok) {
+        const uint32_t t0 = clock_lo();
+        do ok = __all_sync(0xffffffffu, mbar_poll(bar, parity)) != 0;
+        while (!ok && __all_sync(0xffffffffu, clock_lo() - t0 < 2000000000u));
+        if (!ok && dev_status) atomicExch(dev_status, code);
+    }
+    return ok;
 }
 __device__ __forceinline__ bool mbar_wait_lane(uint64_t* bar, uint32_t parity, int32_t* dev_status, int32_t code) {
-    return mbar_poll(bar, parity) || mbar_wait_longer(bar, parity, dev_status, code, __activemask());
+    bool ok = mbar_poll(bar, parity);
+    if (!ok) {
+        const uint32_t t0 = clock_lo();
+        do ok = mbar_poll(bar, parity);
+        while (!ok && clock_lo() - t0 < 2000000000u);
+        if (!ok && dev_status) atomicExch(dev_status, code);
+    }
+    return ok;
 }
 
 // 16-byte aligned bulk copy global -> shared, completion counted on an mbarrier.
