@@ -519,57 +519,20 @@ def hq_attention(qkv, Nb: int, heads: int, out, dev_status=None, stream=None) ->
            "hq_attention")
 
 
-def _here(name: str, t) -> None:
-    """A tensor whose address is handed to a kernel lies on the current device: another's may fault there, the host's does."""
-    import torch
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name}: a tensor on {t.device}, not on the current CUDA device")
+_device_now = None
 
 
-def _heads_matrix(name: str, t, heads: int, dh: int, rows: int, dtype) -> int:
-    """Checks a matrix [rows, heads * dh] whose columns are next to one another (rows may be further apart); returns its pitch."""
-    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != heads * dh or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{name}: expected {dtype} [{rows}, {heads} x {dh}] with contiguous columns, got {t.dtype} {tuple(t.shape)} "
-                         f"with strides {t.stride()}")
-    _here(name, t)
-    return t.stride(0) if rows > 1 else heads * dh
-
-
-def _vector(name: str, t, dtype, *shape):
-    """Checks an optional dense tensor of the given shape; returns its address."""
-    if t is None:
-        return None
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a dense {dtype} tensor of shape {shape}, got {t.dtype} {tuple(t.shape)}")
-    _here(name, t)
-    return t.data_ptr()
-
-
-def _workspace(t):
-    """(address, bytes) of an optional workspace."""
-    if t is None:
-        return None, 0
-    if not t.is_contiguous():
-        raise ValueError("workspace: a dense tensor")
-    _here("workspace", t)
-    return t.data_ptr(), t.nbytes
-
-
-def _rope_arguments(q, k, heads: int, kv_heads: int, gamma_q, gamma_k, cos, sin, positions):
-    import torch
-    rows, width = q.shape
-    if heads <= 0 or width % heads != 0:
-        raise ValueError(f"{width} columns do not hold {heads} heads")
-    if (k is None) != (kv_heads == 0):
-        raise ValueError("keys are given with their heads, or neither")
-    dh = width // heads
-    if (cos is None) != (sin is None) or (cos is not None and cos.dim() != 2):
-        raise ValueError("cos and sin: two tables [positions, rot / 2]")
-    npos, half = (0, 0) if cos is None else cos.shape
-    f32 = torch.float32
-    return rows, dh, (_vector("gamma_q", gamma_q, f32, dh), _vector("gamma_k", gamma_k, f32, dh)), (
-        _vector("cos", cos, f32, npos, half), _vector("sin", sin, f32, npos, half), npos, 2 * half,
-        _vector("positions", positions, torch.int32, rows))
+def _stream_and_device(stream):
+    """(stream, current device) as the native calls take them; without a CUDA device a device number that no tensor has."""
+    global _device_now
+    if _device_now is None:
+        import torch
+        _hqcall.bind_attention(torch.float32, torch.bfloat16, torch.int32, *(C.cast(getattr(lib, n), C.c_void_p).value for n in (
+            "hq_qk_norm_rope", "hq_qk_norm_rope_bwd", "hq_attention_fwd", "hq_attention_bwd")))
+        if not torch.cuda.is_available():
+            return 0, -2
+        _device_now = torch._C._cuda_getDevice
+    return _stream(stream), _device_now()
 
 
 def hq_qk_norm_rope(q, k, heads: int, kv_heads: int, gamma_q, gamma_k, eps: float, cos, sin, q_out, k_out, positions=None,
@@ -577,14 +540,9 @@ def hq_qk_norm_rope(q, k, heads: int, kv_heads: int, gamma_q, gamma_k, eps: floa
     """RMS norm of each head of q [rows, heads * dh] and k [rows, kv_heads * dh] (fp32 / bf16; slices of a fused projection as they
     are) with gamma [dh] or None, then the rotation by the tables cos, sin [positions, rot / 2] (None: no rotation) at the token's
     position (None: row modulo the table's length).  q_out / k_out may be q / k; k None with kv_heads 0: queries only."""
-    rows, dh, gamma, table = _rope_arguments(q, k, heads, kv_heads, gamma_q, gamma_k, cos, sin, positions)
-    code = _dtype_code(q)
-    ldq, ldqo = _heads_matrix("q", q, heads, dh, rows, q.dtype), _heads_matrix("q_out", q_out, heads, dh, rows, q.dtype)
-    ldk = ldko = 0
-    if k is not None:
-        ldk, ldko = _heads_matrix("k", k, kv_heads, dh, rows, q.dtype), _heads_matrix("k_out", k_out, kv_heads, dh, rows, q.dtype)
-    _check(lib.hq_qk_norm_rope(_dptr(q), ldq, _dptr(k), ldk, code, rows, heads, kv_heads, dh, *gamma, eps, *table, int(interleaved),
-                               _dptr(q_out), ldqo, _dptr(k_out) if k is not None else None, ldko, _stream(stream)), "hq_qk_norm_rope")
+    at, device = _stream_and_device(stream)
+    _check(_hqcall.qk_rope(q, k, heads, kv_heads, gamma_q, gamma_k, eps, cos, sin, q_out, k_out, positions, interleaved, at, device),
+           "hq_qk_norm_rope")
 
 
 def hq_qk_norm_rope_bwd_workspace_size(rows: int, heads: int, kv_heads: int, dh: int) -> int:
@@ -597,25 +555,9 @@ def hq_qk_norm_rope_bwd(q, k, heads: int, kv_heads: int, gamma_q, gamma_k, eps: 
                         dgamma_k, workspace, positions=None, interleaved: bool = False, stream=None) -> None:
     """Gradients of hq_qk_norm_rope: dq, dk (and fp32 dgamma_q, dgamma_k [dh] unless None) from those of its outputs and its inputs q, k.
     workspace: hq_qk_norm_rope_bwd_workspace_size bytes on the device (None where no dgamma is wanted)."""
-    import torch
-    rows, dh, gamma, table = _rope_arguments(q, k, heads, kv_heads, gamma_q, gamma_k, cos, sin, positions)
-    code = _dtype_code(q)
-    ld = [_heads_matrix(n, t, heads, dh, rows, q.dtype) for n, t in (("q", q), ("dq_out", dq_out), ("dq", dq))]
-    ldk = [0, 0, 0]
-    if k is not None:
-        ldk = [_heads_matrix(n, t, kv_heads, dh, rows, q.dtype) for n, t in (("k", k), ("dk_out", dk_out), ("dk", dk))]
-    else:
-        dk_out = dk = None
-    _check(lib.hq_qk_norm_rope_bwd(_dptr(q), ld[0], _dptr(k), ldk[0], code, rows, heads, kv_heads, dh, *gamma, eps, *table,
-                                   int(interleaved), _dptr(dq_out), ld[1], _dptr(dk_out), ldk[1], _dptr(dq), ld[2], _dptr(dk), ldk[2],
-                                   _vector("dgamma_q", dgamma_q, torch.float32, dh), _vector("dgamma_k", dgamma_k, torch.float32, dh),
-                                   *_workspace(workspace), _stream(stream)), "hq_qk_norm_rope_bwd")
-
-
-def _attention_shape(q, k, Nb: int, heads: int, kv_heads: int):
-    if Nb <= 0 or heads <= 0 or kv_heads <= 0 or q.shape[0] % Nb or k.shape[0] % Nb or q.shape[1] % heads:
-        raise ValueError(f"queries {tuple(q.shape)} and keys {tuple(k.shape)} are not {Nb} samples of {heads} / {kv_heads} heads")
-    return q.shape[0] // Nb, k.shape[0] // Nb, q.shape[1] // heads
+    at, device = _stream_and_device(stream)
+    _check(_hqcall.qk_rope_bwd(q, k, heads, kv_heads, gamma_q, gamma_k, eps, cos, sin, dq_out, dk_out, dq, dk, dgamma_q, dgamma_k, workspace,
+                               positions, interleaved, at, device), "hq_qk_norm_rope_bwd")
 
 
 def hq_attention_fwd_workspace_size(Nb: int, Lq: int, Lk: int, heads: int, kv_heads: int, dh: int) -> int:
@@ -634,34 +576,18 @@ def hq_attention_fwd(q, k, v, Nb: int, heads: int, kv_heads: int, out, lse, work
                      scale: float | None = None, dev_status=None, stream=None) -> None:
     """q, out [Nb * Lq, heads * dh], k, v [Nb * Lk, kv_heads * dh] (bf16; slices of a fused projection as they are), lse fp32
     [Nb, heads, Lq].  q_lens, k_lens: int32 [Nb] on the device, or None; scale: None for 1 / sqrt(dh)."""
-    import torch
-    Lq, Lk, dh = _attention_shape(q, k, Nb, heads, kv_heads)
-    bf = torch.bfloat16
-    ld = [_heads_matrix(n, t, h, dh, Nb * L, bf) for n, t, h, L in (("q", q, heads, Lq), ("k", k, kv_heads, Lk), ("v", v, kv_heads, Lk),
-                                                                    ("out", out, heads, Lq))]
-    _check(lib.hq_attention_fwd(_dptr(q), ld[0], _dptr(k), ld[1], _dptr(v), ld[2], Nb, Lq, Lk, heads, kv_heads, dh,
-                                dh ** -0.5 if scale is None else scale, int(causal), _vector("q_lens", q_lens, torch.int32, Nb),
-                                _vector("k_lens", k_lens, torch.int32, Nb), _dptr(out), ld[3],
-                                _vector("lse", lse, torch.float32, Nb, heads, Lq), *_workspace(workspace),
-                                _vector("dev_status", dev_status, torch.int32, 1), _stream(stream)), "hq_attention_fwd")
+    at, device = _stream_and_device(stream)
+    _check(_hqcall.attention_fwd(q, k, v, Nb, heads, kv_heads, out, lse, workspace, q_lens, k_lens, causal, scale, dev_status, at, device),
+           "hq_attention_fwd")
 
 
 def hq_attention_bwd(q, k, v, out, lse, dout, Nb: int, heads: int, kv_heads: int, dq, dk, dv, workspace, q_lens=None, k_lens=None,
                      causal: bool = False, scale: float | None = None, dev_status=None, stream=None) -> None:
     """Gradients dq, dk, dv of hq_attention_fwd from dout, its inputs and its results out and lse (the other arguments as there).
     workspace: hq_attention_bwd_workspace_size bytes on the device."""
-    import torch
-    Lq, Lk, dh = _attention_shape(q, k, Nb, heads, kv_heads)
-    bf = torch.bfloat16
-    ld = [_heads_matrix(n, t, h, dh, Nb * L, bf) for n, t, h, L in (
-        ("q", q, heads, Lq), ("k", k, kv_heads, Lk), ("v", v, kv_heads, Lk), ("out", out, heads, Lq), ("dout", dout, heads, Lq),
-        ("dq", dq, heads, Lq), ("dk", dk, kv_heads, Lk), ("dv", dv, kv_heads, Lk))]
-    _check(lib.hq_attention_bwd(_dptr(q), ld[0], _dptr(k), ld[1], _dptr(v), ld[2], _dptr(out), ld[3],
-                                _vector("lse", lse, torch.float32, Nb, heads, Lq), _dptr(dout), ld[4], Nb, Lq, Lk, heads, kv_heads, dh,
-                                dh ** -0.5 if scale is None else scale, int(causal), _vector("q_lens", q_lens, torch.int32, Nb),
-                                _vector("k_lens", k_lens, torch.int32, Nb), _dptr(dq), ld[5], _dptr(dk), ld[6], _dptr(dv), ld[7],
-                                *_workspace(workspace), _vector("dev_status", dev_status, torch.int32, 1), _stream(stream)),
-           "hq_attention_bwd")
+    at, device = _stream_and_device(stream)
+    _check(_hqcall.attention_bwd(q, k, v, out, lse, dout, Nb, heads, kv_heads, dq, dk, dv, workspace, q_lens, k_lens, causal, scale, dev_status,
+                                 at, device), "hq_attention_bwd")
 
 
 def hq_qlinear_fused(x, pw: PreparedWeight, bias, a_bits: int, y, static_scale=None, dev_status=None, stream=None) -> None:

@@ -42,8 +42,8 @@ struct BwdParams {
     unsigned* taken;                               // items taken beyond the first of every CTA
     __nv_bfloat16 *dq, *dk, *dv;
     int64_t lddq, lddk, lddv;
-    int q_tiles;
-    unsigned key_items, items;
+    int q_tiles, k_tiles;
+    unsigned key_items, items, key_chunk, chunk;   // order of the items (attn_order)
     int32_t* dev_status;
 };
 struct BwdMaps { CUtensorMap q, k, v, dout, dq, dk, dv; };
@@ -70,8 +70,9 @@ __device__ __forceinline__ BwdItem bwd_item(const BwdParams& p, unsigned index) 
     BwdItem t;
     // tiles of keys first (they walk every head of their group); under the causal mask the first keys and the last queries walk the most
     t.keys = index < p.key_items;
-    const unsigned at = t.keys ? index : index - p.key_items, heads = unsigned(t.keys ? s.kv_heads : s.heads), per = unsigned(s.Nb) * heads;
-    const unsigned block = at / per, bh = at - block * per;
+    const unsigned heads = unsigned(t.keys ? s.kv_heads : s.heads);
+    unsigned block, bh;
+    attn_order(t.keys ? index : index - p.key_items, unsigned(t.keys ? p.k_tiles : p.q_tiles), unsigned(s.Nb) * heads, t.keys ? p.key_chunk : p.chunk, block, bh);
     t.n = int(bh / heads);
     t.head = int(bh - unsigned(t.n) * heads);
     t.tile = !t.keys && s.causal ? p.q_tiles - 1 - int(block) : int(block);
@@ -593,7 +594,10 @@ extern "C" hq_status hq_attention_bwd(const void* q, int64_t ldq, const void* k,
     p.taken = reinterpret_cast<unsigned*>(static_cast<unsigned char*>(workspace) + stat_bytes);
     p.dq = static_cast<__nv_bfloat16*>(dq); p.dk = static_cast<__nv_bfloat16*>(dk); p.dv = static_cast<__nv_bfloat16*>(dv);
     p.lddq = lddq; p.lddk = lddk; p.lddv = lddv;
-    p.q_tiles = int(q_tiles); p.key_items = unsigned(key_items); p.items = unsigned(items); p.dev_status = dev_status;
+    p.q_tiles = int(q_tiles); p.k_tiles = int(k_tiles);
+    p.key_chunk = attn_chunk(causal != 0, k_tiles, Nb * kv_heads, sm_count());
+    p.chunk = attn_chunk(causal != 0, q_tiles, Nb * heads, sm_count());
+    p.key_items = unsigned(key_items); p.items = unsigned(items); p.dev_status = dev_status;
     const int rows_per_cta = 8 * (32 / (dh / 8));
     int64_t stat_ctas = (q_tiles * kAttnTile + rows_per_cta - 1) / rows_per_cta;
     if (stat_ctas > 64) stat_ctas = 64;

@@ -36,6 +36,24 @@ __device__ __forceinline__ int attn_key_limit(const AttnShape& s, const AttnSamp
     return s.causal ? min(r.kl, max(0, i + r.shift + 1)) : r.kl;
 }
 
+// The order in which tiles of (sample, head) pairs are worked on: tiles of `chunk` pairs, tile by tile.  One pair: the CTAs at work
+// share its other side's tiles in L2 (64 x 1024 tokens, 8 heads of 64, forward: 243 us with all pairs' first tiles first).  Under
+// the causal mask tiles differ in length and the longest go first among pairs enough to fill the device four times.
+__host__ inline unsigned attn_chunk(bool causal, int64_t tiles, int64_t pairs, int64_t slots) {
+    const int64_t c = causal ? (4 * slots + tiles - 1) / tiles : 1;
+    return unsigned(c < 1 ? 1 : c < pairs ? c : pairs);
+}
+__device__ __forceinline__ void attn_order(unsigned index, unsigned tiles, unsigned pairs, unsigned chunk, unsigned& tile, unsigned& pair) {
+    if (chunk == 1) {
+        pair = index / tiles;
+        tile = index - pair * tiles;
+        return;
+    }
+    const unsigned c = index / (chunk * tiles), r = index - c * (chunk * tiles), n = min(chunk, pairs - c * chunk);
+    tile = r / n;
+    pair = c * chunk + (r - tile * n);
+}
+
 // A tile is NH parts of 128 rows x 64 channels (128-byte rows, 128-byte swizzle), parts one after the other.
 constexpr int kAttnPart = kAttnTile * 128;
 template <int NH>
