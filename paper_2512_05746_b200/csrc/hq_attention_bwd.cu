@@ -44,6 +44,7 @@ struct BwdParams {
     int64_t lddq, lddk, lddv;
     int q_tiles, k_tiles;
     unsigned key_items, items, key_chunk, chunk;   // order of the items (attn_order)
+    int ragged;                                    // rows outside the lengths may lie in a tile
     int32_t* dev_status;
 };
 struct BwdMaps { CUtensorMap q, k, v, dout, dq, dk, dv; };
@@ -65,7 +66,8 @@ struct BwdItem {
     AttnSample sm;
     int first, last, total;                        // tiles [first, last) of each of its heads; steps over all of them
 };
-__device__ __forceinline__ BwdItem bwd_item(const BwdParams& p, unsigned index) {
+// `block_rows`: of the other side's tiles.
+__device__ __forceinline__ BwdItem bwd_item(const BwdParams& p, unsigned index, int block_rows = kAttnTile) {
     const AttnShape& s = p.s;
     BwdItem t;
     // tiles of keys first (they walk every head of their group); under the causal mask the first keys and the last queries walk the most
@@ -79,12 +81,12 @@ __device__ __forceinline__ BwdItem bwd_item(const BwdParams& p, unsigned index) 
     t.row0 = t.tile * kAttnTile;
     t.sm = attn_sample(s, t.n);
     if (t.keys) {
-        t.first = max(t.sm.q_lo, s.causal ? t.row0 - t.sm.shift : 0) / kAttnTile;
-        t.last = t.row0 < t.sm.kl ? (t.sm.q_hi + kAttnTile - 1) / kAttnTile : 0;
+        t.first = max(t.sm.q_lo, s.causal ? t.row0 - t.sm.shift : 0) / block_rows;
+        t.last = t.row0 < t.sm.kl ? (t.sm.q_hi + block_rows - 1) / block_rows : 0;
     } else {
         const int end = min(t.row0 + kAttnTile, t.sm.q_hi) - 1;
         t.first = 0;
-        t.last = t.row0 > end || end < t.sm.q_lo ? 0 : (attn_key_limit(s, t.sm, end) + kAttnTile - 1) / kAttnTile;
+        t.last = t.row0 > end || end < t.sm.q_lo ? 0 : (attn_key_limit(s, t.sm, end) + block_rows - 1) / block_rows;
     }
     t.total = max(0, t.last - t.first) * (t.keys ? s.heads / s.kv_heads : 1);
     return t;
@@ -487,6 +489,298 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
     if (warp == 0) tmem_dealloc(tmem_base, 512);
 }
 
+// ---- up to 64 channels: small CTAs, two an SM, one tile each.  The other side comes in blocks of 64, so that S, dP and the sums of a
+// CTA fit 256 columns of tensor memory; what one CTA waits for, the other's work covers.  Warps 0-7: thread = lane, four warps per half
+// of the 64 columns; one lane of warp 8 issues, warp 9 loads and clears rows outside the lengths.
+constexpr int kSmallBlock = 64, kSmallStages = 3, kSmallThreads = 320, kSmallPart = kSmallBlock * 128;
+constexpr size_t kSmallSmem = size_t(2) * kAttnPart + size_t(kSmallStages) * (2 * kSmallPart + 2 * kSmallBlock * 4) + 1024;
+
+struct SmallBars { uint64_t keep, full[kSmallStages], ready[kSmallStages], empty[kSmallStages], s, dp[2], read, ds[2], acc; };
+
+// KEYS: A0 = K, A1 = V, B0 = Q, B1 = dout; else A0 = Q, A1 = dout, B0 = K, B1 = V.  Columns: S at 0, dP at 64 (queries: a second
+// buffer at 128), the sums at 128 (dv) and 192 (dk, dq).
+template <bool KEYS>
+__device__ __forceinline__ bool small_run(const BwdMaps& m, const BwdParams& p, const BwdItem& t, unsigned char* smem, SmallBars& bar, uint32_t tmem_base) {
+    constexpr uint32_t kTile = kAttnPart;
+    const AttnShape& s = p.s;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    unsigned char* sB = smem + 2 * kTile;
+    float* stat = reinterpret_cast<float*>(sB + kSmallStages * 2 * kSmallPart);              // of a stage: -lse log2(e), -D of 64 queries
+    const int group = s.heads / s.kv_heads, first = t.first, last = t.last, total = t.total;
+    bool ok = true;
+
+    if (warp == 9) {
+        const CUtensorMap *a0 = KEYS ? &m.k : &m.q, *a1 = KEYS ? &m.v : &m.dout, *b0 = KEYS ? &m.q : &m.k, *b1 = KEYS ? &m.dout : &m.v;
+        // rows of tokens outside the lengths (zero as they come behind the last row of the matrix) are made zero where they would meet
+        // zero probabilities in a sum: queries and their gradients, or keys
+        const int lo = KEYS ? t.sm.q_lo : 0, hi = KEYS ? t.sm.q_hi : t.sm.kl, exist = KEYS ? s.Lq : s.Lk;
+        auto make_ready = [&](int i, int block) {
+            const int stage = i % kSmallStages, r0 = block * kSmallBlock;
+            if (!mbar_wait_warp(&bar.full[stage], uint32_t(i / kSmallStages) & 1u, p.dev_status, kStatusBwdTma)) return false;
+            if (lo > r0 || hi < min(r0 + kSmallBlock, exist)) {
+                unsigned char* at = sB + stage * 2 * kSmallPart;
+                for (int f = lane; f < kSmallBlock * 8; f += 32) {
+                    const int r = r0 + (f >> 3);
+                    if (r < lo || r >= hi) {
+                        *reinterpret_cast<uint4*>(at + f * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        if (KEYS) *reinterpret_cast<uint4*>(at + kSmallPart + f * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.ready[stage]);
+            return true;
+        };
+        if (elect_one()) {
+            mbar_expect_tx(&bar.keep, 2 * kTile);
+            for (int x = 0; x < 2; ++x) {          // boxes of 64 rows
+                tma_load_4d(smem + x * kSmallPart, a0, &bar.keep, 0, t.head, t.row0 + x * kSmallBlock, t.n);
+                tma_load_4d(smem + kTile + x * kSmallPart, a1, &bar.keep, 0, t.head, t.row0 + x * kSmallBlock, t.n);
+            }
+        }
+        __syncwarp();
+        int head = KEYS ? t.head * group : t.head / group, block = first, before = first, i = 0;
+        for (; i < total; ++i) {
+            const int stage = i % kSmallStages, use = i / kSmallStages;
+            if (use > 0) ok = mbar_wait_warp(&bar.empty[stage], uint32_t(use - 1) & 1u, p.dev_status, kStatusBwdWait);
+            if (!ok) break;
+            if (elect_one()) {
+                unsigned char* to = sB + stage * 2 * kSmallPart;
+                mbar_expect_tx(&bar.full[stage], 2 * kSmallPart + (KEYS ? 2 * kSmallBlock * 4 : 0));
+                tma_load_4d(to, b0, &bar.full[stage], 0, head, block * kSmallBlock, t.n);
+                tma_load_4d(to + kSmallPart, b1, &bar.full[stage], 0, head, block * kSmallBlock, t.n);
+                if (KEYS) {
+                    const float* from = p.stats + (int64_t(t.n * s.heads + head) * p.q_tiles + (block >> 1)) * (2 * kAttnTile) + (block & 1) * kSmallBlock;
+                    bulk_load(stat + stage * 2 * kSmallBlock, from, kSmallBlock * 4, &bar.full[stage]);
+                    bulk_load(stat + stage * 2 * kSmallBlock + kSmallBlock, from + kAttnTile, kSmallBlock * 4, &bar.full[stage]);
+                }
+            }
+            __syncwarp();
+            if (p.ragged && i > 0) {               // one step behind the loads
+                ok = make_ready(i - 1, before);
+                if (!ok) { ++i; break; }
+                if (++before == last) before = first;
+            }
+            if (++block == last) { block = first; ++head; }
+        }
+        if (ok && p.ragged) ok = make_ready(total - 1, before);
+        // what was requested lands before the CTA's shared memory is given up, on every way out
+        mbar_wait_warp(&bar.keep, 0, nullptr, 0);
+        for (int x = max(0, i - kSmallStages); x < i; ++x) mbar_wait_warp(&bar.full[x % kSmallStages], uint32_t(x / kSmallStages) & 1u, nullptr, 0);
+    } else if (warp == 8) {
+        if (elect_one()) {
+            const uint32_t idesc_s = make_idesc_bf16(kAttnTile, kSmallBlock, false), idesc_acc = make_idesc_bf16(kAttnTile, (s.dh + 15) & ~15, true);
+            const int ksteps = (s.dh + 15) / 16;
+            const uint64_t dA = make_sw128_kmajor_desc(smem_u32(smem)), dB = make_sw128_kmajor_desc(smem_u32(sB)), dBt = make_sw128_mnmajor_desc(smem_u32(sB), kSmallPart);
+            auto wait = [&](uint64_t* b, uint32_t parity, int32_t code) { return mbar_wait_lane(b, parity, p.dev_status, code); };
+            auto landed = [&](int i) {
+                const int stage = i % kSmallStages;
+                return wait(p.ragged ? &bar.ready[stage] : &bar.full[stage], uint32_t(i / kSmallStages) & 1u, kStatusBwdTma);
+            };
+            auto score_product = [&](int i, int which, uint32_t column, uint64_t* done) {    // which: 0 scores, 1 dP
+                const uint64_t a = dA + uint64_t(which) * (kTile >> 4), b = dB + uint64_t((i % kSmallStages) * 2 + which) * (kSmallPart >> 4);
+                tc_fence_after();
+                for (int k = 0; k < ksteps; ++k) mma_bf16(tmem_base + column, a + uint64_t(2 * k), b + uint64_t(2 * k), idesc_s, k != 0 ? 1u : 0u);
+                mma_commit(done);
+            };
+            // bf16 operand of each half in the first half of its 32 columns
+            auto acc_product = [&](int i, int which, uint32_t column, uint32_t acc) {
+                const uint64_t b = dBt + uint64_t((i % kSmallStages) * 2 + which) * (kSmallPart >> 4);
+                tc_fence_after();
+#pragma unroll
+                for (int k = 0; k < kSmallBlock / 16; ++k)
+                    mma_bf16_ts(tmem_base + acc, tmem_base + column + uint32_t((k >> 1) * 32 + (k & 1) * 8), b + uint64_t(k * 128), idesc_acc,
+                                (i | k) != 0 ? 1u : 0u);
+            };
+            ok = wait(&bar.keep, 0, kStatusBwdTma) && landed(0);
+            if (ok) {
+                score_product(0, 0, 0u, &bar.s);
+                score_product(0, 1, 64u, &bar.dp[0]);
+            }
+            // Products run in the order of their issue: one that overwrites another's operand in tensor memory is issued behind it.
+            for (int i = 0; i < total && ok; ++i) {
+                const uint32_t par = uint32_t(i) & 1u, next = par ^ 1u;
+                const bool more = i + 1 < total;
+                ok = wait(&bar.read, par, kStatusBwdWait);                     // S read (queries), P in its place (keys)
+                if (!ok) break;
+                if (KEYS) acc_product(i, 1, 0u, 128u);
+                if (more) {
+                    ok = landed(i + 1);
+                    if (!ok) break;
+                    score_product(i + 1, 0, 0u, &bar.s);
+                    if (!KEYS) score_product(i + 1, 1, next ? 128u : 64u, &bar.dp[next]);
+                }
+                ok = wait(&bar.ds[par], uint32_t(i >> 1) & 1u, kStatusBwdWait);
+                if (!ok) break;
+                acc_product(i, 0, KEYS || !par ? 64u : 128u, 192u);
+                mma_commit(&bar.empty[i % kSmallStages]);
+                if (KEYS && more) score_product(i + 1, 1, 64u, &bar.dp[next]);
+            }
+            if (ok) mma_commit(&bar.acc);
+        }
+        __syncwarp();
+    } else {
+        const int half = warp >> 2, row = (warp & 3) * 32 + lane, r = t.row0 + row;
+        const uint32_t t_lane = tmem_base + (uint32_t((warp & 3) * 32) << 16), t_s = t_lane + uint32_t(half * 32);
+        const f32x2 sc2 = pk2(s.scale_log2, s.scale_log2);
+        f32x2 row_lse = 0, row_d = 0;
+        int limit = 0;                                         // queries: keys the row sees
+        if (!KEYS) {
+            const float* stats = p.stats + (int64_t(t.n * s.heads + t.head) * p.q_tiles + t.tile) * (2 * kAttnTile) + row;
+            const float l = __ldg(stats), d = __ldg(stats + kAttnTile);
+            row_lse = pk2(l, l);
+            row_d = pk2(d, d);
+            limit = r < t.sm.q_hi ? attn_key_limit(s, t.sm, r) : 0;
+            if (limit == 1) limit = 0;                         // a weight of 1, whatever its score: no gradient
+        }
+        int block = first;
+        for (int i = 0; i < total; ++i) {
+            const uint32_t par = uint32_t(i) & 1u;
+            const int c0 = block * kSmallBlock + half * 32, stage = i % kSmallStages;        // the first column's query or key
+            if (++block == last) block = first;
+            ok = mbar_wait_warp(&bar.s, par, p.dev_status, kStatusBwdWait);
+            if (KEYS) ok = ok && mbar_wait_warp(&bar.full[stage], uint32_t(i / kSmallStages) & 1u, p.dev_status, kStatusBwdTma);
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t sr[32], w[16];
+            tmem_ld_32x32(t_s, sr);
+            tmem_ld_wait_32(sr);
+            if (!KEYS) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bar.read);
+            }
+            const float* nl = stat + stage * 2 * kSmallBlock + half * 32;
+            f32x2 pr[16];
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                f32x2 l0 = row_lse, l1 = row_lse;
+                if (KEYS) {
+                    const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(nl + 2 * e);
+                    l0 = l.x; l1 = l.y;
+                }
+                float z[4];
+                upk2(fma2(pk2(__uint_as_float(sr[2 * e]), __uint_as_float(sr[2 * e + 1])), sc2, l0), z[0], z[1]);
+                upk2(fma2(pk2(__uint_as_float(sr[2 * e + 2]), __uint_as_float(sr[2 * e + 3])), sc2, l1), z[2], z[3]);
+                pr[e] = pk2(ex2(z[0]), ex2(z[1]));
+                pr[e + 1] = pk2(ex2(z[2]), ex2(z[3]));
+            }
+            if (KEYS) {
+                const int from = s.causal ? r - t.sm.shift - c0 : 0;           // the first query that sees the row's key
+                if (__any_sync(0xffffffffu, from > 0)) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float a, b;
+                        upk2(pr[e], a, b);
+                        pr[e] = pk2(2 * e < from ? 0.f : a, 2 * e + 1 < from ? 0.f : b);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    float a, b;
+                    upk2(pr[e], a, b);
+                    w[e] = pack_bf16(a, b);
+                }
+                tmem_st_32x16(t_s, w);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bar.read);
+            }
+            ok = mbar_wait_warp(&bar.dp[par], uint32_t(i >> 1) & 1u, p.dev_status, kStatusBwdWait);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t t_dp = t_s + (KEYS || !par ? 64u : 128u);
+            tmem_ld_32x32(t_dp, sr);
+            tmem_ld_wait_32(sr);
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                f32x2 d0 = row_d, d1 = row_d;
+                if (KEYS) {
+                    const ulonglong2 d = *reinterpret_cast<const ulonglong2*>(nl + kSmallBlock + 2 * e);
+                    d0 = d.x; d1 = d.y;
+                }
+                float a, b;
+                upk2(mul2(pr[e], add2(pk2(__uint_as_float(sr[2 * e]), __uint_as_float(sr[2 * e + 1])), d0)), a, b);
+                w[e] = pack_bf16(a, b);
+                upk2(mul2(pr[e + 1], add2(pk2(__uint_as_float(sr[2 * e + 2]), __uint_as_float(sr[2 * e + 3])), d1)), a, b);
+                w[e + 1] = pack_bf16(a, b);
+            }
+            if (KEYS) {
+                if (t.sm.kl == 1) {                            // every query sees one key only
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w[e] = 0u;
+                }
+            } else {
+                const int valid = limit - c0;                  // what lies behind may be anything
+                if (__any_sync(0xffffffffu, valid < 32)) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w[e] &= 2 * e + 1 < valid ? 0xFFFFFFFFu : 2 * e < valid ? 0xFFFFu : 0u;
+                }
+            }
+            tmem_st_32x16(t_dp, w);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.ds[par]);
+        }
+        if (ok) ok = mbar_wait_warp(&bar.acc, 0, p.dev_status, kStatusBwdWait);
+        if (ok) {
+            tc_fence_after();
+            const bool kept = KEYS ? r < t.sm.kl : r >= t.sm.q_lo && r < t.sm.q_hi;
+            stage_rows<1>(t_s + 192u, smem, row, half, s.dh, kept, s.scale);
+            if (KEYS) stage_rows<1>(t_s + 128u, smem + kTile, row, half, s.dh, kept, 1.0f);
+            fence_proxy_async_smem();
+        }
+    }
+    return ok;
+}
+
+__global__ void __launch_bounds__(kSmallThreads, 2) attention_bwd_small_kernel(const __grid_constant__ BwdMaps m, const BwdParams p) {
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    __shared__ SmallBars bar;
+    __shared__ uint32_t tmem_slot;
+    const AttnShape& s = p.s;
+    const int warp = threadIdx.x >> 5;
+    const BwdItem t = bwd_item(p, blockIdx.x, kSmallBlock);
+    if (t.total == 0) {                            // nothing seen: the gradient is zero
+        if (t.keys) {
+            const int rows = min(kAttnTile, s.Lk - t.row0);
+            const int64_t at = int64_t(t.n) * s.Lk + t.row0;
+            zero_rows(p.dk + at * p.lddk + t.head * s.dh, p.lddk, rows, s.dh, int(threadIdx.x), kSmallThreads);
+            zero_rows(p.dv + at * p.lddv + t.head * s.dh, p.lddv, rows, s.dh, int(threadIdx.x), kSmallThreads);
+        } else {
+            zero_rows(p.dq + (int64_t(t.n) * s.Lq + t.row0) * p.lddq + t.head * s.dh, p.lddq, min(kAttnTile, s.Lq - t.row0), s.dh, int(threadIdx.x), kSmallThreads);
+        }
+        return;
+    }
+    if (threadIdx.x == 0) {
+        mbar_init(&bar.keep, 1);
+        for (int i = 0; i < kSmallStages; ++i) { mbar_init(&bar.full[i], 1); mbar_init(&bar.ready[i], 1); mbar_init(&bar.empty[i], 1); }
+        mbar_init(&bar.s, 1); mbar_init(&bar.acc, 1); mbar_init(&bar.read, 8);
+        for (int i = 0; i < 2; ++i) { mbar_init(&bar.dp[i], 1); mbar_init(&bar.ds[i], 8); }
+        fence_barrier_init();
+    }
+    if (warp == 9 && (threadIdx.x & 31) < 7) tma_prefetch_desc(&m.q + (threadIdx.x & 31));
+    if (warp == 8) { __syncwarp(); tmem_alloc(&tmem_slot, 256); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = tmem_slot;
+    const bool ok = t.keys ? small_run<true>(m, p, t, smem, bar, tmem_base) : small_run<false>(m, p, t, smem, bar, tmem_base);
+    tc_fence_before();
+    const bool all = __syncthreads_and(ok);
+    if (warp == 8) tmem_dealloc(tmem_base, 256);
+    if (all && threadIdx.x == 0) {
+        tma_store_4d(t.keys ? &m.dk : &m.dq, smem, 0, t.head, t.row0, t.n);
+        if (t.keys) tma_store_4d(&m.dv, smem + kAttnPart, 0, t.head, t.row0, t.n);
+        bulk_commit_group();
+        bulk_wait_read_all();
+    }
+}
+
 // Per query and head: -D, D = dout . out in fp32, and -lse * log2(e), in tiles of 128 rows as the gradient kernel loads them.  Rows
 // without a key, outside the lengths or behind the last get lse = +inf and D = 0: their probabilities are exp2(-inf) = 0.  A group of
 // dh / 8 lanes takes a row; memory-bound, two reads.  Also clears the count of items taken.
@@ -533,21 +827,28 @@ __global__ void __launch_bounds__(256) attention_stats_kernel(const __nv_bfloat1
 
 template <int NH>
 hq_status launch_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* dout, int64_t lddo,
-                     const BwdParams& p, cudaStream_t st) {
+                     BwdParams p, cudaStream_t st) {
     const AttnShape& s = p.s;
+    const uint32_t block = NH == 1 ? kSmallBlock : kAttnTile;  // rows of the other side's tiles; the kept ones take two boxes of 64 then
     BwdMaps m;
-    if (!encode_heads_bf16(&m.q, q, s.dh, s.heads, s.Lq, s.Nb, ldq, kAttnTile) ||
-        !encode_heads_bf16(&m.k, k, s.dh, s.kv_heads, s.Lk, s.Nb, ldk, kAttnTile) ||
-        !encode_heads_bf16(&m.v, v, s.dh, s.kv_heads, s.Lk, s.Nb, ldv, kAttnTile) ||
-        !encode_heads_bf16(&m.dout, dout, s.dh, s.heads, s.Lq, s.Nb, lddo, kAttnTile) ||
+    if (!encode_heads_bf16(&m.q, q, s.dh, s.heads, s.Lq, s.Nb, ldq, block) || !encode_heads_bf16(&m.k, k, s.dh, s.kv_heads, s.Lk, s.Nb, ldk, block) ||
+        !encode_heads_bf16(&m.v, v, s.dh, s.kv_heads, s.Lk, s.Nb, ldv, block) || !encode_heads_bf16(&m.dout, dout, s.dh, s.heads, s.Lq, s.Nb, lddo, block) ||
         !encode_heads_bf16(&m.dq, p.dq, s.dh, s.heads, s.Lq, s.Nb, p.lddq, kAttnTile) ||
         !encode_heads_bf16(&m.dk, p.dk, s.dh, s.kv_heads, s.Lk, s.Nb, p.lddk, kAttnTile) ||
         !encode_heads_bf16(&m.dv, p.dv, s.dh, s.kv_heads, s.Lk, s.Nb, p.lddv, kAttnTile))
         return HQ_ERR_CUDA;
-    if (cudaFuncSetAttribute(attention_bwd_kernel<NH>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bwd_smem<NH>())) != cudaSuccess)
-        return HQ_ERR_CUDA;
-    const unsigned sms = unsigned(sm_count()), grid = p.items < sms ? p.items : sms;
-    attention_bwd_kernel<NH><<<grid, kBwdThreads, bwd_smem<NH>(), st>>>(m, p);
+    const unsigned sms = unsigned(sm_count());
+    const int64_t slots = NH == 1 ? 2 * int64_t(sms) : int64_t(sms);
+    p.key_chunk = attn_chunk(s.causal != 0, p.k_tiles, int64_t(s.Nb) * s.kv_heads, slots);
+    p.chunk = attn_chunk(s.causal != 0, p.q_tiles, int64_t(s.Nb) * s.heads, slots);
+    if constexpr (NH == 1) {
+        if (cudaFuncSetAttribute(attention_bwd_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmallSmem)) != cudaSuccess) return HQ_ERR_CUDA;
+        attention_bwd_small_kernel<<<p.items, kSmallThreads, kSmallSmem, st>>>(m, p);
+    } else {
+        if (cudaFuncSetAttribute(attention_bwd_kernel<NH>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bwd_smem<NH>())) != cudaSuccess)
+            return HQ_ERR_CUDA;
+        attention_bwd_kernel<NH><<<p.items < sms ? p.items : sms, kBwdThreads, bwd_smem<NH>(), st>>>(m, p);
+    }
     return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }
 
@@ -595,9 +896,8 @@ extern "C" hq_status hq_attention_bwd(const void* q, int64_t ldq, const void* k,
     p.dq = static_cast<__nv_bfloat16*>(dq); p.dk = static_cast<__nv_bfloat16*>(dk); p.dv = static_cast<__nv_bfloat16*>(dv);
     p.lddq = lddq; p.lddk = lddk; p.lddv = lddv;
     p.q_tiles = int(q_tiles); p.k_tiles = int(k_tiles);
-    p.key_chunk = attn_chunk(causal != 0, k_tiles, Nb * kv_heads, sm_count());
-    p.chunk = attn_chunk(causal != 0, q_tiles, Nb * heads, sm_count());
     p.key_items = unsigned(key_items); p.items = unsigned(items); p.dev_status = dev_status;
+    p.ragged = q_lens != nullptr || k_lens != nullptr || (causal && Lq > Lk);
     const int rows_per_cta = 8 * (32 / (dh / 8));
     int64_t stat_ctas = (q_tiles * kAttnTile + rows_per_cta - 1) / rows_per_cta;
     if (stat_ctas > 64) stat_ctas = 64;
