@@ -43,7 +43,9 @@ struct BwdParams {
     __nv_bfloat16 *dq, *dk, *dv;
     int64_t lddq, lddk, lddv;
     int q_tiles, k_tiles;
-    unsigned key_items, items, key_chunk, chunk;   // order of the items (attn_order)
+    unsigned key_items, items, key_chunk, chunk;   // tiles of keys (each in `parts` items), items; their order (attn_order)
+    int parts;                                     // shares of a tile of keys' steps, each an item; 1: no shares
+    float* partial;                                // [parts][key_items][dk, dv][NH * 16][128][4] sums of the shares
     int ragged;                                    // rows outside the lengths may lie in a tile
     int32_t* dev_status;
 };
@@ -54,7 +56,7 @@ template <int NH> struct BwdBars {
     uint64_t keep_full[R::kKeep], keep_empty[R::kKeep], b0_full[R::kB0], b0_empty[R::kB0], b1_full[R::kB1], b1_empty[R::kB1];
     // dP and dS of a step alternate between two barriers: where the next dP does not wait for this dS, one could come round twice
     // before a slow warp has looked at it
-    uint64_t s, p, dp[2], ds[2], acc, staged[R::kKeep], item_full[2], item_empty[2];
+    uint64_t s, p, dp[2], ds[2], acc, drain, staged[R::kKeep], item_full[2], item_empty[2];
     uint32_t item[2], tmem_slot;
 };
 template <int NH> constexpr size_t bwd_smem() { return size_t(BwdRings<NH>::kTiles + BwdRings<NH>::kStats) + sizeof(BwdBars<NH>); }
@@ -64,17 +66,20 @@ struct BwdItem {
     bool keys;
     int n, head, tile, row0;
     AttnSample sm;
-    int first, last, total;                        // tiles [first, last) of each of its heads; steps over all of them
+    int first, last, begin, total, whole;          // tiles [first, last) of each of its heads; its steps of the `whole` over all of them
+    unsigned part, base;                           // which share of which tile of keys
 };
 // `block_rows`: of the other side's tiles.
 __device__ __forceinline__ BwdItem bwd_item(const BwdParams& p, unsigned index, int block_rows = kAttnTile) {
     const AttnShape& s = p.s;
     BwdItem t;
     // tiles of keys first (they walk every head of their group); under the causal mask the first keys and the last queries walk the most
-    t.keys = index < p.key_items;
+    t.keys = index < p.key_items * unsigned(p.parts);
+    t.base = t.keys ? index / unsigned(p.parts) : index - p.key_items * unsigned(p.parts);
+    t.part = t.keys ? index - t.base * unsigned(p.parts) : 0u;
     const unsigned heads = unsigned(t.keys ? s.kv_heads : s.heads);
     unsigned block, bh;
-    attn_order(t.keys ? index : index - p.key_items, unsigned(t.keys ? p.k_tiles : p.q_tiles), unsigned(s.Nb) * heads, t.keys ? p.key_chunk : p.chunk, block, bh);
+    attn_order(t.base, unsigned(t.keys ? p.k_tiles : p.q_tiles), unsigned(s.Nb) * heads, t.keys ? p.key_chunk : p.chunk, block, bh);
     t.n = int(bh / heads);
     t.head = int(bh - unsigned(t.n) * heads);
     t.tile = !t.keys && s.causal ? p.q_tiles - 1 - int(block) : int(block);
@@ -88,7 +93,12 @@ __device__ __forceinline__ BwdItem bwd_item(const BwdParams& p, unsigned index, 
         t.first = 0;
         t.last = t.row0 > end || end < t.sm.q_lo ? 0 : (attn_key_limit(s, t.sm, end) + block_rows - 1) / block_rows;
     }
-    t.total = max(0, t.last - t.first) * (t.keys ? s.heads / s.kv_heads : 1);
+    t.whole = t.total = max(0, t.last - t.first) * (t.keys ? s.heads / s.kv_heads : 1);
+    t.begin = 0;
+    if (t.keys && p.parts > 1) {
+        t.begin = int(int64_t(t.whole) * t.part / p.parts);
+        t.total = int(int64_t(t.whole) * (t.part + 1) / p.parts) - t.begin;
+    }
     return t;
 }
 
@@ -124,7 +134,8 @@ __device__ __forceinline__ void bwd_load(const BwdMaps& m, const BwdParams& p, u
         load_tile<NH>(to + R::kTile, t.keys ? &m.v : &m.dout, &bar.keep_full[keep.slot], t.head, t.row0, t.n);
         keep.next();
         ++keeps;
-        int head = t.keys ? t.head * group : t.head / group, tile = t.first;
+        const int per_head = t.last - t.first;
+        int head = t.keys ? t.head * group + t.begin / per_head : t.head / group, tile = t.first + t.begin % per_head;
         for (int i = 0; i < t.total; ++i) {
             const float* stats = p.stats + (int64_t(t.n * p.s.heads + head) * p.q_tiles + tile) * (2 * kAttnTile);
             ok = mbar_wait_lane(&bar.b0_empty[b0.slot], b0.phase ^ 1u, p.dev_status, kStatusBwdWait);
@@ -202,7 +213,7 @@ __device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* sme
         if (t.total == 0) continue;
         // rows of tokens outside the lengths (zero as they come behind the last row of the matrix) are made zero where they would
         // meet zero probabilities in a sum: queries and their gradients, or keys
-        int tile = t.first;
+        int tile = t.first + t.begin % (t.last - t.first);
         const int outer_lo = t.keys ? t.sm.q_lo : 0, outer_hi = t.keys ? t.sm.q_hi : t.sm.kl, exist = t.keys ? s.Lq : s.Lk;
         auto clear = [&](unsigned char* at, int which_tile) {
             const int r0 = which_tile * kAttnTile;
@@ -289,7 +300,7 @@ __device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdI
         limit = r < t.sm.q_hi ? attn_key_limit(s, t.sm, r) : 0;
         if (limit == 1) limit = 0;                             // a weight of 1, whatever its score: no gradient
     }
-    int tile = t.first;
+    int tile = t.first + t.begin % (t.last - t.first);
     for (int i = 0; i < t.total; ++i) {
         const int c0 = tile * kAttnTile + quarter * 32;        // the first column's query or key
         if (++tile == t.last) tile = t.first;
@@ -386,6 +397,43 @@ __device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdI
     return true;
 }
 
+// 32 columns of a share's sums (which: 0 dk, 1 dv) as they are: 16 bytes of a row, rows side by side.
+__device__ __forceinline__ void store_share(const BwdParams& p, const BwdItem& t, uint32_t taddr, int which, int row, int c0, int parts64) {
+    if (c0 >= p.s.dh) return;
+    uint32_t r[32];
+    tmem_ld_32x32(taddr, r);
+    tmem_ld_wait_32(r);
+    float4* to = reinterpret_cast<float4*>(p.partial) +
+                 ((int64_t(t.part) * p.key_items + t.base) * 2 + which) * (parts64 * 16 * kAttnTile) + (c0 / 4) * kAttnTile + row;
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+        to[c * kAttnTile] = make_float4(__uint_as_float(r[4 * c]), __uint_as_float(r[4 * c + 1]), __uint_as_float(r[4 * c + 2]), __uint_as_float(r[4 * c + 3]));
+}
+// dk and dv of a tile of keys from its shares, in their order: blockIdx.x the tile, blockIdx.y dk or dv.
+__global__ void __launch_bounds__(256) attention_bwd_join_kernel(const BwdParams p, int parts64, int block_rows) {
+    const AttnShape& s = p.s;
+    const BwdItem t = bwd_item(p, blockIdx.x * unsigned(p.parts), block_rows);
+    const int which = blockIdx.y, rows = min(kAttnTile, s.Lk - t.row0);
+    const int64_t ld = which == 0 ? p.lddk : p.lddv, at = (int64_t(t.n) * s.Lk + t.row0) * ld + t.head * s.dh;
+    __nv_bfloat16* to = (which == 0 ? p.dk : p.dv) + at;
+    const float mul = which == 0 ? s.scale : 1.0f;
+    const int64_t tile = int64_t(parts64) * 16 * kAttnTile, step = int64_t(p.key_items) * 2 * tile;
+    const float4* from = reinterpret_cast<const float4*>(p.partial) + (int64_t(t.base) * 2 + which) * tile;
+    for (int f = threadIdx.x; f < kAttnTile * (s.dh / 8); f += 256) {
+        const int c = f / kAttnTile, row = f - c * kAttnTile;
+        float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (row < rows && t.row0 + row < t.sm.kl)
+            for (int x = 0; x < p.parts; ++x) {
+                if (int64_t(t.whole) * x / p.parts == int64_t(t.whole) * (x + 1) / p.parts) continue;      // a share without steps
+                const float4 u = __ldcg(from + x * step + (2 * c) * kAttnTile + row), v = __ldcg(from + x * step + (2 * c + 1) * kAttnTile + row);
+                a[0] += u.x; a[1] += u.y; a[2] += u.z; a[3] += u.w; a[4] += v.x; a[5] += v.y; a[6] += v.z; a[7] += v.w;
+            }
+        if (row < rows)
+            *reinterpret_cast<uint4*>(to + int64_t(row) * ld + c * 8) = make_uint4(pack_bf16(a[0] * mul, a[1] * mul), pack_bf16(a[2] * mul, a[3] * mul),
+                                                                               pack_bf16(a[4] * mul, a[5] * mul), pack_bf16(a[6] * mul, a[7] * mul));
+    }
+}
+
 template <int NH>
 __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __grid_constant__ BwdMaps m, const BwdParams p) {
     using R = BwdRings<NH>;
@@ -402,7 +450,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
         for (int i = 0; i < R::kKeep; ++i) { mbar_init(&bar.keep_full[i], 1); mbar_init(&bar.keep_empty[i], 1); }
         for (int i = 0; i < R::kB0; ++i) { mbar_init(&bar.b0_full[i], 1); mbar_init(&bar.b0_empty[i], 1); }
         for (int i = 0; i < R::kB1; ++i) { mbar_init(&bar.b1_full[i], 1); mbar_init(&bar.b1_empty[i], 1); }
-        mbar_init(&bar.s, 1); mbar_init(&bar.p, kBwdWarps); mbar_init(&bar.acc, 1);
+        mbar_init(&bar.s, 1); mbar_init(&bar.p, kBwdWarps); mbar_init(&bar.acc, 1); mbar_init(&bar.drain, 1);
         for (int i = 0; i < R::kKeep; ++i) mbar_init(&bar.staged[i], kBwdWarps);
         for (int i = 0; i < 2; ++i) { mbar_init(&bar.dp[i], 1); mbar_init(&bar.ds[i], kBwdWarps); }
         for (int i = 0; i < 2; ++i) { mbar_init(&bar.item_full[i], 1); mbar_init(&bar.item_empty[i], kBwdWarps + 2); }
@@ -420,6 +468,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
         __syncwarp();
     } else if (warp == 0) {
         bwd_issue<NH>(p, smem, bar, tmem_base, lane);
+        __syncwarp();
+        if (elect_one()) mma_drain(&bar.drain);                // the lane that issued
+        __syncwarp();
     } else if (warp == 2) {
         RingAt<2> told;
         RingAt<R::kKeep> keep;
@@ -431,14 +482,16 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
             if (!mbar_wait_warp(&bar.staged[keep.slot], keep.phase, p.dev_status, kStatusBwdWait)) break;
             if (elect_one()) {
                 const unsigned char* from = smem + 2 * keep.slot * R::kTile;
+                if (!t.keys || p.parts == 1) {                 // the shares' sums went to memory as they are
 #pragma unroll
-                for (int h = 0; h < NH; ++h) tma_store_4d(t.keys ? &m.dk : &m.dq, from + h * kAttnPart, 64 * h, t.head, t.row0, t.n);
-                if (t.keys) {
+                    for (int h = 0; h < NH; ++h) tma_store_4d(t.keys ? &m.dk : &m.dq, from + h * kAttnPart, 64 * h, t.head, t.row0, t.n);
+                    if (t.keys) {
 #pragma unroll
-                    for (int h = 0; h < NH; ++h) tma_store_4d(&m.dv, from + R::kTile + h * kAttnPart, 64 * h, t.head, t.row0, t.n);
+                        for (int h = 0; h < NH; ++h) tma_store_4d(&m.dv, from + R::kTile + h * kAttnPart, 64 * h, t.head, t.row0, t.n);
+                    }
+                    bulk_commit_group();
+                    bulk_wait_read_all();
                 }
-                bulk_commit_group();
-                bulk_wait_read_all();
                 mbar_arrive(&bar.keep_empty[keep.slot]);
             }
             __syncwarp();
@@ -457,6 +510,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
             if (index >= p.items) break;
             const BwdItem t = bwd_item(p, index);
             if (t.total == 0) {                                // nothing seen: the gradient is zero
+                if (t.keys && p.parts > 1) continue;
                 if (t.keys) {
                     const int rows = min(kAttnTile, s.Lk - t.row0);
                     const int64_t at = int64_t(t.n) * s.Lk + t.row0;
@@ -472,6 +526,16 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
                                      : bwd_probabilities<NH, false>(p, t, stat0, stat1, bar, b0, b1, step, t_s, r, quarter, lane);
             if (!done || !mbar_wait_warp(&bar.acc, item_par, p.dev_status, kStatusBwdWait)) break;
             tc_fence_after();
+            if (t.keys && p.parts > 1) {
+                store_share(p, t, t_s + 384u, 0, row, quarter * 32, NH);
+                store_share(p, t, t_s + 256u, 1, row, quarter * 32, NH);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bar.staged[keep.slot]);
+                keep.next();
+                item_par ^= 1u;
+                continue;
+            }
             unsigned char* stage = smem + 2 * keep.slot * R::kTile;
             const bool kept = t.keys ? r < t.sm.kl : r >= t.sm.q_lo && r < t.sm.q_hi;
             stage_rows<NH>(t_s + 384u, stage, row, quarter, s.dh, kept, s.scale);
@@ -495,7 +559,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
 constexpr int kSmallBlock = 64, kSmallStages = 3, kSmallThreads = 320, kSmallPart = kSmallBlock * 128;
 constexpr size_t kSmallSmem = size_t(2) * kAttnPart + size_t(kSmallStages) * (2 * kSmallPart + 2 * kSmallBlock * 4) + 1024;
 
-struct SmallBars { uint64_t keep, full[kSmallStages], ready[kSmallStages], empty[kSmallStages], s, dp[2], read, ds[2], acc; };
+struct SmallBars { uint64_t drain, keep, full[kSmallStages], ready[kSmallStages], empty[kSmallStages], s, dp[2], read, ds[2], acc; };
 
 // KEYS: A0 = K, A1 = V, B0 = Q, B1 = dout; else A0 = Q, A1 = dout, B0 = K, B1 = V.  Columns: S at 0, dP at 64 (queries: a second
 // buffer at 128), the sums at 128 (dv) and 192 (dk, dq).
@@ -540,7 +604,7 @@ __device__ __forceinline__ bool small_run(const BwdMaps& m, const BwdParams& p, 
             }
         }
         __syncwarp();
-        int head = KEYS ? t.head * group : t.head / group, block = first, before = first, i = 0;
+        int head = KEYS ? t.head * group + t.begin / (last - first) : t.head / group, block = first + t.begin % (last - first), before = block, i = 0;
         for (; i < total; ++i) {
             const int stage = i % kSmallStages, use = i / kSmallStages;
             if (use > 0) ok = mbar_wait_warp(&bar.empty[stage], uint32_t(use - 1) & 1u, p.dev_status, kStatusBwdWait);
@@ -618,6 +682,7 @@ __device__ __forceinline__ bool small_run(const BwdMaps& m, const BwdParams& p, 
                 if (KEYS && more) score_product(i + 1, 1, 64u, &bar.dp[next]);
             }
             if (ok) mma_commit(&bar.acc);
+            mma_drain(&bar.drain);
         }
         __syncwarp();
     } else {
@@ -634,7 +699,7 @@ __device__ __forceinline__ bool small_run(const BwdMaps& m, const BwdParams& p, 
             limit = r < t.sm.q_hi ? attn_key_limit(s, t.sm, r) : 0;
             if (limit == 1) limit = 0;                         // a weight of 1, whatever its score: no gradient
         }
-        int block = first;
+        int block = first + t.begin % (last - first);
         for (int i = 0; i < total; ++i) {
             const uint32_t par = uint32_t(i) & 1u;
             const int c0 = block * kSmallBlock + half * 32, stage = i % kSmallStages;        // the first column's query or key
@@ -728,6 +793,11 @@ __device__ __forceinline__ bool small_run(const BwdMaps& m, const BwdParams& p, 
         if (ok) ok = mbar_wait_warp(&bar.acc, 0, p.dev_status, kStatusBwdWait);
         if (ok) {
             tc_fence_after();
+            if (KEYS && p.parts > 1) {
+                store_share(p, t, t_s + 192u, 0, row, half * 32, 1);
+                store_share(p, t, t_s + 128u, 1, row, half * 32, 1);
+                return true;
+            }
             const bool kept = KEYS ? r < t.sm.kl : r >= t.sm.q_lo && r < t.sm.q_hi;
             stage_rows<1>(t_s + 192u, smem, row, half, s.dh, kept, s.scale);
             if (KEYS) stage_rows<1>(t_s + 128u, smem + kTile, row, half, s.dh, kept, 1.0f);
@@ -746,6 +816,7 @@ __global__ void __launch_bounds__(kSmallThreads, 2) attention_bwd_small_kernel(c
     const int warp = threadIdx.x >> 5;
     const BwdItem t = bwd_item(p, blockIdx.x, kSmallBlock);
     if (t.total == 0) {                            // nothing seen: the gradient is zero
+        if (t.keys && p.parts > 1) return;
         if (t.keys) {
             const int rows = min(kAttnTile, s.Lk - t.row0);
             const int64_t at = int64_t(t.n) * s.Lk + t.row0;
@@ -757,7 +828,7 @@ __global__ void __launch_bounds__(kSmallThreads, 2) attention_bwd_small_kernel(c
         return;
     }
     if (threadIdx.x == 0) {
-        mbar_init(&bar.keep, 1);
+        mbar_init(&bar.keep, 1); mbar_init(&bar.drain, 1);
         for (int i = 0; i < kSmallStages; ++i) { mbar_init(&bar.full[i], 1); mbar_init(&bar.ready[i], 1); mbar_init(&bar.empty[i], 1); }
         mbar_init(&bar.s, 1); mbar_init(&bar.acc, 1); mbar_init(&bar.read, 8);
         for (int i = 0; i < 2; ++i) { mbar_init(&bar.dp[i], 1); mbar_init(&bar.ds[i], 8); }
@@ -773,7 +844,7 @@ __global__ void __launch_bounds__(kSmallThreads, 2) attention_bwd_small_kernel(c
     tc_fence_before();
     const bool all = __syncthreads_and(ok);
     if (warp == 8) tmem_dealloc(tmem_base, 256);
-    if (all && threadIdx.x == 0) {
+    if (all && threadIdx.x == 0 && !(t.keys && p.parts > 1)) {
         tma_store_4d(t.keys ? &m.dk : &m.dq, smem, 0, t.head, t.row0, t.n);
         if (t.keys) tma_store_4d(&m.dv, smem + kAttnPart, 0, t.head, t.row0, t.n);
         bulk_commit_group();
@@ -849,11 +920,38 @@ hq_status launch_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, con
             return HQ_ERR_CUDA;
         attention_bwd_kernel<NH><<<p.items < sms ? p.items : sms, kBwdThreads, bwd_smem<NH>(), st>>>(m, p);
     }
+    if (p.parts > 1) {
+        if (cudaGetLastError() != cudaSuccess) return HQ_ERR_CUDA;
+        attention_bwd_join_kernel<<<dim3(p.key_items, 2), 256, 0, st>>>(p, NH, int(block));
+    }
     return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }
 
-// statistics, then the count of items taken
-int64_t stats_bytes(int64_t Nb, int64_t Lq, int heads) { return Nb * heads * ((Lq + kAttnTile - 1) / kAttnTile) * 2 * kStatBytes; }
+// Shares of a tile of keys' steps: enough that the longest item takes about half the time an SM has for all of them, where a share has
+// eight steps at least.  8 x 4096 queries on 77 keys, 8 heads of 40 (64 tiles of keys) 80 us in one share, 2 x 4096 causal, 16 / 2 heads
+// of 128 (128 tiles of up to 256 steps) 535.
+int bwd_parts(int64_t Nb, int64_t Lq, int64_t Lk, int heads, int kv_heads, int dh) {
+    const int64_t block = dh <= 64 ? kSmallBlock : kAttnTile, slots = int64_t(sm_count()) * (dh <= 64 ? 2 : 1);
+    const int64_t key_steps = heads / kv_heads * ((Lq + block - 1) / block), query_steps = (Lk + block - 1) / block + 2;
+    const int64_t keys = Nb * kv_heads * ((Lk + kAttnTile - 1) / kAttnTile), queries = Nb * heads * ((Lq + kAttnTile - 1) / kAttnTile);
+    const int64_t work = keys * key_steps + queries * query_steps;
+    int64_t parts = work > 0 ? (2 * key_steps * slots + work - 1) / work : 1;
+    if (parts > key_steps / 8) parts = key_steps / 8;
+    return int(parts < 1 ? 1 : parts < 16 ? parts : 16);
+}
+
+// statistics, the count of items taken, the shares' sums
+struct BwdWorkspace { int64_t stats, taken, partial, bytes; int parts; };
+BwdWorkspace bwd_workspace(int64_t Nb, int64_t Lq, int64_t Lk, int heads, int kv_heads, int dh) {
+    BwdWorkspace w;
+    w.parts = bwd_parts(Nb, Lq, Lk, heads, kv_heads, dh);
+    w.stats = 0;
+    w.taken = Nb * heads * ((Lq + kAttnTile - 1) / kAttnTile) * 2 * kStatBytes;
+    w.partial = w.taken + 16;
+    const int64_t tile = int64_t(dh <= 64 ? 64 : 128) * kAttnTile * 4, keys = Nb * kv_heads * ((Lk + kAttnTile - 1) / kAttnTile);
+    w.bytes = w.partial + (w.parts > 1 ? w.parts * keys * 2 * tile : 0);
+    return w;
+}
 
 }  // namespace
 }  // namespace hq
@@ -863,7 +961,7 @@ extern "C" hq_status hq_attention_bwd_workspace_size(int64_t Nb, int64_t Lq, int
     if (bytes == nullptr) return HQ_ERR_INVALID_ARG;
     const hq_status e = attn_check(Nb, Lq, Lk, heads, kv_heads, dh, 1.0f);
     if (e != HQ_OK) return e;
-    *bytes = size_t(stats_bytes(Nb, Lq, heads)) + 16;
+    *bytes = size_t(bwd_workspace(Nb, Lq, Lk, heads, kv_heads, dh).bytes);
     return HQ_OK;
 }
 
@@ -883,16 +981,18 @@ extern "C" hq_status hq_attention_bwd(const void* q, int64_t ldq, const void* k,
         return e;
     if (lse == nullptr || workspace == nullptr) return HQ_ERR_INVALID_ARG;
     if (!aligned16(workspace)) return HQ_ERR_ALIGNMENT;
-    const int64_t stat_bytes = stats_bytes(Nb, Lq, heads);
-    if (int64_t(ws_bytes) < stat_bytes + 16) return HQ_ERR_WORKSPACE;
+    const BwdWorkspace w = bwd_workspace(Nb, Lq, Lk, heads, kv_heads, dh);
+    if (int64_t(ws_bytes) < w.bytes) return HQ_ERR_WORKSPACE;
     const int64_t q_tiles = (Lq + kAttnTile - 1) / kAttnTile, k_tiles = (Lk + kAttnTile - 1) / kAttnTile;
-    const int64_t key_items = Nb * kv_heads * k_tiles, items = key_items + Nb * heads * q_tiles;
+    const int64_t key_items = Nb * kv_heads * k_tiles, items = key_items * w.parts + Nb * heads * q_tiles;
     if (items > 0x3fffffff) return HQ_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     BwdParams p{};
     p.s = AttnShape{q_lens, k_lens, int(Nb), int(Lq), int(Lk), heads, kv_heads, dh, causal != 0, scale, float(double(scale) * 1.4426950408889634)};
     p.stats = static_cast<const float*>(workspace);
-    p.taken = reinterpret_cast<unsigned*>(static_cast<unsigned char*>(workspace) + stat_bytes);
+    p.taken = reinterpret_cast<unsigned*>(static_cast<unsigned char*>(workspace) + w.taken);
+    p.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + w.partial);
+    p.parts = w.parts;
     p.dq = static_cast<__nv_bfloat16*>(dq); p.dk = static_cast<__nv_bfloat16*>(dk); p.dv = static_cast<__nv_bfloat16*>(dv);
     p.lddq = lddq; p.lddk = lddk; p.lddv = lddv;
     p.q_tiles = int(q_tiles); p.k_tiles = int(k_tiles);

@@ -41,7 +41,7 @@ attention_fwd_kernel(const __grid_constant__ FwdMaps m, const FwdParams p) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* sQ = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     unsigned char *sK = sQ + NH * kAttnPart, *sV = sK + NH * kPart, *sP = sV + NH * kPart;     // P: unswizzled core matrices
-    __shared__ uint64_t bar_q, bar_k, bar_v, bar_s, bar_o, bar_read, bar_p;
+    __shared__ uint64_t bar_q, bar_k, bar_v, bar_s, bar_o, bar_read, bar_p, bar_drain;
     __shared__ uint32_t tmem_slot;
     constexpr uint32_t kPGroup = (KB / 8) * 128;
 
@@ -63,7 +63,7 @@ attention_fwd_kernel(const __grid_constant__ FwdMaps m, const FwdParams p) {
     }
     if (tid == 0) {
         mbar_init(&bar_q, 1); mbar_init(&bar_k, 1); mbar_init(&bar_v, 1);
-        mbar_init(&bar_s, 1); mbar_init(&bar_o, 1); mbar_init(&bar_read, 4); mbar_init(&bar_p, 4);
+        mbar_init(&bar_s, 1); mbar_init(&bar_o, 1); mbar_init(&bar_read, 4); mbar_init(&bar_p, 4); mbar_init(&bar_drain, 1);
         fence_barrier_init();
     }
     if (warp == 4 && lane < 4) tma_prefetch_desc(&m.q + lane);
@@ -129,7 +129,8 @@ attention_fwd_kernel(const __grid_constant__ FwdMaps m, const FwdParams p) {
                 mma_commit(&bar_o);
             }
             // what was requested lands before the CTA's shared memory is given up, on every way out
-            wait(&bar_q, 0, 0);
+            mma_drain(&bar_drain);
+            mbar_wait_lane(&bar_q, 0, nullptr, 0);
             mbar_wait_lane(&bar_k, uint32_t(k_loads - 1) & 1u, nullptr, 0);
             mbar_wait_lane(&bar_v, uint32_t(v_loads - 1) & 1u, nullptr, 0);
         }

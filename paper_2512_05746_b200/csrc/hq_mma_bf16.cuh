@@ -108,6 +108,13 @@ __device__ __forceinline__ bool mbar_wait_lane(uint64_t* bar, uint32_t parity, i
     return ok;
 }
 
+// What this thread has issued is complete before it gives up the tensor memory and the tiles (one lane; `bar`: count 1, used once): a
+// CTA that a wait of another kind has ended early must not leave products running.
+__device__ __forceinline__ void mma_drain(uint64_t* bar) {
+    mma_commit(bar);
+    mbar_wait_lane(bar, 0, nullptr, 0);
+}
+
 // 16-byte aligned bulk copy global -> shared, completion counted on an mbarrier.
 __device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"

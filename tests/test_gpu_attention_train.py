@@ -80,7 +80,7 @@ SHAPES = [                                       # Nb, Lq, Lk, heads, kv_heads, 
     (1, 1, 1, 1, 1, 8), (2, 1, 300, 2, 1, 64), (1, 300, 1, 2, 2, 64), (2, 64, 64, 2, 2, 64), (1, 127, 129, 2, 2, 40),
     (1, 128, 128, 1, 1, 128), (2, 129, 127, 3, 3, 72), (1, 256, 256, 2, 2, 96), (1, 257, 385, 4, 2, 128), (2, 200, 77, 6, 1, 80),
     (1, 513, 640, 2, 2, 32), (1, 640, 513, 2, 1, 48), (3, 65, 191, 2, 2, 56), (1, 383, 130, 2, 1, 120), (1, 1100, 900, 1, 1, 64),
-    (1, 2000, 60, 2, 1, 64), (1, 40, 2000, 2, 1, 96)]
+    (1, 2000, 60, 2, 1, 64), (1, 40, 2000, 2, 1, 96), (1, 2100, 150, 2, 1, 128), (2, 1111, 200, 4, 1, 72)]
 
 
 @pytest.mark.parametrize("causal", [False, True])
@@ -100,7 +100,7 @@ def test_scale_and_peaked_rows(hq, scale):
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("dh,H,G", [(64, 2, 1), (72, 2, 2), (128, 2, 1)])
 @pytest.mark.parametrize("garbage", [math.nan, math.inf])
-@pytest.mark.parametrize("Lq,Lk", [(260, 300), (250, 100)])
+@pytest.mark.parametrize("Lq,Lk", [(260, 300), (250, 100), (2100, 140)])
 def test_padded_batch(hq, causal, dh, H, G, garbage, Lq, Lk):
     """Lengths of 0, 1, around the tiles' edges and beyond the matrix (clamped); what lies behind them is never read into a result."""
     ql = torch.tensor([Lq, 0, 1, 128, 129, Lq - 5, 100, 9999, Lq], dtype=torch.int32, device="cuda")
@@ -181,9 +181,9 @@ def test_against_differences(hq):
         assert abs((true[which] * d).sum() - slope) <= 1e-6 * (1 + slope.abs() + (true[which] * d).abs().sum()), which
 
 
-@pytest.mark.parametrize("dh,Lk", [(64, 700), (128, 700), (64, 90)])
-def test_same_bits_on_every_run_and_stream(hq, dh, Lk):
-    Nb, L, H, G = 2, 700, 4, 2
+@pytest.mark.parametrize("dh,L,Lk", [(64, 700, 700), (128, 700, 700), (64, 700, 90), (64, 1500, 90), (128, 1500, 200)])
+def test_same_bits_on_every_run_and_stream(hq, dh, L, Lk):
+    Nb, H, G = 2, 4, 2
     q, k, v, dout = make(9, Nb, L, Lk, H, G, dh)
     out, lse = fwd(hq, q, k, v, Nb, H, G, causal=True)
     first = bwd(hq, q, k, v, out, lse, dout, Nb, H, G, causal=True)
