@@ -409,28 +409,34 @@ __device__ __forceinline__ void store_share(const BwdParams& p, const BwdItem& t
     for (int c = 0; c < 8; ++c)
         to[c * kAttnTile] = make_float4(__uint_as_float(r[4 * c]), __uint_as_float(r[4 * c + 1]), __uint_as_float(r[4 * c + 2]), __uint_as_float(r[4 * c + 3]));
 }
-// dk and dv of a tile of keys from its shares, in their order: blockIdx.x the tile, blockIdx.y dk or dv.
+// dk and dv of a tile of keys from its shares, in their order: blockIdx.x the tile, blockIdx.y dk or dv, blockIdx.z 16 channels.
 __global__ void __launch_bounds__(256) attention_bwd_join_kernel(const BwdParams p, int parts64, int block_rows) {
     const AttnShape& s = p.s;
+    const int which = blockIdx.y, c = blockIdx.z * 2 + (threadIdx.x >> 7), row = threadIdx.x & 127;
+    if (c >= s.dh / 8) return;
     const BwdItem t = bwd_item(p, blockIdx.x * unsigned(p.parts), block_rows);
-    const int which = blockIdx.y, rows = min(kAttnTile, s.Lk - t.row0);
-    const int64_t ld = which == 0 ? p.lddk : p.lddv, at = (int64_t(t.n) * s.Lk + t.row0) * ld + t.head * s.dh;
-    __nv_bfloat16* to = (which == 0 ? p.dk : p.dv) + at;
-    const float mul = which == 0 ? s.scale : 1.0f;
     const int64_t tile = int64_t(parts64) * 16 * kAttnTile, step = int64_t(p.key_items) * 2 * tile;
-    const float4* from = reinterpret_cast<const float4*>(p.partial) + (int64_t(t.base) * 2 + which) * tile;
-    for (int f = threadIdx.x; f < kAttnTile * (s.dh / 8); f += 256) {
-        const int c = f / kAttnTile, row = f - c * kAttnTile;
-        float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (row < rows && t.row0 + row < t.sm.kl)
-            for (int x = 0; x < p.parts; ++x) {
-                if (int64_t(t.whole) * x / p.parts == int64_t(t.whole) * (x + 1) / p.parts) continue;      // a share without steps
-                const float4 u = __ldcg(from + x * step + (2 * c) * kAttnTile + row), v = __ldcg(from + x * step + (2 * c + 1) * kAttnTile + row);
-                a[0] += u.x; a[1] += u.y; a[2] += u.z; a[3] += u.w; a[4] += v.x; a[5] += v.y; a[6] += v.z; a[7] += v.w;
-            }
-        if (row < rows)
-            *reinterpret_cast<uint4*>(to + int64_t(row) * ld + c * 8) = make_uint4(pack_bf16(a[0] * mul, a[1] * mul), pack_bf16(a[2] * mul, a[3] * mul),
-                                                                               pack_bf16(a[4] * mul, a[5] * mul), pack_bf16(a[6] * mul, a[7] * mul));
+    const float4* from = reinterpret_cast<const float4*>(p.partial) + (int64_t(t.base) * 2 + which) * tile + 2 * c * kAttnTile + row;
+    float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    auto add = [&](int x) {
+        const float4 u = __ldcg(from + x * step), v = __ldcg(from + x * step + kAttnTile);
+        a[0] += u.x; a[1] += u.y; a[2] += u.z; a[3] += u.w; a[4] += v.x; a[5] += v.y; a[6] += v.z; a[7] += v.w;
+    };
+    if (t.row0 + row < t.sm.kl) {
+        if (t.whole >= p.parts) {
+#pragma unroll 4
+            for (int x = 0; x < p.parts; ++x) add(x);
+        } else {                                               // shares without steps have written nothing
+            for (int x = 0; x < p.parts; ++x)
+                if (int64_t(t.whole) * x / p.parts != int64_t(t.whole) * (x + 1) / p.parts) add(x);
+        }
+    }
+    if (t.row0 + row < s.Lk) {
+        const int64_t ld = which == 0 ? p.lddk : p.lddv;
+        const float mul = which == 0 ? s.scale : 1.0f;
+        *reinterpret_cast<uint4*>((which == 0 ? p.dk : p.dv) + (int64_t(t.n) * s.Lk + t.row0 + row) * ld + t.head * s.dh + c * 8) =
+            make_uint4(pack_bf16(a[0] * mul, a[1] * mul), pack_bf16(a[2] * mul, a[3] * mul), pack_bf16(a[4] * mul, a[5] * mul),
+                       pack_bf16(a[6] * mul, a[7] * mul));
     }
 }
 
@@ -863,35 +869,43 @@ __global__ void __launch_bounds__(256) attention_stats_kernel(const __nv_bfloat1
     const int bh = blockIdx.y, n = bh / s.heads, head = bh - n * s.heads;
     const AttnSample sm = attn_sample(s, n);
     const int rows = q_tiles * kAttnTile;
-    for (int i0 = (blockIdx.x * 8 + warp) * per_warp; i0 < rows; i0 += gridDim.x * 8 * per_warp) {
-        const int i = i0 + sub;
-        const bool mine = sub < per_warp && i < rows, live = mine && i >= sm.q_lo && i < sm.q_hi;
-        float d = 0.f;
-        if (live) {
-            const int64_t row = int64_t(n) * s.Lq + i;
-            const uint4 a = __ldg(reinterpret_cast<const uint4*>(out + row * ldo + head * s.dh) + pos);
-            const uint4 b = __ldg(reinterpret_cast<const uint4*>(dout + row * lddo + head * s.dh) + pos);
-            const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+    constexpr int kAhead = 4;                      // rows of a group of lanes requested together
+    const int stride = gridDim.x * 8 * per_warp;
+    for (int i0 = (blockIdx.x * 8 + warp) * per_warp; i0 < rows; i0 += kAhead * stride) {
+        uint4 a[kAhead], b[kAhead];
+        float given[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = i0 + u * stride + sub;
+            a[u] = b[u] = make_uint4(0u, 0u, 0u, 0u);
+            given[u] = -INFINITY;
+            if (sub < per_warp && i >= sm.q_lo && i < sm.q_hi) {
+                const int64_t row = int64_t(n) * s.Lq + i;
+                a[u] = __ldg(reinterpret_cast<const uint4*>(out + row * ldo + head * s.dh) + pos);
+                b[u] = __ldg(reinterpret_cast<const uint4*>(dout + row * lddo + head * s.dh) + pos);
+                if (pos == 0) given[u] = __ldg(lse + int64_t(bh) * s.Lq + i);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = i0 + u * stride + sub;
+            const uint32_t x[4] = {a[u].x, a[u].y, a[u].z, a[u].w}, y[4] = {b[u].x, b[u].y, b[u].z, b[u].w};
+            float d = 0.f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 d = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), d);
                 d = fmaf(__uint_as_float(x[e] & 0xFFFF0000u), __uint_as_float(y[e] & 0xFFFF0000u), d);
             }
-        }
 #pragma unroll
-        for (int off = 8; off > 0; off >>= 1) {
-            const float o = __shfl_down_sync(0xffffffffu, d, off);
-            if (pos < off && pos + off < v) d += o;
-        }
-        if (mine && pos == 0) {
-            float* to = stats + (int64_t(bh) * q_tiles + i / kAttnTile) * (2 * kAttnTile) + i % kAttnTile;
-            float l = -INFINITY;
-            if (live) {
-                const float given = __ldg(lse + int64_t(bh) * s.Lq + i);
-                if (given != -INFINITY) l = given * -1.4426950408889634f;
+            for (int off = 8; off > 0; off >>= 1) {
+                const float o = __shfl_down_sync(0xffffffffu, d, off);
+                if (pos < off && pos + off < v) d += o;
             }
-            to[0] = l;
-            to[kAttnTile] = -d;
+            if (sub < per_warp && pos == 0 && i < rows) {
+                float* to = stats + (int64_t(bh) * q_tiles + i / kAttnTile) * (2 * kAttnTile) + i % kAttnTile;
+                to[0] = given[u] == -INFINITY ? -INFINITY : given[u] * -1.4426950408889634f;
+                to[kAttnTile] = -d;
+            }
         }
     }
 }
@@ -922,7 +936,7 @@ hq_status launch_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, con
     }
     if (p.parts > 1) {
         if (cudaGetLastError() != cudaSuccess) return HQ_ERR_CUDA;
-        attention_bwd_join_kernel<<<dim3(p.key_items, 2), 256, 0, st>>>(p, NH, int(block));
+        attention_bwd_join_kernel<<<dim3(p.key_items, 2, unsigned(s.dh / 8 + 1) / 2), 256, 0, st>>>(p, NH, int(block));
     }
     return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }
@@ -998,7 +1012,8 @@ extern "C" hq_status hq_attention_bwd(const void* q, int64_t ldq, const void* k,
     p.q_tiles = int(q_tiles); p.k_tiles = int(k_tiles);
     p.key_items = unsigned(key_items); p.items = unsigned(items); p.dev_status = dev_status;
     p.ragged = q_lens != nullptr || k_lens != nullptr || (causal && Lq > Lk);
-    const int rows_per_cta = 8 * (32 / (dh / 8));
+    // four rows of a group together once there are CTAs enough
+    const int rows_per_cta = 8 * (32 / (dh / 8)) * (q_tiles * Nb * heads >= 2 * int64_t(sm_count()) ? 4 : 1);
     int64_t stat_ctas = (q_tiles * kAttnTile + rows_per_cta - 1) / rows_per_cta;
     if (stat_ctas > 64) stat_ctas = 64;
     attention_stats_kernel<<<dim3(unsigned(stat_ctas), unsigned(Nb * heads)), 256, 0, st>>>(

@@ -306,21 +306,24 @@ __global__ void __launch_bounds__(kRopeThreads, GRAD ? 2 : sizeof(T) == 4 ? 3 : 
     }
 }
 
-// gamma's gradient from the CTAs' shares: one CTA for queries and one for keys, thread = (channel, every so-many-th share)
-__global__ void __launch_bounds__(1024) qk_rope_gamma_kernel(const RopeParams p, int blocks) {
-    __shared__ float sums[1024];
-    const RopeSide& s = blockIdx.x == 0 ? p.q : p.k;
+// gamma's gradient from the CTAs' shares: blockIdx.x 8 channels, blockIdx.y queries or keys; thread = (channel, every 32nd share), the 32
+// sums in order (one CTA for all channels took 15 us for the 1184 shares of a large call).
+__global__ void __launch_bounds__(256) qk_rope_gamma_kernel(const RopeParams p, int blocks) {
+    __shared__ float sums[256];
+    const RopeSide& s = blockIdx.y == 0 ? p.q : p.k;
     if (s.dgamma == nullptr) return;
-    const int ways = 1024 / p.dh, way = threadIdx.x / p.dh, c = threadIdx.x - way * p.dh;
+    const int c = blockIdx.x * 8 + (threadIdx.x & 7), way = threadIdx.x >> 3;
+    const float* from = p.partial + int64_t(blockIdx.y) * blocks * p.dh + c;
     float sum = 0.f;
-    if (way < ways)
-        for (int b = way; b < blocks; b += ways) sum += p.partial[(int64_t(blockIdx.x) * blocks + b) * p.dh + c];
+#pragma unroll 8
+    for (int b = way; b < blocks; b += 32) sum += __ldcg(from + int64_t(b) * p.dh);
     sums[threadIdx.x] = sum;
     __syncthreads();
-    if (int(threadIdx.x) < p.dh) {
+    if (threadIdx.x < 8) {
         float total = 0.f;
-        for (int w = 0; w < ways; ++w) total += sums[w * p.dh + threadIdx.x];
-        s.dgamma[threadIdx.x] = total;
+#pragma unroll
+        for (int w = 0; w < 32; ++w) total += sums[w * 8 + threadIdx.x];
+        s.dgamma[c] = total;
     }
 }
 
@@ -383,7 +386,7 @@ hq_status run(RopeParams p, hq_dtype dt, int interleaved, bool grad, cudaStream_
     if (grad) e = dt == HQ_BF16 ? launch_width<__nv_bfloat16, true>(p, pairs, vec, grid, st) : launch_width<float, true>(p, pairs, vec, grid, st);
     else e = dt == HQ_BF16 ? launch_width<__nv_bfloat16, false>(p, pairs, vec, grid, st) : launch_width<float, false>(p, pairs, vec, grid, st);
     if (e != HQ_OK || (p.q.dgamma == nullptr && p.k.dgamma == nullptr)) return e;
-    qk_rope_gamma_kernel<<<grid.y, 1024, 0, st>>>(p, blocks);
+    qk_rope_gamma_kernel<<<dim3(unsigned(p.dh / 8), grid.y), 256, 0, st>>>(p, blocks);
     return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }
 
