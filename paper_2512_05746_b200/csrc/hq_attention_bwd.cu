@@ -294,7 +294,7 @@ __device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdI
     int limit = 0;                                             // queries: keys the row sees
     if (!KEYS) {
         const float* stats = p.stats + (int64_t(t.n * s.heads + t.head) * p.q_tiles + t.tile) * (2 * kAttnTile) + (r - t.row0);
-        const float l = __ldg(stats), d = __ldg(stats + kAttnTile);
+        const float l = ld_dependent(stats), d = ld_dependent(stats + kAttnTile);
         row_lse = pk2(l, l);
         row_d = pk2(d, d);
         limit = r < t.sm.q_hi ? attn_key_limit(s, t.sm, r) : 0;
@@ -413,13 +413,14 @@ __device__ __forceinline__ void store_share(const BwdParams& p, const BwdItem& t
 __global__ void __launch_bounds__(256) attention_bwd_join_kernel(const BwdParams p, int parts64, int block_rows) {
     const AttnShape& s = p.s;
     const int which = blockIdx.y, c = blockIdx.z * 2 + (threadIdx.x >> 7), row = threadIdx.x & 127;
+    griddep_wait();
     if (c >= s.dh / 8) return;
     const BwdItem t = bwd_item(p, blockIdx.x * unsigned(p.parts), block_rows);
     const int64_t tile = int64_t(parts64) * 16 * kAttnTile, step = int64_t(p.key_items) * 2 * tile;
     const float4* from = reinterpret_cast<const float4*>(p.partial) + (int64_t(t.base) * 2 + which) * tile + 2 * c * kAttnTile + row;
     float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     auto add = [&](int x) {
-        const float4 u = __ldcg(from + x * step), v = __ldcg(from + x * step + kAttnTile);
+        const float4 u = ld_dependent_cg(from + x * step), v = ld_dependent_cg(from + x * step + kAttnTile);
         a[0] += u.x; a[1] += u.y; a[2] += u.z; a[3] += u.w; a[4] += v.x; a[5] += v.y; a[6] += v.z; a[7] += v.w;
     };
     if (t.row0 + row < t.sm.kl) {
@@ -468,6 +469,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = bar.tmem_slot;
+    griddep_wait();                                // the statistics; the call's operands were complete before that kernel began
 
     if (warp == 1) {
         if (elect_one()) bwd_load<NH>(m, p, smem, stat0, stat1, bar);
@@ -699,7 +701,7 @@ __device__ __forceinline__ bool small_run(const BwdMaps& m, const BwdParams& p, 
         int limit = 0;                                         // queries: keys the row sees
         if (!KEYS) {
             const float* stats = p.stats + (int64_t(t.n * s.heads + t.head) * p.q_tiles + t.tile) * (2 * kAttnTile) + row;
-            const float l = __ldg(stats), d = __ldg(stats + kAttnTile);
+            const float l = ld_dependent(stats), d = ld_dependent(stats + kAttnTile);
             row_lse = pk2(l, l);
             row_d = pk2(d, d);
             limit = r < t.sm.q_hi ? attn_key_limit(s, t.sm, r) : 0;
@@ -822,6 +824,7 @@ __global__ void __launch_bounds__(kSmallThreads, 2) attention_bwd_small_kernel(c
     const int warp = threadIdx.x >> 5;
     const BwdItem t = bwd_item(p, blockIdx.x, kSmallBlock);
     if (t.total == 0) {                            // nothing seen: the gradient is zero
+        griddep_wait();                            // no CTA ends before the kernel in front has
         if (t.keys && p.parts > 1) return;
         if (t.keys) {
             const int rows = min(kAttnTile, s.Lk - t.row0);
@@ -846,6 +849,7 @@ __global__ void __launch_bounds__(kSmallThreads, 2) attention_bwd_small_kernel(c
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = tmem_slot;
+    griddep_wait();                                // the statistics; the call's operands were complete before that kernel began
     const bool ok = t.keys ? small_run<true>(m, p, t, smem, bar, tmem_base) : small_run<false>(m, p, t, smem, bar, tmem_base);
     tc_fence_before();
     const bool all = __syncthreads_and(ok);
@@ -928,17 +932,20 @@ hq_status launch_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, con
     p.chunk = attn_chunk(s.causal != 0, p.q_tiles, int64_t(s.Nb) * s.heads, slots);
     if constexpr (NH == 1) {
         if (cudaFuncSetAttribute(attention_bwd_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmallSmem)) != cudaSuccess) return HQ_ERR_CUDA;
-        attention_bwd_small_kernel<<<p.items, kSmallThreads, kSmallSmem, st>>>(m, p);
+        // few CTAs are placed while the statistics are still computed: 2 x 64 tokens, 8 heads of 64 12.7 us a call otherwise
+        if (launch_dependent(attention_bwd_small_kernel, dim3(p.items), kSmallThreads, kSmallSmem, st, p.items <= slots, m, p) != cudaSuccess) return HQ_ERR_CUDA;
     } else {
         if (cudaFuncSetAttribute(attention_bwd_kernel<NH>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bwd_smem<NH>())) != cudaSuccess)
             return HQ_ERR_CUDA;
-        attention_bwd_kernel<NH><<<p.items < sms ? p.items : sms, kBwdThreads, bwd_smem<NH>(), st>>>(m, p);
+        if (launch_dependent(attention_bwd_kernel<NH>, dim3(p.items < sms ? p.items : sms), kBwdThreads, bwd_smem<NH>(), st, p.items <= sms, m, p) != cudaSuccess)
+            return HQ_ERR_CUDA;
     }
     if (p.parts > 1) {
-        if (cudaGetLastError() != cudaSuccess) return HQ_ERR_CUDA;
-        attention_bwd_join_kernel<<<dim3(p.key_items, 2, unsigned(s.dh / 8 + 1) / 2), 256, 0, st>>>(p, NH, int(block));
+        const dim3 grid(p.key_items, 2, unsigned(s.dh / 8 + 1) / 2);
+        if (launch_dependent(attention_bwd_join_kernel, grid, 256, 0, st, dependent_launch(int64_t(grid.x) * 2 * grid.z), p, NH, int(block)) != cudaSuccess)
+            return HQ_ERR_CUDA;
     }
-    return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+    return HQ_OK;
 }
 
 // Shares of a tile of keys' steps: enough that the longest item takes about half the time an SM has for all of them, where a share has

@@ -311,12 +311,13 @@ __global__ void __launch_bounds__(kRopeThreads, GRAD ? 2 : sizeof(T) == 4 ? 3 : 
 __global__ void __launch_bounds__(256) qk_rope_gamma_kernel(const RopeParams p, int blocks) {
     __shared__ float sums[256];
     const RopeSide& s = blockIdx.y == 0 ? p.q : p.k;
+    griddep_wait();                                // the shares; no CTA ends before the kernel in front has
     if (s.dgamma == nullptr) return;
     const int c = blockIdx.x * 8 + (threadIdx.x & 7), way = threadIdx.x >> 3;
     const float* from = p.partial + int64_t(blockIdx.y) * blocks * p.dh + c;
     float sum = 0.f;
 #pragma unroll 8
-    for (int b = way; b < blocks; b += 32) sum += __ldcg(from + int64_t(b) * p.dh);
+    for (int b = way; b < blocks; b += 32) sum += ld_dependent(from + int64_t(b) * p.dh);
     sums[threadIdx.x] = sum;
     __syncthreads();
     if (threadIdx.x < 8) {
@@ -386,8 +387,8 @@ hq_status run(RopeParams p, hq_dtype dt, int interleaved, bool grad, cudaStream_
     if (grad) e = dt == HQ_BF16 ? launch_width<__nv_bfloat16, true>(p, pairs, vec, grid, st) : launch_width<float, true>(p, pairs, vec, grid, st);
     else e = dt == HQ_BF16 ? launch_width<__nv_bfloat16, false>(p, pairs, vec, grid, st) : launch_width<float, false>(p, pairs, vec, grid, st);
     if (e != HQ_OK || (p.q.dgamma == nullptr && p.k.dgamma == nullptr)) return e;
-    qk_rope_gamma_kernel<<<dim3(unsigned(p.dh / 8), grid.y), 256, 0, st>>>(p, blocks);
-    return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+    const dim3 few(unsigned(p.dh / 8), grid.y);
+    return launch_dependent(qk_rope_gamma_kernel, few, 256, 0, st, dependent_launch(int64_t(few.x) * few.y), p, blocks) == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }
 
 }  // namespace
