@@ -3,20 +3,21 @@
 //   P_ij = exp(scale q_i . k_j - lse_i),  dP = dout V^T,  D_i = dout_i . out_i,  dS = P o (dP - D)
 //   dq = scale dS K,   dk = scale sum over the heads that share k of dS^T Q,   dv = sum of P^T dout
 //
-// Two kinds of CTA in one launch, each with the sums it owns in tensor memory for its whole life, so that nothing is added up in
-// memory and the same inputs give the same bits:
+// A first kernel leaves -lse log2(e) and -D of every query.  Then two kinds of item in one launch, each with the sums it owns in tensor
+// memory from its first step to its last, so that nothing is added up in memory and the same inputs give the same bits:
 //   keys     a tile of 128 keys of one (sample, key head) walks the queries of every head of its group: S^T = K Q^T, dP^T = V dout^T
 //            with the keys along the lanes, P^T and dS^T as bf16 over the columns they were computed from, dv += P^T dout,
 //            dk += dS^T Q;
 //   queries  a tile of 128 queries of one (sample, head) walks the keys: S = Q K^T, dP = dout V^T, dq += dS K.
 // The scores are computed twice (seven products a pair of tiles where five would do); what that buys is that P and dS never leave
 // tensor memory (as operands of the second products they are read where they were written), no fp32 partial dq in memory and no
-// order of additions that changes from run to run.
+// order of additions that changes from run to run.  Where tiles of keys are few and long each is cut into shares whose sums a last
+// kernel adds in their order (bwd_parts).  P and dS are rounded to bf16 (the products' type); all sums are fp32.
 //
-// The kernel is persistent: a CTA takes an item (a tile of one kind), then the next that no other has taken.  Warp 0 issues, warp 1
-// takes items and loads, warp 2 stores; warps 4-19: thread = lane, four warps per quarter of the 128 columns.  The tile an item keeps
-// (K and V, or Q and dout) stays in shared memory, where its gradient is staged at the end; the other side's two kinds of tiles come
-// through a ring each.
+// Up to 64 channels an item is a CTA of its own, two an SM (attention_bwd_small_kernel); above, persistent CTAs take item after item
+// (attention_bwd_kernel).  Measured, the statistics' kernel included: 64 x 1024 tokens, 8 heads of 64 (481 GFLOP in seven products)
+// 680 us, held to 1.6 GHz by the power limit, 239 us of it two passes of exponentials (16 a clock in an SM); 2 x 4096 causal, 16 / 2
+// heads of 128 496 us; 8 x 4096 queries on 77 keys, 8 heads of 40 86 us; 2 x 64 tokens, 8 heads of 64 12.3 us a call.
 #include "hq_attention_tile.cuh"
 
 namespace hq {
@@ -28,12 +29,11 @@ constexpr int kBwdWarps = 16, kBwdFirst = 4;                   // of the probabi
 constexpr int kBwdThreads = (kBwdFirst + kBwdWarps) * 32;
 constexpr uint32_t kStatBytes = kAttnTile * 4;                 // of one query tile: -lse * log2(e), and as many for -D
 
-// Rings: tiles of 16 KB up to 64 channels, 32 KB above, where two kept tiles, three and two take all but 2 KB of the shared memory.
-template <int NH> struct BwdRings {
-    static constexpr int kKeep = NH == 1 ? 2 : 1;              // kept pairs: the next item's loads begin under this one's last steps
-    static constexpr int kB0 = NH == 1 ? 4 : 3, kB1 = NH == 1 ? 4 : 2;
-    static constexpr int kTile = NH * kAttnPart;
-    static constexpr int kTiles = (2 * kKeep + kB0 + kB1) * kTile, kStats = (kB0 + kB1) * int(kStatBytes);
+// Rings of the kernel above 64 channels: tiles of 32 KB, of which two kept ones, three and two take all but 2 KB of the shared memory.
+struct BwdRings {
+    static constexpr int kParts = 2, kB0 = 3, kB1 = 2;         // kParts: of 64 channels
+    static constexpr int kTile = kParts * kAttnPart;
+    static constexpr int kTiles = (2 + kB0 + kB1) * kTile, kStats = (kB0 + kB1) * int(kStatBytes);
 };
 
 struct BwdParams {
@@ -45,21 +45,21 @@ struct BwdParams {
     int q_tiles, k_tiles;
     unsigned key_items, items, key_chunk, chunk;   // tiles of keys (each in `parts` items), items; their order (attn_order)
     int parts;                                     // shares of a tile of keys' steps, each an item; 1: no shares
-    float* partial;                                // [parts][key_items][dk, dv][NH * 16][128][4] sums of the shares
+    float* partial;                                // [parts][key_items][dk, dv][16 a part of 64 channels][128][4] sums of the shares
     int ragged;                                    // rows outside the lengths may lie in a tile
     int32_t* dev_status;
 };
 struct BwdMaps { CUtensorMap q, k, v, dout, dq, dk, dv; };
 
-template <int NH> struct BwdBars {
-    using R = BwdRings<NH>;
-    uint64_t keep_full[R::kKeep], keep_empty[R::kKeep], b0_full[R::kB0], b0_empty[R::kB0], b1_full[R::kB1], b1_empty[R::kB1];
+struct BwdBars {
+    using R = BwdRings;
+    uint64_t keep_full, keep_empty, b0_full[R::kB0], b0_empty[R::kB0], b1_full[R::kB1], b1_empty[R::kB1];
     // dP and dS of a step alternate between two barriers: where the next dP does not wait for this dS, one could come round twice
     // before a slow warp has looked at it
-    uint64_t s, p, dp[2], ds[2], acc, drain, staged[R::kKeep], item_full[2], item_empty[2];
+    uint64_t s, p, dp[2], ds[2], acc, drain, staged, item_full[2], item_empty[2];
     uint32_t item[2], tmem_slot;
 };
-template <int NH> constexpr size_t bwd_smem() { return size_t(BwdRings<NH>::kTiles + BwdRings<NH>::kStats) + sizeof(BwdBars<NH>); }
+constexpr size_t kBwdSmem = size_t(BwdRings::kTiles + BwdRings::kStats) + sizeof(BwdBars);
 
 // What an item is: a tile of keys of one (sample, key head) or of queries of one (sample, head), and the other side's tiles it walks.
 struct BwdItem {
@@ -102,18 +102,38 @@ __device__ __forceinline__ BwdItem bwd_item(const BwdParams& p, unsigned index, 
     return t;
 }
 
+// ---- above 64 channels: persistent CTAs, one an SM; an item, then the next that no other has taken.  Warp 0 issues, warp 1 takes items
+// and loads, warp 2 stores; warps 4-19: thread = lane, four warps per quarter of the 128 columns.  The tile an item keeps (K and V, or Q
+// and dout) stays in shared memory, where its gradient is staged at the end; the other side's two kinds of tiles come through a ring each.
+
+// Rows of a landed tile outside [lo, hi) become zeros (one warp): they belong to tokens outside the lengths, whose values may be
+// infinite or not numbers, and would meet zero weights in a product.
+__device__ __forceinline__ void clear_rows(unsigned char* tile, int lo, int hi, int lane) {
+    for (int h = 0; h < BwdRings::kParts; ++h)
+        for (int f = lane; f < kAttnTile * 8; f += 32) {
+            const int row = f >> 3;
+            if (row < lo || row >= hi) *reinterpret_cast<uint4*>(tile + h * kAttnPart + f * 16) = make_uint4(0u, 0u, 0u, 0u);
+        }
+}
+
+// A place in a ring and how often it has come round.
+template <int N> struct RingAt {
+    int slot = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next() { if (++slot == N) { slot = 0; phase ^= 1u; } }
+};
+
 // ---- warp 1, one lane: takes items, tells the others, loads their tiles
-template <int NH>
-__device__ __forceinline__ void bwd_load(const BwdMaps& m, const BwdParams& p, unsigned char* smem, float* stat0, float* stat1, BwdBars<NH>& bar) {
-    using R = BwdRings<NH>;
-    unsigned char *sB0 = smem + 2 * R::kKeep * R::kTile, *sB1 = sB0 + R::kB0 * R::kTile;
+__device__ __forceinline__ void bwd_load(const BwdMaps& m, const BwdParams& p, unsigned char* smem, float* stat0, float* stat1, BwdBars& bar) {
+    using R = BwdRings;
+    unsigned char *sB0 = smem + 2 * R::kTile, *sB1 = sB0 + R::kB0 * R::kTile;
     const int group = p.s.heads / p.s.kv_heads;
-    RingAt<R::kKeep> keep;
+    uint32_t keep = 0;
     RingAt<R::kB0> b0;
     RingAt<R::kB1> b1;
     RingAt<2> told;
-    int keeps = 0, n0 = 0, n1 = 0;                 // begun so far
-    bool ok = true;
+    int n0 = 0, n1 = 0;                 // begun so far
+    bool ok = true, kept = false;
     unsigned index = blockIdx.x;
     while (ok) {
         ok = mbar_wait_lane(&bar.item_empty[told.slot], told.phase ^ 1u, p.dev_status, kStatusBwdWait);
@@ -126,14 +146,13 @@ __device__ __forceinline__ void bwd_load(const BwdMaps& m, const BwdParams& p, u
         const BwdItem t = bwd_item(p, index);
         index = following;
         if (t.total == 0) continue;
-        ok = mbar_wait_lane(&bar.keep_empty[keep.slot], keep.phase ^ 1u, p.dev_status, kStatusBwdWait);
+        ok = mbar_wait_lane(&bar.keep_empty, keep ^ 1u, p.dev_status, kStatusBwdWait);
         if (!ok) break;
-        unsigned char* to = smem + 2 * keep.slot * R::kTile;
-        mbar_expect_tx(&bar.keep_full[keep.slot], 2 * R::kTile);
-        load_tile<NH>(to, t.keys ? &m.k : &m.q, &bar.keep_full[keep.slot], t.head, t.row0, t.n);
-        load_tile<NH>(to + R::kTile, t.keys ? &m.v : &m.dout, &bar.keep_full[keep.slot], t.head, t.row0, t.n);
-        keep.next();
-        ++keeps;
+        mbar_expect_tx(&bar.keep_full, 2 * R::kTile);
+        load_tile<BwdRings::kParts>(smem, t.keys ? &m.k : &m.q, &bar.keep_full, t.head, t.row0, t.n);
+        load_tile<BwdRings::kParts>(smem + R::kTile, t.keys ? &m.v : &m.dout, &bar.keep_full, t.head, t.row0, t.n);
+        keep ^= 1u;
+        kept = true;
         const int per_head = t.last - t.first;
         int head = t.keys ? t.head * group + t.begin / per_head : t.head / group, tile = t.first + t.begin % per_head;
         for (int i = 0; i < t.total; ++i) {
@@ -141,14 +160,14 @@ __device__ __forceinline__ void bwd_load(const BwdMaps& m, const BwdParams& p, u
             ok = mbar_wait_lane(&bar.b0_empty[b0.slot], b0.phase ^ 1u, p.dev_status, kStatusBwdWait);
             if (!ok) break;
             mbar_expect_tx(&bar.b0_full[b0.slot], R::kTile + (t.keys ? kStatBytes : 0));
-            load_tile<NH>(sB0 + b0.slot * R::kTile, t.keys ? &m.q : &m.k, &bar.b0_full[b0.slot], head, tile * kAttnTile, t.n);
+            load_tile<BwdRings::kParts>(sB0 + b0.slot * R::kTile, t.keys ? &m.q : &m.k, &bar.b0_full[b0.slot], head, tile * kAttnTile, t.n);
             if (t.keys) bulk_load(stat0 + b0.slot * kAttnTile, stats, kStatBytes, &bar.b0_full[b0.slot]);
             b0.next();
             ++n0;
             ok = mbar_wait_lane(&bar.b1_empty[b1.slot], b1.phase ^ 1u, p.dev_status, kStatusBwdWait);
             if (!ok) break;
             mbar_expect_tx(&bar.b1_full[b1.slot], R::kTile + (t.keys ? kStatBytes : 0));
-            load_tile<NH>(sB1 + b1.slot * R::kTile, t.keys ? &m.dout : &m.v, &bar.b1_full[b1.slot], head, tile * kAttnTile, t.n);
+            load_tile<BwdRings::kParts>(sB1 + b1.slot * R::kTile, t.keys ? &m.dout : &m.v, &bar.b1_full[b1.slot], head, tile * kAttnTile, t.n);
             if (t.keys) bulk_load(stat1 + b1.slot * kAttnTile, stats + kAttnTile, kStatBytes, &bar.b1_full[b1.slot]);
             b1.next();
             ++n1;
@@ -156,14 +175,13 @@ __device__ __forceinline__ void bwd_load(const BwdMaps& m, const BwdParams& p, u
         }
     }
     // what was requested lands before the CTA's shared memory is given up, on every way out
-    for (int i = max(0, keeps - R::kKeep); i < keeps; ++i) mbar_wait_lane(&bar.keep_full[i % R::kKeep], uint32_t(i / R::kKeep) & 1u, nullptr, 0);
+    if (kept) mbar_wait_lane(&bar.keep_full, keep ^ 1u, nullptr, 0);
     for (int i = max(0, n0 - R::kB0); i < n0; ++i) mbar_wait_lane(&bar.b0_full[i % R::kB0], uint32_t(i / R::kB0) & 1u, nullptr, 0);
     for (int i = max(0, n1 - R::kB1); i < n1; ++i) mbar_wait_lane(&bar.b1_full[i % R::kB1], uint32_t(i / R::kB1) & 1u, nullptr, 0);
 }
 
 // The next item's number (p.items and beyond: none, or a wait ran out), the same in every lane.
-template <int NH>
-__device__ __forceinline__ unsigned bwd_next(const BwdParams& p, BwdBars<NH>& bar, RingAt<2>& told, int lane) {
+__device__ __forceinline__ unsigned bwd_next(const BwdParams& p, BwdBars& bar, RingAt<2>& told, int lane) {
     if (!mbar_wait_warp(&bar.item_full[told.slot], told.phase, p.dev_status, kStatusBwdWait)) return 0xffffffffu;
     const unsigned index = *const_cast<volatile uint32_t*>(&bar.item[told.slot]);
     __syncwarp();
@@ -175,11 +193,10 @@ __device__ __forceinline__ unsigned bwd_next(const BwdParams& p, BwdBars<NH>& ba
 // ---- warp 0: products.  Tensor memory: S at columns 0, dP at 128; keys: dv at 256, dk at 384; queries: dP's second buffer at 256,
 // dq at 384.  Products run in the order of their issue: one that overwrites another's operand or result in tensor memory, or an
 // accumulator that the other warps have read before they handed over the operand it waits for, is issued behind it.
-template <int NH>
-__device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* smem, BwdBars<NH>& bar, uint32_t tmem_base, int lane) {
-    using R = BwdRings<NH>;
+__device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* smem, BwdBars& bar, uint32_t tmem_base, int lane) {
+    using R = BwdRings;
     const AttnShape& s = p.s;
-    unsigned char *sB0 = smem + 2 * R::kKeep * R::kTile, *sB1 = sB0 + R::kB0 * R::kTile;
+    unsigned char *sB0 = smem + 2 * R::kTile, *sB1 = sB0 + R::kB0 * R::kTile;
     const uint32_t idesc_s = make_idesc_bf16(kAttnTile, kAttnTile, false);
     const uint32_t idesc_acc = make_idesc_bf16(kAttnTile, (s.dh + 15) & ~15, true);
     const int ksteps = (s.dh + 15) / 16;
@@ -201,13 +218,13 @@ __device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* sme
                         add || k != 0 ? 1u : 0u);
     };
     auto wait = [&](uint64_t* b, uint32_t parity, int32_t code) { return mbar_wait_warp(b, parity, p.dev_status, code); };
-    RingAt<R::kKeep> keep;
+    uint32_t keep = 0;
     RingAt<R::kB0> s0, a0;                         // B0's tile of the next score product / of the next sum
     RingAt<R::kB1> s1, a1;
     RingAt<2> told;
     uint32_t step = 0;                             // over all items
     for (;;) {
-        const unsigned index = bwd_next<NH>(p, bar, told, lane);
+        const unsigned index = bwd_next(p, bar, told, lane);
         if (index >= p.items) return;
         const BwdItem t = bwd_item(p, index);
         if (t.total == 0) continue;
@@ -218,20 +235,19 @@ __device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* sme
         auto clear = [&](unsigned char* at, int which_tile) {
             const int r0 = which_tile * kAttnTile;
             if (outer_lo > r0 || outer_hi < min(r0 + kAttnTile, exist)) {
-                clear_rows<NH>(at, outer_lo - r0, outer_hi - r0, lane);
+                clear_rows(at, outer_lo - r0, outer_hi - r0, lane);
                 fence_proxy_async_smem();
                 __syncwarp();
             }
         };
-        const uint64_t a = dA + uint64_t(keep.slot) * (2 * kTileUnits);
-        if (!wait(&bar.keep_full[keep.slot], keep.phase, kStatusBwdTma)) return;
-        keep.next();
+        if (!wait(&bar.keep_full, keep, kStatusBwdTma)) return;
+        keep ^= 1u;
         auto scores = [&](int which_tile) {        // S of the next tile
             if (!wait(&bar.b0_full[s0.slot], s0.phase, kStatusBwdTma)) return false;
             clear(sB0 + s0.slot * R::kTile, which_tile);
             if (elect_one()) {
                 tc_fence_after();
-                score_product(a, dB0 + uint64_t(s0.slot) * kTileUnits, 0u);
+                score_product(dA, dB0 + uint64_t(s0.slot) * kTileUnits, 0u);
                 mma_commit(&bar.s);
             }
             __syncwarp();
@@ -243,7 +259,7 @@ __device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* sme
             if (t.keys) clear(sB1 + s1.slot * R::kTile, which_tile);
             if (elect_one()) {
                 tc_fence_after();
-                score_product(a + kTileUnits, dB1 + uint64_t(s1.slot) * kTileUnits, column);
+                score_product(dA + kTileUnits, dB1 + uint64_t(s1.slot) * kTileUnits, column);
                 mma_commit(&bar.dp[of & 1u]);
                 if (!t.keys) mma_commit(&bar.b1_empty[s1.slot]);
             }
@@ -284,9 +300,9 @@ __device__ __forceinline__ void bwd_issue(const BwdParams& p, unsigned char* sme
 }
 
 // ---- warps 4-19: probabilities and their gradients
-template <int NH, bool KEYS>
-__device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdItem& t, const float* stat0, const float* stat1, BwdBars<NH>& bar,
-                                                  RingAt<BwdRings<NH>::kB0>& b0, RingAt<BwdRings<NH>::kB1>& b1, uint32_t& step,
+template <bool KEYS>
+__device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdItem& t, const float* stat0, const float* stat1, BwdBars& bar,
+                                                  RingAt<BwdRings::kB0>& b0, RingAt<BwdRings::kB1>& b1, uint32_t& step,
                                                   uint32_t t_s, int r, int quarter, int lane) {
     const AttnShape& s = p.s;
     const f32x2 sc2 = pk2(s.scale_log2, s.scale_log2);
@@ -441,12 +457,11 @@ __global__ void __launch_bounds__(256) attention_bwd_join_kernel(const BwdParams
     }
 }
 
-template <int NH>
 __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __grid_constant__ BwdMaps m, const BwdParams p) {
-    using R = BwdRings<NH>;
+    using R = BwdRings;
     extern __shared__ __align__(1024) unsigned char smem[];
     float *stat0 = reinterpret_cast<float*>(smem + R::kTiles), *stat1 = stat0 + R::kB0 * kAttnTile;
-    BwdBars<NH>& bar = *reinterpret_cast<BwdBars<NH>*>(smem + R::kTiles + R::kStats);
+    BwdBars& bar = *reinterpret_cast<BwdBars*>(smem + R::kTiles + R::kStats);
     const AttnShape& s = p.s;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((smem_u32(smem) & 1023u) != 0) {                       // the tiles' swizzle needs it; dynamic shared memory begins there
@@ -454,11 +469,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
         return;
     }
     if (threadIdx.x == 0) {
-        for (int i = 0; i < R::kKeep; ++i) { mbar_init(&bar.keep_full[i], 1); mbar_init(&bar.keep_empty[i], 1); }
+        mbar_init(&bar.keep_full, 1); mbar_init(&bar.keep_empty, 1); mbar_init(&bar.staged, kBwdWarps);
         for (int i = 0; i < R::kB0; ++i) { mbar_init(&bar.b0_full[i], 1); mbar_init(&bar.b0_empty[i], 1); }
         for (int i = 0; i < R::kB1; ++i) { mbar_init(&bar.b1_full[i], 1); mbar_init(&bar.b1_empty[i], 1); }
         mbar_init(&bar.s, 1); mbar_init(&bar.p, kBwdWarps); mbar_init(&bar.acc, 1); mbar_init(&bar.drain, 1);
-        for (int i = 0; i < R::kKeep; ++i) mbar_init(&bar.staged[i], kBwdWarps);
         for (int i = 0; i < 2; ++i) { mbar_init(&bar.dp[i], 1); mbar_init(&bar.ds[i], kBwdWarps); }
         for (int i = 0; i < 2; ++i) { mbar_init(&bar.item_full[i], 1); mbar_init(&bar.item_empty[i], kBwdWarps + 2); }
         fence_barrier_init();
@@ -472,49 +486,48 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
     griddep_wait();                                // the statistics; the call's operands were complete before that kernel began
 
     if (warp == 1) {
-        if (elect_one()) bwd_load<NH>(m, p, smem, stat0, stat1, bar);
+        if (elect_one()) bwd_load(m, p, smem, stat0, stat1, bar);
         __syncwarp();
     } else if (warp == 0) {
-        bwd_issue<NH>(p, smem, bar, tmem_base, lane);
+        bwd_issue(p, smem, bar, tmem_base, lane);
         __syncwarp();
         if (elect_one()) mma_drain(&bar.drain);                // the lane that issued
         __syncwarp();
     } else if (warp == 2) {
         RingAt<2> told;
-        RingAt<R::kKeep> keep;
+        uint32_t keep = 0;
         for (;;) {
-            const unsigned index = bwd_next<NH>(p, bar, told, lane);
+            const unsigned index = bwd_next(p, bar, told, lane);
             if (index >= p.items) break;
             const BwdItem t = bwd_item(p, index);
             if (t.total == 0) continue;
-            if (!mbar_wait_warp(&bar.staged[keep.slot], keep.phase, p.dev_status, kStatusBwdWait)) break;
+            if (!mbar_wait_warp(&bar.staged, keep, p.dev_status, kStatusBwdWait)) break;
             if (elect_one()) {
-                const unsigned char* from = smem + 2 * keep.slot * R::kTile;
                 if (!t.keys || p.parts == 1) {                 // the shares' sums went to memory as they are
 #pragma unroll
-                    for (int h = 0; h < NH; ++h) tma_store_4d(t.keys ? &m.dk : &m.dq, from + h * kAttnPart, 64 * h, t.head, t.row0, t.n);
+                    for (int h = 0; h < R::kParts; ++h) tma_store_4d(t.keys ? &m.dk : &m.dq, smem + h * kAttnPart, 64 * h, t.head, t.row0, t.n);
                     if (t.keys) {
 #pragma unroll
-                        for (int h = 0; h < NH; ++h) tma_store_4d(&m.dv, from + R::kTile + h * kAttnPart, 64 * h, t.head, t.row0, t.n);
+                        for (int h = 0; h < R::kParts; ++h) tma_store_4d(&m.dv, smem + R::kTile + h * kAttnPart, 64 * h, t.head, t.row0, t.n);
                     }
                     bulk_commit_group();
                     bulk_wait_read_all();
                 }
-                mbar_arrive(&bar.keep_empty[keep.slot]);
+                mbar_arrive(&bar.keep_empty);
             }
             __syncwarp();
-            keep.next();
+            keep ^= 1u;
         }
     } else if (warp >= kBwdFirst) {
         const int quarter = (warp - kBwdFirst) >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t t_lane = tmem_base + (uint32_t((warp & 3) * 32) << 16), t_s = t_lane + uint32_t(quarter * 32);
         RingAt<2> told;
-        RingAt<R::kKeep> keep;
+        uint32_t keep = 0;
         RingAt<R::kB0> b0;
         RingAt<R::kB1> b1;
         uint32_t step = 0, item_par = 0;
         for (;;) {
-            const unsigned index = bwd_next<NH>(p, bar, told, lane);
+            const unsigned index = bwd_next(p, bar, told, lane);
             if (index >= p.items) break;
             const BwdItem t = bwd_item(p, index);
             if (t.total == 0) {                                // nothing seen: the gradient is zero
@@ -530,29 +543,28 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attention_bwd_kernel(const __g
                 continue;
             }
             const int r = t.row0 + row;
-            const bool done = t.keys ? bwd_probabilities<NH, true>(p, t, stat0, stat1, bar, b0, b1, step, t_s, r, quarter, lane)
-                                     : bwd_probabilities<NH, false>(p, t, stat0, stat1, bar, b0, b1, step, t_s, r, quarter, lane);
+            const bool done = t.keys ? bwd_probabilities<true>(p, t, stat0, stat1, bar, b0, b1, step, t_s, r, quarter, lane)
+                                     : bwd_probabilities<false>(p, t, stat0, stat1, bar, b0, b1, step, t_s, r, quarter, lane);
             if (!done || !mbar_wait_warp(&bar.acc, item_par, p.dev_status, kStatusBwdWait)) break;
             tc_fence_after();
             if (t.keys && p.parts > 1) {
-                store_share(p, t, t_s + 384u, 0, row, quarter * 32, NH);
-                store_share(p, t, t_s + 256u, 1, row, quarter * 32, NH);
+                store_share(p, t, t_s + 384u, 0, row, quarter * 32, R::kParts);
+                store_share(p, t, t_s + 256u, 1, row, quarter * 32, R::kParts);
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bar.staged[keep.slot]);
-                keep.next();
+                if (lane == 0) mbar_arrive(&bar.staged);
+                keep ^= 1u;
                 item_par ^= 1u;
                 continue;
             }
-            unsigned char* stage = smem + 2 * keep.slot * R::kTile;
             const bool kept = t.keys ? r < t.sm.kl : r >= t.sm.q_lo && r < t.sm.q_hi;
-            stage_rows<NH>(t_s + 384u, stage, row, quarter, s.dh, kept, s.scale);
-            if (t.keys) stage_rows<NH>(t_s + 256u, stage + R::kTile, row, quarter, s.dh, kept, 1.0f);
+            stage_rows<BwdRings::kParts>(t_s + 384u, smem, row, quarter, s.dh, kept, s.scale);
+            if (t.keys) stage_rows<BwdRings::kParts>(t_s + 256u, smem + R::kTile, row, quarter, s.dh, kept, 1.0f);
             tc_fence_before();
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bar.staged[keep.slot]);
-            keep.next();
+            if (lane == 0) mbar_arrive(&bar.staged);
+            keep ^= 1u;
             item_par ^= 1u;
         }
     }
@@ -935,9 +947,8 @@ hq_status launch_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, con
         // few CTAs are placed while the statistics are still computed: 2 x 64 tokens, 8 heads of 64 12.7 us a call otherwise
         if (launch_dependent(attention_bwd_small_kernel, dim3(p.items), kSmallThreads, kSmallSmem, st, p.items <= slots, m, p) != cudaSuccess) return HQ_ERR_CUDA;
     } else {
-        if (cudaFuncSetAttribute(attention_bwd_kernel<NH>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bwd_smem<NH>())) != cudaSuccess)
-            return HQ_ERR_CUDA;
-        if (launch_dependent(attention_bwd_kernel<NH>, dim3(p.items < sms ? p.items : sms), kBwdThreads, bwd_smem<NH>(), st, p.items <= sms, m, p) != cudaSuccess)
+        if (cudaFuncSetAttribute(attention_bwd_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kBwdSmem)) != cudaSuccess) return HQ_ERR_CUDA;
+        if (launch_dependent(attention_bwd_kernel, dim3(p.items < sms ? p.items : sms), kBwdThreads, kBwdSmem, st, p.items <= sms, m, p) != cudaSuccess)
             return HQ_ERR_CUDA;
     }
     if (p.parts > 1) {

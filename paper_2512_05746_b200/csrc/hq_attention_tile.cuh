@@ -61,24 +61,6 @@ __device__ __forceinline__ void load_tile(unsigned char* dst, const CUtensorMap*
 #pragma unroll
     for (int h = 0; h < NH; ++h) tma_load_4d(dst + h * kAttnPart, tm, bar, 64 * h, head, row, sample);
 }
-// Rows of a landed tile outside [lo, hi) become zeros (one warp): they belong to tokens outside the lengths, whose values may be
-// infinite or not numbers, and would meet zero weights in a product.
-template <int NH>
-__device__ __forceinline__ void clear_rows(unsigned char* tile, int lo, int hi, int lane) {
-    for (int h = 0; h < NH; ++h)
-        for (int f = lane; f < kAttnTile * 8; f += 32) {
-            const int row = f >> 3;
-            if (row < lo || row >= hi) *reinterpret_cast<uint4*>(tile + h * kAttnPart + f * 16) = make_uint4(0u, 0u, 0u, 0u);
-        }
-}
-
-// A place in a ring and how often it has come round.
-template <int N> struct RingAt {
-    int slot = 0;
-    uint32_t phase = 0;
-    __device__ __forceinline__ void next() { if (++slot == N) { slot = 0; phase ^= 1u; } }
-};
-
 // 32 columns of an accumulator as scaled bf16 into the staging tile (rows of 128 bytes, 128-byte swizzle); rows not kept become zeros.
 template <int NH>
 __device__ __forceinline__ void stage_rows(uint32_t taddr, unsigned char* tile, int row, int quarter, int dh, bool keep, float mul) {
