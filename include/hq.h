@@ -408,17 +408,21 @@ hq_status hq_qk_norm_rope_bwd(const void* q, int64_t ldq, const void* k, int64_t
  *   q, out     device bf16 [Nb*Lq] x heads heads; k, v [Nb*Lk] x kv_heads heads; lse device fp32 [Nb][heads][Lq].
  *   q_lens, k_lens   device int32 [Nb], or NULL (Lq, Lk): queries and keys of sample n that are there (values are clamped to
  *              0 .. L).  Rows behind them are never part of a result, whatever they hold.
- *   causal     != 0: query i sees keys j <= i + k_len - q_len (the last query sees every key).
+ *   causal     != 0: query i sees keys j <= i + k_len - q_len (the last query sees every key).  Keys and values within the lengths are
+ *              finite: one that the mask hides from a query may meet it with weight zero.
  *   A query that sees no key, and one behind its sample's length: out = 0, lse = -infinity.
  *   scale      positive and finite.  bf16 operands on the tensor cores, fp32 accumulation and softmax; the weights are rounded to
  *              bf16 before they multiply the values.
- *   workspace  hq_attention_fwd_workspace_size bytes, 16-byte aligned (NULL where that is 0).
+ *   limits     Nb * heads <= 65535, Lq and Lk 1 .. 2^24 (samples without tokens: lengths of 0), L * ld < 2^38 elements.
+ *   workspace  hq_attention_fwd_workspace_size bytes (0 in this version), 16-byte aligned; NULL where that is 0.
  * hq_attention_bwd: the gradients dq, dk, dv of the same call from dout, its inputs and its results out and lse:
  *   P = exp(scale q k^T - lse), dS = P o (dout v^T - rowsum(dout o out)), dq = scale dS k, dk = scale dS^T q, dv = P^T dout, the last
  *   two summed over the heads that share k and v.  P and dS are rounded to bf16 before they enter the second products.
+ *   The score of a query that sees one key has no gradient (its weight is 1): its dq is zero, not the difference of two roundings.
  *   Every sum runs in a fixed order: the same inputs give the same bits.  Rows behind the lengths, and of queries that see no key: zeros.
  *   dq, dk, dv  device bf16, laid out as q, k, v with pitches of their own.
- *   workspace  hq_attention_bwd_workspace_size bytes, 16-byte aligned; it need not be cleared, and calls that may overlap on the GPU
+ *   workspace  hq_attention_bwd_workspace_size bytes (asked with the device current that the call runs on: its number of SMs counts),
+ *              16-byte aligned; it need not be cleared, and calls that may overlap on the GPU
  *              (other streams, captured graphs that run side by side) need one each. */
 hq_status hq_attention_fwd_workspace_size(int64_t Nb, int64_t Lq, int64_t Lk, int heads, int kv_heads, int dh, size_t* bytes);
 hq_status hq_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int64_t Nb, int64_t Lq,
