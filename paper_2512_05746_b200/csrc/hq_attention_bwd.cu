@@ -969,7 +969,10 @@ int bwd_parts(int64_t Nb, int64_t Lq, int64_t Lk, int heads, int kv_heads, int d
     const int64_t work = keys * key_steps + queries * query_steps;
     int64_t parts = work > 0 ? (2 * key_steps * slots + work - 1) / work : 1;
     if (parts > key_steps / 8) parts = key_steps / 8;
-    return int(parts < 1 ? 1 : parts < 16 ? parts : 16);
+    parts = parts < 1 ? 1 : parts < 16 ? parts : 16;
+    // the persistent CTAs' warps wait for whole items, and waits end after a second: 2^17 steps of 2 us are a quarter of that
+    const int64_t least = dh <= 64 ? 1 : (key_steps + (1 << 17) - 1) >> 17;
+    return int(parts > least ? parts : least);
 }
 
 // statistics, the count of items taken, the shares' sums

@@ -122,3 +122,11 @@ def test_binding_refuses(hq):
     with pytest.raises(TypeError):
         h = x.half()
         hq.hq_qk_norm_rope(h, None, 2, 0, None, None, 1e-6, None, None, h, None)
+
+
+def test_no_item_of_the_gradient_outlasts_a_wait(hq):
+    """64 query heads on one key head, 2^22 queries: a tile of keys has 2^21 steps and comes in 16 shares at least, whose fp32 sums of
+    dk and dv the workspace holds."""
+    Lq, Lk, heads, dh = 1 << 22, 16384, 64, 128
+    stats, shares = heads * Lq * 2 * 4, 16 * (Lk // 128) * 2 * (128 * dh * 4)
+    assert hq.hq_attention_bwd_workspace_size(1, Lq, Lk, heads, 1, dh) >= stats + shares
