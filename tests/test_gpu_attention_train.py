@@ -195,6 +195,27 @@ def test_same_bits_on_every_run_and_stream(hq, dh, L, Lk):
         assert all(torch.equal(a, b) for a, b in zip(first, again))
 
 
+def test_calls_that_overlap(hq):
+    """Training steps of four widths at the same time, each on a stream and a workspace of its own: the bits of the calls one by one."""
+    steps = []
+    for seed, (Nb, L, Lk, H, G, dh) in enumerate([(4, 500, 500, 8, 8, 64), (2, 700, 700, 8, 2, 128), (8, 900, 77, 4, 4, 40), (3, 300, 300, 6, 3, 72)]):
+        q, k, v, dout = make(50 + seed, Nb, L, Lk, H, G, dh)
+        out, lse = fwd(hq, q, k, v, Nb, H, G, causal=True)
+        want = [out, lse, *bwd(hq, q, k, v, out, lse, dout, Nb, H, G, causal=True)]
+        got = [torch.full_like(t, math.nan) for t in want]
+        ws = workspace(hq.hq_attention_bwd_workspace_size(Nb, L, Lk, H, G, dh))
+        steps.append((q, k, v, dout, Nb, H, G, want, got, ws, torch.zeros((1,), dtype=torch.int32, device="cuda"), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for q, k, v, dout, Nb, H, G, want, got, ws, status, stream in steps:
+            hq.hq_attention_fwd(q, k, v, Nb, H, G, got[0], got[1], causal=True, dev_status=status, stream=stream)
+            hq.hq_attention_bwd(q, k, v, got[0], got[1], dout, Nb, H, G, *got[2:], ws, causal=True, dev_status=status, stream=stream)
+    torch.cuda.synchronize()
+    for *_, want, got, ws, status, stream in steps:
+        hq.hq_check_status(status)
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
 @pytest.mark.parametrize("Lk", [190, 100])
 def test_captured_and_replayed(hq, Lk):
     """A forward and backward pass in one graph, replayed on inputs and lengths that change in place."""
