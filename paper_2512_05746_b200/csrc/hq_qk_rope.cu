@@ -278,7 +278,8 @@ __global__ void __launch_bounds__(kRopeThreads, GRAD ? 2 : sizeof(T) == 4 ? 3 : 
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const f32x2 xh = mul2(x[e], inv2);
-                        dgamma[e] = fma2(w[e], xh, dgamma[e]);                               // zeros where there is no head
+                        // a lane without a head has no part in the sum: 1 / rms of nothing is infinite where eps is 0, and its table row nobody's
+                        if (live && head < heads) dgamma[e] = fma2(w[e], xh, dgamma[e]);
                         x[e] = mul2(inv2, fma2(xh, less, o[e]));
                     }
                 }

@@ -191,3 +191,62 @@ def test_a_block_s_attention_forward_and_backward(hq, graph):
         size = go.double().abs().max() * 64 * 2.0 ** -23 * math.sqrt(dh) * 8
         assert bool(((dx.double() - gx).abs() <= u * gx.abs() + size).all())
         assert bool(((dg.double() - gg).abs() <= 1e-4 * gg.abs().max()).all())
+
+
+def check_gradient(hq, q, k, H, G, gq, gk, eps, cos, sin, pos, interleaved, wanted=(True, True), stream=None):
+    """Forward and gradient of the given inputs against 64 bits, element by element, with the bounds of `run`; returns what was computed."""
+    rows, dtype, dh = q.shape[0], q.dtype, q.shape[1] // H
+    gen = torch.Generator(device="cuda").manual_seed(rows + dh)
+    grads_out = [torch.randn((rows, n * dh), generator=gen, device="cuda").to(dtype) for n in (H, G)]
+    outs, dx = ([torch.full((rows, n * dh), math.nan, dtype=dtype, device="cuda") for n in (H, G)] for _ in range(2))
+    dg = [torch.full((dh,), math.nan, device="cuda") if want else None for want in wanted]
+    ws = torch.empty((hq.hq_qk_norm_rope_bwd_workspace_size(rows, H, G, dh),), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    torch.cuda.synchronize()                     # the calls may run on another stream than the fills
+    hq.hq_qk_norm_rope(q, k, H, G, gq, gk, eps, cos, sin, *outs, positions=pos, interleaved=interleaved, stream=stream)
+    hq.hq_qk_norm_rope_bwd(q, k, H, G, gq, gk, eps, cos, sin, *grads_out, *dx, *dg, ws, positions=pos, interleaved=interleaved, stream=stream)
+    torch.cuda.synchronize()
+    u, f = unit(dtype), 2.0 ** -23
+    for x, heads, g, y, go, d, dgamma in zip((q, k), (H, G), (gq, gk), outs, grads_out, dx, dg):
+        leaves = [x.double().clone().requires_grad_(), g.double().clone().requires_grad_()]
+        want = rope(leaves[0], heads, leaves[1], eps, cos, sin, pos, interleaved)
+        grads = torch.autograd.grad(want, leaves, go.double())
+        by_head = lambda t: t.double().reshape(rows, heads, dh)  # noqa: E731
+        whole = lambda t: t.expand(-1, -1, dh).flatten(1)  # noqa: E731
+        bound = u * want.detach().abs() + 64 * f * whole(by_head(want.detach()).abs().amax(-1, keepdim=True))
+        assert bool(((y.double() - want.detach()).abs() <= bound).all())
+        inv = (by_head(x).square().mean(-1, keepdim=True) + eps).rsqrt()
+        bound = u * grads[0].abs() + 64 * f * whole(inv * g.abs().max().item() * 2 * by_head(go).norm(dim=-1, keepdim=True))
+        assert bool(((d.double() - grads[0]).abs() <= bound).all())
+        if dgamma is not None:
+            terms = ((by_head(x) * inv).abs() * 2 * by_head(go).abs().amax(-1, keepdim=True)).sum((0, 1))
+            assert bool(((dgamma.double() - grads[1]).abs() <= (16 + math.sqrt(rows * heads)) * f * terms + 1e-12).all())
+    return outs + dx + dg
+
+
+def block_inputs(rows, H, G, dh, dtype, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    return rand(rows, H * dh).to(dtype), rand(rows, G * dh).to(dtype), 1 + 0.3 * rand(dh), 1 + 0.3 * rand(dh)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,H,G,dh", [(5, 3, 6, 64), (33, 6, 3, 64), (7, 1, 1, 128), (3, 2, 2, 72), (9, 1, 2, 32), (1, 5, 1, 40)])
+def test_no_epsilon(hq, rows, H, G, dh, dtype):
+    """eps = 0 on rows that are not zero: lanes without a head or a row, which divide by the norm of nothing, have no part in gamma's sums."""
+    q, k, gq, gk = block_inputs(rows, H, G, dh, dtype, 71)
+    check_gradient(hq, q, k, H, G, gq, gk, 0.0, *tables(rows, dh // 2), None, True)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("garbage", [math.nan, math.inf])
+@pytest.mark.parametrize("H,G", [(3, 6), (1, 2)])
+def test_table_rows_that_no_token_takes(hq, interleaved, garbage, H, G):
+    """Whatever the first row of the tables holds, where no token stands there."""
+    rows, dh, npos = 37, 64, 20
+    q, k, gq, gk = block_inputs(rows, H, G, dh, torch.bfloat16, 72)
+    cos, sin = tables(npos, dh)
+    pos = (torch.arange(rows, device="cuda") % (npos - 1) + 1).to(torch.int32)
+    want = check_gradient(hq, q, k, H, G, gq, gk, EPS, cos, sin, pos, interleaved)
+    cos[0], sin[0] = garbage, garbage
+    got = check_gradient(hq, q, k, H, G, gq, gk, EPS, cos, sin, pos, interleaved)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
