@@ -418,7 +418,8 @@ hq_status hq_qk_norm_rope_bwd(const void* q, int64_t ldq, const void* k, int64_t
  * hq_attention_bwd: the gradients dq, dk, dv of the same call from dout, its inputs and its results out and lse:
  *   P = exp(scale q k^T - lse), dS = P o (dout v^T - rowsum(dout o out)), dq = scale dS k, dk = scale dS^T q, dv = P^T dout, the last
  *   two summed over the heads that share k and v.  P and dS are rounded to bf16 before they enter the second products.
- *   The score of a query that sees one key has no gradient (its weight is 1): its dq is zero, not the difference of two roundings.
+ *   The score of a query that sees one key has no gradient (its weight is 1): its dq is zero and its part of dk too, not the difference
+ *   of two roundings.
  *   Every sum runs in a fixed order: the same inputs give the same bits.  Rows behind the lengths, and of queries that see no key: zeros.
  *   dq, dk, dv  device bf16, laid out as q, k, v with pitches of their own.
  *   workspace  hq_attention_bwd_workspace_size bytes (asked with the device current that the call runs on: its number of SMs counts),

@@ -394,6 +394,12 @@ __device__ __forceinline__ bool bwd_probabilities(const BwdParams& p, const BwdI
 #pragma unroll
                 for (int e = 0; e < 16; ++e) w[e] = 0u;
             }
+            // causal, as many queries as keys or more: the first that sees a key sees this one only, a weight of 1 whatever its score
+            const int one = r == 0 ? -t.sm.shift - c0 : -1;
+            if (s.causal && __any_sync(0xffffffffu, unsigned(one) < 32u)) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] &= one == 2 * e ? 0xFFFF0000u : one == 2 * e + 1 ? 0xFFFFu : 0xFFFFFFFFu;
+            }
         } else {
             const int valid = limit - c0;                      // what lies behind may be anything
             if (__any_sync(0xffffffffu, valid < 32)) {
@@ -796,6 +802,12 @@ __device__ __forceinline__ bool small_run(const BwdMaps& m, const BwdParams& p, 
                 if (t.sm.kl == 1) {                            // every query sees one key only
 #pragma unroll
                     for (int e = 0; e < 16; ++e) w[e] = 0u;
+                }
+                // causal, as many queries as keys or more: the first that sees a key sees this one only, a weight of 1 whatever its score
+                const int one = r == 0 ? -t.sm.shift - c0 : -1;
+                if (s.causal && __any_sync(0xffffffffu, unsigned(one) < 32u)) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w[e] &= one == 2 * e ? 0xFFFF0000u : one == 2 * e + 1 ? 0xFFFFu : 0xFFFFFFFFu;
                 }
             } else {
                 const int valid = limit - c0;                  // what lies behind may be anything

@@ -6,7 +6,7 @@ import math
 import pytest
 import torch
 
-from attention_train_reference import backward, forward
+from attention_train_reference import backward, forward, visible
 
 pytestmark = pytest.mark.gpu
 BF = torch.bfloat16
@@ -276,3 +276,18 @@ def test_agrees_with_the_inference_attention(hq):
     want, _, bound, _ = forward(q, k, v, Nb, H, H, dh ** -0.5)
     within(out, want, bound, "out")
     within(old, want, 2 * bound, "hq_attention")
+
+
+@pytest.mark.parametrize("dh,H,G", [(40, 8, 4), (64, 8, 8), (72, 8, 8), (128, 8, 2)])
+@pytest.mark.parametrize("Lq,Lk,lens", [(2, 2, False), (300, 130, False), (200, 200, True), (2100, 140, False), (2100, 140, True)])
+def test_queries_that_see_one_key(hq, dh, H, G, Lq, Lk, lens):
+    """Under the causal mask the query that sees the first key only has a weight of 1 whatever its score: with the gradients of all other
+    outputs zero, dq and dk are zero, to the bit, and dv is not."""
+    ql, kl = (torch.tensor(t, dtype=torch.int32, device="cuda") for t in ([Lq, 77, 2, 90], [Lk, 77, 2, 70])) if lens else (None, None)
+    Nb = 4 if lens else 2
+    q, k, v, dout = make(61 + dh, Nb, Lq, Lk, H, G, dh)
+    one = (visible(Nb, Lq, Lk, True, ql, kl, "cuda").sum(-1) == 1).flatten()
+    assert one.sum() == Nb
+    dout[~one] = 0
+    _, _, (dq, dk, dv) = check(hq, q, k, v, dout, Nb, H, G, causal=True, q_lens=ql, k_lens=kl)
+    assert not dq.any() and not dk.any() and dv.any()
