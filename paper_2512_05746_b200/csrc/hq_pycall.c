@@ -4,6 +4,7 @@
  * binding.py hands over (bind): nothing is linked against either library, and the GIL is released during the call. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <limits.h>
 #include <stdint.h>
 
 #include "../../include/hq.h"
@@ -66,6 +67,10 @@ static int integer(PyObject* v, int64_t* out) {
 static int small(PyObject* v, int* out) {
     const long r = PyLong_AsLong(v);
     if (r == -1 && PyErr_Occurred()) return -1;
+    if (r < INT_MIN || r > INT_MAX) {
+        PyErr_Format(PyExc_OverflowError, "%ld is not a number of 32 bits", r);
+        return -1;
+    }
     *out = (int)r;
     return 0;
 }
@@ -421,6 +426,10 @@ static int rope_shape_of(PyObject* const* a, PyObject* positions, PyObject* inte
     s->eps = (float)PyFloat_AsDouble(a[6]);
     s->interleaved = PyObject_IsTrue(interleaved);
     if (PyErr_Occurred() || (a[7] != Py_None && shape(a[7], 2, table))) return -1;
+    if (table[1] > INT_MAX / 2) {
+        PyErr_Format(PyExc_OverflowError, "tables of %lld columns", (long long)table[1]);
+        return -1;
+    }
     s->npos = table[0];
     s->rot = (int)(2 * table[1]);
     return dense("gamma_q", a[4], dt_f32, 1, s->dh, 0, 0, dev, &s->gq) || dense("gamma_k", a[5], dt_f32, 1, s->dh, 0, 0, dev, &s->gk) ||

@@ -130,3 +130,27 @@ def test_no_item_of_the_gradient_outlasts_a_wait(hq):
     Lq, Lk, heads, dh = 1 << 22, 16384, 64, 128
     stats, shares = heads * Lq * 2 * 4, 16 * (Lk // 128) * 2 * (128 * dh * 4)
     assert hq.hq_attention_bwd_workspace_size(1, Lq, Lk, heads, 1, dh) >= stats + shares
+
+
+@pytest.mark.parametrize("big", [(1 << 32) + 2, -(1 << 32) + 2, 1 << 31])
+def test_counts_beyond_32_bits(hq, big):
+    """A number of heads is not taken modulo 2^32, and neither is the tables' width."""
+    bf = torch.bfloat16
+    q, lse = torch.zeros((8, 128), dtype=bf), torch.zeros((2, 2, 4))
+    ws = torch.zeros(1 << 16, dtype=torch.uint8)
+    for H, G in ((big, 2), (2, big)):
+        with pytest.raises(OverflowError):
+            hq.hq_attention_fwd(q, q, q, 2, H, G, q, lse)
+        with pytest.raises(OverflowError):
+            hq.hq_attention_bwd(q, q, q, q, lse, q, 2, H, G, q, q, q, ws)
+        with pytest.raises(OverflowError):
+            hq.hq_qk_norm_rope(q, q, H, G, None, None, 1e-6, None, None, q, q)
+        with pytest.raises(OverflowError):
+            hq.hq_qk_norm_rope_bwd(q, q, H, G, None, None, 1e-6, None, None, q, q, q, q, None, None, None)
+
+
+def test_tables_beyond_32_bits(hq):
+    """2^31 + 32 columns are no rotation of 64 channels."""
+    q, cos = torch.zeros((8, 128)), torch.empty((0, (1 << 31) + 32))
+    with pytest.raises(OverflowError):
+        hq.hq_qk_norm_rope(q, q, 2, 2, None, None, 1e-6, cos, cos, q, q)
