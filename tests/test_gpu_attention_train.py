@@ -291,3 +291,25 @@ def test_queries_that_see_one_key(hq, dh, H, G, Lq, Lk, lens):
     dout[~one] = 0
     _, _, (dq, dk, dv) = check(hq, q, k, v, dout, Nb, H, G, causal=True, q_lens=ql, k_lens=kl)
     assert not dq.any() and not dk.any() and dv.any()
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("of", ["queries", "keys"])
+@pytest.mark.parametrize("Lq,Lk,H,G,dh", [(260, 77, 4, 4, 40), (2100, 140, 2, 1, 64), (300, 300, 3, 1, 72), (2100, 140, 2, 1, 128)])
+def test_lengths_of_one_side(hq, Lq, Lk, H, G, dh, of, causal):
+    """Text tokens of several lengths under images of one (k_lens alone), and padded queries on keys of one length (q_lens alone); what
+    lies behind the lengths may be anything."""
+    L = Lk if of == "keys" else Lq
+    lens = torch.tensor([L, 0, 1, L // 2, L - 1], dtype=torch.int32, device="cuda")
+    Nb = lens.numel()
+    q, k, v, dout = make(81 + dh, Nb, Lq, Lk, H, G, dh)
+    kw = dict(causal=causal, q_lens=lens if of == "queries" else None, k_lens=lens if of == "keys" else None)
+    clean = check(hq, q, k, v, dout, Nb, H, G, **kw)
+    dead = (torch.arange(L, device="cuda")[None] >= lens[:, None]).flatten()
+    for t in (q, dout) if of == "queries" else (k, v):
+        t[dead] = math.nan
+    out, lse = fwd(hq, q, k, v, Nb, H, G, **kw)
+    grads = bwd(hq, q, k, v, out, lse, dout, Nb, H, G, **kw)
+    assert torch.equal(out, clean[0]) and torch.equal(lse, clean[1]) and all(torch.equal(a, b) for a, b in zip(grads, clean[2]))
+    for g in grads[:1] if of == "queries" else grads[1:]:
+        assert not g[dead].any()

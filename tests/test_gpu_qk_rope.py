@@ -250,3 +250,74 @@ def test_table_rows_that_no_token_takes(hq, interleaved, garbage, H, G):
     cos[0], sin[0] = garbage, garbage
     got = check_gradient(hq, q, k, H, G, gq, gk, EPS, cos, sin, pos, interleaved)
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def off_by_one_float(t):
+    """The same values, dense, at an address that is a multiple of 4 bytes and no more."""
+    wide = torch.empty((t.numel() + 1,), dtype=t.dtype, device=t.device)
+    wide[1:] = t.flatten()
+    return wide[1:].view(t.shape)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dh,rot", [(32, 32), (64, 64), (64, 16), (72, 48), (128, 128)])
+def test_tables_off_the_16_byte_boundary(hq, dh, rot, interleaved, dtype):
+    rows, H, G = 45, 3, 2
+    q, k, gq, gk = block_inputs(rows, H, G, dh, dtype, 73)
+    cos, sin = (off_by_one_float(t) for t in tables(20, rot))
+    assert cos.is_contiguous() and cos.data_ptr() % 16 == 4
+    check_gradient(hq, q, k, H, G, off_by_one_float(gq), off_by_one_float(gk), EPS, cos, sin, None, interleaved)
+
+
+@pytest.mark.parametrize("wanted", [(True, False), (False, True), (False, False)])
+def test_gradient_of_one_gamma(hq, wanted):
+    q, k, gq, gk = block_inputs(300, 4, 2, 64, torch.bfloat16, 74)
+    args = (hq, q, k, 4, 2, gq, gk, EPS, *tables(300, 64), None, False)
+    both, some = check_gradient(*args), check_gradient(*args, wanted=wanted)
+    assert all(b is None or torch.equal(a, b) for a, b in zip(both, some))
+    assert [b is not None for b in some[4:]] == list(wanted)
+
+
+def test_streams_and_calls_that_overlap(hq):
+    """On another stream, and steps of several widths at the same time, each with a workspace of its own: the bits of the calls one by one."""
+    steps = []
+    for seed, (rows, H, G, dh, dtype) in enumerate([(30000, 8, 8, 64, torch.bfloat16), (20, 8, 8, 64, torch.bfloat16),
+                                                    (9000, 6, 3, 72, torch.float32), (5000, 16, 2, 128, torch.bfloat16)]):
+        q, k, gq, gk = block_inputs(rows, H, G, dh, dtype, 75 + seed)
+        table, stream = tables(250, dh), torch.cuda.Stream()
+        want = check_gradient(hq, q, k, H, G, gq, gk, EPS, *table, None, False, stream=stream)
+        # the gradients of the outputs that check_gradient drew
+        gen = torch.Generator(device="cuda").manual_seed(rows + dh)
+        go = [torch.randn((rows, n * dh), generator=gen, device="cuda").to(dtype) for n in (H, G)]
+        got = [torch.full_like(t, math.nan) for t in want]
+        ws = torch.empty((hq.hq_qk_norm_rope_bwd_workspace_size(rows, H, G, dh),), dtype=torch.uint8, device="cuda").fill_(0xFF)
+        steps.append(((q, k, H, G, gq, gk, EPS, *table), go, want, got, ws, stream))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for args, go, _, got, ws, stream in steps:
+            hq.hq_qk_norm_rope(*args, *got[:2], stream=stream)
+            hq.hq_qk_norm_rope_bwd(*args, *go, *got[2:], ws, stream=stream)
+    torch.cuda.synchronize()
+    for _, _, want, got, _, _ in steps:
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_offsets_past_32_bits(hq, dtype):
+    """Rows 4 Mi elements apart: the last ones lie beyond 2^31 elements."""
+    rows, H, G, dh = 600, 2, 1, 64
+    q, k, gq, gk = block_inputs(rows, H, G, dh, dtype, 76)
+    args = (H, G, gq, gk, EPS, *tables(rows, dh))
+    want = check_gradient(hq, q, k, *args, None, False)
+    gen = torch.Generator(device="cuda").manual_seed(rows + dh)
+    go = [torch.randn((rows, n * dh), generator=gen, device="cuda").to(dtype) for n in (H, G)]
+    wide = torch.empty((rows, 1 << 22), dtype=dtype, device="cuda")            # 5 or 10 GB
+    cols = [wide[:, 128 * i: 128 * i + t.shape[1]] for i, t in enumerate([q, k, *go, *want[:4]])]
+    for c, t in zip(cols, (q, k, *go)):
+        c.copy_(t)
+    dg = [torch.empty_like(gq) for _ in range(2)]
+    ws = torch.empty((hq.hq_qk_norm_rope_bwd_workspace_size(rows, H, G, dh),), dtype=torch.uint8, device="cuda")
+    hq.hq_qk_norm_rope(*cols[:2], *args, *cols[4:6])
+    hq.hq_qk_norm_rope_bwd(*cols[:2], *args, *cols[2:4], *cols[6:], *dg, ws)
+    assert all(torch.equal(a, b) for a, b in zip(want, cols[4:] + dg))
