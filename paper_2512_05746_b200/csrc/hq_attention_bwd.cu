@@ -971,10 +971,14 @@ hq_status launch_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, con
     return HQ_OK;
 }
 
-// Shares of a tile of keys' steps: enough that the longest item takes about half the time an SM has for all of them, where a share has
-// eight steps at least.  8 x 4096 queries on 77 keys, 8 heads of 40 (64 tiles of keys) 80 us in one share, 2 x 4096 causal, 16 / 2 heads
-// of 128 (128 tiles of up to 256 steps) 535.
-int bwd_parts(int64_t Nb, int64_t Lq, int64_t Lk, int heads, int kv_heads, int dh) {
+// Shares of a tile of keys' steps: enough that the longest item takes about half the time a slot (an SM, or half of one) has for all of
+// them, where a share has eight steps at least, and only where that saves more than it costs.  Saved is what the longest item takes
+// beyond a slot's average; tiles do not fill the slots evenly, so that whole items count for four tenths more than they take.  The shares'
+// sums and the kernel that joins them cost twelve steps of 64 queries, and a quarter of one for each tile.  Whole / in shares: 16 x 1024
+// queries on 77 keys, 8 heads of 64 53 / 67 us, 4 x 2027 causal, 4 heads of 64 61 / 79, 4 x 1575 on 300, 8 heads of 64 42 / 48, 2 x 4096, 16 / 2
+// heads of 128 848 / 867, causal 513 / 478, 8 x 4096 on 77, 8 heads of 40 84 / 83, 1051 on 77, 4 heads of 64 27 / 21, 2 x 4096 on 77, 8 heads of
+// 64 95 / 42, one sample of 4096, 8 / 1 heads of 64 574 / 155.
+int bwd_parts(int64_t Nb, int64_t Lq, int64_t Lk, int heads, int kv_heads, int dh, bool causal) {
     const int64_t block = dh <= 64 ? kSmallBlock : kAttnTile, slots = int64_t(sm_count()) * (dh <= 64 ? 2 : 1);
     const int64_t key_steps = heads / kv_heads * ((Lq + block - 1) / block), query_steps = (Lk + block - 1) / block + 2;
     const int64_t keys = Nb * kv_heads * ((Lk + kAttnTile - 1) / kAttnTile), queries = Nb * heads * ((Lq + kAttnTile - 1) / kAttnTile);
@@ -982,21 +986,25 @@ int bwd_parts(int64_t Nb, int64_t Lq, int64_t Lk, int heads, int kv_heads, int d
     int64_t parts = work > 0 ? (2 * key_steps * slots + work - 1) / work : 1;
     if (parts > key_steps / 8) parts = key_steps / 8;
     parts = parts < 1 ? 1 : parts < 16 ? parts : 16;
+    const int64_t average = (causal ? work / 2 : work) / slots;
+    const int64_t then = key_steps / parts > average ? key_steps / parts : average;          // the longest item, or all of them evenly
+    if ((14 * key_steps / 10 - then) * block < (12 + keys / 4) * 64) parts = 1;
     // the persistent CTAs' warps wait for whole items, and waits end after a second: 2^17 steps of 2 us are a quarter of that
     const int64_t least = dh <= 64 ? 1 : (key_steps + (1 << 17) - 1) >> 17;
     return int(parts > least ? parts : least);
 }
 
-// statistics, the count of items taken, the shares' sums
+// statistics, the count of items taken, the shares' sums (room for those of the causal mask and of none: the size is asked without it)
 struct BwdWorkspace { int64_t stats, taken, partial, bytes; int parts; };
-BwdWorkspace bwd_workspace(int64_t Nb, int64_t Lq, int64_t Lk, int heads, int kv_heads, int dh) {
+BwdWorkspace bwd_workspace(int64_t Nb, int64_t Lq, int64_t Lk, int heads, int kv_heads, int dh, bool causal) {
     BwdWorkspace w;
-    w.parts = bwd_parts(Nb, Lq, Lk, heads, kv_heads, dh);
+    w.parts = bwd_parts(Nb, Lq, Lk, heads, kv_heads, dh, causal);
+    const int other = bwd_parts(Nb, Lq, Lk, heads, kv_heads, dh, !causal), most = w.parts > other ? w.parts : other;
     w.stats = 0;
     w.taken = Nb * heads * ((Lq + kAttnTile - 1) / kAttnTile) * 2 * kStatBytes;
     w.partial = w.taken + 16;
     const int64_t tile = int64_t(dh <= 64 ? 64 : 128) * kAttnTile * 4, keys = Nb * kv_heads * ((Lk + kAttnTile - 1) / kAttnTile);
-    w.bytes = w.partial + (w.parts > 1 ? w.parts * keys * 2 * tile : 0);
+    w.bytes = w.partial + (most > 1 ? most * keys * 2 * tile : 0);
     return w;
 }
 
@@ -1008,7 +1016,7 @@ extern "C" hq_status hq_attention_bwd_workspace_size(int64_t Nb, int64_t Lq, int
     if (bytes == nullptr) return HQ_ERR_INVALID_ARG;
     const hq_status e = attn_check(Nb, Lq, Lk, heads, kv_heads, dh, 1.0f);
     if (e != HQ_OK) return e;
-    *bytes = size_t(bwd_workspace(Nb, Lq, Lk, heads, kv_heads, dh).bytes);
+    *bytes = size_t(bwd_workspace(Nb, Lq, Lk, heads, kv_heads, dh, false).bytes);
     return HQ_OK;
 }
 
@@ -1028,7 +1036,7 @@ extern "C" hq_status hq_attention_bwd(const void* q, int64_t ldq, const void* k,
         return e;
     if (lse == nullptr || workspace == nullptr) return HQ_ERR_INVALID_ARG;
     if (!aligned16(workspace)) return HQ_ERR_ALIGNMENT;
-    const BwdWorkspace w = bwd_workspace(Nb, Lq, Lk, heads, kv_heads, dh);
+    const BwdWorkspace w = bwd_workspace(Nb, Lq, Lk, heads, kv_heads, dh, causal != 0);
     if (int64_t(ws_bytes) < w.bytes) return HQ_ERR_WORKSPACE;
     const int64_t q_tiles = (Lq + kAttnTile - 1) / kAttnTile, k_tiles = (Lk + kAttnTile - 1) / kAttnTile;
     const int64_t key_items = Nb * kv_heads * k_tiles, items = key_items * w.parts + Nb * heads * q_tiles;

@@ -154,3 +154,19 @@ def test_tables_beyond_32_bits(hq):
     q, cos = torch.zeros((8, 128)), torch.empty((0, (1 << 31) + 32))
     with pytest.raises(OverflowError):
         hq.hq_qk_norm_rope(q, q, 2, 2, None, None, 1e-6, cos, cos, q, q)
+
+
+def test_tiles_of_keys_come_in_shares_where_that_saves_time(hq):
+    """The workspace holds the shares' sums (dk and dv of 128 keys in fp32 each) where a call makes shares, and else the statistics: 16 x
+    1024 queries on 77 keys took 52 us whole and 68 in shares, 4 x 2027 causal, 4 heads of 64 61 and 79; one sample of 4096, 8 / 1 heads
+    of 64 575 and 156, 2 x 4096 causal, 16 / 2 heads of 128 520 and 485 (unmasked 863 and 887, the same workspace)."""
+    def shares(Nb, Lq, Lk, heads, kv_heads, dh):
+        width, keys = 64 if dh <= 64 else 128, Nb * kv_heads * (-(-Lk // 128))
+        stats = Nb * heads * (-(-Lq // 128)) * 1024 + 16
+        return (hq.hq_attention_bwd_workspace_size(Nb, Lq, Lk, heads, kv_heads, dh) - stats) / (keys * 2 * 128 * width * 4)
+    assert shares(16, 1024, 77, 8, 8, 64) == 0
+    assert shares(4, 2027, 2027, 4, 4, 64) == 0
+    assert shares(8, 1075, 77, 16, 16, 40) == 0
+    assert shares(1, 4096, 4096, 8, 1, 64) >= 8
+    assert shares(2, 4096, 77, 8, 8, 64) >= 4
+    assert shares(2, 4096, 4096, 16, 2, 128) >= 2
