@@ -378,14 +378,14 @@ hq_status hq_attention(const void* qkv, int64_t Nb, int64_t L, int64_t C, int he
  * the statistic its gradient needs, and both gradients (no counterpart in the paper's equations; its training differentiates the
  * network around the quantized layers).  Matrices are [rows][ld] with the heads side by side (head h at columns h*dh ..), so that the
  * thirds of a fused QKV projection are passed in place: q, q + heads*dh, q + (heads + kv_heads)*dh with one pitch.  Query head h
- * uses key head h / (heads / kv_heads).  dh: a multiple of 8 up to 128.  Base pointers 16-byte aligned, pitches multiples of 16
- * bytes.  Outputs may not overlap inputs, except where said. ----------------------------------------------------------------------
+ * uses key head h / (heads / kv_heads).  dh: a multiple of 8 up to 128.  The matrices' base pointers 16-byte aligned, their pitches
+ * multiples of 16 bytes; gammas, tables, positions, lengths and lse as their type.  Outputs may not overlap inputs, except where said. -----
  *
  * hq_qk_norm_rope: per row and head y = x / sqrt(mean(x^2) + eps) * gamma, then the rotation of the first `rot` channels (even, <= dh;
  *   0: none): pairs (j, j + rot/2), or (2j, 2j + 1) when interleaved != 0, become (a c_j - b s_j, b c_j + a s_j).
  *   q, q_out   device [rows] x heads heads, fp32 or bf16 (xdt); k, k_out [rows] x kv_heads heads of the same type, or NULL with
  *              kv_heads 0 (queries only; keys of another length take a call of their own as `q`).  q_out may be q, k_out may be k.
- *   gamma_q, gamma_k   device fp32 [dh], or NULL (1).
+ *   gamma_q, gamma_k   device fp32 [dh], or NULL (1).  eps >= 0; a head of zeros has no norm where it is 0 (NaN).
  *   cos, sin   device fp32 [npos][rot/2]; positions device int32 [rows], the table row of each token (clamped to the table), or
  *              NULL: token r takes row r mod npos (samples of npos tokens).
  * hq_qk_norm_rope_bwd: dq, dk from dq_out, dk_out and the inputs q, k of the forward call; dgamma_q, dgamma_k (device fp32 [dh],

@@ -16,8 +16,9 @@
 //
 // Up to 64 channels an item is a CTA of its own, two an SM (attention_bwd_small_kernel); above, persistent CTAs take item after item
 // (attention_bwd_kernel).  Measured, the statistics' kernel included: 64 x 1024 tokens, 8 heads of 64 (481 GFLOP in seven products)
-// 680 us, held to 1.6 GHz by the power limit, 239 us of it two passes of exponentials (16 a clock in an SM); 2 x 4096 causal, 16 / 2
-// heads of 128 496 us; 8 x 4096 queries on 77 keys, 8 heads of 40 86 us; 2 x 64 tokens, 8 heads of 64 12.3 us a call.
+// 684 us in a run of calls, which the power limit holds to 1.6 GHz (650 in a short one), 239 us of it two passes of exponentials (16 a
+// clock in an SM); 2 x 4096 causal, 16 / 2 heads of 128 501 us (460); 8 x 4096 queries on 77 keys, 8 heads of 40 86 us; 2 x 64 tokens, 8 heads
+// of 64 12.1 us a call.
 #include "hq_attention_tile.cuh"
 
 namespace hq {
@@ -29,7 +30,8 @@ constexpr int kBwdWarps = 16, kBwdFirst = 4;                   // of the probabi
 constexpr int kBwdThreads = (kBwdFirst + kBwdWarps) * 32;
 constexpr uint32_t kStatBytes = kAttnTile * 4;                 // of one query tile: -lse * log2(e), and as many for -D
 
-// Rings of the kernel above 64 channels: tiles of 32 KB, of which two kept ones, three and two take all but 2 KB of the shared memory.
+// Rings of the kernel above 64 channels: tiles of 32 KB, of which two kept ones, three and two take all but 3 KB of the 227 KB of shared
+// memory; the statistics of the ring's tiles and the barriers take 2.75 KB of those.
 struct BwdRings {
     static constexpr int kParts = 2, kB0 = 3, kB1 = 2;         // kParts: of 64 channels
     static constexpr int kTile = kParts * kAttnPart;
@@ -60,6 +62,7 @@ struct BwdBars {
     uint32_t item[2], tmem_slot;
 };
 constexpr size_t kBwdSmem = size_t(BwdRings::kTiles + BwdRings::kStats) + sizeof(BwdBars);
+static_assert(kBwdSmem <= 227 * 1024, "the rings, their statistics and the barriers fit the shared memory of an SM");
 
 // What an item is: a tile of keys of one (sample, key head) or of queries of one (sample, head), and the other side's tiles it walks.
 struct BwdItem {
@@ -956,7 +959,8 @@ hq_status launch_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, con
     p.chunk = attn_chunk(s.causal != 0, p.q_tiles, int64_t(s.Nb) * s.heads, slots);
     if constexpr (NH == 1) {
         if (cudaFuncSetAttribute(attention_bwd_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmallSmem)) != cudaSuccess) return HQ_ERR_CUDA;
-        // few CTAs are placed while the statistics are still computed: 2 x 64 tokens, 8 heads of 64 12.7 us a call otherwise
+        // the launch of few CTAs is prepared while the statistics are computed (they are placed when the last of those CTAs has ended,
+        // which does not call griddep_launch): 2 x 64 tokens, 8 heads of 64 12.7 us a call otherwise, 12.3 so
         if (launch_dependent(attention_bwd_small_kernel, dim3(p.items), kSmallThreads, kSmallSmem, st, p.items <= slots, m, p) != cudaSuccess) return HQ_ERR_CUDA;
     } else {
         if (cudaFuncSetAttribute(attention_bwd_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kBwdSmem)) != cudaSuccess) return HQ_ERR_CUDA;

@@ -8,11 +8,13 @@
 //   P = exp2(c S - c m) as bf16 through shared memory, so that S of the next block is computed during this one's softmax
 //   O += P V         V read along its keys without a transpose, O in dh columns
 // What a CTA waits for, the others' exponentials cover: persistent CTAs of two tiles with blocks of 128 keys, P in tensor memory and 8 or
-// 16 softmax warps came to 245-265 us at 64 x 1024 tokens, 8 heads of 64 (201 so) and 174 at 2 x 4096 causal, 16 / 2 heads of 128 (144).
+// 16 softmax warps came to 245-265 us at 64 x 1024 tokens, 8 heads of 64 (201 so) and 174 at 2 x 4096 causal, 16 / 2 heads of 128 (144), both
+// timed on a cool GPU; in a run of calls this form takes 219 and 166 us.  Unmasked, 2 x 4096 with 16 heads of 128, those took 290-305
+// where this takes 337.
 // The running maximum moves only when a block's maximum exceeds it by more than 2^8 in the exponent: the weights stay below 2^8, the
 // division by the row sum at the end is the same, and O is read and rescaled in tensor memory almost never.  P is rounded to bf16
 // (the products' type), the row sum runs over the unrounded weights in fp32.
-// Bound by the exponentials (16 a clock in an SM: 119 us of the 201) and the waits between a block's steps.
+// Bound by the exponentials (16 a clock in an SM: 119 us of the 219) and the waits between a block's steps.
 #include "hq_attention_tile.cuh"
 
 namespace hq {

@@ -10,6 +10,10 @@
 // Memory-bound: every value is read and written once, tables and gamma come from the caches.  A group of dh / 8 lanes holds one head of
 // one row, 8 channels a lane (16 bytes of bf16), so that the row's sums are a few shuffles; 32 / (dh / 8) heads a warp.  Sums and
 // the rotation in fp32, one rounding at the end.
+//
+// 65536 rows of 8 + 8 heads of 64 in bf16: 65 us, 63 % of the copy rate, the gradient 101 (61 %); in fp32 92 and 137 us (89 %).  Between
+// the bounds in bf16: 20 instructions a value (24) at 66 % (49 %) of the issue slots, 46 % (48 %) of the DRAM rate and 44 % (24 %) of the
+// warps, which ask for a row, wait for it, compute and store before they ask for the next.
 #include "hq_common.cuh"
 #include "hq_fwht.cuh"
 
