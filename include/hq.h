@@ -437,6 +437,81 @@ hq_status hq_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ld
                            int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv, void* workspace, size_t ws_bytes,
                            int32_t* dev_status, void* stream);
 
+/* ---- What a training step of a transformer block needs around its linears and its attention: the gated residual with the norms before and
+ * after a block, the embedding lookup, both with their gradients, and the norm of all gradients with clipping (no counterpart in the paper's
+ * equations).  Matrices [rows][ld] with contiguous columns, base pointers 16-byte aligned, pitches multiples of 16 bytes, numbers of columns
+ * multiples of 8.  Outputs may not overlap inputs, except where said.  Every sum runs in a fixed order: the same inputs give the same
+ * bits. -----
+ *
+ * hq_gate_norm: the end of one block and the norm in front of the next.  Per row r, with the vectors of its group n = r / rows_per_group (a
+ *   sample; rows_per_group 0: one group of all rows):
+ *     t = h, or norm(h) * post_weight                     (post: the kind of norm, HQ_NORM_NONE: none)
+ *     x_out = residual_scale * x + gate[n] * t
+ *     y = norm(x_out) * (weight_plus + weight[n]) + bias[n]     (norm: its kind; of x_out before it is rounded to xdt)
+ *   HQ_NORM_LAYER: (v - mean(v)) / sqrt(var(v) + eps), biased variance; HQ_NORM_RMS: v / sqrt(mean(v^2) + eps); over the row's cols values.
+ *   eps >= 0; a row without variance has no norm where it is 0 (NaN).  With weight_plus 1 a modulation's scale and shift are passed as they are.
+ *   x, x_out   fp32 or bf16 (xdt); h, y of hdt, the same or the other.  cols <= 4096.  x_out may be x; y may be h.  x_out NULL: not wanted.
+ *   h          NULL: x_out = x (gate NULL, post NONE, residual_scale 1), a norm alone.  y NULL with norm HQ_NORM_NONE: the residual alone,
+ *              in front of a call that normalises on its own (hq_ln_qlinear).
+ *   gate, weight, bias   device fp32 [groups] with pitches of their own (slices of one modulation), 16-byte aligned, or NULL (1, 1, 0: without
+ *              a weight weight_plus is not added).  post_weight: fp32 [cols], or NULL.
+ *   lens       device int32 [groups], or NULL: rows of each group that are there (clamped to 0 .. rows_per_group).  Rows behind them are not
+ *              read: zeros in x_out, y and stats.  Needs rows_per_group > 0.
+ *   stats      device fp32 [rows][4], 16-byte aligned, or NULL: mean and 1 / standard deviation of x_out, then of h; what the gradient needs.
+ *              (0, 1) for a norm that is not taken, mean 0 for HQ_NORM_RMS.
+ * hq_gate_norm_bwd: the gradients of the same call from those of its outputs (dx_out, dy; dx_out NULL: nothing else uses x_out; dy NULL with
+ *   HQ_NORM_NONE), its results x_out and stats and its input h.  A norm alone: x_out is its input x.  x_out is read where a norm is taken.
+ *   dx, dh     NULL: not wanted.  dx may be dx_out, dh may be dy or h.  Rows behind lens: zeros.
+ *   dgate, dweight, dbias   device fp32 [groups] with pitches of their own, 16-byte aligned, NULL: not wanted; dpost_weight fp32 [cols].
+ *              h is read where dgate is wanted or a post norm was taken.
+ *   workspace  hq_gate_norm_bwd_workspace_size bytes, 16-byte aligned (NULL where none of the four is wanted); it need not be cleared, and
+ *              calls that may overlap on the GPU (other streams, captured graphs that run side by side) need one each. */
+typedef enum { HQ_NORM_LAYER = 0, HQ_NORM_RMS = 1, HQ_NORM_NONE = 2 } hq_norm;
+hq_status hq_gate_norm(const void* x, int64_t ldx, hq_dtype xdt, const void* h, int64_t ldh, hq_dtype hdt, int64_t rows, int64_t cols,
+                       int64_t rows_per_group, const int32_t* lens, hq_norm post, const float* post_weight, const float* gate,
+                       int64_t ld_gate, float residual_scale, hq_norm norm, const float* weight, int64_t ld_weight, const float* bias,
+                       int64_t ld_bias, float weight_plus, float eps, void* x_out, int64_t ldx_out, void* y, int64_t ldy, float* stats,
+                       void* stream);
+hq_status hq_gate_norm_bwd_workspace_size(int64_t rows, int64_t cols, int64_t rows_per_group, size_t* bytes);
+hq_status hq_gate_norm_bwd(const void* x_out, int64_t ldx_out, hq_dtype xdt, const void* h, int64_t ldh, hq_dtype hdt, const float* stats,
+                           int64_t rows, int64_t cols, int64_t rows_per_group, const int32_t* lens, hq_norm post, const float* post_weight,
+                           const float* gate, int64_t ld_gate, float residual_scale, hq_norm norm, const float* weight, int64_t ld_weight,
+                           float weight_plus, const void* dx_out, int64_t lddx_out, const void* dy, int64_t lddy, void* dx, int64_t lddx,
+                           void* dh, int64_t lddh, float* dpost_weight, float* dgate, int64_t ld_dgate, float* dweight,
+                           int64_t ld_dweight, float* dbias, int64_t ld_dbias, void* workspace, size_t ws_bytes, void* stream);
+
+/* hq_embedding: out[t] = scale * table[ids[t]]; a row of zeros for an id outside 0 .. classes - 1.
+ *   ids        device int32 or int64 (id_bytes 4 or 8) [tokens].  table [classes], out [tokens] rows of dim values, fp32 or bf16 each.
+ * hq_embedding_bwd: dtable[v] = base[v] + scale * sum of dout[t] over the tokens t of id v, in ascending order, in fp32; ids outside the
+ *   table have no part.  base: rows of dtable's type, or NULL (zeros: every row of dtable is written); base may be dtable (the gradient of an
+ *   earlier micro-batch: rows without tokens are not touched).  With scale 1 it is the gradient of hq_class_embed_add's table, too.
+ *   workspace  hq_embedding_bwd_workspace_size bytes, 16-byte aligned; as above.  dim <= 65536. */
+hq_status hq_embedding(const void* ids, int id_bytes, int64_t tokens, const void* table, hq_dtype tdt, int64_t classes, int64_t dim,
+                       int64_t ld_table, float scale, void* out, hq_dtype odt, int64_t ld_out, void* stream);
+hq_status hq_embedding_bwd_workspace_size(int64_t tokens, int64_t classes, int64_t dim, size_t* bytes);
+hq_status hq_embedding_bwd(const void* ids, int id_bytes, int64_t tokens, const void* dout, hq_dtype ddt, int64_t ld_dout, int64_t classes,
+                           int64_t dim, float scale, const void* base, int64_t ld_base, void* dtable, hq_dtype gdt, int64_t ld_dtable,
+                           void* workspace, size_t ws_bytes, void* stream);
+
+/* hq_grad_norm: norm[0] = sqrt of the sum of all squares of n dense tensors (squares joined in fp64).  hq_grad_clip: norm as there,
+ *   c = min(1, max_norm / (norm + eps)), out = c * grad for every tensor, coef[0] = c (coef NULL: not wanted).  A norm that is not finite gives
+ *   the c of the formula (0, NaN): look at norm where that may happen.
+ *   tensors    HOST array, read during the call only (a captured call keeps the addresses in its graph).  grad: device, `count` values of
+ *              dtype, aligned as their type; out: NULL for grad itself (in place, dtype), or count values of out_dtype.  Tensors of a call
+ *              do not overlap, an out and its own grad excepted, where they are the same.  count 0: skipped.
+ *   max_norm, eps   >= 0 (max_norm infinity: nothing is clipped).   norm, coef: device fp32 [1].
+ *   workspace  hq_grad_workspace_size bytes (the same for every call), 8-byte aligned; as above. */
+typedef struct {
+    const void* grad;
+    void* out;
+    int64_t count;
+    int32_t dtype, out_dtype;   /* hq_dtype */
+} hq_grad_tensor;
+hq_status hq_grad_workspace_size(size_t* bytes);
+hq_status hq_grad_norm(const hq_grad_tensor* tensors, int64_t n, float* norm, void* workspace, size_t ws_bytes, void* stream);
+hq_status hq_grad_clip(const hq_grad_tensor* tensors, int64_t n, float max_norm, float eps, float* norm, float* coef, void* workspace,
+                       size_t ws_bytes, void* stream);
+
 /* ---- Fused linear layer that allocates nothing and takes no workspace (the paper has no counterpart: this is a
  * packaging of hq_qlinear for a particular kind of caller, not another operation). ---------------------------------
  * Who it is for: code that must not, or cannot, obtain device memory at the moment it runs a layer -- an inference

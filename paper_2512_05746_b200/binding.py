@@ -19,6 +19,7 @@ HQ_OK = 0
 HQ_F32, HQ_BF16 = 0, 1
 HQ_CODES_NIBBLE, HQ_CODES_INT8 = 0, 1
 HQ_SCALE_PER_ROW, HQ_SCALE_STATIC = 0, 1
+HQ_NORM_LAYER, HQ_NORM_RMS, HQ_NORM_NONE = 0, 1, 2
 HQ_W_PLAIN, HQ_W_FOLDED, HQ_W_DOUBLE, HQ_W_PLAIN_A2 = 0, 1, 2, 3
 WEIGHT_MODES = {"plain": HQ_W_PLAIN, "folded": HQ_W_FOLDED, "double": HQ_W_DOUBLE, "plain_a2": HQ_W_PLAIN_A2}
 
@@ -30,7 +31,9 @@ EXPORTS = ["hq_version", "hq_status_string", "hq_check_status", "hq_hadamard_qua
            "hq_conv2d_direct", "hq_attention", "hq_hadamard_quant_width2", "hq_qlinear_fused", "hq_set_pair_gemm", "hq_mma_i8_probe_pair",
            "hq_hadamard_quant_cat", "hq_gn_silu_quant_cat", "hq_gn_silu_qconv_cat", "hq_qconv_cat",
            "hq_qlinear_add", "hq_gn_silu_qconv_add", "hq_qk_norm_rope", "hq_qk_norm_rope_bwd", "hq_qk_norm_rope_bwd_workspace_size",
-           "hq_attention_fwd", "hq_attention_fwd_workspace_size", "hq_attention_bwd", "hq_attention_bwd_workspace_size"]
+           "hq_attention_fwd", "hq_attention_fwd_workspace_size", "hq_attention_bwd", "hq_attention_bwd_workspace_size",
+           "hq_gate_norm", "hq_gate_norm_bwd", "hq_gate_norm_bwd_workspace_size", "hq_embedding", "hq_embedding_bwd",
+           "hq_embedding_bwd_workspace_size", "hq_grad_workspace_size", "hq_grad_norm", "hq_grad_clip"]
 HQ_NOALLOC_SCRATCH_BYTES = 8 * 1024 * 1024
 
 
@@ -117,6 +120,17 @@ def _load():
     L.hq_qk_norm_rope_bwd_workspace_size.argtypes = [i64, i32, i32, i32, C.POINTER(C.c_size_t)]
     L.hq_attention_fwd_workspace_size.argtypes = [i64, i64, i64, i32, i32, i32, C.POINTER(C.c_size_t)]
     L.hq_attention_bwd_workspace_size.argtypes = [i64, i64, i64, i32, i32, i32, C.POINTER(C.c_size_t)]
+    L.hq_gate_norm.argtypes = [p, i64, i32, p, i64, i32, i64, i64, i64, p, i32, p, p, i64, C.c_float, i32, p, i64, p, i64, C.c_float, C.c_float, p,
+                               i64, p, i64, p, p]
+    L.hq_gate_norm_bwd.argtypes = [p, i64, i32, p, i64, i32, p, i64, i64, i64, p, i32, p, p, i64, C.c_float, i32, p, i64, C.c_float, p, i64, p, i64,
+                                   p, i64, p, i64, p, p, i64, p, i64, p, i64, p, C.c_size_t, p]
+    L.hq_gate_norm_bwd_workspace_size.argtypes = [i64, i64, i64, C.POINTER(C.c_size_t)]
+    L.hq_embedding.argtypes = [p, i32, i64, p, i32, i64, i64, i64, C.c_float, p, i32, i64, p]
+    L.hq_embedding_bwd.argtypes = [p, i32, i64, p, i32, i64, i64, i64, C.c_float, p, i64, p, i32, i64, p, C.c_size_t, p]
+    L.hq_embedding_bwd_workspace_size.argtypes = [i64, i64, i64, C.POINTER(C.c_size_t)]
+    L.hq_grad_workspace_size.argtypes = [C.POINTER(C.c_size_t)]
+    L.hq_grad_norm.argtypes = [p, i64, p, p, C.c_size_t, p]
+    L.hq_grad_clip.argtypes = [p, i64, C.c_float, C.c_float, p, p, p, C.c_size_t, p]
     L.hq_alpha_for.restype = C.c_float
     L.hq_hadamard_quant_cat.argtypes = [p, i64, p, i64, i64, i32, i64, i64, i32, i32, i32, p, p, i32, i64, p, p]
     L.hq_gn_silu_quant_cat.argtypes = [p, p, i64, i32, i64, i64, i64, i64, i32, p, p, p, C.c_float, i32, i32, i32, p, p, i32,
@@ -134,7 +148,9 @@ def _load():
                  "hq_upsample_nearest2x", "hq_concat_channels", "hq_groupnorm_act", "hq_conv2d_direct", "hq_attention",
                  "hq_hadamard_quant_cat", "hq_gn_silu_quant_cat", "hq_gn_silu_qconv_cat", "hq_qconv_cat",
                  "hq_qlinear_add", "hq_gn_silu_qconv_add", "hq_qk_norm_rope", "hq_qk_norm_rope_bwd", "hq_qk_norm_rope_bwd_workspace_size",
-                 "hq_attention_fwd", "hq_attention_fwd_workspace_size", "hq_attention_bwd", "hq_attention_bwd_workspace_size"):
+                 "hq_attention_fwd", "hq_attention_fwd_workspace_size", "hq_attention_bwd", "hq_attention_bwd_workspace_size",
+                 "hq_gate_norm", "hq_gate_norm_bwd", "hq_gate_norm_bwd_workspace_size", "hq_embedding", "hq_embedding_bwd",
+                 "hq_embedding_bwd_workspace_size", "hq_grad_workspace_size", "hq_grad_norm", "hq_grad_clip"):
         getattr(L, name).restype = C.c_int
     return L
 
@@ -529,6 +545,8 @@ def _stream_and_device(stream):
         import torch
         _hqcall.bind_attention(torch.float32, torch.bfloat16, torch.int32, *(C.cast(getattr(lib, n), C.c_void_p).value for n in (
             "hq_qk_norm_rope", "hq_qk_norm_rope_bwd", "hq_attention_fwd", "hq_attention_bwd")))
+        _hqcall.bind_block(torch.int64, *(C.cast(getattr(lib, n), C.c_void_p).value for n in ("hq_gate_norm", "hq_gate_norm_bwd", "hq_embedding",
+                                                                                            "hq_embedding_bwd")))
         if not torch.cuda.is_available():
             return 0, -2
         _device_now = torch._C._cuda_getDevice
@@ -588,6 +606,160 @@ def hq_attention_bwd(q, k, v, out, lse, dout, Nb: int, heads: int, kv_heads: int
     at, device = _stream_and_device(stream)
     _check(_hqcall.attention_bwd(q, k, v, out, lse, dout, Nb, heads, kv_heads, dq, dk, dv, workspace, q_lens, k_lens, causal, scale, dev_status,
                                  at, device), "hq_attention_bwd")
+
+
+def hq_gate_norm(x, h, gate, weight, bias, x_out, y, stats=None, rows_per_group: int = 0, lens=None, post: int = HQ_NORM_NONE, post_weight=None,
+                 norm: int = HQ_NORM_LAYER, weight_plus: float = 0.0, residual_scale: float = 1.0, eps: float = 1e-6, stream=None) -> None:
+    """x_out = residual_scale * x + gate * t with t = h or norm(h) * post_weight, y = norm(x_out) * (weight_plus + weight) + bias: x, x_out
+    [rows, cols] (fp32 / bf16), h, y [rows, cols] (of either type); gate, weight, bias fp32 [groups, cols] ([cols] for one group; slices of
+    a modulation as they are) or None, one row for rows_per_group rows (0: one for all).  post, norm: HQ_NORM_*.  h None: a norm of x alone;
+    y None with norm HQ_NORM_NONE: the residual alone; x_out None: not wanted.  lens: int32 [groups], rows of each group that are there;
+    stats: fp32 [rows, 4], for the gradient.  x_out may be x, y may be h."""
+    at, device = _stream_and_device(stream)
+    _check(_hqcall.gate_norm(x, h, gate, weight, bias, x_out, y, stats, rows_per_group, lens, post, post_weight, norm, weight_plus, residual_scale,
+                             eps, at, device), "hq_gate_norm")
+
+
+def hq_gate_norm_bwd_workspace_size(rows: int, cols: int, rows_per_group: int = 0) -> int:
+    out = C.c_size_t(0)
+    _check(lib.hq_gate_norm_bwd_workspace_size(rows, cols, rows_per_group, C.byref(out)), "hq_gate_norm_bwd_workspace_size")
+    return int(out.value)
+
+
+def hq_gate_norm_bwd(x_out, h, stats, gate, weight, dx_out, dy, dx, dh, dgate, dweight, dbias, workspace, rows_per_group: int = 0, lens=None,
+                     post: int = HQ_NORM_NONE, post_weight=None, dpost_weight=None, norm: int = HQ_NORM_LAYER, weight_plus: float = 0.0,
+                     residual_scale: float = 1.0, stream=None) -> None:
+    """Gradients of hq_gate_norm: dx, dh and fp32 dgate, dweight, dbias [groups, cols], dpost_weight [cols] (each None: not wanted) from dx_out
+    and dy (None: none), its results x_out and stats and its input h (the other arguments as there).  dx may be dx_out, dh may be dy or h.
+    workspace: hq_gate_norm_bwd_workspace_size bytes on the device (None where no sum over rows is wanted)."""
+    at, device = _stream_and_device(stream)
+    _check(_hqcall.gate_norm_bwd(x_out, h, stats, gate, weight, dx_out, dy, dx, dh, dgate, dweight, dbias, workspace, rows_per_group, lens, post,
+                                 post_weight, dpost_weight, norm, weight_plus, residual_scale, at, device), "hq_gate_norm_bwd")
+
+
+def hq_embedding(ids, table, out, scale: float = 1.0, stream=None) -> None:
+    """out = scale * table[ids], zeros for ids outside the table: ids int32 / int64, dense, of any shape; table [classes, dim]; out [..., dim]
+    (fp32 / bf16 each; rows may be further apart where out has two dimensions)."""
+    at, device = _stream_and_device(stream)
+    if ids.dim() != 1 or out.dim() != 2:
+        if tuple(out.shape[:-1]) != tuple(ids.shape):
+            raise ValueError(f"hq_embedding: ids {tuple(ids.shape)} and rows {tuple(out.shape)}")
+        ids, out = ids.view(-1), out.view(-1, out.shape[-1])
+    _check(_hqcall.embedding(ids, table, out, scale, at, device), "hq_embedding")
+
+
+def hq_embedding_bwd_workspace_size(tokens: int, classes: int, dim: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib.hq_embedding_bwd_workspace_size(tokens, classes, dim, C.byref(out)), "hq_embedding_bwd_workspace_size")
+    return int(out.value)
+
+
+def hq_embedding_bwd(ids, dout, dtable, workspace, scale: float = 1.0, base=None, stream=None) -> None:
+    """dtable [classes, dim] = base + scale * the sums of dout's rows by id (ids and dout as ids and out of hq_embedding; base: a table of
+    dtable's type, dtable itself to add to what it holds, or None for zeros).  workspace: hq_embedding_bwd_workspace_size bytes."""
+    at, device = _stream_and_device(stream)
+    if ids.dim() != 1 or dout.dim() != 2:
+        if tuple(dout.shape[:-1]) != tuple(ids.shape):
+            raise ValueError(f"hq_embedding_bwd: ids {tuple(ids.shape)} and rows {tuple(dout.shape)}")
+        ids, dout = ids.view(-1), dout.view(-1, dout.shape[-1])
+    _check(_hqcall.embedding_bwd(ids, dout, dtable, workspace, scale, base, at, device), "hq_embedding_bwd")
+
+
+class _GradTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("count", C.c_int64), ("dtype", C.c_int32), ("out_dtype", C.c_int32)]
+
+
+def _is_dense(t) -> bool:
+    """Whether a tensor's elements fill one run of memory, in whatever order of its dimensions."""
+    size = 1
+    for stride, n in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != size:
+            return False
+        size *= n
+    return True
+
+
+class GradList:
+    """The gradients of a step (and, where they are written elsewhere, the tensors `outs` of the same shapes and strides, fp32 / bf16) as
+    hq_grad_norm and hq_grad_clip take them: checked and laid out once for tensors that stay where they are, which it keeps alive.
+    Gradients that get new memory (set to None between steps) need a new list."""
+
+    def __init__(self, grads, outs=None):
+        grads = [g.detach() for g in grads]
+        outs = None if outs is None else [o.detach() for o in outs]
+        if outs is not None and len(outs) != len(grads):
+            raise ValueError(f"GradList: {len(grads)} gradients and {len(outs)} outputs")
+        self.grads, self.outs, self.n = grads, outs, len(grads)
+        self.device = grads[0].get_device() if grads else None
+        self.table = (_GradTensor * max(1, self.n))()
+        spans = []                                 # (first byte, end, written, gradient)
+        for i, g in enumerate(grads):
+            o = g if outs is None else outs[i]
+            for t in (g, o):
+                if not t.is_cuda or t.get_device() != self.device:
+                    raise ValueError(f"GradList: tensor {i} is not on the CUDA device of the first")
+                if not _is_dense(t):
+                    raise ValueError(f"GradList: tensor {i} {tuple(t.shape)} with strides {t.stride()} is not dense")
+            if o.shape != g.shape or any(a != b for a, b, n in zip(o.stride(), g.stride(), g.shape) if n > 1 and g.numel() > 0):
+                raise ValueError(f"GradList: gradient {i} {tuple(g.shape)} {g.stride()} and its output {tuple(o.shape)} {o.stride()}")
+            same = o.data_ptr() == g.data_ptr() and o.dtype == g.dtype
+            self.table[i] = _GradTensor(g.data_ptr(), None if same else o.data_ptr(), g.numel(), _dtype_code(g), _dtype_code(o))
+            if g.numel():
+                spans.append((g.data_ptr(), g.data_ptr() + g.nbytes, same, i))
+                if not same:
+                    spans.append((o.data_ptr(), o.data_ptr() + o.nbytes, True, i))
+        reach, written = (0, None), (0, None)      # the furthest ends so far: of all, of those that are written
+        for first, end, write, i in sorted(spans, key=lambda s: s[:2]):
+            end_of, other = reach if write else written
+            if first < end_of:
+                raise ValueError(f"GradList: tensors {other} and {i} overlap")
+            reach = max(reach, (end, i), key=lambda e: e[0])
+            written = max(written, (end, i), key=lambda e: e[0]) if write else written
+
+
+def _grad_list(grads, what: str):
+    grads = grads if isinstance(grads, GradList) else GradList(grads)
+    at, device = _stream_and_device(None)
+    if grads.n and device != grads.device:
+        raise ValueError(f"{what}: the gradients are on CUDA device {grads.device}, the current one is {device}")
+    return grads, device
+
+
+def _scalar(t, name: str, what: str, device):
+    if t is None:
+        return None
+    import torch
+    if t.dtype != torch.float32 or t.numel() != 1 or t.get_device() != device:
+        raise ValueError(f"{what}: {name} is one fp32 value on the current CUDA device")
+    return t.data_ptr()
+
+
+def _bytes(workspace, what: str, device):
+    if not workspace.is_contiguous() or workspace.get_device() != device:
+        raise ValueError(f"{what}: workspace is a dense tensor on the current CUDA device")
+    return workspace.data_ptr(), workspace.nbytes
+
+
+def hq_grad_workspace_size() -> int:
+    out = C.c_size_t(0)
+    _check(lib.hq_grad_workspace_size(C.byref(out)), "hq_grad_workspace_size")
+    return int(out.value)
+
+
+def hq_grad_norm(grads, norm, workspace, stream=None) -> None:
+    """norm (one fp32 value on the device) = the norm of all gradients: a GradList, or the tensors themselves.  workspace:
+    hq_grad_workspace_size bytes."""
+    grads, device = _grad_list(grads, "hq_grad_norm")
+    _check(lib.hq_grad_norm(grads.table, grads.n, _scalar(norm, "norm", "hq_grad_norm", device), *_bytes(workspace, "hq_grad_norm", device),
+                            _stream(stream)), "hq_grad_norm")
+
+
+def hq_grad_clip(grads, max_norm: float, norm, workspace, eps: float = 1e-6, coef=None, stream=None) -> None:
+    """norm as hq_grad_norm; every gradient times coef = min(1, max_norm / (norm + eps)), in place or into the list's outs.  norm, coef (or
+    None): one fp32 value each on the device."""
+    grads, device = _grad_list(grads, "hq_grad_clip")
+    _check(lib.hq_grad_clip(grads.table, grads.n, max_norm, eps, _scalar(norm, "norm", "hq_grad_clip", device), _scalar(coef, "coef", "hq_grad_clip", device),
+                            *_bytes(workspace, "hq_grad_clip", device), _stream(stream)), "hq_grad_clip")
 
 
 def hq_qlinear_fused(x, pw: PreparedWeight, bias, a_bits: int, y, static_scale=None, dev_status=None, stream=None) -> None:

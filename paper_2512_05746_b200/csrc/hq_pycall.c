@@ -481,6 +481,194 @@ static PyObject* py_rope_bwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     return PyLong_FromLong(r);
 }
 
+/* ---- the gated residual with its norms, and the embedding: the same ---- */
+typedef hq_status (*gate_norm_fn)(const void*, int64_t, hq_dtype, const void*, int64_t, hq_dtype, int64_t, int64_t, int64_t, const int32_t*, hq_norm,
+                                  const float*, const float*, int64_t, float, hq_norm, const float*, int64_t, const float*, int64_t, float, float,
+                                  void*, int64_t, void*, int64_t, float*, void*);
+typedef hq_status (*gate_norm_bwd_fn)(const void*, int64_t, hq_dtype, const void*, int64_t, hq_dtype, const float*, int64_t, int64_t, int64_t,
+                                      const int32_t*, hq_norm, const float*, const float*, int64_t, float, hq_norm, const float*, int64_t, float,
+                                      const void*, int64_t, const void*, int64_t, void*, int64_t, void*, int64_t, float*, float*, int64_t, float*,
+                                      int64_t, float*, int64_t, void*, size_t, void*);
+typedef hq_status (*embedding_fn)(const void*, int, int64_t, const void*, hq_dtype, int64_t, int64_t, int64_t, float, void*, hq_dtype, int64_t, void*);
+typedef hq_status (*embedding_bwd_fn)(const void*, int, int64_t, const void*, hq_dtype, int64_t, int64_t, int64_t, float, const void*, int64_t, void*,
+                                      hq_dtype, int64_t, void*, size_t, void*);
+static gate_norm_fn f_gate_norm;
+static gate_norm_bwd_fn f_gate_norm_bwd;
+static embedding_fn f_embedding;
+static embedding_bwd_fn f_embedding_bwd;
+static PyObject *dt_i64;
+
+typedef struct { void* p; int64_t ld; } matrix;
+static int optional(const char* name, PyObject* t, PyObject* type, int64_t rows, int64_t width, int64_t device, matrix* m) {
+    m->p = NULL;
+    m->ld = width;
+    return t == Py_None ? 0 : heads_matrix(name, t, type, rows, width, device, &m->p, &m->ld);
+}
+/* [groups, cols] with contiguous columns, or [cols] where there is one group */
+static int vectors(const char* name, PyObject* t, int64_t groups, int64_t cols, int64_t device, matrix* m) {
+    if (t != Py_None && groups == 1) {
+        PyObject* s = PyObject_GetAttr(t, s_shape);
+        if (s == NULL) return -1;
+        const Py_ssize_t n = PyObject_Length(s);
+        Py_DECREF(s);
+        if (n < 0) return -1;
+        m->ld = cols;
+        if (n == 1) return dense(name, t, dt_f32, 1, cols, 0, 0, device, &m->p);
+    }
+    return optional(name, t, dt_f32, groups, cols, device, m);
+}
+static PyObject* first_of(PyObject* a, PyObject* b, PyObject* c) { return a != Py_None ? a : b != Py_None ? b : c; }
+static int real(PyObject* v, float* out) {
+    *out = (float)PyFloat_AsDouble(v);
+    return PyErr_Occurred() ? -1 : 0;
+}
+/* the types of both sides and the sizes: of the first matrix that is given */
+typedef struct { hq_dtype xdt, hdt; PyObject *xtype, *htype; int64_t rows, cols, per, groups; int post, norm; } norm_shape;
+static int norm_shape_of(PyObject* x, PyObject* h, PyObject* per, PyObject* post, PyObject* norm, norm_shape* s) {
+    int64_t dim[2];
+    PyObject* any = x != Py_None ? x : h;
+    if (any == Py_None) {
+        PyErr_SetString(PyExc_ValueError, "no matrix is given");
+        return -1;
+    }
+    if (shape(any, 2, dim) || integer(per, &s->per) || small(post, &s->post) || small(norm, &s->norm)) return -1;
+    if (dtype(any, &s->xdt)) return -1;
+    s->hdt = s->xdt;
+    if (h != Py_None && dtype(h, &s->hdt)) return -1;
+    s->xtype = s->xdt == HQ_F32 ? dt_f32 : dt_bf16;
+    s->htype = s->hdt == HQ_F32 ? dt_f32 : dt_bf16;
+    s->rows = dim[0];
+    s->cols = dim[1];
+    if (s->per < 0) {
+        PyErr_SetString(PyExc_ValueError, "rows_per_group: 0 or more");
+        return -1;
+    }
+    s->groups = s->per > 0 ? s->rows / s->per + (s->rows % s->per != 0) : 1;
+    return 0;
+}
+
+/* gate_norm(x, h, gate, weight, bias, x_out, y, stats, rows_per_group, lens, post, post_weight, norm, weight_plus, residual_scale, eps, stream, device) */
+static PyObject* py_gate_norm(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    (void)self;
+    norm_shape s;
+    matrix x, h, gate, weight, bias, x_out, y;
+    void *stats, *lens, *pw;
+    float plus, residual, eps;
+    int64_t stream, dev;
+    if (arguments(n, 18, f_gate_norm) || integer(a[16], &stream) || integer(a[17], &dev) || norm_shape_of(a[0], first_of(a[1], a[6], Py_None), a[8], a[10], a[12], &s) ||
+        real(a[13], &plus) || real(a[14], &residual) || real(a[15], &eps) || optional("x", a[0], s.xtype, s.rows, s.cols, dev, &x) ||
+        optional("h", a[1], s.htype, s.rows, s.cols, dev, &h) || vectors("gate", a[2], s.groups, s.cols, dev, &gate) ||
+        vectors("weight", a[3], s.groups, s.cols, dev, &weight) || vectors("bias", a[4], s.groups, s.cols, dev, &bias) ||
+        optional("x_out", a[5], s.xtype, s.rows, s.cols, dev, &x_out) || optional("y", a[6], s.htype, s.rows, s.cols, dev, &y) ||
+        dense("stats", a[7], dt_f32, 2, s.rows, 4, 0, dev, &stats) || dense("lens", a[9], dt_i32, 1, s.groups, 0, 0, dev, &lens) ||
+        dense("post_weight", a[11], dt_f32, 1, s.cols, 0, 0, dev, &pw))
+        return NULL;
+    hq_status r;
+    Py_BEGIN_ALLOW_THREADS
+    r = f_gate_norm(x.p, x.ld, s.xdt, h.p, h.ld, s.hdt, s.rows, s.cols, s.per, lens, (hq_norm)s.post, pw, gate.p, gate.ld, residual, (hq_norm)s.norm,
+                    weight.p, weight.ld, bias.p, bias.ld, plus, eps, x_out.p, x_out.ld, y.p, y.ld, stats, (void*)(intptr_t)stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(r);
+}
+
+/* gate_norm_bwd(x_out, h, stats, gate, weight, dx_out, dy, dx, dh, dgate, dweight, dbias, workspace, rows_per_group, lens, post, post_weight, dpost_weight,
+ *               norm, weight_plus, residual_scale, stream, device) */
+static PyObject* py_gate_norm_bwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    (void)self;
+    norm_shape s;
+    matrix x, h, gate, weight, dxo, dy, dx, dh, dgate, dweight, dbias;
+    void *stats, *lens, *pw, *dpw, *ws;
+    size_t ws_bytes;
+    float plus, residual;
+    int64_t stream, dev;
+    if (arguments(n, 23, f_gate_norm_bwd) || integer(a[21], &stream) || integer(a[22], &dev) ||
+        norm_shape_of(first_of(a[0], a[5], a[7]), first_of(a[1], a[6], a[8]), a[13], a[15], a[18], &s) || real(a[19], &plus) || real(a[20], &residual) ||
+        optional("x_out", a[0], s.xtype, s.rows, s.cols, dev, &x) || optional("h", a[1], s.htype, s.rows, s.cols, dev, &h) ||
+        dense("stats", a[2], dt_f32, 2, s.rows, 4, 0, dev, &stats) || vectors("gate", a[3], s.groups, s.cols, dev, &gate) ||
+        vectors("weight", a[4], s.groups, s.cols, dev, &weight) || optional("dx_out", a[5], s.xtype, s.rows, s.cols, dev, &dxo) ||
+        optional("dy", a[6], s.htype, s.rows, s.cols, dev, &dy) || optional("dx", a[7], s.xtype, s.rows, s.cols, dev, &dx) ||
+        optional("dh", a[8], s.htype, s.rows, s.cols, dev, &dh) || vectors("dgate", a[9], s.groups, s.cols, dev, &dgate) ||
+        vectors("dweight", a[10], s.groups, s.cols, dev, &dweight) || vectors("dbias", a[11], s.groups, s.cols, dev, &dbias) ||
+        workspace_of(a[12], dev, &ws, &ws_bytes) || dense("lens", a[14], dt_i32, 1, s.groups, 0, 0, dev, &lens) ||
+        dense("post_weight", a[16], dt_f32, 1, s.cols, 0, 0, dev, &pw) || dense("dpost_weight", a[17], dt_f32, 1, s.cols, 0, 0, dev, &dpw))
+        return NULL;
+    hq_status r;
+    Py_BEGIN_ALLOW_THREADS
+    r = f_gate_norm_bwd(x.p, x.ld, s.xdt, h.p, h.ld, s.hdt, stats, s.rows, s.cols, s.per, lens, (hq_norm)s.post, pw, gate.p, gate.ld, residual,
+                        (hq_norm)s.norm, weight.p, weight.ld, plus, dxo.p, dxo.ld, dy.p, dy.ld, dx.p, dx.ld, dh.p, dh.ld, dpw, dgate.p, dgate.ld, dweight.p,
+                        dweight.ld, dbias.p, dbias.ld, ws, ws_bytes, (void*)(intptr_t)stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(r);
+}
+
+/* dense ids of 32 or 64 bits */
+static int ids_of(PyObject* t, int64_t tokens, int64_t dev, void** p, int* bytes) {
+    PyObject* d = PyObject_GetAttr(t, s_dtype);
+    if (d == NULL) return -1;
+    const int wide = d == dt_i64;
+    Py_DECREF(d);
+    *bytes = wide ? 8 : 4;
+    return dense("ids", t, wide ? dt_i64 : dt_i32, 1, tokens, 0, 0, dev, p);
+}
+/* embedding(ids, table, out, scale, stream, device) */
+static PyObject* py_embedding(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    (void)self;
+    int64_t rows[2], tab[2], stream, dev;
+    matrix table, out;
+    void* ids;
+    float scale;
+    hq_dtype tdt, odt;
+    int bytes;
+    if (arguments(n, 6, f_embedding) || integer(a[4], &stream) || integer(a[5], &dev) || shape(a[2], 2, rows) || shape(a[1], 2, tab) || real(a[3], &scale) ||
+        dtype(a[1], &tdt) || dtype(a[2], &odt) || ids_of(a[0], rows[0], dev, &ids, &bytes) ||
+        optional("table", a[1], tdt == HQ_F32 ? dt_f32 : dt_bf16, tab[0], tab[1], dev, &table) ||
+        optional("out", a[2], odt == HQ_F32 ? dt_f32 : dt_bf16, rows[0], tab[1], dev, &out))
+        return NULL;
+    hq_status r;
+    Py_BEGIN_ALLOW_THREADS
+    r = f_embedding(ids, bytes, rows[0], table.p, tdt, tab[0], tab[1], table.ld, scale, out.p, odt, out.ld, (void*)(intptr_t)stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(r);
+}
+/* embedding_bwd(ids, dout, dtable, workspace, scale, base, stream, device) */
+static PyObject* py_embedding_bwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    (void)self;
+    int64_t rows[2], tab[2], stream, dev;
+    matrix dout, base, dtable;
+    void *ids, *ws;
+    size_t ws_bytes;
+    float scale;
+    hq_dtype ddt, gdt;
+    int bytes;
+    if (arguments(n, 8, f_embedding_bwd) || integer(a[6], &stream) || integer(a[7], &dev) || shape(a[1], 2, rows) || shape(a[2], 2, tab) || real(a[4], &scale) ||
+        dtype(a[1], &ddt) || dtype(a[2], &gdt) || ids_of(a[0], rows[0], dev, &ids, &bytes) ||
+        optional("dout", a[1], ddt == HQ_F32 ? dt_f32 : dt_bf16, rows[0], tab[1], dev, &dout) ||
+        optional("base", a[5], gdt == HQ_F32 ? dt_f32 : dt_bf16, tab[0], tab[1], dev, &base) ||
+        optional("dtable", a[2], gdt == HQ_F32 ? dt_f32 : dt_bf16, tab[0], tab[1], dev, &dtable) || workspace_of(a[3], dev, &ws, &ws_bytes))
+        return NULL;
+    hq_status r;
+    Py_BEGIN_ALLOW_THREADS
+    r = f_embedding_bwd(ids, bytes, rows[0], dout.p, ddt, dout.ld, tab[0], tab[1], scale, base.p, base.ld, dtable.p, gdt, dtable.ld, ws, ws_bytes,
+                        (void*)(intptr_t)stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(r);
+}
+
+/* bind_block(int64, gate_norm, gate_norm_bwd, embedding, embedding_bwd), behind bind_attention */
+static PyObject* py_bind_block(PyObject* self, PyObject* args) {
+    (void)self;
+    PyObject* d;
+    unsigned long long p[4];
+    if (!PyArg_ParseTuple(args, "OKKKK", &d, &p[0], &p[1], &p[2], &p[3])) return NULL;
+    Py_INCREF(d);
+    Py_XSETREF(dt_i64, d);
+    f_gate_norm = (gate_norm_fn)(uintptr_t)p[0];
+    f_gate_norm_bwd = (gate_norm_bwd_fn)(uintptr_t)p[1];
+    f_embedding = (embedding_fn)(uintptr_t)p[2];
+    f_embedding_bwd = (embedding_bwd_fn)(uintptr_t)p[3];
+    Py_RETURN_NONE;
+}
+
 /* bind_attention(float32, bfloat16, int32, qk_rope, qk_rope_bwd, attention_fwd, attention_bwd): torch's types and the entry points' addresses */
 static PyObject* py_bind_attention(PyObject* self, PyObject* args) {
     (void)self;
@@ -504,6 +692,11 @@ static PyMethodDef methods[] = {
     {"qk_rope_bwd", (PyCFunction)(void (*)(void))py_rope_bwd, METH_FASTCALL, NULL},
     {"attention_fwd", (PyCFunction)(void (*)(void))py_attn_fwd, METH_FASTCALL, NULL},
     {"attention_bwd", (PyCFunction)(void (*)(void))py_attn_bwd, METH_FASTCALL, NULL},
+    {"bind_block", py_bind_block, METH_VARARGS, NULL},
+    {"gate_norm", (PyCFunction)(void (*)(void))py_gate_norm, METH_FASTCALL, NULL},
+    {"gate_norm_bwd", (PyCFunction)(void (*)(void))py_gate_norm_bwd, METH_FASTCALL, NULL},
+    {"embedding", (PyCFunction)(void (*)(void))py_embedding, METH_FASTCALL, NULL},
+    {"embedding_bwd", (PyCFunction)(void (*)(void))py_embedding_bwd, METH_FASTCALL, NULL},
     {"bind", py_bind, METH_VARARGS, NULL},
     {"qlinear", (PyCFunction)(void (*)(void))py_qlinear, METH_FASTCALL, NULL},
     {"qconv", (PyCFunction)(void (*)(void))py_qconv, METH_FASTCALL, NULL},
