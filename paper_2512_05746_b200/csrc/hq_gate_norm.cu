@@ -11,8 +11,9 @@
 //   dgate[n] = sum d t,  dweight[n] = sum dy xh,  dbias[n] = sum dy,  dpost_weight = sum gate d hh over all rows
 //
 // Memory-bound: every row is read and written once, the vectors come from the caches once for a run of rows.  A team of ceil(cols / 256)
-// warps holds a row, 8 values a thread, so that the rows' sums are shuffles and one exchange through shared memory, and the sums over rows
-// stay in the registers of the thread that owns the columns.
+// warps takes a run of rows, 8 columns a thread.  Rows are copied ahead into shared memory, by each thread for itself (no barrier stands
+// between the copy and its use, and no register holds what is on the way); two rows are computed together, so that their sums share the
+// shuffles; sums over rows stay in the registers of the thread that owns the columns.
 #include "hq_common.cuh"
 #include "hq_vec8.cuh"
 
@@ -29,8 +30,7 @@ struct Vectors { const float* p; int64_t ld; };    // [groups][cols]
 struct VectorsOut { float* p; int64_t ld; };
 
 struct GateNormParams {
-    int64_t rows, group;                           // group: rows that share their vectors
-    int64_t chunk;                                 // rows of a team (forward), of a CTA (gradient)
+    uint32_t rows, group, chunk;                   // group: rows that share their vectors; chunk: rows of a team
     int cols, warps;                               // warps of a team
     int layer, post_layer;                         // the norms' kind: 1 with a mean
     const int32_t* lens;                           // [groups] rows that are there, or NULL
@@ -43,454 +43,516 @@ struct GateNormParams {
     Matrix dx_out, dy;
     MatrixOut dx, dh;
     VectorsOut dgate, dweight, dbias;
-    float *dpost, *parts, *post_parts;             // parts: [CTAs][first, last segment][weight, bias, gate][cols]; post_parts: [CTAs][cols]
+    float *dpost, *parts, *post_parts;             // parts: [teams][first, last group][weight, bias, gate][cols]; post_parts: [teams][cols]
 };
 
-// Rows [row, row + n) of one group, the first `live` of them within its length.
-struct Batch { int64_t row, g; int n, live; };
-__device__ __forceinline__ Batch batch_at(const GateNormParams& p, int64_t row, int64_t g, int64_t end) {
-    const int64_t first = g * p.group, last = min(first + p.group, end);
-    Batch b{row, g, 0, 0};
-    if (row < last) {
-        b.n = int(min(int64_t(kRows), last - row));
-        b.live = b.n;
-        if (p.lens != nullptr) b.live = int(min(max(first + p.lens[g] - row, int64_t(0)), int64_t(b.n)));
+// ---- a team's walk over its rows ----
+
+// Rows [row, row + n) of group g, the first `live` of them within its length.
+struct Walk {
+    uint32_t row, g, group_end, live_end;          // first row behind the group, and behind its length
+    int n, live;
+    __device__ __forceinline__ void count(uint32_t end) {
+        n = row < end ? int(min(uint32_t(kRows), min(group_end, end) - row)) : 0;
+        live = row < live_end ? min(n, int(min(uint32_t(kRows), live_end - row))) : 0;
     }
-    return b;
+    __device__ __forceinline__ void enter(const GateNormParams& p, uint32_t first, uint32_t end) {       // the group that begins at `first`
+        group_end = p.rows - first > p.group ? first + p.group : p.rows;
+        live_end = group_end;
+        if (p.lens != nullptr && first < end) live_end = min(group_end, first + uint32_t(max(p.lens[g], 0)));
+    }
+    __device__ __forceinline__ void start(const GateNormParams& p, uint32_t at, uint32_t end) {
+        row = at;
+        g = at / p.group;
+        enter(p, g * p.group, end);
+        count(end);
+    }
+    __device__ __forceinline__ void next(const GateNormParams& p, uint32_t end) {
+        row += uint32_t(n);
+        if (row == group_end) { ++g; enter(p, row, end); }
+        count(end);
+    }
+};
+
+// ---- a team, and its exchange of sums: two buffers in turn, so that one barrier stands between the writes and the reads of an exchange and
+// none behind it.  Teams of several warps are CTAs of their own, teams of one warp need no barrier. ----
+struct Team {
+    int lane, warp, warps, c0;
+    bool col;                                      // the thread has columns
+    float share, per_warp, per_row;                // columns of warp (lane & 15); 1 / columns of this warp, of the row
+    float2* room;                                  // [2][32]
+    int turn;
+};
+__device__ __forceinline__ Team team_of(const GateNormParams& p, float2* room) {
+    Team t;
+    t.lane = int(threadIdx.x & 31);
+    t.warps = p.warps;
+    t.warp = p.warps == 1 ? 0 : int(threadIdx.x >> 5);
+    t.c0 = (t.warp * 32 + t.lane) * 8;
+    t.col = t.c0 < p.cols;
+    t.share = float(max(0, min(256, p.cols - (t.lane & 15) * 256)));
+    t.per_warp = 1.f / float(min(256, p.cols - t.warp * 256));
+    t.per_row = 1.f / float(p.cols);
+    t.room = room;
+    t.turn = 0;
+    return t;
+}
+__device__ __forceinline__ uint32_t team_index(const GateNormParams& p) {
+    return p.warps == 1 ? blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
+}
+__device__ __forceinline__ float sum8(const f32x2 (&v)[4]) { return pair_sum(add2(add2(v[0], v[1]), add2(v[2], v[3]))); }
+__device__ __forceinline__ float xor_add(float x, int off) { return x + __shfl_xor_sync(0xffffffffu, x, off); }
+__device__ __forceinline__ float from_lane(float x, int lane) { return __shfl_sync(0xffffffffu, x, lane); }
+// Two values' sums over the warp: lanes 0 .. 15 have the first's, lanes 16 .. 31 the second's.
+__device__ __forceinline__ float sum_of_two(float a, float b, int lane) {
+    const bool low = lane < 16;
+    float s = (low ? a : b) + __shfl_xor_sync(0xffffffffu, low ? b : a, 16);
+    s = xor_add(s, 8); s = xor_add(s, 4); s = xor_add(s, 2);
+    return xor_add(s, 1);
 }
 
+// The sums of a pair of values of each of two rows over the team.
+__device__ __forceinline__ void team_sums(Team& t, float2& a, float2& b) {
+    const bool low = t.lane < 16, left = (t.lane & 8) == 0;
+    const float2 mine = low ? a : b, other = low ? b : a;
+    const float x = mine.x + __shfl_xor_sync(0xffffffffu, other.x, 16), y = mine.y + __shfl_xor_sync(0xffffffffu, other.y, 16);
+    float s = (left ? x : y) + __shfl_xor_sync(0xffffffffu, left ? y : x, 8);                // eight lanes a value: a.x, a.y, b.x, b.y
+    s = xor_add(s, 4); s = xor_add(s, 2); s = xor_add(s, 1);
+    if (t.warps > 1) {
+        float* room = reinterpret_cast<float*>(t.room + t.turn * 32);                        // [4][kMaxWarps]
+        t.turn ^= 1;
+        if ((t.lane & 7) == 0) room[(t.lane >> 3) * kMaxWarps + t.warp] = s;
+        __syncthreads();
+        const int w = t.lane & 7, from = (t.lane >> 3) * kMaxWarps + w;
+        s = w < t.warps ? room[from] : 0.f;
+        if (w + 8 < t.warps) s += room[from + 8];
+        s = xor_add(s, 4); s = xor_add(s, 2); s = xor_add(s, 1);
+    }
+    a = make_float2(from_lane(s, 0), from_lane(s, 8));
+    b = make_float2(from_lane(s, 16), from_lane(s, 24));
+}
+
+// Mean (0 unless `layer`) and 1 / standard deviation of both rows.  A warp takes the mean of its own values first and its squares about
+// that, and the warps' parts are joined about the row's mean: no difference of large sums, and one exchange.
+__device__ __forceinline__ void moments(Team& t, const f32x2 (&v)[kRows][4], int layer, float eps, float (&mean)[kRows], float (&inv)[kRows]) {
+    float m = 0.f;                                 // of row lane / 16
+    mean[0] = mean[1] = 0.f;
+    if (layer) {
+        m = sum_of_two(t.col ? sum8(v[0]) : 0.f, t.col ? sum8(v[1]) : 0.f, t.lane) * t.per_warp;
+        mean[0] = from_lane(m, 0);
+        mean[1] = from_lane(m, 16);
+    }
+    float q[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const f32x2 less = pk2(-mean[i], -mean[i]);
+        f32x2 sq = pk2(0.f, 0.f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { const f32x2 d = add2(v[i][e], less); sq = fma2(d, d, sq); }
+        q[i] = t.col ? pair_sum(sq) : 0.f;
+    }
+    float m2 = sum_of_two(q[0], q[1], t.lane);
+    if (t.warps > 1) {
+        float2* room = t.room + t.turn * 32;       // [kRows][kMaxWarps]
+        t.turn ^= 1;
+        if ((t.lane & 15) == 0) room[t.lane + t.warp] = make_float2(m, m2);
+        __syncthreads();
+        const float2 o = (t.lane & 15) < t.warps ? room[t.lane] : make_float2(0.f, 0.f);
+        m = 0.f;
+        if (layer) {
+            m = t.share * o.x;
+            m = xor_add(m, 8); m = xor_add(m, 4); m = xor_add(m, 2);
+            m = xor_add(m, 1) * t.per_row;
+            mean[0] = from_lane(m, 0);
+            mean[1] = from_lane(m, 16);
+        }
+        m2 = o.y + t.share * ((o.x - m) * (o.x - m));
+        m2 = xor_add(m2, 8); m2 = xor_add(m2, 4); m2 = xor_add(m2, 2);
+        m2 = xor_add(m2, 1);
+    }
+    m2 = rsqrtf(m2 * t.per_row + eps);
+    inv[0] = from_lane(m2, 0);
+    inv[1] = from_lane(m2, 16);
+}
+
+// ---- vectors of a thread's columns ----
 __device__ __forceinline__ void fill(f32x2 (&v)[4], float x) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = pk2(x, x);
 }
 // A group's values for this thread's columns, plus `add`; `none` without a vector.
-__device__ __forceinline__ void load_vector(f32x2 (&v)[4], const Vectors& from, int64_t g, int c0, bool col, float add, float none) {
-    if (from.p == nullptr || !col) { fill(v, none); return; }
-    const float4* q = reinterpret_cast<const float4*>(from.p + g * from.ld + c0);
+__device__ __forceinline__ void load_vector(f32x2 (&v)[4], const Vectors& from, uint32_t g, const Team& t, float add, float none) {
+    if (from.p == nullptr || !t.col) { fill(v, none); return; }
+    const float4* q = reinterpret_cast<const float4*>(from.p + int64_t(g) * from.ld + t.c0);
     const float4 a = q[0], b = q[1];
     v[0] = pk2(a.x + add, a.y + add); v[1] = pk2(a.z + add, a.w + add); v[2] = pk2(b.x + add, b.y + add); v[3] = pk2(b.z + add, b.w + add);
 }
-__device__ __forceinline__ void store_vector(float* to, const f32x2 (&v)[4]) {
-    float4 a, b;
-    upk2(v[0], a.x, a.y); upk2(v[1], a.z, a.w); upk2(v[2], b.x, b.y); upk2(v[3], b.z, b.w);
-    reinterpret_cast<float4*>(to)[0] = a;
-    reinterpret_cast<float4*>(to)[1] = b;
-}
 
-// A thread's place: lane, warp of its team, its 8 columns; and the team's exchange of sums, two buffers in turn, so that one barrier
-// stands between the writes and the reads of an exchange and none behind it.
-struct Team {
-    int lane, warp, warps, id, c0, cols;
-    bool col;
-    float2* room;                                  // [2][kRows][kMaxWarps], this team's warps first
-    int turn;
-    __device__ __forceinline__ void sync() const {
-        if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "r"(warps * 32) : "memory");
-        else __syncwarp();
-    }
-};
-__device__ __forceinline__ Team team_of(const GateNormParams& p, float2* room) {
-    Team t;
-    const int warp = int(threadIdx.x >> 5);
-    t.lane = int(threadIdx.x & 31);
-    t.warps = p.warps;
-    t.id = warp / p.warps;
-    t.warp = warp - t.id * p.warps;
-    t.c0 = (t.warp * 32 + t.lane) * 8;
-    t.cols = p.cols;
-    t.col = t.c0 < p.cols;
-    t.room = room + t.id * p.warps;
-    t.turn = 0;
-    return t;
+// ---- rows on their way through shared memory: each thread's own 16 or 32 bytes of a row, in planes of 16 bytes a thread ----
+template <typename T> constexpr int kPlanes = int(sizeof(T)) * 8 / 16;
+__device__ __forceinline__ void copy_ahead(uint32_t to, const void* from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ float warp_sum(float x) {
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
-    return x;
-}
-__device__ __forceinline__ float sum8(const f32x2 (&v)[4]) { return pair_sum(add2(add2(v[0], v[1]), add2(v[2], v[3]))); }
-
-// Two sums of every row over the team.
-__device__ __forceinline__ void team_sums(Team& t, float2 (&s)[kRows]) {
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) s[i] = make_float2(warp_sum(s[i].x), warp_sum(s[i].y));
-    if (t.warps == 1) return;
-    float2* room = t.room + t.turn * kRows * kMaxWarps;
-    t.turn ^= 1;
-    if (t.lane == 0) {
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) room[i * kMaxWarps + t.warp] = s[i];
-    }
-    t.sync();
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        float2 a = make_float2(0.f, 0.f);
-        for (int w = 0; w < t.warps; ++w) {
-            const float2 o = room[i * kMaxWarps + w];
-            a.x += o.x; a.y += o.y;
-        }
-        s[i] = a;
-    }
-}
-
-// Mean (0 unless `layer`) and 1 / standard deviation of every row.  A warp takes the mean of its own values first and its squares about
-// that, and the warps' parts are joined about the row's mean: no difference of large sums, and one exchange.
-__device__ __forceinline__ void moments(Team& t, const f32x2 (&v)[kRows][4], int layer, float eps, float (&mean)[kRows], float (&inv)[kRows]) {
-    const float mine = float(min(256, t.cols - t.warp * 256)), all = float(t.cols);
-    float q[kRows];
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) mean[i] = layer ? warp_sum(t.col ? sum8(v[i]) : 0.f) / mine : 0.f;
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const f32x2 m = pk2(-mean[i], -mean[i]);
-        f32x2 sq = pk2(0.f, 0.f);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { const f32x2 d = add2(v[i][e], m); sq = fma2(d, d, sq); }
-        q[i] = warp_sum(t.col ? pair_sum(sq) : 0.f);
-    }
-    if (t.warps > 1) {
-        float2* room = t.room + t.turn * kRows * kMaxWarps;
-        t.turn ^= 1;
-        if (t.lane == 0) {
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) room[i * kMaxWarps + t.warp] = make_float2(mean[i], q[i]);
-        }
-        t.sync();
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            float sum = 0.f, m2 = 0.f;
-            for (int w = 0; w < t.warps; ++w) sum += room[i * kMaxWarps + w].x * float(min(256, t.cols - w * 256));
-            const float m = sum / all;
-            for (int w = 0; w < t.warps; ++w) {
-                const float2 o = room[i * kMaxWarps + w];
-                m2 += o.y + float(min(256, t.cols - w * 256)) * ((o.x - m) * (o.x - m));
-            }
-            mean[i] = m;
-            q[i] = m2;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) inv[i] = rsqrtf(q[i] / all + eps);
-}
-
+__device__ __forceinline__ void copies_sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// `at`: this thread's place in the batch's first plane; zeros for rows that are not there.
 template <typename T>
-__device__ __forceinline__ void request(Vec8<T> (&v)[kRows], const Matrix& m, const Batch& b, const Team& t) {
+__device__ __forceinline__ void send(uint32_t at, const Matrix& m, const Walk& b, const Team& t) {
+    const uint32_t plane = blockDim.x * 16u;
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-        v[i].clear();
-        if (i < b.live && t.col) v[i].load(m.p, (b.row + i) * m.ld + t.c0);
+        const bool there = i < b.live && t.col;
+        const T* from = static_cast<const T*>(m.p) + (there ? int64_t(b.row + i) * m.ld + t.c0 : 0);
+#pragma unroll
+        for (int k = 0; k < kPlanes<T>; ++k) copy_ahead(at + uint32_t(i * kPlanes<T> + k) * plane, from + k * (16 / int(sizeof(T))), there);
     }
 }
+__device__ __forceinline__ uint4 plane_at(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void take(f32x2 (&v)[4], uint32_t at, int i) {
+    const uint32_t plane = blockDim.x * 16u;
+    Vec8<T> raw;
+    if constexpr (sizeof(T) == 2) {
+        raw.w = plane_at(at + uint32_t(i) * plane);
+    } else {
+        const uint4 a = plane_at(at + uint32_t(2 * i) * plane), b = plane_at(at + uint32_t(2 * i + 1) * plane);
+        raw.a = make_float4(__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w));
+        raw.b = make_float4(__uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w));
+    }
+    raw.get(v);
+}
+template <typename T>
+__device__ __forceinline__ void put(const MatrixOut& m, const Walk& b, int i, const Team& t, f32x2 (&v)[4]) {
+    if (i >= b.live) fill(v, 0.f);
+    if (i < b.n && t.col) Vec8<T>::store(m.p, int64_t(b.row + i) * m.ld + t.c0, v);
+}
+
+// Batches on their way: what keeps about 40 KB an SM in flight at 15 warps and more.
+template <typename S, typename B> constexpr int kForwardPlanes = kRows * (kPlanes<S> + kPlanes<B>);
+template <typename S, typename B> constexpr int kGradPlanes = 2 * kForwardPlanes<S, B>;
+constexpr int kForwardStages = 3, kGradStages = 2;
+constexpr size_t kMostShared = 224 * 1024;
 
 // S: type of x and x', B: of h and y.
 template <typename S, typename B, bool POST>
-__global__ void __launch_bounds__(kMaxWarps * 32) gate_norm_kernel(const GateNormParams p) {
-    __shared__ float2 room[2 * kRows * kMaxWarps];
+__global__ void __maxnreg__(96) gate_norm_kernel(const GateNormParams p) {
+    extern __shared__ uint4 ring[];
+    __shared__ float2 room[2 * 32];
+    constexpr int kStages = kForwardStages;
     Team t = team_of(p, room);
-    const int teams = int(blockDim.x >> 5) / p.warps;
-    const int64_t r0 = (int64_t(blockIdx.x) * teams + t.id) * p.chunk, r1 = min(r0 + p.chunk, p.rows);
+    const uint32_t r0 = team_index(p) * p.chunk, r1 = min(r0 + p.chunk, p.rows);
     if (r0 >= r1) return;
-    Batch b = batch_at(p, r0, r0 / p.group, r1);
+    const uint32_t plane = blockDim.x * 16u, batch = plane * kForwardPlanes<S, B>, h_at = plane * kRows * kPlanes<S>;
+    const uint32_t base = smem_u32(ring) + threadIdx.x * 16u;
+    const bool branch = p.h.p != nullptr, normed = p.y.p != nullptr;
+    Walk b, ahead;
+    b.start(p, r0, r1);
+    ahead = b;
+    uint32_t to = base;
+    auto send_next = [&]() {
+        if (ahead.n > 0) {
+            send<S>(to, p.x, ahead, t);
+            if (branch) send<B>(to + h_at, p.h, ahead, t);
+            ahead.next(p, r1);
+        }
+        copies_sent();
+        to = to == base + (kStages - 1) * batch ? base : to + batch;
+    };
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) send_next();
     f32x2 gate[4], weight[4], bias[4], post_weight[4];
-    if (POST) load_vector(post_weight, Vectors{p.post_weight, 0}, 0, t.c0, t.col, 0.f, 1.f);
-    int64_t loaded = -1;
-    Vec8<S> x_in[kRows];
-    Vec8<B> h_in[kRows];
-    request(x_in, p.x, b, t);
-    if (p.h.p != nullptr) request(h_in, p.h, b, t);
+    if (POST) load_vector(post_weight, Vectors{p.post_weight, 0}, 0, t, 0.f, 1.f);
+    uint32_t loaded = 0xffffffffu, at = base;
     while (b.n > 0) {
         if (b.g != loaded) {
-            load_vector(gate, p.gate, b.g, t.c0, t.col, 0.f, 1.f);
-            if (p.y.p != nullptr) {
-                load_vector(weight, p.weight, b.g, t.c0, t.col, p.plus, 1.f);
-                load_vector(bias, p.bias, b.g, t.c0, t.col, 0.f, 0.f);
+            load_vector(gate, p.gate, b.g, t, 0.f, 1.f);
+            if (normed) {
+                load_vector(weight, p.weight, b.g, t, p.plus, 1.f);
+                load_vector(bias, p.bias, b.g, t, 0.f, 0.f);
             }
             loaded = b.g;
         }
-        const int64_t next_row = b.row + b.n;
-        const Batch next = batch_at(p, next_row, b.g + (next_row == (b.g + 1) * p.group), r1);
-        f32x2 v[kRows][4], u[kRows][4];
+        copies_wait<kStages - 2>();
+        f32x2 v[kRows][4];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) x_in[i].get(v[i]);
-        request(x_in, p.x, next, t);                           // in flight while this batch is computed
-        float mean[kRows], inv[kRows], post_mean[kRows], post_inv[kRows];
+        for (int i = 0; i < kRows; ++i) take<S>(v[i], at, i);
+        float mean[kRows] = {0.f, 0.f}, inv[kRows] = {1.f, 1.f}, post_mean[kRows] = {0.f, 0.f}, post_inv[kRows] = {1.f, 1.f};
+        if (branch) {
+            f32x2 u[kRows][4];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) { mean[i] = 0.f; inv[i] = 1.f; post_mean[i] = 0.f; post_inv[i] = 1.f; }
-        if (p.h.p != nullptr) {
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) h_in[i].get(u[i]);
-            request(h_in, p.h, next, t);
+            for (int i = 0; i < kRows; ++i) take<B>(u[i], at + h_at, i);
             if (POST) moments(t, u, p.post_layer, p.eps, post_mean, post_inv);
             const f32x2 residual = pk2(p.residual, p.residual);
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
-                const f32x2 m = pk2(-post_mean[i], -post_mean[i]), s = pk2(post_inv[i], post_inv[i]);
+                const f32x2 less = pk2(-post_mean[i], -post_mean[i]), s = pk2(post_inv[i], post_inv[i]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if (POST) u[i][e] = mul2(mul2(add2(u[i][e], m), s), post_weight[e]);
+                    if (POST) u[i][e] = mul2(mul2(add2(u[i][e], less), s), post_weight[e]);
                     v[i][e] = fma2(residual, v[i][e], mul2(gate[e], u[i][e]));
                 }
             }
         }
+        send_next();                               // into the place of the batch before this one
+        at = at == base + (kStages - 1) * batch ? base : at + batch;
         if (p.x_out.p != nullptr) {
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                if (i >= b.live) fill(v[i], 0.f);
-                if (i < b.n && t.col) Vec8<S>::store(p.x_out.p, (b.row + i) * p.x_out.ld + t.c0, v[i]);
-            }
+            for (int i = 0; i < kRows; ++i) put<S>(p.x_out, b, i, t, v[i]);
         }
-        if (p.y.p != nullptr) {
+        if (normed) {
             moments(t, v, p.layer, p.eps, mean, inv);
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
-                const f32x2 m = pk2(-mean[i], -mean[i]), s = pk2(inv[i], inv[i]);
+                const f32x2 less = pk2(-mean[i], -mean[i]), s = pk2(inv[i], inv[i]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[i][e] = fma2(mul2(add2(v[i][e], m), s), weight[e], bias[e]);
-                if (i >= b.live) fill(v[i], 0.f);
-                if (i < b.n && t.col) Vec8<B>::store(p.y.p, (b.row + i) * p.y.ld + t.c0, v[i]);
+                for (int e = 0; e < 4; ++e) v[i][e] = fma2(mul2(add2(v[i][e], less), s), weight[e], bias[e]);
+                put<B>(p.y, b, i, t, v[i]);
             }
         }
-        if (p.stats != nullptr && t.warp == 0 && t.lane == 0) {
+        if (p.stats != nullptr && t.c0 == 0) {
 #pragma unroll
             for (int i = 0; i < kRows; ++i)
                 if (i < b.n)
                     reinterpret_cast<float4*>(p.stats)[b.row + i] = i < b.live ? make_float4(mean[i], inv[i], post_mean[i], post_inv[i])
                                                                                : make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        b = next;
+        b.next(p, r1);
     }
 }
 
-// A CTA takes `chunk` rows, its teams their batches in turn.  Where a group ends (and behind the last row) the teams' sums over the group's
-// rows are joined in order and leave: to the gradient itself where the whole group lay in this CTA, else to the CTA's part (the first of its
-// two for the group that its first row belongs to, else the second), which gate_norm_sums_kernel joins.
-template <typename S, typename B, bool POST>
-__global__ void __launch_bounds__(kMaxWarps * 32) gate_norm_grad_kernel(const GateNormParams p) {
-    __shared__ float2 room[2 * kRows * kMaxWarps];
-    __shared__ float lines[8 * 256];               // sums of several teams: at most 8 warps of 256 columns
+// Where a group ends (and behind a team's last row) its sums leave: to the gradient itself where the whole group was this team's, else to the
+// team's part (the first of its two for the group of its first row, else the second), which gate_norm_sums_kernel joins.
+template <typename S, typename B, bool POST, int kStages>
+__global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
+    extern __shared__ uint4 ring[];
+    __shared__ float2 room[2 * 32];
     Team t = team_of(p, room);
-    const int teams = int(blockDim.x >> 5) / p.warps;
-    const int64_t r0 = int64_t(blockIdx.x) * p.chunk, r1 = min(r0 + p.chunk, p.rows);
-    const bool normed = p.dy.p != nullptr, gated = p.dgate.p != nullptr, later = p.dx_out.p != nullptr;
-    const bool branch = POST || gated;             // h itself is read
-    f32x2 post_weight[4], dpost[4];
+    const uint32_t team = team_index(p), r0 = team * p.chunk, r1 = min(r0 + p.chunk, p.rows);
+    if (r0 >= r1) return;
+    const uint32_t plane = blockDim.x * 16u, batch = plane * kGradPlanes<S, B>, s_size = plane * kRows * kPlanes<S>, b_size = plane * kRows * kPlanes<B>;
+    const uint32_t base = smem_u32(ring) + threadIdx.x * 16u, y_at = s_size, d_at = s_size + b_size, h_at = 2 * s_size + b_size;
+    const bool normed = p.dy.p != nullptr, gated = p.dgate.p != nullptr, later = p.dx_out.p != nullptr, branch = POST || gated;       // h itself is read
+    Walk b, ahead;
+    b.start(p, r0, r1);
+    ahead = b;
+    uint32_t to = base, at = base;
+    auto send_next = [&]() {
+        if (ahead.n > 0) {
+            if (normed) { send<S>(to, p.x, ahead, t); send<B>(to + y_at, p.dy, ahead, t); }
+            if (later) send<S>(to + d_at, p.dx_out, ahead, t);
+            if (branch) send<B>(to + h_at, p.h, ahead, t);
+            ahead.next(p, r1);
+        }
+        copies_sent();
+        to = to == base + (kStages - 1) * batch ? base : to + batch;
+    };
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) send_next();
+    f32x2 post_weight[4], dpost[4], gate[4], weight[4], dweight[4], dbias[4], dgate[4];
     fill(dpost, 0.f);
-    if (POST) load_vector(post_weight, Vectors{p.post_weight, 0}, 0, t.c0, t.col, 0.f, 1.f);
-    const float per = 1.f / float(p.cols);
-    for (int64_t g = r0 / p.group; g * p.group < r1; ++g) {
-        const int64_t first = max(g * p.group, r0), last = min((g + 1) * p.group, r1);
-        f32x2 gate[4], weight[4], dweight[4], dbias[4], dgate[4];
-        fill(dweight, 0.f); fill(dbias, 0.f); fill(dgate, 0.f);
-        load_vector(gate, p.gate, g, t.c0, t.col, 0.f, 1.f);
-        load_vector(weight, p.weight, g, t.c0, t.col, p.plus, 1.f);
-        for (int64_t row = first + t.id * kRows; row < last; row += teams * kRows) {
-            const Batch b = batch_at(p, row, g, last);
-            Vec8<S> x_in[kRows], d_in[kRows];
-            Vec8<B> y_in[kRows], h_in[kRows];
-            float4 stats[kRows];
+    if (POST) load_vector(post_weight, Vectors{p.post_weight, 0}, 0, t, 0.f, 1.f);
+    bool fresh = true;
+    while (b.n > 0) {
+        if (fresh) {
+            load_vector(gate, p.gate, b.g, t, 0.f, 1.f);
+            load_vector(weight, p.weight, b.g, t, p.plus, 1.f);
+            fill(dweight, 0.f); fill(dbias, 0.f); fill(dgate, 0.f);
+            fresh = false;
+        }
+        float4 stats[kRows];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            stats[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i < b.live && (normed || POST)) stats[i] = reinterpret_cast<const float4*>(p.stats)[b.row + i];
+        }
+        send_next();                               // into the place of the batch before this one
+        copies_wait<kStages - 1>();
+        f32x2 d[kRows][4];
+        if (normed) {
+            f32x2 xh[kRows][4];
+            float2 s[kRows];
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
-                stats[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (i < b.live && (normed || POST)) stats[i] = reinterpret_cast<const float4*>(p.stats)[b.row + i];
-            }
-            if (normed) { request(x_in, p.x, b, t); request(y_in, p.dy, b, t); }
-            if (later) request(d_in, p.dx_out, b, t);
-            if (branch) request(h_in, p.h, b, t);
-            f32x2 d[kRows][4];
-            if (normed) {
-                f32x2 xh[kRows][4];
-                float2 s[kRows];
+                const f32x2 less = pk2(-stats[i].x, -stats[i].x), inv = pk2(stats[i].y, stats[i].y);
+                f32x2 a = pk2(0.f, 0.f), c = pk2(0.f, 0.f);
+                take<S>(xh[i], at, i);
+                take<B>(d[i], at + y_at, i);
 #pragma unroll
-                for (int i = 0; i < kRows; ++i) {
-                    const f32x2 m = pk2(-stats[i].x, -stats[i].x), inv = pk2(stats[i].y, stats[i].y);
-                    f32x2 a = pk2(0.f, 0.f), c = pk2(0.f, 0.f);
-                    x_in[i].get(xh[i]);
-                    y_in[i].get(d[i]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        xh[i][e] = mul2(add2(xh[i][e], m), inv);
-                        dbias[e] = add2(dbias[e], d[i][e]);
-                        dweight[e] = fma2(d[i][e], xh[i][e], dweight[e]);
-                        d[i][e] = mul2(d[i][e], weight[e]);
-                        a = add2(a, d[i][e]);
-                        c = fma2(d[i][e], xh[i][e], c);
-                    }
-                    s[i] = t.col ? make_float2(pair_sum(a), pair_sum(c)) : make_float2(0.f, 0.f);
+                for (int e = 0; e < 4; ++e) {
+                    xh[i][e] = mul2(add2(xh[i][e], less), inv);
+                    dbias[e] = add2(dbias[e], d[i][e]);
+                    dweight[e] = fma2(d[i][e], xh[i][e], dweight[e]);
+                    d[i][e] = mul2(d[i][e], weight[e]);
+                    a = add2(a, d[i][e]);
+                    c = fma2(d[i][e], xh[i][e], c);
                 }
-                team_sums(t, s);
-#pragma unroll
-                for (int i = 0; i < kRows; ++i) {
-                    const float mg = p.layer ? -s[i].x * per : 0.f, mx = -s[i].y * per;
-                    const f32x2 inv = pk2(stats[i].y, stats[i].y), g2 = pk2(mg, mg), x2 = pk2(mx, mx);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) d[i][e] = mul2(inv, fma2(xh[i][e], x2, add2(d[i][e], g2)));
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < kRows; ++i) fill(d[i], 0.f);
+                s[i] = t.col ? make_float2(pair_sum(a), pair_sum(c)) : make_float2(0.f, 0.f);
             }
+            team_sums(t, s[0], s[1]);
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const float mg = p.layer ? -s[i].x * t.per_row : 0.f, mx = -s[i].y * t.per_row;
+                const f32x2 inv = pk2(stats[i].y, stats[i].y), g2 = pk2(mg, mg), x2 = pk2(mx, mx);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[i][e] = mul2(inv, fma2(xh[i][e], x2, add2(d[i][e], g2)));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) fill(d[i], 0.f);
+        }
+        const f32x2 residual = pk2(p.residual, p.residual);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            f32x2 o[4];
             if (later) {
+                take<S>(o, at + d_at, i);
 #pragma unroll
-                for (int i = 0; i < kRows; ++i) {
-                    f32x2 o[4];
-                    d_in[i].get(o);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) d[i][e] = add2(d[i][e], o[e]);
-                }
+                for (int e = 0; e < 4; ++e) d[i][e] = add2(d[i][e], o[e]);
             }
             if (p.dx.p != nullptr) {
-                const f32x2 residual = pk2(p.residual, p.residual);
 #pragma unroll
-                for (int i = 0; i < kRows; ++i) {
-                    f32x2 o[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[e] = mul2(residual, d[i][e]);
-                    if (i >= b.live) fill(o, 0.f);
-                    if (i < b.n && t.col) Vec8<S>::store(p.dx.p, (b.row + i) * p.dx.ld + t.c0, o);
-                }
+                for (int e = 0; e < 4; ++e) o[e] = mul2(residual, d[i][e]);
+                put<S>(p.dx, b, i, t, o);
             }
-            if (POST) {
-                f32x2 hh[kRows][4];
-                float2 s[kRows];
+        }
+        if (POST) {
+            f32x2 hh[kRows][4];
+            float2 s[kRows];
 #pragma unroll
-                for (int i = 0; i < kRows; ++i) {
-                    const f32x2 m = pk2(-stats[i].z, -stats[i].z), inv = pk2(stats[i].w, stats[i].w);
-                    f32x2 a = pk2(0.f, 0.f), c = pk2(0.f, 0.f);
-                    h_in[i].get(hh[i]);
+            for (int i = 0; i < kRows; ++i) {
+                const f32x2 less = pk2(-stats[i].z, -stats[i].z), inv = pk2(stats[i].w, stats[i].w);
+                f32x2 a = pk2(0.f, 0.f), c = pk2(0.f, 0.f);
+                take<B>(hh[i], at + h_at, i);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        hh[i][e] = mul2(add2(hh[i][e], m), inv);
-                        dgate[e] = fma2(d[i][e], hh[i][e], dgate[e]);          // both sums' part: dgate = post_weight times it, dpost gate times it
-                        d[i][e] = mul2(mul2(d[i][e], gate[e]), post_weight[e]);
-                        a = add2(a, d[i][e]);
-                        c = fma2(d[i][e], hh[i][e], c);
-                    }
-                    s[i] = t.col ? make_float2(pair_sum(a), pair_sum(c)) : make_float2(0.f, 0.f);
+                for (int e = 0; e < 4; ++e) {
+                    hh[i][e] = mul2(add2(hh[i][e], less), inv);
+                    dgate[e] = fma2(d[i][e], hh[i][e], dgate[e]);              // both sums' part: dgate is post_weight times it, dpost gate times it
+                    d[i][e] = mul2(mul2(d[i][e], gate[e]), post_weight[e]);
+                    a = add2(a, d[i][e]);
+                    c = fma2(d[i][e], hh[i][e], c);
                 }
-                if (p.dh.p != nullptr) {
-                    team_sums(t, s);
-#pragma unroll
-                    for (int i = 0; i < kRows; ++i) {
-                        const float mg = p.post_layer ? -s[i].x * per : 0.f, mx = -s[i].y * per;
-                        const f32x2 inv = pk2(stats[i].w, stats[i].w), g2 = pk2(mg, mg), x2 = pk2(mx, mx);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) d[i][e] = mul2(inv, fma2(hh[i][e], x2, add2(d[i][e], g2)));
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < kRows; ++i) {
-                    f32x2 o[4];
-                    if (gated) h_in[i].get(o);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (gated) dgate[e] = fma2(d[i][e], o[e], dgate[e]);
-                        d[i][e] = mul2(d[i][e], gate[e]);
-                    }
-                }
+                s[i] = t.col ? make_float2(pair_sum(a), pair_sum(c)) : make_float2(0.f, 0.f);
             }
             if (p.dh.p != nullptr) {
+                team_sums(t, s[0], s[1]);
 #pragma unroll
                 for (int i = 0; i < kRows; ++i) {
-                    if (i >= b.live) fill(d[i], 0.f);
-                    if (i < b.n && t.col) Vec8<B>::store(p.dh.p, (b.row + i) * p.dh.ld + t.c0, d[i]);
+                    const float mg = p.post_layer ? -s[i].x * t.per_row : 0.f, mx = -s[i].y * t.per_row;
+                    const f32x2 inv = pk2(stats[i].w, stats[i].w), g2 = pk2(mg, mg), x2 = pk2(mx, mx);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) d[i][e] = mul2(inv, fma2(hh[i][e], x2, add2(d[i][e], g2)));
+                    put<B>(p.dh, b, i, t, d[i]);
                 }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                f32x2 o[4];
+                if (gated) take<B>(o, at + h_at, i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (gated) dgate[e] = fma2(d[i][e], o[e], dgate[e]);
+                    d[i][e] = mul2(d[i][e], gate[e]);
+                }
+                if (p.dh.p != nullptr) put<B>(p.dh, b, i, t, d[i]);
             }
         }
-        if (teams > 1) {                           // the other teams' sums, in order
-            float* line = lines + t.id * t.warps * 256 + t.c0;
-            f32x2* sums[3] = {dweight, dbias, dgate};
+        at = at == base + (kStages - 1) * batch ? base : at + batch;
+        const Walk was = b;
+        b.next(p, r1);
+        if (b.n > 0 && b.g == was.g) continue;
+        fresh = true;                              // the group's sums leave
+        if (!t.col) continue;
+        if (POST) {
 #pragma unroll
-            for (int k = 0; k < 3; ++k) {
-                __syncthreads();
-                if (t.id > 0) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) { float a, c; upk2(sums[k][e], a, c); line[2 * e] = a; line[2 * e + 1] = c; }
-                }
-                __syncthreads();
-                if (t.id == 0) {
-                    for (int o = 1; o < teams; ++o) {
-                        const float* other = line + o * t.warps * 256;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) sums[k][e] = add2(sums[k][e], pk2(other[2 * e], other[2 * e + 1]));
-                    }
-                }
-            }
+            for (int e = 0; e < 4; ++e) dpost[e] = fma2(gate[e], dgate[e], dpost[e]);
         }
-        if (t.id == 0 && t.col) {
-            if (POST) {
+        const uint32_t first = was.g * p.group;
+        if (first >= r0 && was.group_end <= r1) {
+            if (POST && gated) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) dpost[e] = fma2(gate[e], dgate[e], dpost[e]);
+                for (int e = 0; e < 4; ++e) dgate[e] = mul2(dgate[e], post_weight[e]);
             }
-            const int64_t whole_end = min((g + 1) * p.group, p.rows);
-            if (first == g * p.group && last == whole_end) {
-                if (POST && gated) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) dgate[e] = mul2(dgate[e], post_weight[e]);
-                }
-                if (p.dweight.p != nullptr) store_vector(p.dweight.p + g * p.dweight.ld + t.c0, dweight);
-                if (p.dbias.p != nullptr) store_vector(p.dbias.p + g * p.dbias.ld + t.c0, dbias);
-                if (gated) store_vector(p.dgate.p + g * p.dgate.ld + t.c0, dgate);
-            } else if (p.parts != nullptr) {
-                float* to = p.parts + (int64_t(blockIdx.x) * 2 + (first == r0 ? 0 : 1)) * 3 * p.cols + t.c0;
-                if (p.dweight.p != nullptr) store_vector(to, dweight);
-                if (p.dbias.p != nullptr) store_vector(to + p.cols, dbias);
-                if (gated) store_vector(to + 2 * p.cols, dgate);
-            }
+            if (p.dweight.p != nullptr) Vec8<float>::store(p.dweight.p, int64_t(was.g) * p.dweight.ld + t.c0, dweight);
+            if (p.dbias.p != nullptr) Vec8<float>::store(p.dbias.p, int64_t(was.g) * p.dbias.ld + t.c0, dbias);
+            if (gated) Vec8<float>::store(p.dgate.p, int64_t(was.g) * p.dgate.ld + t.c0, dgate);
+        } else if (p.parts != nullptr) {
+            const int64_t part = (int64_t(team) * 2 + (first <= r0 ? 0 : 1)) * 3 * p.cols + t.c0;
+            if (p.dweight.p != nullptr) Vec8<float>::store(p.parts, part, dweight);
+            if (p.dbias.p != nullptr) Vec8<float>::store(p.parts, part + p.cols, dbias);
+            if (gated) Vec8<float>::store(p.parts, part + 2 * p.cols, dgate);
         }
     }
-    if (POST && p.dpost != nullptr && t.id == 0 && t.col) store_vector(p.post_parts + int64_t(blockIdx.x) * p.cols + t.c0, dpost);
+    if (POST && p.dpost != nullptr && t.col) Vec8<float>::store(p.post_parts, int64_t(team) * p.cols + t.c0, dpost);
 }
 
-// The parts of groups that lie in several CTAs, and of dpost_weight, joined in order.  blockIdx.x: `wide` columns; y: a group, or, where
-// there are more groups than CTAs, the group at a border of two CTAs' rows, which the first border inside it takes; z: the sum (0 weight,
-// 1 bias, 2 gate, 3 post_weight).  Thread = (column, every 256 / wide'th part).
-__global__ void __launch_bounds__(256) gate_norm_sums_kernel(const GateNormParams p, int ctas, int wide, int by_group) {
-    __shared__ float sums[256];
-    const int z = int(blockIdx.z), ways = 256 / wide, c = int(blockIdx.x) * wide + int(threadIdx.x) % wide, way = int(threadIdx.x) / wide;
-    const VectorsOut out = z == 0 ? p.dweight : z == 1 ? p.dbias : z == 2 ? p.dgate : VectorsOut{p.dpost, 0};
-    griddep_wait();                                // the parts; no CTA ends before the kernel in front has
-    if (out.p == nullptr || (z < 3 ? p.parts == nullptr : blockIdx.y > 0)) return;
-    int64_t g = 0, from = 0, to = ctas - 1;
+// The parts of groups that several teams took, joined in order, and dpost_weight's.  blockIdx.x: `wide` columns; y: a group, or, where there
+// are more groups than teams, the group at a border of two teams' rows, which the first border inside it takes; the last y: dpost_weight.
+// Thread = (column, every 256 / wide'th part).
+__global__ void __launch_bounds__(256) gate_norm_sums_kernel(const GateNormParams p, uint32_t teams, int group_wide, int post_wide, int by_group, uint32_t heads) {
+    __shared__ float sums[3][256];
+    const bool post = blockIdx.y == heads;
+    const int wide = post ? post_wide : group_wide, ways = 256 / wide;
+    const int c = int(blockIdx.x) * wide + int(threadIdx.x) % wide, way = int(threadIdx.x) / wide;
+    if (int(blockIdx.x) * wide >= p.cols) return;
+    uint32_t g = 0, from = 0, to = teams - 1;
     bool second = false;
-    if (z < 3) {
-        g = by_group ? int64_t(blockIdx.y) : (int64_t(blockIdx.y) + 1) * p.chunk / p.group;
-        const int64_t first = g * p.group, last = min(first + p.group, p.rows) - 1;
+    if (!post) {
+        g = by_group ? blockIdx.y : (blockIdx.y + 1) * p.chunk / p.group;
+        const uint32_t first = g * p.group, last = (p.rows - first > p.group ? first + p.group : p.rows) - 1;
         from = first / p.chunk;
         to = last / p.chunk;
-        if (from == to || (!by_group && from != int64_t(blockIdx.y))) return;
-        second = first != from * p.chunk;          // the group is not the one of that CTA's first row
+        if (from == to || (!by_group && from != blockIdx.y)) return;
+        second = first != from * p.chunk;          // the group is not the one of that team's first row
     }
-    float sum = 0.f;
+    griddep_wait();                                // the parts; no CTA that writes ends before the kernel in front has
+    float sum[3] = {0.f, 0.f, 0.f};
+    const bool want[3] = {post || p.dweight.p != nullptr, !post && p.dbias.p != nullptr, !post && p.dgate.p != nullptr};
     if (c < p.cols) {
-        const float* parts = z < 3 ? p.parts + z * p.cols + c : p.post_parts + c;
-        const int64_t step = z < 3 ? int64_t(6) * p.cols : p.cols;
-#pragma unroll 8
-        for (int64_t i = from + way; i <= to; i += ways) sum += ld_dependent(parts + i * step + (second && i == from ? 3 * p.cols : 0));
+        const float* parts = post ? p.post_parts + c : p.parts + c;
+        const int64_t step = post ? p.cols : int64_t(6) * p.cols;
+#pragma unroll 4
+        for (uint32_t i = from + way; i <= to; i += ways) {
+            const float* part = parts + i * step + (second && i == from ? 3 * p.cols : 0);
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+                if (want[k]) sum[k] += ld_dependent(part + k * p.cols);
+        }
     }
-    sums[threadIdx.x] = sum;
-    __syncthreads();
-    if (way == 0 && c < p.cols) {
-        for (int w = 1; w < ways; ++w) sum += sums[w * wide + threadIdx.x];
-        if (z == 2 && p.post_weight != nullptr) sum *= p.post_weight[c];
-        out.p[g * out.ld + c] = sum;
+    if (ways > 1) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) sums[k][threadIdx.x] = sum[k];
+        __syncthreads();
+        if (way > 0) return;
+        for (int w = 1; w < ways; ++w) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) sum[k] += sums[k][w * wide + threadIdx.x];
+        }
     }
+    if (c >= p.cols) return;
+    if (post) { p.dpost[c] = sum[0]; return; }
+    if (want[0]) p.dweight.p[g * p.dweight.ld + c] = sum[0];
+    if (want[1]) p.dbias.p[g * p.dbias.ld + c] = sum[1];
+    if (want[2]) p.dgate.p[g * p.dgate.ld + c] = p.post_weight != nullptr ? sum[2] * p.post_weight[c] : sum[2];
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
 
 int team_warps(int64_t cols) { return int((cols + 255) / 256); }
-// Teams of a CTA: up to 8 warps, and no more than a group's rows keep busy.
-int team_count(int64_t cols, int64_t group) {
-    const int64_t most = 8 / team_warps(cols), busy = (group + kRows - 1) / kRows;
-    return int(most < 1 ? 1 : most < busy ? most : busy);
-}
 constexpr int kGradWarps = 148 * 15;               // warps at a time, on every device: gradients are summed in one order
-int64_t grad_chunk(int64_t rows, int64_t cols, int64_t group) {
-    const int teams = team_count(cols, group), warps = teams * team_warps(cols);
-    const int64_t ctas = kGradWarps / warps, least = int64_t(teams) * kRows * 2;
-    const int64_t chunk = (rows + ctas - 1) / ctas;
-    return chunk < least ? least : chunk;
+int64_t grad_chunk(int64_t rows, int64_t cols) {
+    const int64_t teams = kGradWarps / team_warps(cols), chunk = (rows + teams - 1) / teams;
+    return chunk < 2 * kRows ? 2 * kRows : chunk;
+}
+// CTAs and their size for this many teams: teams of one warp share a CTA.
+struct Launch { unsigned grid, threads; };
+Launch launch_of(int64_t teams, int warps) {
+    if (warps > 1) return Launch{unsigned(teams), unsigned(warps * 32)};
+    return Launch{unsigned((teams + 7) / 8), 256u};
 }
 
 hq_status check_matrix(const void* x, int64_t ld, int64_t cols, hq_dtype dt) {
@@ -521,17 +583,24 @@ hq_status check_sizes(hq_dtype xdt, hq_dtype hdt, int64_t rows, int64_t cols, in
     return HQ_OK;
 }
 
-template <typename S, typename B>
-cudaError_t launch_forward(const GateNormParams& p, bool post, unsigned grid, unsigned threads, cudaStream_t st) {
-    if (post) gate_norm_kernel<S, B, true><<<grid, threads, 0, st>>>(p);
-    else gate_norm_kernel<S, B, false><<<grid, threads, 0, st>>>(p);
+cudaError_t launch_kernel(void (*kern)(GateNormParams), const GateNormParams& p, Launch l, int planes, int stages, cudaStream_t st) {
+    const size_t smem = size_t(planes) * stages * l.threads * 16;
+    const cudaError_t e = smem <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    if (e != cudaSuccess) { (void)cudaGetLastError(); return e; }
+    kern<<<l.grid, l.threads, smem, st>>>(p);
     return cudaGetLastError();
 }
 template <typename S, typename B>
-cudaError_t launch_grad(const GateNormParams& p, bool post, unsigned grid, unsigned threads, cudaStream_t st) {
-    if (post) gate_norm_grad_kernel<S, B, true><<<grid, threads, 0, st>>>(p);
-    else gate_norm_grad_kernel<S, B, false><<<grid, threads, 0, st>>>(p);
-    return cudaGetLastError();
+cudaError_t launch_forward(const GateNormParams& p, bool post, Launch l, cudaStream_t st) {
+    return launch_kernel(post ? gate_norm_kernel<S, B, true> : gate_norm_kernel<S, B, false>, p, l, kForwardPlanes<S, B>, kForwardStages, st);
+}
+template <typename S, typename B>
+cudaError_t launch_grad(const GateNormParams& p, bool post, Launch l, cudaStream_t st) {
+    // the widest rows of fp32 on both sides: 256 KB in two stages
+    if (size_t(kGradPlanes<S, B>) * kGradStages * l.threads * 16 > kMostShared)
+        return launch_kernel(post ? gate_norm_grad_kernel<S, B, true, 1> : gate_norm_grad_kernel<S, B, false, 1>, p, l, kGradPlanes<S, B>, 1, st);
+    return launch_kernel(post ? gate_norm_grad_kernel<S, B, true, kGradStages> : gate_norm_grad_kernel<S, B, false, kGradStages>, p, l, kGradPlanes<S, B>,
+                         kGradStages, st);
 }
 
 }  // namespace
@@ -558,22 +627,22 @@ extern "C" hq_status hq_gate_norm(const void* x, int64_t ldx, hq_dtype xdt, cons
         return e;
     if (!aligned16(stats)) return HQ_ERR_ALIGNMENT;
     GateNormParams p{};
-    p.rows = rows; p.group = group; p.cols = int(cols); p.warps = team_warps(cols); p.lens = lens;
+    p.rows = uint32_t(rows); p.group = uint32_t(group < rows ? group : rows); p.cols = int(cols); p.warps = team_warps(cols); p.lens = lens;
     p.layer = norm == HQ_NORM_LAYER; p.post_layer = post == HQ_NORM_LAYER; p.post_weight = post_weight;
     p.gate = Vectors{gate, ld_gate}; p.weight = Vectors{weight, ld_weight}; p.bias = Vectors{bias, ld_bias};
     p.residual = residual_scale; p.plus = weight_plus; p.eps = eps; p.stats = stats;
     p.x = Matrix{x, ldx}; p.h = Matrix{h, ldh}; p.x_out = MatrixOut{x_out, ldx_out}; p.y = MatrixOut{y, ldy};
-    const int teams = p.warps > 8 ? 1 : 8 / p.warps;
-    const int64_t most = int64_t(sm_count()) * (24 / p.warps);             // teams at a time
-    p.chunk = (rows + most - 1) / most;
-    if (p.chunk < kRows) p.chunk = kRows;
-    const int64_t used = (rows + p.chunk - 1) / p.chunk;
-    const unsigned grid = unsigned((used + teams - 1) / teams), threads = unsigned(teams * p.warps * 32);
+    // teams at a time: 96 registers leave room for 20 warps an SM, the rows on their way for as many as share 224 KB
+    const int planes = kRows * ((xdt == HQ_BF16 ? 1 : 2) + (hdt == HQ_BF16 ? 1 : 2));
+    const int64_t fit = int64_t(kMostShared / (size_t(planes) * kForwardStages * p.warps * 32 * 16)), by_warps = 20 / p.warps;
+    const int64_t most = int64_t(sm_count()) * (fit < by_warps ? fit : by_warps), chunk = (rows + most - 1) / most;
+    p.chunk = uint32_t(chunk < kRows ? kRows : chunk);
+    const Launch l = launch_of((rows + p.chunk - 1) / p.chunk, p.warps);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool after = post != HQ_NORM_NONE;
     cudaError_t c;
-    if (xdt == HQ_BF16) c = hdt == HQ_BF16 ? launch_forward<__nv_bfloat16, __nv_bfloat16>(p, after, grid, threads, st) : launch_forward<__nv_bfloat16, float>(p, after, grid, threads, st);
-    else c = hdt == HQ_BF16 ? launch_forward<float, __nv_bfloat16>(p, after, grid, threads, st) : launch_forward<float, float>(p, after, grid, threads, st);
+    if (xdt == HQ_BF16) c = hdt == HQ_BF16 ? launch_forward<__nv_bfloat16, __nv_bfloat16>(p, after, l, st) : launch_forward<__nv_bfloat16, float>(p, after, l, st);
+    else c = hdt == HQ_BF16 ? launch_forward<float, __nv_bfloat16>(p, after, l, st) : launch_forward<float, float>(p, after, l, st);
     return c == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }
 
@@ -583,8 +652,8 @@ extern "C" hq_status hq_gate_norm_bwd_workspace_size(int64_t rows, int64_t cols,
     int64_t group = 0;
     const hq_status e = check_sizes(HQ_BF16, HQ_BF16, rows, cols, rows_per_group, nullptr, HQ_NORM_NONE, nullptr, HQ_NORM_NONE, nullptr, nullptr, 1.f, &group);
     if (e != HQ_OK) return e;
-    const int64_t chunk = grad_chunk(rows, cols, group), ctas = (rows + chunk - 1) / chunk;
-    *bytes = size_t(ctas) * 7 * size_t(cols) * sizeof(float);
+    const int64_t chunk = grad_chunk(rows, cols), teams = (rows + chunk - 1) / chunk;
+    *bytes = size_t(teams) * 7 * size_t(cols) * sizeof(float);
     return HQ_OK;
 }
 
@@ -622,12 +691,12 @@ extern "C" hq_status hq_gate_norm_bwd(const void* x_out, int64_t ldx_out, hq_dty
     if ((normed || after) && stats == nullptr) return HQ_ERR_INVALID_ARG;
     if (!aligned16(stats) || !aligned16(dpost_weight)) return HQ_ERR_ALIGNMENT;
     GateNormParams p{};
-    p.rows = rows; p.group = group; p.cols = int(cols); p.warps = team_warps(cols); p.lens = lens;
-    p.chunk = grad_chunk(rows, cols, group);
-    const int64_t ctas = (rows + p.chunk - 1) / p.chunk;
+    p.rows = uint32_t(rows); p.group = uint32_t(group < rows ? group : rows); p.cols = int(cols); p.warps = team_warps(cols); p.lens = lens;
+    p.chunk = uint32_t(grad_chunk(rows, cols));
+    const int64_t teams = (rows + p.chunk - 1) / p.chunk;
     const bool sums = dgate != nullptr || dweight != nullptr || dbias != nullptr;
-    // a part for a group that lies in several CTAs; without a sum over rows, or where every group lies in one CTA, none is written
-    const bool split = sums && (p.chunk % group != 0) && ctas > 1;
+    // parts are for groups that several teams took; without a sum over rows, or where every group is one team's, there are none
+    const bool split = sums && p.chunk % p.group != 0 && teams > 1;
     if (split || dpost_weight != nullptr) {
         size_t need = 0;
         if (workspace == nullptr) return HQ_ERR_INVALID_ARG;
@@ -643,19 +712,19 @@ extern "C" hq_status hq_gate_norm_bwd(const void* x_out, int64_t ldx_out, hq_dty
     p.dgate = VectorsOut{dgate, ld_dgate}; p.dweight = VectorsOut{dweight, ld_dweight}; p.dbias = VectorsOut{dbias, ld_dbias};
     p.dpost = dpost_weight;
     p.parts = split ? static_cast<float*>(workspace) : nullptr;
-    p.post_parts = static_cast<float*>(workspace) + size_t(ctas) * 6 * cols;
-    const int teams = team_count(cols, group);
-    const unsigned grid = unsigned(ctas), threads = unsigned(teams * p.warps * 32);
+    p.post_parts = static_cast<float*>(workspace) + size_t(teams) * 6 * cols;
+    const Launch l = launch_of(teams, p.warps);
     cudaError_t c;
-    if (xdt == HQ_BF16) c = hdt == HQ_BF16 ? launch_grad<__nv_bfloat16, __nv_bfloat16>(p, after, grid, threads, st) : launch_grad<__nv_bfloat16, float>(p, after, grid, threads, st);
-    else c = hdt == HQ_BF16 ? launch_grad<float, __nv_bfloat16>(p, after, grid, threads, st) : launch_grad<float, float>(p, after, grid, threads, st);
+    if (xdt == HQ_BF16) c = hdt == HQ_BF16 ? launch_grad<__nv_bfloat16, __nv_bfloat16>(p, after, l, st) : launch_grad<__nv_bfloat16, float>(p, after, l, st);
+    else c = hdt == HQ_BF16 ? launch_grad<float, __nv_bfloat16>(p, after, l, st) : launch_grad<float, float>(p, after, l, st);
     if (c != cudaSuccess) return HQ_ERR_CUDA;
     if (!split && dpost_weight == nullptr) return HQ_OK;
-    const int by_group = groups <= ctas - 1;
-    const int64_t heads = !split ? 1 : by_group ? groups : ctas - 1;
-    int wide = 8;                                  // columns a CTA: as few as keep the number of CTAs in the thousands
-    while (wide < 128 && (cols + wide - 1) / wide * heads > 2048) wide *= 2;
-    const dim3 few(unsigned((cols + wide - 1) / wide), unsigned(heads), dpost_weight != nullptr ? 4u : 3u);
-    return launch_dependent(gate_norm_sums_kernel, few, 256, 0, st, dependent_launch(int64_t(few.x) * few.y * few.z), p, int(ctas), wide, by_group) == cudaSuccess
+    const int by_group = groups < teams;
+    const uint32_t heads = !split ? 0u : uint32_t(by_group ? groups : teams - 1);
+    // columns a CTA: with few parts a group a thread takes them all, else up to 32 threads, 8 parts each or more
+    auto wide_for = [](int64_t parts) { int wide = 256; while (wide > 8 && parts > 256 / wide * 8) wide /= 2; return wide; };
+    const int wide = wide_for(p.group / p.chunk + 2), post_wide = wide_for(teams), least = dpost_weight != nullptr && post_wide < wide ? post_wide : wide;
+    const dim3 few(unsigned((cols + least - 1) / least), heads + (dpost_weight != nullptr ? 1u : 0u));
+    return launch_dependent(gate_norm_sums_kernel, few, 256, 0, st, dependent_launch(int64_t(few.x) * few.y), p, uint32_t(teams), wide, post_wide, by_group, heads) == cudaSuccess
                ? HQ_OK : HQ_ERR_CUDA;
 }
