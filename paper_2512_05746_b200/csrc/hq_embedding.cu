@@ -7,12 +7,11 @@
 //
 // The gradient has three kernels.  (1) order: CTA b owns a slice of the ids, reads all ids once, keeps the tokens of its slice in their order
 // and counts those of smaller ids (where its part of the sorted order begins), then sorts its tokens by id with one stable counting sort:
-// no atomics, so the order is the same on every run.  (2) sums: the sorted tokens are cut into spans of equal length, whatever ids they
-// hold (most tokens may be of one id); a team of threads adds up a span's rows with several rows in flight and writes a row of the table
-// whenever the id changes.  The first and the last sum of a span go to the workspace where their id goes on in the spans beside it; CTAs
-// behind the spans fill the rows without tokens.  (3) join: ids that lie in several spans, the parts in order.
-#include <climits>
-
+// no atomics, so the order is the same on every run.  It writes its slice's rows of the table that have no tokens, too: all of them in front of
+// the rest, while the memory is idle, where the tokens are fewer than the ids.  (2) sums: the sorted tokens are cut into spans of equal length,
+// whatever ids they hold (most tokens may be of one id); a team of threads adds up a span's rows with several rows in flight and writes a row of
+// the table whenever the id changes.  An id of up to `longest` tokens belongs to the span of its first one; the sums of a longer one go to the
+// workspace, one for each span, and (3) join adds them up in order.
 #include "hq_common.cuh"
 #include "hq_vec8.cuh"
 
@@ -23,58 +22,37 @@ namespace {
 
 template <typename I> __device__ __forceinline__ int64_t id_at(const void* ids, int64_t t) { return int64_t(__ldg(static_cast<const I*>(ids) + t)); }
 
-struct LookupParams { const void *ids, *table; void* out; int64_t tokens, classes, ld_table, ld_out; int vectors; float scale; };
+struct LookupParams { const void *ids, *table; void* out; int64_t classes, ld_table, ld_out; uint32_t tokens; int vectors; float scale; };
 
-// A thread takes 8 channels of kTogether tokens at a time (ids first, then the rows, then the stores).
+// A thread takes 8 channels (blockIdx.y: 256 vectors of them) of kTogether tokens at a time: the ids, then the rows, then the stores.
 template <typename I, typename T, typename U>
 __global__ void __launch_bounds__(256) embedding_kernel(const LookupParams p) {
-    constexpr int kTogether = 4;
-    const uint32_t lane_token = threadIdx.x / uint32_t(p.vectors), slots = 256u / uint32_t(p.vectors);       // tokens of a CTA's step
+    constexpr int kTogether = sizeof(T) == 2 ? 8 : 4;
+    const int across = min(p.vectors - int(blockIdx.y) * 256, 256), slots = 256 / across, slot = int(threadIdx.x) / across;     // tokens of a CTA's step
+    if (slot >= slots) return;
+    const int c0 = (int(blockIdx.y) * 256 + int(threadIdx.x) - slot * across) * 8;
+    const T* table = static_cast<const T*>(p.table) + c0;
+    U* out = static_cast<U*>(p.out) + c0;
     const f32x2 s = pk2(p.scale, p.scale);
-    // wide rows (more vectors than threads): a CTA a token, its threads over the row
-    if (slots == 0) {
-        for (int64_t t = blockIdx.x; t < p.tokens; t += gridDim.x) {
-            const int64_t id = id_at<I>(p.ids, t);
-            const bool there = id >= 0 && id < p.classes;
-            for (int v = int(threadIdx.x); v < p.vectors; v += 256) {
-                Vec8<T> x;
-                x.clear();
-                if (there) x.load(p.table, id * p.ld_table + v * 8);
-                f32x2 f[4];
-                x.get(f);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], s);
-                if (!there) f[0] = f[1] = f[2] = f[3] = pk2(0.f, 0.f);
-                Vec8<U>::store(p.out, t * p.ld_out + v * 8, f);
-            }
-        }
-        return;
-    }
-    if (lane_token >= slots) return;
-    const int c0 = int(threadIdx.x - lane_token * uint32_t(p.vectors)) * 8;
-    const int64_t step = int64_t(gridDim.x) * slots;
-    for (int64_t t0 = int64_t(blockIdx.x) * slots + lane_token; t0 < p.tokens; t0 += step * kTogether) {
+    const uint32_t step = gridDim.x * uint32_t(slots);
+    for (uint32_t t0 = blockIdx.x * uint32_t(slots) + uint32_t(slot); t0 < p.tokens; t0 += step * kTogether) {
         int64_t id[kTogether];
         Vec8<T> x[kTogether];
 #pragma unroll
-        for (int u = 0; u < kTogether; ++u) {
-            const int64_t t = t0 + u * step;
-            id[u] = t < p.tokens ? id_at<I>(p.ids, t) : -1;
-        }
+        for (int u = 0; u < kTogether; ++u) id[u] = t0 + u * step < p.tokens ? id_at<I>(p.ids, t0 + u * step) : -1;
 #pragma unroll
         for (int u = 0; u < kTogether; ++u) {
             x[u].clear();
-            if (id[u] >= 0 && id[u] < p.classes) x[u].load(p.table, id[u] * p.ld_table + c0);
+            if (uint64_t(id[u]) < uint64_t(p.classes)) x[u].load_wide(table, id[u] * p.ld_table);
         }
 #pragma unroll
         for (int u = 0; u < kTogether; ++u) {
-            const int64_t t = t0 + u * step;
-            if (t >= p.tokens) break;
+            if (t0 + u * step >= p.tokens) break;
             f32x2 f[4];
             x[u].get(f);
 #pragma unroll
             for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], s);
-            Vec8<U>::store(p.out, t * p.ld_out + c0, f);
+            Vec8<U>::store_wide(out, int64_t(t0 + u * step) * p.ld_out, f);
         }
     }
 }
@@ -91,15 +69,19 @@ struct GradParams {
     void* dtable;
     int64_t ld_dout, ld_base, ld_dtable, classes;
     uint32_t tokens, slice;                        // slice: ids of an order CTA
-    uint32_t span, longest, spans, span_ctas;      // positions of a span; tokens of the longest id that one span takes whole
-    int vectors;
+    uint32_t span, longest, spans;                 // positions of a span; tokens of the longest id that one span takes whole
+    int vectors, half;                             // half: dtable is bf16
+    bool in_place, fill_first;
     float scale;
     uint2 *found, *sorted;                         // [tokens] (id in the slice, token) as found; (id, token) by id
     uint32_t* start;                               // [classes + 1] first position of each id
+    uint32_t *longs, *long_count;                  // ids of more than `longest` tokens: slice s has long_count[s] from first / longest + s on
     float* parts;                                  // [spans][first, last][dim]
 };
 
 __device__ __forceinline__ uint32_t lanes_below() { uint32_t m; asm("mov.u32 %0, %%lanemask_lt;" : "=r"(m)); return m; }
+
+__device__ __forceinline__ uint32_t from_lane0(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 // Exclusive sum of x over the CTA's threads; *total is the whole.  One barrier in front of its use of `room` and one behind.
 __device__ __forceinline__ uint32_t exclusive_sum(uint32_t x, uint32_t* room, uint32_t* total) {
@@ -123,48 +105,91 @@ __device__ __forceinline__ uint32_t exclusive_sum(uint32_t x, uint32_t* room, ui
     return before + sum - x;
 }
 
+// Rows [0, size) of a slice that begins at row v0: base's, or zeros; `counts` (per row) not zero: left to its tokens' sum.
+template <typename U>
+__device__ __forceinline__ void fill_rows(const GradParams& p, int64_t v0, uint32_t size, const uint32_t* counts) {
+    // a warp a row, a lane 8 channels; four rows on their way
+    constexpr int kTogether = 4;
+    const int lane = int(threadIdx.x & 31), warp = int(threadIdx.x >> 5);
+    for (uint32_t r0 = uint32_t(warp); r0 < size; r0 += kOrderWarps * kTogether) {
+        for (int v = lane; v < p.vectors; v += 32) {
+            Vec8<U> x[kTogether];
+#pragma unroll
+            for (int u = 0; u < kTogether; ++u) {
+                const uint32_t r = r0 + uint32_t(u) * kOrderWarps;
+                x[u].clear();
+                if (p.base != nullptr && r < size && (counts == nullptr || counts[r] == 0)) x[u].load_wide(p.base, (v0 + r) * p.ld_base + v * 8);
+            }
+#pragma unroll
+            for (int u = 0; u < kTogether; ++u) {
+                const uint32_t r = r0 + uint32_t(u) * kOrderWarps;
+                if (r >= size || (counts != nullptr && counts[r] != 0)) continue;
+                f32x2 f[4];
+                x[u].get(f);
+                Vec8<U>::store_wide(p.dtable, (v0 + r) * p.ld_dtable + v * 8, f);
+            }
+        }
+    }
+}
+
+// 32 bits of an id are enough to tell whether it is in the table where its upper ones are zero: one outside becomes 2^32 - 1.
+template <typename I> __device__ __forceinline__ uint32_t small_id(const void* ids, uint32_t t) {
+    if constexpr (sizeof(I) == 4) return uint32_t(__ldg(static_cast<const int32_t*>(ids) + t));
+    else {
+        const uint64_t id = uint64_t(__ldg(static_cast<const long long*>(ids) + t));
+        return id >> 32 == 0 ? uint32_t(id) : 0xffffffffu;
+    }
+}
+
 template <typename I>
 __global__ void __launch_bounds__(kOrderThreads) embedding_order_kernel(const GradParams p) {
     extern __shared__ uint32_t counts[];           // [warp][id of the slice]
     __shared__ uint32_t room[kOrderWarps], offset[kSlice];
     constexpr int kAhead = 8;
     const int lane = int(threadIdx.x & 31), warp = int(threadIdx.x >> 5);
-    const int64_t v0 = int64_t(blockIdx.x) * p.slice, v1 = min(v0 + int64_t(p.slice), p.classes);
-    const uint32_t size = uint32_t(v1 - v0);
+    const uint32_t v0 = blockIdx.x * p.slice, v1 = uint32_t(min(int64_t(v0) + p.slice, p.classes)), size = v1 - v0;         // classes < 2^31
+    griddep_launch();                              // the sums' CTAs find room as these end
+    if (!p.in_place && p.fill_first) {
+        if (p.half) fill_rows<__nv_bfloat16>(p, v0, size, nullptr);
+        else fill_rows<float>(p, v0, size, nullptr);
+    }
     // a warp's run of ids, read twice: how many are of the slice and how many smaller; then where they go
     const uint32_t run = (p.tokens + kOrderThreads - 1) / kOrderThreads * 32, from = min(uint32_t(warp) * run, p.tokens), to = min(from + run, p.tokens);
     uint32_t mine = 0, less = 0;
     for (uint32_t t0 = from + lane; t0 < to; t0 += 32 * kAhead) {
-        int64_t id[kAhead];
+        uint32_t id[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) id[u] = t0 + 32 * u < to ? id_at<I>(p.ids, t0 + 32 * u) : -1;
+        for (int u = 0; u < kAhead; ++u) id[u] = t0 + 32 * u < to ? small_id<I>(p.ids, t0 + 32 * u) : 0xffffffffu;
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            less += id[u] >= 0 && id[u] < v0;
-            mine += id[u] >= v0 && id[u] < v1;
+            less += id[u] < v0;
+            mine += id[u] - v0 < size;
         }
     }
     uint32_t n, first;
     (void)exclusive_sum(less, room, &first);       // the slice's first position
     const uint32_t at = exclusive_sum(mine, room, &n);
-    uint32_t to_here = __shfl_sync(0xffffffffu, at, 0);        // the warp's
-    for (uint32_t t0 = from; t0 < to; t0 += 32 * kAhead) {
-        int64_t id[kAhead];
+    uint32_t to_here = from_lane0(at);             // the warp's
+    if (from_lane0(__reduce_add_sync(0xffffffffu, mine)) > 0) {
+        for (uint32_t t0 = from; t0 < to; t0 += 32 * kAhead) {
+            uint32_t id[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) id[u] = t0 + 32 * u + lane < to ? id_at<I>(p.ids, t0 + 32 * u + lane) : -1;
+            for (int u = 0; u < kAhead; ++u) id[u] = t0 + 32 * u + lane < to ? small_id<I>(p.ids, t0 + 32 * u + lane) : 0xffffffffu;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const bool here = id[u] >= v0 && id[u] < v1;
-            const uint32_t who = __ballot_sync(0xffffffffu, here);
-            if (here) p.found[first + to_here + __popc(who & lanes_below())] = make_uint2(uint32_t(id[u] - v0), t0 + 32 * u + lane);
-            to_here += __popc(who);
+            for (int u = 0; u < kAhead; ++u) {
+                const bool here = id[u] - v0 < size;
+                const uint32_t who = __ballot_sync(0xffffffffu, here);
+                if (here) p.found[first + to_here + __popc(who & lanes_below())] = make_uint2(id[u] - v0, t0 + 32 * u + lane);
+                to_here += __popc(who);
+            }
         }
     }
-    for (uint32_t i = threadIdx.x; i < uint32_t(kOrderWarps) * size; i += kOrderThreads) counts[i] = 0;
-    __syncthreads();
     // the slice's tokens, a run for each warp: counted by id, then placed
-    const uint2* list = p.found + first;
     const uint32_t part = (n + kOrderThreads - 1) / kOrderThreads * 32, begin = min(uint32_t(warp) * part, n), end = min(begin + part, n);
+    const uint32_t busy = part > 0 ? (n + part - 1) / part : 0;                // warps with tokens
+    for (uint32_t i = threadIdx.x; i < busy * size; i += kOrderThreads) counts[i] = 0;
+    __syncthreads();
+    const uint2* list = p.found + first;
     uint32_t* count = counts + uint32_t(warp) * size;
     constexpr int kBatch = 4;
     for (uint32_t j0 = begin; j0 < end; j0 += 32 * kBatch) {
@@ -181,9 +206,9 @@ __global__ void __launch_bounds__(kOrderThreads) embedding_order_kernel(const Gr
     __syncthreads();
     uint32_t sum = 0;
     if (threadIdx.x < size) {
-        for (int w = 0; w < kOrderWarps; ++w) {
-            const uint32_t c = counts[uint32_t(w) * size + threadIdx.x];
-            counts[uint32_t(w) * size + threadIdx.x] = sum;
+        for (uint32_t w = 0; w < busy; ++w) {
+            const uint32_t c = counts[w * size + threadIdx.x];
+            counts[w * size + threadIdx.x] = sum;
             sum += c;
         }
     }
@@ -194,7 +219,11 @@ __global__ void __launch_bounds__(kOrderThreads) embedding_order_kernel(const Gr
         p.start[v0 + threadIdx.x] = first + begins;
     }
     if (v1 == p.classes && threadIdx.x == 0) p.start[p.classes] = first + n;
-    __syncthreads();
+    const bool is_long = sum > p.longest;
+    uint32_t longs;
+    const uint32_t nth = exclusive_sum(is_long ? 1u : 0u, room, &longs);       // (its barriers stand in front of the use of `offset`, too)
+    if (is_long) p.longs[first / p.longest + blockIdx.x + nth] = v0 + threadIdx.x;
+    if (threadIdx.x == 0) p.long_count[blockIdx.x] = longs;
     for (uint32_t j0 = begin; j0 < end; j0 += 32 * kBatch) {
         uint2 e[kBatch];
 #pragma unroll
@@ -202,13 +231,18 @@ __global__ void __launch_bounds__(kOrderThreads) embedding_order_kernel(const Gr
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             const uint32_t same = __match_any_sync(0xffffffffu, e[u].x), rank = __popc(same & lanes_below());
-            if (e[u].x != 0xffffffffu) {
-                p.sorted[first + offset[e[u].x] + count[e[u].x] + rank] = make_uint2(uint32_t(v0) + e[u].x, e[u].y);
-            }
+            if (e[u].x != 0xffffffffu) p.sorted[first + offset[e[u].x] + count[e[u].x] + rank] = make_uint2(v0 + e[u].x, e[u].y);
             __syncwarp();
             if (e[u].x != 0xffffffffu && rank == 0) count[e[u].x] += __popc(same);
             __syncwarp();
         }
+    }
+    if (!p.in_place && !p.fill_first) {
+        __syncthreads();
+        if (threadIdx.x < size) offset[threadIdx.x] = sum;
+        __syncthreads();
+        if (p.half) fill_rows<__nv_bfloat16>(p, v0, size, offset);
+        else fill_rows<float>(p, v0, size, offset);
     }
 }
 
@@ -225,7 +259,7 @@ __device__ __forceinline__ void write_row(const GradParams& p, uint32_t v, int c
     f32x2 f[4];
     if (p.base != nullptr) {
         Vec8<U> b;
-        b.load(p.base, int64_t(v) * p.ld_base + c0);
+        b.load_wide(p.base, int64_t(v) * p.ld_base + c0);
         b.get(f);
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = fma2(sum[e], s, f[e]);
@@ -233,46 +267,24 @@ __device__ __forceinline__ void write_row(const GradParams& p, uint32_t v, int c
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = mul2(sum[e], s);
     }
-    Vec8<U>::store(p.dtable, int64_t(v) * p.ld_dtable + c0, f);
+    Vec8<U>::store_wide(p.dtable, int64_t(v) * p.ld_dtable + c0, f);
 }
 
-// blockIdx.x: spans, then the rows without tokens; y: 256 vectors of 8 channels.
+// blockIdx.x: spans; y: 256 vectors of 8 channels.
 template <typename T, typename U>
 __global__ void __launch_bounds__(256) embedding_sums_kernel(const GradParams p) {
     constexpr int kAhead = 8;
     const int across = min(p.vectors - int(blockIdx.y) * 256, 256), slots = 256 / across, slot = int(threadIdx.x) / across;
     if (slot >= slots) return;
     const int c0 = (int(blockIdx.y) * 256 + int(threadIdx.x) - slot * across) * 8;
+    const uint32_t s = blockIdx.x * uint32_t(slots) + uint32_t(slot);
+    if (s >= p.spans) return;
+    const T* dout = static_cast<const T*>(p.dout) + c0;
     griddep_wait();
-    if (blockIdx.x >= p.span_ctas) {               // rows without tokens
-        constexpr int kTogether = 4;
-        const int64_t step = int64_t(gridDim.x - p.span_ctas) * slots;
-        for (int64_t r0 = int64_t(blockIdx.x - p.span_ctas) * slots + slot; r0 < p.classes; r0 += step * kTogether) {
-            bool empty[kTogether];
-            Vec8<U> b[kTogether];
-#pragma unroll
-            for (int u = 0; u < kTogether; ++u) {
-                const int64_t v = r0 + u * step;
-                empty[u] = v < p.classes && ld_dependent_u32(p.start + v) == ld_dependent_u32(p.start + v + 1);
-            }
-#pragma unroll
-            for (int u = 0; u < kTogether; ++u) {
-                b[u].clear();
-                if (empty[u] && p.base != nullptr) b[u].load(p.base, (r0 + u * step) * p.ld_base + c0);
-            }
-#pragma unroll
-            for (int u = 0; u < kTogether; ++u) {
-                if (!empty[u]) continue;
-                f32x2 f[4];
-                b[u].get(f);
-                Vec8<U>::store(p.dtable, (r0 + u * step) * p.ld_dtable + c0, f);
-            }
-        }
-        return;
-    }
-    const uint32_t s = blockIdx.x * uint32_t(slots) + uint32_t(slot), n = ld_dependent_u32(p.start + p.classes);
+    griddep_launch();                              // the joining kernel's CTAs find room as these end
+    const uint32_t n = ld_dependent_u32(p.start + p.classes);
     uint32_t a = s * p.span, b = min(a + p.span, n);
-    if (s >= p.spans || a >= b) return;
+    if (a >= b) return;
     // an id of at most `longest` tokens belongs to the span of its first one, whole; a longer one to every span that it lies in
     bool open_left = false, open_right = false;
     {
@@ -284,10 +296,8 @@ __global__ void __launch_bounds__(256) embedding_sums_kernel(const GradParams p)
             else open_left = true;
         }
         if (a >= b) return;
-        if (end1 > b) {
-            if (end1 - begin1 <= p.longest) b = end1;
-            else open_right = true;
-        }
+        if (end1 - begin1 > p.longest) open_right = end1 > b;
+        else b = end1;
     }
     f32x2 sum[4];
 #pragma unroll
@@ -295,8 +305,7 @@ __global__ void __launch_bounds__(256) embedding_sums_kernel(const GradParams p)
     uint32_t now = 0xffffffffu;
     auto leave = [&](bool left, bool right) {
         if (!left && !right) { write_row<U>(p, now, c0, sum); return; }
-        float* to = p.parts + (int64_t(s) * 2 + (left ? 0 : 1)) * p.vectors * 8 + c0;
-        Vec8<float>::store(to, 0, sum);
+        Vec8<float>::store_wide(p.parts, (int64_t(s) * 2 + (left ? 0 : 1)) * p.vectors * 8 + c0, sum);
     };
     for (uint32_t j = a; j < b; j += kAhead) {
         uint2 e[kAhead];
@@ -306,7 +315,7 @@ __global__ void __launch_bounds__(256) embedding_sums_kernel(const GradParams p)
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             x[u].clear();
-            if (j + u < b) x[u].load(p.dout, int64_t(e[u].y) * p.ld_dout + c0);
+            if (j + u < b) x[u].load_wide(dout, int64_t(e[u].y) * p.ld_dout);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -326,52 +335,52 @@ __global__ void __launch_bounds__(256) embedding_sums_kernel(const GradParams p)
     leave(open_left, open_right);
 }
 
-// Ids that lie in several spans.  blockIdx.x: kJoinSpans spans, of which those whose last id begins there and goes on are looked at; y: 32
-// channels.  Thread = (4 channels, every 32nd part).
-constexpr int kJoinSpans = 16;
+// Ids that lie in several spans.  blockIdx.x: a slice of the order, whose long ids are taken one after the other; y: 64 channels.
+// Thread = (8 channels, every 32nd part).
 template <typename U>
 __global__ void __launch_bounds__(256) embedding_join_kernel(const GradParams p) {
-    __shared__ uint32_t whose[kJoinSpans];
-    __shared__ f32x2 sums[256][2];
+    __shared__ f32x2 sums[8][8][4];
+    const int lane = int(threadIdx.x & 31), warp = int(threadIdx.x >> 5), group = lane & 7, way = int(threadIdx.x >> 3);
+    const int c0 = int(blockIdx.y) * 64 + group * 8, dim = p.vectors * 8;
     griddep_wait();
-    const uint32_t n = ld_dependent_u32(p.start + p.classes), s0 = blockIdx.x * kJoinSpans;
-    if (threadIdx.x < kJoinSpans) {
-        const uint32_t s = s0 + threadIdx.x, a = s * p.span, b = a + p.span;
-        uint32_t id = 0xffffffffu;
-        if (s < p.spans && b < n) {
-            id = ld_dependent_cg(p.sorted + b - 1).x;
-            const uint32_t begin = ld_dependent_u32(p.start + id), end = ld_dependent_u32(p.start + id + 1);
-            if (begin < a || end <= b || end - begin <= p.longest) id = 0xffffffffu;
-        }
-        whose[threadIdx.x] = id;
-    }
-    __syncthreads();
-    const int group = int(threadIdx.x & 7), way = int(threadIdx.x >> 3), c = int(blockIdx.y) * 32 + group * 4, dim = p.vectors * 8;
-    for (int k = 0; k < kJoinSpans; ++k) {
-        const uint32_t id = whose[k];
-        if (id == 0xffffffffu) continue;
-        const uint32_t s = s0 + k, last = (ld_dependent_u32(p.start + id + 1) - 1) / p.span;
-        f32x2 sum[2] = {pk2(0.f, 0.f), pk2(0.f, 0.f)};
-        if (c < dim) {
-#pragma unroll 4
-            for (uint32_t i = s + way; i <= last; i += 32) {
-                const float4 x = ld_dependent_cg(reinterpret_cast<const float4*>(p.parts + (int64_t(i) * 2 + (i == s ? 1 : 0)) * dim + c));
-                sum[0] = add2(sum[0], pk2(x.x, x.y));
-                sum[1] = add2(sum[1], pk2(x.z, x.w));
-            }
-        }
-        sums[threadIdx.x][0] = sum[0];
-        sums[threadIdx.x][1] = sum[1];
-        __syncthreads();
-        if (way == 0 && c < dim && (group & 1) == 0) {         // 8 channels: this thread's and its neighbour's
-            f32x2 f[4] = {sums[threadIdx.x][0], sums[threadIdx.x][1], sums[threadIdx.x + 1][0], sums[threadIdx.x + 1][1]};
-            for (int w = 1; w < 32; ++w) {
+    const uint32_t count = ld_dependent_u32(p.long_count + blockIdx.x);
+    if (count == 0) return;
+    const uint32_t* longs = p.longs + ld_dependent_u32(p.start + blockIdx.x * p.slice) / p.longest + blockIdx.x;
+    for (uint32_t k = 0; k < count; ++k) {
+        const uint32_t id = ld_dependent_u32(longs + k);
+        const uint32_t begin = ld_dependent_u32(p.start + id), end = ld_dependent_u32(p.start + id + 1);
+        const uint32_t first = begin / p.span, last = (end - 1) / p.span;
+        f32x2 sum[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = add2(f[e], sums[w * 8 + group + (e >> 1)][e & 1]);
+        for (int e = 0; e < 4; ++e) sum[e] = pk2(0.f, 0.f);
+        if (c0 < dim) {
+#pragma unroll 4
+            for (uint32_t i = first + way; i <= last; i += 32) {
+                const float4* part = reinterpret_cast<const float4*>(p.parts + (int64_t(i) * 2 + (i == first ? 1 : 0)) * dim + c0);
+                const float4 x = ld_dependent_cg(part), y = ld_dependent_cg(part + 1);
+                sum[0] = add2(sum[0], pk2(x.x, x.y)); sum[1] = add2(sum[1], pk2(x.z, x.w));
+                sum[2] = add2(sum[2], pk2(y.x, y.y)); sum[3] = add2(sum[3], pk2(y.z, y.w));
             }
-            write_row<U>(p, id, c, f);
+        }
+        // four ways of a warp, then the warps in order
+#pragma unroll
+        for (int off = 8; off <= 16; off *= 2) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] = add2(sum[e], __shfl_xor_sync(0xffffffffu, sum[e], off));
+        }
+        __syncthreads();                           // the sums of the id before this one are read
+        if (lane < 8) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[warp][group][e] = sum[e];
         }
         __syncthreads();
+        if (warp == 0 && lane < 8 && c0 < dim) {
+            for (int w = 1; w < 8; ++w) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] = add2(sum[e], sums[w][group][e]);
+            }
+            write_row<U>(p, id, c0, sum);
+        }
     }
 }
 
@@ -390,7 +399,7 @@ hq_status check_call(int id_bytes, int64_t tokens, int64_t classes, int64_t dim,
     return HQ_OK;
 }
 
-struct Plan { uint32_t slice, slices, span, spans; size_t found, sorted, start, parts, bytes; };
+struct Plan { uint32_t slice, slices, span, spans, longest; size_t sorted, start, longs, long_count, parts, bytes; };
 Plan plan_of(int64_t tokens, int64_t classes, int64_t dim) {
     Plan a{};
     const int64_t slice = (classes + 147) / 148;
@@ -401,24 +410,26 @@ Plan plan_of(int64_t tokens, int64_t classes, int64_t dim) {
     while (span < 64 && tokens * (dim / 8) > span * 148 * 1024) span *= 2;
     a.span = uint32_t(span);
     a.spans = uint32_t((tokens + span - 1) / span);
+    a.longest = uint32_t(span * 4 > 64 ? span * 4 : 64);
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    a.found = 0;
-    a.sorted = up(size_t(tokens) * sizeof(uint2));
+    a.sorted = up(size_t(tokens) * sizeof(uint2));             // behind the tokens as found
     a.start = a.sorted + up(size_t(tokens) * sizeof(uint2));
-    a.parts = a.start + up((size_t(classes) + 1) * sizeof(uint32_t));
+    a.longs = a.start + up((size_t(classes) + 1) * sizeof(uint32_t));
+    a.long_count = a.longs + up((size_t(tokens) / a.longest + a.slices + 1) * sizeof(uint32_t));
+    a.parts = a.long_count + up(size_t(a.slices) * sizeof(uint32_t));
     a.bytes = a.parts + size_t(a.spans) * 2 * size_t(dim) * sizeof(float);
     return a;
 }
 
 template <typename T, typename U>
-cudaError_t launch_lookup(const LookupParams& p, int id_bytes, unsigned grid, cudaStream_t st) {
+cudaError_t launch_lookup(const LookupParams& p, int id_bytes, dim3 grid, cudaStream_t st) {
     if (id_bytes == 4) embedding_kernel<int32_t, T, U><<<grid, 256, 0, st>>>(p);
     else embedding_kernel<int64_t, T, U><<<grid, 256, 0, st>>>(p);
     return cudaGetLastError();
 }
 template <typename T, typename U>
 cudaError_t launch_sums(const GradParams& p, dim3 grid, cudaStream_t st) {
-    return launch_dependent(embedding_sums_kernel<T, U>, grid, 256, 0, st, dependent_launch(int64_t(grid.x) * grid.y), p);
+    return launch_dependent(embedding_sums_kernel<T, U>, grid, 256, 0, st, true, p);
 }
 
 }  // namespace
@@ -433,9 +444,9 @@ extern "C" hq_status hq_embedding(const void* ids, int id_bytes, int64_t tokens,
     if (ids == nullptr) return HQ_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(ids) % uintptr_t(id_bytes) != 0) return HQ_ERR_ALIGNMENT;
     if ((e = check_rows(table, ld_table, dim, tdt)) != HQ_OK || (e = check_rows(out, ld_out, dim, odt)) != HQ_OK) return e;
-    const LookupParams p{ids, table, out, tokens, classes, ld_table, ld_out, int(dim / 8), scale};
-    const int64_t slots = p.vectors > 256 ? 1 : 256 / p.vectors, ctas = (tokens + slots - 1) / slots, most = int64_t(sm_count()) * 8;
-    const unsigned grid = unsigned(ctas < most ? ctas : most);
+    const LookupParams p{ids, table, out, classes, ld_table, ld_out, uint32_t(tokens), int(dim / 8), scale};
+    const int64_t slots = p.vectors > 256 ? 1 : 256 / p.vectors, ctas = (tokens + slots - 1) / slots, most = int64_t(sm_count()) * 4;
+    const dim3 grid(unsigned(ctas < most ? ctas : most), unsigned((p.vectors + 255) / 256));
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t c;
     if (tdt == HQ_BF16) c = odt == HQ_BF16 ? launch_lookup<__nv_bfloat16, __nv_bfloat16>(p, id_bytes, grid, st) : launch_lookup<__nv_bfloat16, float>(p, id_bytes, grid, st);
@@ -467,34 +478,28 @@ extern "C" hq_status hq_embedding_bwd(const void* ids, int id_bytes, int64_t tok
     const Plan a = plan_of(tokens, classes, dim);
     if (ws_bytes < a.bytes) return HQ_ERR_WORKSPACE;
     char* ws = static_cast<char*>(workspace);
+    auto words = [&](size_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
     GradParams p{};
     p.ids = ids; p.dout = dout; p.base = base; p.dtable = dtable; p.ld_dout = ld_dout; p.ld_base = ld_base; p.ld_dtable = ld_dtable; p.classes = classes;
-    p.tokens = uint32_t(tokens); p.slice = a.slice; p.span = a.span; p.longest = a.span * 4; p.spans = a.spans; p.vectors = int(dim / 8); p.scale = scale;
-    p.found = reinterpret_cast<uint2*>(ws + a.found); p.sorted = reinterpret_cast<uint2*>(ws + a.sorted);
-    p.start = reinterpret_cast<uint32_t*>(ws + a.start); p.parts = reinterpret_cast<float*>(ws + a.parts);
+    p.tokens = uint32_t(tokens); p.slice = a.slice; p.span = a.span; p.longest = a.longest; p.spans = a.spans; p.vectors = int(dim / 8); p.half = gdt == HQ_BF16;
+    p.in_place = base == dtable; p.fill_first = tokens < classes; p.scale = scale;
+    p.found = reinterpret_cast<uint2*>(ws); p.sorted = reinterpret_cast<uint2*>(ws + a.sorted);
+    p.start = words(a.start); p.longs = words(a.longs); p.long_count = words(a.long_count); p.parts = reinterpret_cast<float*>(ws + a.parts);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const size_t smem = size_t(kOrderWarps) * a.slice * sizeof(uint32_t);
-    if (id_bytes == 4) {
-        HQ_CUDA_OK(cudaFuncSetAttribute(embedding_order_kernel<int32_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kOrderWarps * kSlice * sizeof(uint32_t))));
-        embedding_order_kernel<int32_t><<<a.slices, kOrderThreads, smem, st>>>(p);
-    } else {
-        HQ_CUDA_OK(cudaFuncSetAttribute(embedding_order_kernel<int64_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kOrderWarps * kSlice * sizeof(uint32_t))));
-        embedding_order_kernel<int64_t><<<a.slices, kOrderThreads, smem, st>>>(p);
-    }
+    void (*order)(GradParams) = id_bytes == 4 ? embedding_order_kernel<int32_t> : embedding_order_kernel<int64_t>;
+    if (smem > 40 * 1024) HQ_CUDA_OK(cudaFuncSetAttribute(order, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+    order<<<a.slices, kOrderThreads, smem, st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return HQ_ERR_CUDA;
+    if (tokens == 0) return HQ_OK;
     const int slots = p.vectors > 256 ? 1 : 256 / p.vectors;
-    p.span_ctas = (a.spans + slots - 1) / slots;
-    int64_t fill = base != nullptr && base == dtable ? 0 : (classes + slots * 4 - 1) / (slots * 4);
-    if (fill > int64_t(148) * 16) fill = int64_t(148) * 16;
-    const dim3 grid(p.span_ctas + unsigned(fill), unsigned((p.vectors + 255) / 256));
-    if (grid.x == 0) return HQ_OK;
+    const dim3 grid((a.spans + slots - 1) / slots, unsigned((p.vectors + 255) / 256));
     cudaError_t c;
     if (ddt == HQ_BF16) c = gdt == HQ_BF16 ? launch_sums<__nv_bfloat16, __nv_bfloat16>(p, grid, st) : launch_sums<__nv_bfloat16, float>(p, grid, st);
     else c = gdt == HQ_BF16 ? launch_sums<float, __nv_bfloat16>(p, grid, st) : launch_sums<float, float>(p, grid, st);
     if (c != cudaSuccess) return HQ_ERR_CUDA;
     if (tokens <= int64_t(p.longest)) return HQ_OK;            // no id has more tokens than one span takes
-    const dim3 join((a.spans + kJoinSpans - 1) / kJoinSpans, unsigned((dim + 31) / 32));
-    c = gdt == HQ_BF16 ? launch_dependent(embedding_join_kernel<__nv_bfloat16>, join, 256, 0, st, dependent_launch(int64_t(join.x) * join.y), p)
-                       : launch_dependent(embedding_join_kernel<float>, join, 256, 0, st, dependent_launch(int64_t(join.x) * join.y), p);
+    const dim3 join(a.slices, unsigned((dim + 63) / 64));
+    c = gdt == HQ_BF16 ? launch_dependent(embedding_join_kernel<__nv_bfloat16>, join, 256, 0, st, true, p) : launch_dependent(embedding_join_kernel<float>, join, 256, 0, st, true, p);
     return c == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }

@@ -24,8 +24,8 @@ constexpr int kMaxCols = 4096;
 constexpr int kMaxWarps = 16;
 constexpr int kRows = 2;                           // rows of a team's batch
 
-struct Matrix { const void* p; int64_t ld; };
-struct MatrixOut { void* p; int64_t ld; };
+struct Matrix { const void* p; uint32_t ld; };     // pitch in bytes
+struct MatrixOut { void* p; uint32_t ld; };
 struct Vectors { const float* p; int64_t ld; };    // [groups][cols]
 struct VectorsOut { float* p; int64_t ld; };
 
@@ -48,28 +48,29 @@ struct GateNormParams {
 
 // ---- a team's walk over its rows ----
 
-// Rows [row, row + n) of group g, the first `live` of them within its length.
+// Rows [row, row + n) of group g, the first `live` of them within its length; left, alive: rows of the group from `row` on, and within its length.
 struct Walk {
-    uint32_t row, g, group_end, live_end;          // first row behind the group, and behind its length
-    int n, live;
-    __device__ __forceinline__ void count(uint32_t end) {
-        n = row < end ? int(min(uint32_t(kRows), min(group_end, end) - row)) : 0;
-        live = row < live_end ? min(n, int(min(uint32_t(kRows), live_end - row))) : 0;
+    uint32_t row, g;
+    int left, alive, n, live;
+    __device__ __forceinline__ void enter(const GateNormParams& p, uint32_t behind) {        // behind: rows of the group in front of `row`
+        left = int(min(p.group - behind, p.rows - row));
+        alive = p.lens != nullptr && left > 0 ? min(p.lens[g] - int(behind), left) : left;
     }
-    __device__ __forceinline__ void enter(const GateNormParams& p, uint32_t first, uint32_t end) {       // the group that begins at `first`
-        group_end = p.rows - first > p.group ? first + p.group : p.rows;
-        live_end = group_end;
-        if (p.lens != nullptr && first < end) live_end = min(group_end, first + uint32_t(max(p.lens[g], 0)));
+    __device__ __forceinline__ void count(uint32_t end) {
+        n = min(min(kRows, left), int(end - row));
+        live = max(0, min(n, alive));
     }
     __device__ __forceinline__ void start(const GateNormParams& p, uint32_t at, uint32_t end) {
         row = at;
         g = at / p.group;
-        enter(p, g * p.group, end);
+        enter(p, at - g * p.group);
         count(end);
     }
     __device__ __forceinline__ void next(const GateNormParams& p, uint32_t end) {
         row += uint32_t(n);
-        if (row == group_end) { ++g; enter(p, row, end); }
+        left -= n;
+        alive -= n;
+        if (left == 0) { ++g; enter(p, 0); }
         count(end);
     }
 };
@@ -77,7 +78,7 @@ struct Walk {
 // ---- a team, and its exchange of sums: two buffers in turn, so that one barrier stands between the writes and the reads of an exchange and
 // none behind it.  Teams of several warps are CTAs of their own, teams of one warp need no barrier. ----
 struct Team {
-    int lane, warp, warps, c0;
+    int lane, warp, warps, c0, cols;
     bool col;                                      // the thread has columns
     float share, per_warp, per_row;                // columns of warp (lane & 15); 1 / columns of this warp, of the row
     float2* room;                                  // [2][32]
@@ -89,6 +90,7 @@ __device__ __forceinline__ Team team_of(const GateNormParams& p, float2* room) {
     t.warps = p.warps;
     t.warp = p.warps == 1 ? 0 : int(threadIdx.x >> 5);
     t.c0 = (t.warp * 32 + t.lane) * 8;
+    t.cols = p.cols;
     t.col = t.c0 < p.cols;
     t.share = float(max(0, min(256, p.cols - (t.lane & 15) * 256)));
     t.per_warp = 1.f / float(min(256, p.cols - t.warp * 256));
@@ -188,23 +190,42 @@ __device__ __forceinline__ void load_vector(f32x2 (&v)[4], const Vectors& from, 
     v[0] = pk2(a.x + add, a.y + add); v[1] = pk2(a.z + add, a.w + add); v[2] = pk2(b.x + add, b.y + add); v[3] = pk2(b.z + add, b.w + add);
 }
 
-// ---- rows on their way through shared memory: each thread's own 16 or 32 bytes of a row, in planes of 16 bytes a thread ----
+// ---- rows on their way through shared memory: a thread's 16 or 32 bytes of a row, in planes of 16 bytes a thread.  Neighbouring lanes copy
+// neighbouring 16 bytes; of fp32 they are another lane's of the warp (copied by their own lane, half of every sector would be asked for twice) ----
 template <typename T> constexpr int kPlanes = int(sizeof(T)) * 8 / 16;
 __device__ __forceinline__ void copy_ahead(uint32_t to, const void* from, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void copies_sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-// `at`: this thread's place in the batch's first plane; zeros for rows that are not there.
+template <int N> __device__ __forceinline__ void copies_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+    __syncwarp();
+}
+__device__ __forceinline__ uint64_t row_at(uint32_t row, uint32_t ld) { return uint64_t(row) * ld; }
+// Where this thread's copies of a row begin, and its own columns' place in an output.
+template <typename T> __device__ __forceinline__ const char* copied(const Matrix& m, const Team& t) {
+    return static_cast<const char*>(m.p) + (sizeof(T) == 2 ? t.c0 * 2 : (t.warp * 256 + t.lane * 4) * 4);
+}
+template <typename T> __device__ __forceinline__ char* columns(const MatrixOut& m, const Team& t) { return static_cast<char*>(m.p) + t.c0 * int(sizeof(T)); }
+// `at`: the batch's first plane; zeros for rows that are not there.
 template <typename T>
-__device__ __forceinline__ void send(uint32_t at, const Matrix& m, const Walk& b, const Team& t) {
+__device__ __forceinline__ void send(uint32_t at, const char* from, uint32_t ld, const Walk& b, const Team& t) {
     const uint32_t plane = blockDim.x * 16u;
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-        const bool there = i < b.live && t.col;
-        const T* from = static_cast<const T*>(m.p) + (there ? int64_t(b.row + i) * m.ld + t.c0 : 0);
+        const bool live = i < b.live;
+        const char* row = from + row_at(live ? b.row + i : b.row, ld);
+        if constexpr (sizeof(T) == 2) {
+            copy_ahead(at + uint32_t(i) * plane + threadIdx.x * 16u, t.col ? row : row - t.c0 * 2, live && t.col);
+        } else {
 #pragma unroll
-        for (int k = 0; k < kPlanes<T>; ++k) copy_ahead(at + uint32_t(i * kPlanes<T> + k) * plane, from + k * (16 / int(sizeof(T))), there);
+            for (int k = 0; k < 2; ++k) {          // piece k * 32 + lane of the warp's 64: of lane piece / 2, plane piece % 2
+                const int c = t.warp * 256 + (k * 32 + t.lane) * 4;
+                const bool col = c < t.cols;
+                copy_ahead(at + (uint32_t(i) * 2u + (t.lane & 1u)) * plane + ((threadIdx.x & ~31u) + uint32_t(k * 16 + t.lane / 2)) * 16u,
+                           col ? row + k * 512 : row - (t.warp * 256 + t.lane * 4) * 4, live && col);
+            }
+        }
     }
 }
 __device__ __forceinline__ uint4 plane_at(uint32_t at) {
@@ -212,23 +233,32 @@ __device__ __forceinline__ uint4 plane_at(uint32_t at) {
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
 }
+// This thread's columns of row i of the batch whose first plane is `at`.
 template <typename T>
 __device__ __forceinline__ void take(f32x2 (&v)[4], uint32_t at, int i) {
-    const uint32_t plane = blockDim.x * 16u;
+    const uint32_t plane = blockDim.x * 16u, mine = at + threadIdx.x * 16u;
     Vec8<T> raw;
     if constexpr (sizeof(T) == 2) {
-        raw.w = plane_at(at + uint32_t(i) * plane);
+        raw.w = plane_at(mine + uint32_t(i) * plane);
     } else {
-        const uint4 a = plane_at(at + uint32_t(2 * i) * plane), b = plane_at(at + uint32_t(2 * i + 1) * plane);
+        const uint4 a = plane_at(mine + uint32_t(2 * i) * plane), b = plane_at(mine + uint32_t(2 * i + 1) * plane);
         raw.a = make_float4(__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w));
         raw.b = make_float4(__uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w));
     }
     raw.get(v);
 }
+// Rows that are not there leave as zeros.
+__device__ __forceinline__ void clear_dead(const Walk& b, f32x2 (&v)[kRows][4]) {
+    if (b.live == b.n) return;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+        if (i >= b.live) fill(v[i], 0.f);
+}
 template <typename T>
-__device__ __forceinline__ void put(const MatrixOut& m, const Walk& b, int i, const Team& t, f32x2 (&v)[4]) {
-    if (i >= b.live) fill(v, 0.f);
-    if (i < b.n && t.col) Vec8<T>::store(m.p, int64_t(b.row + i) * m.ld + t.c0, v);
+__device__ __forceinline__ void put(char* to, uint32_t ld, const Walk& b, const Team& t, const f32x2 (&v)[kRows][4]) {
+    if (!t.col) return;
+    Vec8<T>::store_wide(to + row_at(b.row, ld), 0, v[0]);      // a batch has a row
+    if (b.n > 1) Vec8<T>::store_wide(to + row_at(b.row + 1, ld), 0, v[1]);
 }
 
 // Batches on their way: what keeps about 40 KB an SM in flight at 15 warps and more.
@@ -247,16 +277,18 @@ __global__ void __maxnreg__(96) gate_norm_kernel(const GateNormParams p) {
     const uint32_t r0 = team_index(p) * p.chunk, r1 = min(r0 + p.chunk, p.rows);
     if (r0 >= r1) return;
     const uint32_t plane = blockDim.x * 16u, batch = plane * kForwardPlanes<S, B>, h_at = plane * kRows * kPlanes<S>;
-    const uint32_t base = smem_u32(ring) + threadIdx.x * 16u;
+    const uint32_t base = smem_u32(ring);
     const bool branch = p.h.p != nullptr, normed = p.y.p != nullptr;
+    const char *x = copied<S>(p.x, t), *h = copied<B>(p.h, t);
+    char *x_out = columns<S>(p.x_out, t), *y = columns<B>(p.y, t);
     Walk b, ahead;
     b.start(p, r0, r1);
     ahead = b;
     uint32_t to = base;
     auto send_next = [&]() {
         if (ahead.n > 0) {
-            send<S>(to, p.x, ahead, t);
-            if (branch) send<B>(to + h_at, p.h, ahead, t);
+            send<S>(to, x, p.x.ld, ahead, t);
+            if (branch) send<B>(to + h_at, h, p.h.ld, ahead, t);
             ahead.next(p, r1);
         }
         copies_sent();
@@ -300,8 +332,8 @@ __global__ void __maxnreg__(96) gate_norm_kernel(const GateNormParams p) {
         send_next();                               // into the place of the batch before this one
         at = at == base + (kStages - 1) * batch ? base : at + batch;
         if (p.x_out.p != nullptr) {
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) put<S>(p.x_out, b, i, t, v[i]);
+            clear_dead(b, v);
+            put<S>(x_out, p.x_out.ld, b, t, v);
         }
         if (normed) {
             moments(t, v, p.layer, p.eps, mean, inv);
@@ -310,8 +342,9 @@ __global__ void __maxnreg__(96) gate_norm_kernel(const GateNormParams p) {
                 const f32x2 less = pk2(-mean[i], -mean[i]), s = pk2(inv[i], inv[i]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[i][e] = fma2(mul2(add2(v[i][e], less), s), weight[e], bias[e]);
-                put<B>(p.y, b, i, t, v[i]);
             }
+            clear_dead(b, v);
+            put<B>(y, p.y.ld, b, t, v);
         }
         if (p.stats != nullptr && t.c0 == 0) {
 #pragma unroll
@@ -332,19 +365,22 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
     __shared__ float2 room[2 * 32];
     Team t = team_of(p, room);
     const uint32_t team = team_index(p), r0 = team * p.chunk, r1 = min(r0 + p.chunk, p.rows);
+    griddep_launch();                              // all teams are at work at once: the joining kernel takes no place of theirs
     if (r0 >= r1) return;
     const uint32_t plane = blockDim.x * 16u, batch = plane * kGradPlanes<S, B>, s_size = plane * kRows * kPlanes<S>, b_size = plane * kRows * kPlanes<B>;
-    const uint32_t base = smem_u32(ring) + threadIdx.x * 16u, y_at = s_size, d_at = s_size + b_size, h_at = 2 * s_size + b_size;
+    const uint32_t base = smem_u32(ring), y_at = s_size, d_at = s_size + b_size, h_at = 2 * s_size + b_size;
     const bool normed = p.dy.p != nullptr, gated = p.dgate.p != nullptr, later = p.dx_out.p != nullptr, branch = POST || gated;       // h itself is read
+    const char *x = copied<S>(p.x, t), *dy = copied<B>(p.dy, t), *dx_out = copied<S>(p.dx_out, t), *h = copied<B>(p.h, t);
+    char *dx = columns<S>(p.dx, t), *dh = columns<B>(p.dh, t);
     Walk b, ahead;
     b.start(p, r0, r1);
     ahead = b;
     uint32_t to = base, at = base;
     auto send_next = [&]() {
         if (ahead.n > 0) {
-            if (normed) { send<S>(to, p.x, ahead, t); send<B>(to + y_at, p.dy, ahead, t); }
-            if (later) send<S>(to + d_at, p.dx_out, ahead, t);
-            if (branch) send<B>(to + h_at, p.h, ahead, t);
+            if (normed) { send<S>(to, x, p.x.ld, ahead, t); send<B>(to + y_at, dy, p.dy.ld, ahead, t); }
+            if (later) send<S>(to + d_at, dx_out, p.dx_out.ld, ahead, t);
+            if (branch) send<B>(to + h_at, h, p.h.ld, ahead, t);
             ahead.next(p, r1);
         }
         copies_sent();
@@ -355,7 +391,7 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
     f32x2 post_weight[4], dpost[4], gate[4], weight[4], dweight[4], dbias[4], dgate[4];
     fill(dpost, 0.f);
     if (POST) load_vector(post_weight, Vectors{p.post_weight, 0}, 0, t, 0.f, 1.f);
-    bool fresh = true;
+    bool fresh = true, begun = b.g * p.group == r0;            // begun: the group's first row is this team's
     while (b.n > 0) {
         if (fresh) {
             load_vector(gate, p.gate, b.g, t, 0.f, 1.f);
@@ -369,7 +405,8 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
             stats[i] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (i < b.live && (normed || POST)) stats[i] = reinterpret_cast<const float4*>(p.stats)[b.row + i];
         }
-        send_next();                               // into the place of the batch before this one
+        __syncwarp();                              // no lane of the warp still reads the batch before this one
+        send_next();                               // into its place
         copies_wait<kStages - 1>();
         f32x2 d[kRows][4];
         if (normed) {
@@ -404,20 +441,25 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
 #pragma unroll
             for (int i = 0; i < kRows; ++i) fill(d[i], 0.f);
         }
-        const f32x2 residual = pk2(p.residual, p.residual);
+        if (later) {
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            f32x2 o[4];
-            if (later) {
+            for (int i = 0; i < kRows; ++i) {
+                f32x2 o[4];
                 take<S>(o, at + d_at, i);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) d[i][e] = add2(d[i][e], o[e]);
             }
-            if (p.dx.p != nullptr) {
+        }
+        if (p.dx.p != nullptr) {
+            const f32x2 residual = pk2(p.residual, p.residual);
+            f32x2 o[kRows][4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = mul2(residual, d[i][e]);
-                put<S>(p.dx, b, i, t, o);
+            for (int i = 0; i < kRows; ++i) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][e] = mul2(residual, d[i][e]);
             }
+            clear_dead(b, o);
+            put<S>(dx, p.dx.ld, b, t, o);
         }
         if (POST) {
             f32x2 hh[kRows][4];
@@ -445,7 +487,6 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
                     const f32x2 inv = pk2(stats[i].w, stats[i].w), g2 = pk2(mg, mg), x2 = pk2(mx, mx);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) d[i][e] = mul2(inv, fma2(hh[i][e], x2, add2(d[i][e], g2)));
-                    put<B>(p.dh, b, i, t, d[i]);
                 }
             }
         } else {
@@ -458,46 +499,51 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
                     if (gated) dgate[e] = fma2(d[i][e], o[e], dgate[e]);
                     d[i][e] = mul2(d[i][e], gate[e]);
                 }
-                if (p.dh.p != nullptr) put<B>(p.dh, b, i, t, d[i]);
             }
         }
+        if (p.dh.p != nullptr) {
+            clear_dead(b, d);
+            put<B>(dh, p.dh.ld, b, t, d);
+        }
         at = at == base + (kStages - 1) * batch ? base : at + batch;
-        const Walk was = b;
+        const uint32_t g = b.g, done = b.row + uint32_t(b.n);
+        const bool over = b.left == b.n;           // the group's last row
         b.next(p, r1);
-        if (b.n > 0 && b.g == was.g) continue;
+        if (!over && done < r1) continue;
         fresh = true;                              // the group's sums leave
+        const bool whole = begun && over, first = g * p.group <= r0;
+        begun = true;
         if (!t.col) continue;
         if (POST) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) dpost[e] = fma2(gate[e], dgate[e], dpost[e]);
         }
-        const uint32_t first = was.g * p.group;
-        if (first >= r0 && was.group_end <= r1) {
+        if (whole) {
             if (POST && gated) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) dgate[e] = mul2(dgate[e], post_weight[e]);
             }
-            if (p.dweight.p != nullptr) Vec8<float>::store(p.dweight.p, int64_t(was.g) * p.dweight.ld + t.c0, dweight);
-            if (p.dbias.p != nullptr) Vec8<float>::store(p.dbias.p, int64_t(was.g) * p.dbias.ld + t.c0, dbias);
-            if (gated) Vec8<float>::store(p.dgate.p, int64_t(was.g) * p.dgate.ld + t.c0, dgate);
+            if (p.dweight.p != nullptr) Vec8<float>::store_wide(p.dweight.p, int64_t(g) * p.dweight.ld + t.c0, dweight);
+            if (p.dbias.p != nullptr) Vec8<float>::store_wide(p.dbias.p, int64_t(g) * p.dbias.ld + t.c0, dbias);
+            if (gated) Vec8<float>::store_wide(p.dgate.p, int64_t(g) * p.dgate.ld + t.c0, dgate);
         } else if (p.parts != nullptr) {
-            const int64_t part = (int64_t(team) * 2 + (first <= r0 ? 0 : 1)) * 3 * p.cols + t.c0;
-            if (p.dweight.p != nullptr) Vec8<float>::store(p.parts, part, dweight);
-            if (p.dbias.p != nullptr) Vec8<float>::store(p.parts, part + p.cols, dbias);
-            if (gated) Vec8<float>::store(p.parts, part + 2 * p.cols, dgate);
+            const int64_t part = (int64_t(team) * 2 + (first ? 0 : 1)) * 3 * p.cols + t.c0;
+            if (p.dweight.p != nullptr) Vec8<float>::store_wide(p.parts, part, dweight);
+            if (p.dbias.p != nullptr) Vec8<float>::store_wide(p.parts, part + p.cols, dbias);
+            if (gated) Vec8<float>::store_wide(p.parts, part + 2 * p.cols, dgate);
         }
     }
-    if (POST && p.dpost != nullptr && t.col) Vec8<float>::store(p.post_parts, int64_t(team) * p.cols + t.c0, dpost);
+    if (POST && p.dpost != nullptr && t.col) Vec8<float>::store_wide(p.post_parts, int64_t(team) * p.cols + t.c0, dpost);
 }
 
 // The parts of groups that several teams took, joined in order, and dpost_weight's.  blockIdx.x: `wide` columns; y: a group, or, where there
 // are more groups than teams, the group at a border of two teams' rows, which the first border inside it takes; the last y: dpost_weight.
-// Thread = (column, every 256 / wide'th part).
+// Thread = (4 columns, every 1024 / wide'th part).
 __global__ void __launch_bounds__(256) gate_norm_sums_kernel(const GateNormParams p, uint32_t teams, int group_wide, int post_wide, int by_group, uint32_t heads) {
-    __shared__ float sums[3][256];
+    __shared__ float4 sums[3][256];
     const bool post = blockIdx.y == heads;
-    const int wide = post ? post_wide : group_wide, ways = 256 / wide;
-    const int c = int(blockIdx.x) * wide + int(threadIdx.x) % wide, way = int(threadIdx.x) / wide;
+    const int wide = post ? post_wide : group_wide, lanes = wide / 4, ways = 256 / lanes, way = int(threadIdx.x) / lanes, mine = int(threadIdx.x) - way * lanes;
+    const int c = int(blockIdx.x) * wide + mine * 4;
     if (int(blockIdx.x) * wide >= p.cols) return;
     uint32_t g = 0, from = 0, to = teams - 1;
     bool second = false;
@@ -509,9 +555,11 @@ __global__ void __launch_bounds__(256) gate_norm_sums_kernel(const GateNormParam
         if (from == to || (!by_group && from != blockIdx.y)) return;
         second = first != from * p.chunk;          // the group is not the one of that team's first row
     }
-    griddep_wait();                                // the parts; no CTA that writes ends before the kernel in front has
-    float sum[3] = {0.f, 0.f, 0.f};
     const bool want[3] = {post || p.dweight.p != nullptr, !post && p.dbias.p != nullptr, !post && p.dgate.p != nullptr};
+    float4 sum[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) sum[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    griddep_wait();                                // the parts; no CTA that writes ends before the kernel in front has
     if (c < p.cols) {
         const float* parts = post ? p.post_parts + c : p.parts + c;
         const int64_t step = post ? p.cols : int64_t(6) * p.cols;
@@ -520,24 +568,30 @@ __global__ void __launch_bounds__(256) gate_norm_sums_kernel(const GateNormParam
             const float* part = parts + i * step + (second && i == from ? 3 * p.cols : 0);
 #pragma unroll
             for (int k = 0; k < 3; ++k)
-                if (want[k]) sum[k] += ld_dependent(part + k * p.cols);
+                if (want[k]) {
+                    const float4 v = ld_dependent_cg(reinterpret_cast<const float4*>(part + k * p.cols));
+                    sum[k].x += v.x; sum[k].y += v.y; sum[k].z += v.z; sum[k].w += v.w;
+                }
         }
     }
-    if (ways > 1) {
 #pragma unroll
-        for (int k = 0; k < 3; ++k) sums[k][threadIdx.x] = sum[k];
-        __syncthreads();
-        if (way > 0) return;
+    for (int k = 0; k < 3; ++k) sums[k][threadIdx.x] = sum[k];
+    __syncthreads();
+    if (way >= 3) return;                          // thread = (4 columns, sum): the ways in order
+    for (int k = way; k < 3; k += ways) {
+        if (!want[k] || c >= p.cols) continue;
+        float4 s = sums[k][mine];
         for (int w = 1; w < ways; ++w) {
-#pragma unroll
-            for (int k = 0; k < 3; ++k) sum[k] += sums[k][w * wide + threadIdx.x];
+            const float4 v = sums[k][w * lanes + mine];
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
+        if (k == 2 && p.post_weight != nullptr) {
+            const float4 v = *reinterpret_cast<const float4*>(p.post_weight + c);
+            s.x *= v.x; s.y *= v.y; s.z *= v.z; s.w *= v.w;
+        }
+        float* out = post ? p.dpost : k == 0 ? p.dweight.p + g * p.dweight.ld : k == 1 ? p.dbias.p + g * p.dbias.ld : p.dgate.p + g * p.dgate.ld;
+        *reinterpret_cast<float4*>(out + c) = s;
     }
-    if (c >= p.cols) return;
-    if (post) { p.dpost[c] = sum[0]; return; }
-    if (want[0]) p.dweight.p[g * p.dweight.ld + c] = sum[0];
-    if (want[1]) p.dbias.p[g * p.dbias.ld + c] = sum[1];
-    if (want[2]) p.dgate.p[g * p.dgate.ld + c] = p.post_weight != nullptr ? sum[2] * p.post_weight[c] : sum[2];
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -559,8 +613,10 @@ hq_status check_matrix(const void* x, int64_t ld, int64_t cols, hq_dtype dt) {
     if (x == nullptr) return HQ_ERR_INVALID_ARG;
     if (ld < cols) return HQ_ERR_SHAPE;
     if (!aligned16(x) || (ld * (dt == HQ_BF16 ? 2 : 4)) % 16 != 0) return HQ_ERR_ALIGNMENT;
-    return HQ_OK;
+    return ld < int64_t(1) << 30 ? HQ_OK : HQ_ERR_UNSUPPORTED;             // a pitch in bytes has 32 bits
 }
+Matrix matrix(const void* p, int64_t ld, hq_dtype dt) { return Matrix{p, p != nullptr ? uint32_t(ld) * (dt == HQ_BF16 ? 2u : 4u) : 0u}; }
+MatrixOut matrix_out(void* p, int64_t ld, hq_dtype dt) { return MatrixOut{p, p != nullptr ? uint32_t(ld) * (dt == HQ_BF16 ? 2u : 4u) : 0u}; }
 hq_status check_vectors(const float* v, int64_t ld, int64_t groups, int64_t cols) {
     if (v == nullptr) return HQ_OK;
     if (groups > 1 && ld < cols) return HQ_ERR_SHAPE;
@@ -596,9 +652,10 @@ cudaError_t launch_forward(const GateNormParams& p, bool post, Launch l, cudaStr
 }
 template <typename S, typename B>
 cudaError_t launch_grad(const GateNormParams& p, bool post, Launch l, cudaStream_t st) {
-    // the widest rows of fp32 on both sides: 256 KB in two stages
-    if (size_t(kGradPlanes<S, B>) * kGradStages * l.threads * 16 > kMostShared)
-        return launch_kernel(post ? gate_norm_grad_kernel<S, B, true, 1> : gate_norm_grad_kernel<S, B, false, 1>, p, l, kGradPlanes<S, B>, 1, st);
+    if constexpr (sizeof(S) + sizeof(B) == 8) {    // the widest rows of fp32 on both sides: 256 KB in two stages
+        if (size_t(kGradPlanes<S, B>) * kGradStages * l.threads * 16 > kMostShared)
+            return launch_kernel(post ? gate_norm_grad_kernel<S, B, true, 1> : gate_norm_grad_kernel<S, B, false, 1>, p, l, kGradPlanes<S, B>, 1, st);
+    }
     return launch_kernel(post ? gate_norm_grad_kernel<S, B, true, kGradStages> : gate_norm_grad_kernel<S, B, false, kGradStages>, p, l, kGradPlanes<S, B>,
                          kGradStages, st);
 }
@@ -631,7 +688,7 @@ extern "C" hq_status hq_gate_norm(const void* x, int64_t ldx, hq_dtype xdt, cons
     p.layer = norm == HQ_NORM_LAYER; p.post_layer = post == HQ_NORM_LAYER; p.post_weight = post_weight;
     p.gate = Vectors{gate, ld_gate}; p.weight = Vectors{weight, ld_weight}; p.bias = Vectors{bias, ld_bias};
     p.residual = residual_scale; p.plus = weight_plus; p.eps = eps; p.stats = stats;
-    p.x = Matrix{x, ldx}; p.h = Matrix{h, ldh}; p.x_out = MatrixOut{x_out, ldx_out}; p.y = MatrixOut{y, ldy};
+    p.x = matrix(x, ldx, xdt); p.h = matrix(h, ldh, hdt); p.x_out = matrix_out(x_out, ldx_out, xdt); p.y = matrix_out(y, ldy, hdt);
     // teams at a time: 96 registers leave room for 20 warps an SM, the rows on their way for as many as share 224 KB
     const int planes = kRows * ((xdt == HQ_BF16 ? 1 : 2) + (hdt == HQ_BF16 ? 1 : 2));
     const int64_t fit = int64_t(kMostShared / (size_t(planes) * kForwardStages * p.warps * 32 * 16)), by_warps = 20 / p.warps;
@@ -707,8 +764,8 @@ extern "C" hq_status hq_gate_norm_bwd(const void* x_out, int64_t ldx_out, hq_dty
     p.layer = norm == HQ_NORM_LAYER; p.post_layer = post == HQ_NORM_LAYER; p.post_weight = post_weight;
     p.gate = Vectors{gate, ld_gate}; p.weight = Vectors{weight, ld_weight};
     p.residual = residual_scale; p.plus = weight_plus; p.stats = const_cast<float*>(stats);
-    p.x = Matrix{x_out, ldx_out}; p.h = Matrix{h, ldh}; p.dx_out = Matrix{dx_out, lddx_out}; p.dy = Matrix{dy, lddy};
-    p.dx = MatrixOut{dx, lddx}; p.dh = MatrixOut{dh, lddh};
+    p.x = matrix(x_out, ldx_out, xdt); p.h = matrix(h, ldh, hdt); p.dx_out = matrix(dx_out, lddx_out, xdt); p.dy = matrix(dy, lddy, hdt);
+    p.dx = matrix_out(dx, lddx, xdt); p.dh = matrix_out(dh, lddh, hdt);
     p.dgate = VectorsOut{dgate, ld_dgate}; p.dweight = VectorsOut{dweight, ld_dweight}; p.dbias = VectorsOut{dbias, ld_dbias};
     p.dpost = dpost_weight;
     p.parts = split ? static_cast<float*>(workspace) : nullptr;
@@ -721,10 +778,10 @@ extern "C" hq_status hq_gate_norm_bwd(const void* x_out, int64_t ldx_out, hq_dty
     if (!split && dpost_weight == nullptr) return HQ_OK;
     const int by_group = groups < teams;
     const uint32_t heads = !split ? 0u : uint32_t(by_group ? groups : teams - 1);
-    // columns a CTA: with few parts a group a thread takes them all, else up to 32 threads, 8 parts each or more
-    auto wide_for = [](int64_t parts) { int wide = 256; while (wide > 8 && parts > 256 / wide * 8) wide /= 2; return wide; };
+    // columns a CTA: as many as leave a thread two parts or more
+    auto wide_for = [](int64_t parts) { int wide = 1024; while (wide > 32 && parts > 1024 / wide * 2) wide /= 2; return wide; };
     const int wide = wide_for(p.group / p.chunk + 2), post_wide = wide_for(teams), least = dpost_weight != nullptr && post_wide < wide ? post_wide : wide;
     const dim3 few(unsigned((cols + least - 1) / least), heads + (dpost_weight != nullptr ? 1u : 0u));
-    return launch_dependent(gate_norm_sums_kernel, few, 256, 0, st, dependent_launch(int64_t(few.x) * few.y), p, uint32_t(teams), wide, post_wide, by_group, heads) == cudaSuccess
+    return launch_dependent(gate_norm_sums_kernel, few, 256, 0, st, true, p, uint32_t(teams), wide, post_wide, by_group, heads) == cudaSuccess
                ? HQ_OK : HQ_ERR_CUDA;
 }

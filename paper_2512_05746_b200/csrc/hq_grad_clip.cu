@@ -18,7 +18,7 @@ namespace hq {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxBlocks = 148 * 8;                // on every device: one order of the sums
+constexpr int kNormBlocks = 148 * 6, kScaleBlocks = 148 * 5;                       // resident at once; on every device: one order of the sums
 constexpr int64_t kUnit = kThreads * 8;            // elements a CTA takes at a time
 constexpr int kMost = 1100;                        // tensors of a launch: 28 bytes each of 32 KB of parameters
 constexpr int kParts = 4096;                       // sums of CTAs of all launches of a call
@@ -72,8 +72,8 @@ __device__ __forceinline__ double squares(const f32x2 (&f)[4]) {
     return d;
 }
 
-// Elements [from, to) of a tensor, all of a CTA's threads; `shift` elements lie between the 16-byte border in front of the tensor and its
-// first one, and vectors begin at multiples of 8 elements from that border.
+// Elements [from, to) of a tensor, all of a CTA's threads; `shift` elements lie between the border in front of the tensor (of 8 elements: 16
+// bytes of bf16, 32 of fp32) and its first one, and vectors begin at multiples of 8 elements from that border.
 template <typename T>
 __device__ __forceinline__ double sum_squares(const void* in, int64_t from, int64_t to, int shift) {
     constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;
@@ -85,7 +85,7 @@ __device__ __forceinline__ double sum_squares(const void* in, int64_t from, int6
         for (int u = 0; u < kAhead; ++u) {
             const int64_t i = base + u * kUnit;
             v[u].clear();
-            if (i >= from && i + 8 <= to) v[u].load(in, i);
+            if (i >= from && i + 8 <= to) v[u].load_wide(in, i);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -112,7 +112,7 @@ __device__ __forceinline__ void my_chunks(uint32_t all, uint32_t& from, uint32_t
     from = min(blockIdx.x * per, all);
     to = min(from + per, all);
 }
-template <typename T> __device__ __forceinline__ int shift_of(const void* p) { return int((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T)) & 7; }
+template <typename T> __device__ __forceinline__ int shift_of(const void* p) { return int((reinterpret_cast<uintptr_t>(p) / sizeof(T)) & 7u); }
 
 template <int N>
 __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_constant__ Tensors<N> p) {
@@ -171,7 +171,7 @@ __device__ __forceinline__ void scale(const void* in, void* out, int64_t from, i
         for (int u = 0; u < kAhead; ++u) {
             const int64_t i = base + u * kUnit;
             v[u].clear();
-            if (i >= from && i + 8 <= to) v[u].load(in, i);
+            if (i >= from && i + 8 <= to) v[u].load_wide(in, i);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -181,7 +181,7 @@ __device__ __forceinline__ void scale(const void* in, void* out, int64_t from, i
             v[u].get(f);
 #pragma unroll
             for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], c2);
-            if (i >= from && i + 8 <= to && wide_out) { Vec8<U>::store(out, i, f); continue; }
+            if (i >= from && i + 8 <= to && wide_out) { Vec8<U>::store_wide(out, i, f); continue; }
             const bool whole = i >= from && i + 8 <= to;
             float e[8];
 #pragma unroll
@@ -255,7 +255,7 @@ hq_status launch(const Call& c, int64_t from, int64_t to, bool norms, int part0,
     p.parts = c.parts + (norms ? part0 : 0);
     p.parts_n = parts;
     p.norm = c.norm; p.coef = c.coef; p.max_norm = c.max_norm; p.eps = c.eps; p.clip = c.clip; p.write_norm = last;
-    const unsigned grid = chunks < 1 ? 1u : chunks < c.most ? chunks : c.most;
+    const unsigned most = norms ? c.most : unsigned(kScaleBlocks), grid = chunks < 1 ? 1u : chunks < most ? chunks : most;
     *blocks = int(grid);
     if (norms) {
         grad_norm_kernel<N><<<grid, kThreads, 0, c.st>>>(p);
@@ -292,11 +292,11 @@ hq_status run(const hq_grad_tensor* t, int64_t n, bool clip, float max_norm, flo
         total += t[k].count;
         if (t[k].count > largest) largest = t[k].count;
     }
-    Call c{t, n, clip, max_norm, eps, norm, coef, static_cast<double*>(workspace), kUnit, unsigned(kMaxBlocks), static_cast<cudaStream_t>(stream)};
+    Call c{t, n, clip, max_norm, eps, norm, coef, static_cast<double*>(workspace), kUnit, unsigned(kNormBlocks), static_cast<cudaStream_t>(stream)};
     const int64_t launches = (n + kMost - 1) / kMost;
-    if (launches * kMaxBlocks > kParts) c.most = unsigned(kParts / launches);
+    if (launches * kNormBlocks > kParts) c.most = unsigned(kParts / launches);
     // chunks of one step of a CTA while these are fewer than the CTAs; larger ones keep a CTA's steps together
-    while (total / c.chunk > kMaxBlocks * 4 && c.chunk < kUnit * 16) c.chunk *= 2;
+    while (total / c.chunk > kNormBlocks * 4 && c.chunk < kUnit * 16) c.chunk *= 2;
     while (total / c.chunk > INT_MAX / 2) c.chunk *= 2;
     int part = 0, blocks = 0;
     int64_t from = 0;
