@@ -20,40 +20,58 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------------------- lookup
 
-template <typename I> __device__ __forceinline__ int64_t id_at(const void* ids, int64_t t) { return int64_t(__ldg(static_cast<const I*>(ids) + t)); }
+// 32 bits of an id are enough to tell whether it is in the table where its upper ones are zero: one outside becomes 2^32 - 1.
+template <typename I> __device__ __forceinline__ uint32_t id_at(const void* ids, uint32_t t) {
+    if constexpr (sizeof(I) == 4) return uint32_t(__ldg(static_cast<const int32_t*>(ids) + t));
+    else {
+        const uint64_t id = uint64_t(__ldg(static_cast<const long long*>(ids) + t));
+        return id >> 32 == 0 ? uint32_t(id) : 0xffffffffu;
+    }
+}
 
-struct LookupParams { const void *ids, *table; void* out; int64_t classes, ld_table, ld_out; uint32_t tokens; int vectors; float scale; };
+// A CTA's threads over rows of `vectors` times 8 channels: `across` threads a row (blockIdx.y: 256 of them), as many rows as fit 256 threads.
+struct Spread { int threads, slots; unsigned slices; };
+inline Spread spread(int vectors) {
+    const int across = vectors < 256 ? vectors : 256, slots = 256 / across;
+    return Spread{(across * slots + 31) / 32 * 32, slots, unsigned((vectors + 255) / 256)};
+}
+struct Place { int slots, slot, c0; };             // slot >= slots: a thread without columns
+__device__ __forceinline__ Place place_of(int vectors) {
+    const int across = min(vectors - int(blockIdx.y) * 256, 256), slots = 256 / min(vectors, 256), slot = int(threadIdx.x) / across;
+    return Place{slots, slot, (int(blockIdx.y) * 256 + int(threadIdx.x) - slot * across) * 8};
+}
 
-// A thread takes 8 channels (blockIdx.y: 256 vectors of them) of kTogether tokens at a time: the ids, then the rows, then the stores.
+struct LookupParams { const void *ids, *table; void* out; uint32_t ld_table, ld_out, classes, tokens; int vectors; float scale; };       // pitches in bytes
+
+// A thread takes 8 channels of kTogether tokens: the ids, then the rows, then the stores.
+template <typename T> constexpr int kTogether = sizeof(T) == 2 ? 6 : 4;
 template <typename I, typename T, typename U>
 __global__ void __launch_bounds__(256) embedding_kernel(const LookupParams p) {
-    constexpr int kTogether = sizeof(T) == 2 ? 8 : 4;
-    const int across = min(p.vectors - int(blockIdx.y) * 256, 256), slots = 256 / across, slot = int(threadIdx.x) / across;     // tokens of a CTA's step
-    if (slot >= slots) return;
-    const int c0 = (int(blockIdx.y) * 256 + int(threadIdx.x) - slot * across) * 8;
-    const T* table = static_cast<const T*>(p.table) + c0;
-    U* out = static_cast<U*>(p.out) + c0;
+    constexpr int kN = kTogether<T>;
+    const Place at = place_of(p.vectors);
+    if (at.slot >= at.slots) return;
+    const char* table = static_cast<const char*>(p.table) + at.c0 * int(sizeof(T));
+    char* out = static_cast<char*>(p.out) + at.c0 * int(sizeof(U));
+    const uint32_t t0 = blockIdx.x * uint32_t(at.slots * kN) + uint32_t(at.slot);
+    uint32_t id[kN];
+    Vec8<T> x[kN];
+#pragma unroll
+    for (int u = 0; u < kN; ++u) id[u] = t0 + u * at.slots < p.tokens ? id_at<I>(p.ids, t0 + u * at.slots) : 0xffffffffu;
+#pragma unroll
+    for (int u = 0; u < kN; ++u) {
+        x[u].clear();
+        if (id[u] < p.classes) x[u].load_wide(table + uint64_t(id[u]) * p.ld_table, 0);
+    }
     const f32x2 s = pk2(p.scale, p.scale);
-    const uint32_t step = gridDim.x * uint32_t(slots);
-    for (uint32_t t0 = blockIdx.x * uint32_t(slots) + uint32_t(slot); t0 < p.tokens; t0 += step * kTogether) {
-        int64_t id[kTogether];
-        Vec8<T> x[kTogether];
 #pragma unroll
-        for (int u = 0; u < kTogether; ++u) id[u] = t0 + u * step < p.tokens ? id_at<I>(p.ids, t0 + u * step) : -1;
+    for (int u = 0; u < kN; ++u) {
+        const uint32_t t = t0 + u * at.slots;
+        if (t >= p.tokens) break;
+        f32x2 f[4];
+        x[u].get(f);
 #pragma unroll
-        for (int u = 0; u < kTogether; ++u) {
-            x[u].clear();
-            if (uint64_t(id[u]) < uint64_t(p.classes)) x[u].load_wide(table, id[u] * p.ld_table);
-        }
-#pragma unroll
-        for (int u = 0; u < kTogether; ++u) {
-            if (t0 + u * step >= p.tokens) break;
-            f32x2 f[4];
-            x[u].get(f);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], s);
-            Vec8<U>::store_wide(out, int64_t(t0 + u * step) * p.ld_out, f);
-        }
+        for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], s);
+        Vec8<U>::store_wide(out + uint64_t(t) * p.ld_out, 0, f);
     }
 }
 
@@ -67,15 +85,16 @@ struct GradParams {
     const void* ids;
     const void *dout, *base;
     void* dtable;
-    int64_t ld_dout, ld_base, ld_dtable, classes;
-    uint32_t tokens, slice;                        // slice: ids of an order CTA
+    uint32_t ld_dout, ld_base, ld_dtable;          // pitches in bytes
+    uint32_t classes, tokens, slice;               // slice: ids of an order CTA
     uint32_t span, longest, spans;                 // positions of a span; tokens of the longest id that one span takes whole
     int vectors, half;                             // half: dtable is bf16
     bool in_place, fill_first;
     float scale;
     uint2 *found, *sorted;                         // [tokens] (id in the slice, token) as found; (id, token) by id
     uint32_t* start;                               // [classes + 1] first position of each id
-    uint32_t *longs, *long_count;                  // ids of more than `longest` tokens: slice s has long_count[s] from first / longest + s on
+    uint4* longs;                                  // (id, first position, end) of ids of more than `longest` tokens: slice s has
+    uint32_t* long_count;                          // long_count[s] from its first position / longest + s on
     float* parts;                                  // [spans][first, last][dim]
 };
 
@@ -105,39 +124,20 @@ __device__ __forceinline__ uint32_t exclusive_sum(uint32_t x, uint32_t* room, ui
     return before + sum - x;
 }
 
-// Rows [0, size) of a slice that begins at row v0: base's, or zeros; `counts` (per row) not zero: left to its tokens' sum.
-template <typename U>
-__device__ __forceinline__ void fill_rows(const GradParams& p, int64_t v0, uint32_t size, const uint32_t* counts) {
-    // a warp a row, a lane 8 channels; four rows on their way
-    constexpr int kTogether = 4;
-    const int lane = int(threadIdx.x & 31), warp = int(threadIdx.x >> 5);
-    for (uint32_t r0 = uint32_t(warp); r0 < size; r0 += kOrderWarps * kTogether) {
-        for (int v = lane; v < p.vectors; v += 32) {
-            Vec8<U> x[kTogether];
-#pragma unroll
-            for (int u = 0; u < kTogether; ++u) {
-                const uint32_t r = r0 + uint32_t(u) * kOrderWarps;
-                x[u].clear();
-                if (p.base != nullptr && r < size && (counts == nullptr || counts[r] == 0)) x[u].load_wide(p.base, (v0 + r) * p.ld_base + v * 8);
-            }
-#pragma unroll
-            for (int u = 0; u < kTogether; ++u) {
-                const uint32_t r = r0 + uint32_t(u) * kOrderWarps;
-                if (r >= size || (counts != nullptr && counts[r] != 0)) continue;
-                f32x2 f[4];
-                x[u].get(f);
-                Vec8<U>::store_wide(p.dtable, (v0 + r) * p.ld_dtable + v * 8, f);
-            }
+// Rows [0, size) of a slice that begins at row v0: base's, or zeros; `counts` (per row) not zero: left to its tokens' sum.  A warp a row.
+__device__ __forceinline__ void fill_rows(const GradParams& p, uint32_t v0, uint32_t size, const uint32_t* counts) {
+    const int lane = int(threadIdx.x & 31), pieces = p.half ? p.vectors : 2 * p.vectors;         // of 16 bytes
+    for (uint32_t r = threadIdx.x >> 5; r < size; r += kOrderWarps) {
+        if (counts != nullptr && counts[r] != 0) continue;
+        uint4* to = reinterpret_cast<uint4*>(static_cast<char*>(p.dtable) + uint64_t(v0 + r) * p.ld_dtable);
+        if (p.base == nullptr) {
+#pragma unroll 4
+            for (int v = lane; v < pieces; v += 32) to[v] = make_uint4(0u, 0u, 0u, 0u);
+        } else {
+            const uint4* from = reinterpret_cast<const uint4*>(static_cast<const char*>(p.base) + uint64_t(v0 + r) * p.ld_base);
+#pragma unroll 4
+            for (int v = lane; v < pieces; v += 32) to[v] = from[v];
         }
-    }
-}
-
-// 32 bits of an id are enough to tell whether it is in the table where its upper ones are zero: one outside becomes 2^32 - 1.
-template <typename I> __device__ __forceinline__ uint32_t small_id(const void* ids, uint32_t t) {
-    if constexpr (sizeof(I) == 4) return uint32_t(__ldg(static_cast<const int32_t*>(ids) + t));
-    else {
-        const uint64_t id = uint64_t(__ldg(static_cast<const long long*>(ids) + t));
-        return id >> 32 == 0 ? uint32_t(id) : 0xffffffffu;
     }
 }
 
@@ -147,19 +147,16 @@ __global__ void __launch_bounds__(kOrderThreads) embedding_order_kernel(const Gr
     __shared__ uint32_t room[kOrderWarps], offset[kSlice];
     constexpr int kAhead = 8;
     const int lane = int(threadIdx.x & 31), warp = int(threadIdx.x >> 5);
-    const uint32_t v0 = blockIdx.x * p.slice, v1 = uint32_t(min(int64_t(v0) + p.slice, p.classes)), size = v1 - v0;         // classes < 2^31
+    const uint32_t v0 = blockIdx.x * p.slice, v1 = min(v0 + p.slice, p.classes), size = v1 - v0;
     griddep_launch();                              // the sums' CTAs find room as these end
-    if (!p.in_place && p.fill_first) {
-        if (p.half) fill_rows<__nv_bfloat16>(p, v0, size, nullptr);
-        else fill_rows<float>(p, v0, size, nullptr);
-    }
+    if (!p.in_place && p.fill_first) fill_rows(p, v0, size, nullptr);
     // a warp's run of ids, read twice: how many are of the slice and how many smaller; then where they go
     const uint32_t run = (p.tokens + kOrderThreads - 1) / kOrderThreads * 32, from = min(uint32_t(warp) * run, p.tokens), to = min(from + run, p.tokens);
     uint32_t mine = 0, less = 0;
     for (uint32_t t0 = from + lane; t0 < to; t0 += 32 * kAhead) {
         uint32_t id[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) id[u] = t0 + 32 * u < to ? small_id<I>(p.ids, t0 + 32 * u) : 0xffffffffu;
+        for (int u = 0; u < kAhead; ++u) id[u] = t0 + 32 * u < to ? id_at<I>(p.ids, t0 + 32 * u) : 0xffffffffu;
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             less += id[u] < v0;
@@ -174,7 +171,7 @@ __global__ void __launch_bounds__(kOrderThreads) embedding_order_kernel(const Gr
         for (uint32_t t0 = from; t0 < to; t0 += 32 * kAhead) {
             uint32_t id[kAhead];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) id[u] = t0 + 32 * u + lane < to ? small_id<I>(p.ids, t0 + 32 * u + lane) : 0xffffffffu;
+            for (int u = 0; u < kAhead; ++u) id[u] = t0 + 32 * u + lane < to ? id_at<I>(p.ids, t0 + 32 * u + lane) : 0xffffffffu;
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const bool here = id[u] - v0 < size;
@@ -222,7 +219,7 @@ __global__ void __launch_bounds__(kOrderThreads) embedding_order_kernel(const Gr
     const bool is_long = sum > p.longest;
     uint32_t longs;
     const uint32_t nth = exclusive_sum(is_long ? 1u : 0u, room, &longs);       // (its barriers stand in front of the use of `offset`, too)
-    if (is_long) p.longs[first / p.longest + blockIdx.x + nth] = v0 + threadIdx.x;
+    if (is_long) p.longs[first / p.longest + blockIdx.x + nth] = make_uint4(v0 + threadIdx.x, first + begins, first + begins + sum, 0u);
     if (threadIdx.x == 0) p.long_count[blockIdx.x] = longs;
     for (uint32_t j0 = begin; j0 < end; j0 += 32 * kBatch) {
         uint2 e[kBatch];
@@ -241,8 +238,7 @@ __global__ void __launch_bounds__(kOrderThreads) embedding_order_kernel(const Gr
         __syncthreads();
         if (threadIdx.x < size) offset[threadIdx.x] = sum;
         __syncthreads();
-        if (p.half) fill_rows<__nv_bfloat16>(p, v0, size, offset);
-        else fill_rows<float>(p, v0, size, offset);
+        fill_rows(p, v0, size, offset);
     }
 }
 
@@ -259,7 +255,7 @@ __device__ __forceinline__ void write_row(const GradParams& p, uint32_t v, int c
     f32x2 f[4];
     if (p.base != nullptr) {
         Vec8<U> b;
-        b.load_wide(p.base, int64_t(v) * p.ld_base + c0);
+        b.load_wide(static_cast<const char*>(p.base) + uint64_t(v) * p.ld_base, c0);
         b.get(f);
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = fma2(sum[e], s, f[e]);
@@ -267,59 +263,59 @@ __device__ __forceinline__ void write_row(const GradParams& p, uint32_t v, int c
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = mul2(sum[e], s);
     }
-    Vec8<U>::store_wide(p.dtable, int64_t(v) * p.ld_dtable + c0, f);
+    Vec8<U>::store_wide(static_cast<char*>(p.dtable) + uint64_t(v) * p.ld_dtable, c0, f);
 }
 
-// blockIdx.x: spans; y: 256 vectors of 8 channels.
+// Span blockIdx.x * slots + slot.  The first rows are asked for before it is known whether they are this span's.
 template <typename T, typename U>
 __global__ void __launch_bounds__(256) embedding_sums_kernel(const GradParams p) {
     constexpr int kAhead = 8;
-    const int across = min(p.vectors - int(blockIdx.y) * 256, 256), slots = 256 / across, slot = int(threadIdx.x) / across;
-    if (slot >= slots) return;
-    const int c0 = (int(blockIdx.y) * 256 + int(threadIdx.x) - slot * across) * 8;
-    const uint32_t s = blockIdx.x * uint32_t(slots) + uint32_t(slot);
-    if (s >= p.spans) return;
-    const T* dout = static_cast<const T*>(p.dout) + c0;
+    const Place at = place_of(p.vectors);
+    const uint32_t s = blockIdx.x * uint32_t(at.slots) + uint32_t(at.slot);
+    if (at.slot >= at.slots || s >= p.spans) return;
+    const int c0 = at.c0;
+    const char* dout = static_cast<const char*>(p.dout) + c0 * int(sizeof(T));
+    uint32_t a = s * p.span, b = min(a + p.span, p.tokens), j = a;             // span >= kAhead: the first entries are inside
+    uint2 e[kAhead];
+    Vec8<T> x[kAhead];
     griddep_wait();
     griddep_launch();                              // the joining kernel's CTAs find room as these end
     const uint32_t n = ld_dependent_u32(p.start + p.classes);
-    uint32_t a = s * p.span, b = min(a + p.span, n);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) e[u] = j + u < b ? ld_dependent_cg(p.sorted + j + u) : make_uint2(0u, 0u);
+    b = min(b, n);
     if (a >= b) return;
+    const uint32_t id0 = e[0].x, id1 = ld_dependent_cg(p.sorted + b - 1).x;
+    const uint32_t begin0 = ld_dependent_u32(p.start + id0), end0 = ld_dependent_u32(p.start + id0 + 1);
+    const uint32_t begin1 = ld_dependent_u32(p.start + id1), end1 = ld_dependent_u32(p.start + id1 + 1);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        x[u].clear();
+        if (j + u < b) x[u].load_wide(dout + uint64_t(e[u].y) * p.ld_dout, 0);
+    }
     // an id of at most `longest` tokens belongs to the span of its first one, whole; a longer one to every span that it lies in
     bool open_left = false, open_right = false;
-    {
-        const uint32_t id0 = ld_dependent_cg(p.sorted + a).x, id1 = ld_dependent_cg(p.sorted + b - 1).x;
-        const uint32_t begin0 = ld_dependent_u32(p.start + id0), end0 = ld_dependent_u32(p.start + id0 + 1);
-        const uint32_t begin1 = ld_dependent_u32(p.start + id1), end1 = ld_dependent_u32(p.start + id1 + 1);
-        if (begin0 < a) {
-            if (end0 - begin0 <= p.longest) a = end0;
-            else open_left = true;
-        }
-        if (a >= b) return;
-        if (end1 - begin1 > p.longest) open_right = end1 > b;
-        else b = end1;
+    if (begin0 < a) {
+        if (end0 - begin0 <= p.longest) a = end0;
+        else open_left = true;
     }
+    if (a >= b) return;
+    if (end1 - begin1 > p.longest) open_right = end1 > b;
+    else b = end1;
     f32x2 sum[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] = pk2(0.f, 0.f);
+    for (int k = 0; k < 4; ++k) sum[k] = pk2(0.f, 0.f);
     uint32_t now = 0xffffffffu;
     auto leave = [&](bool left, bool right) {
         if (!left && !right) { write_row<U>(p, now, c0, sum); return; }
         Vec8<float>::store_wide(p.parts, (int64_t(s) * 2 + (left ? 0 : 1)) * p.vectors * 8 + c0, sum);
     };
-    for (uint32_t j = a; j < b; j += kAhead) {
-        uint2 e[kAhead];
-        Vec8<T> x[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) e[u] = j + u < b ? ld_dependent_cg(p.sorted + j + u) : make_uint2(0u, 0u);
+    uint32_t known = min(s * p.span + p.span, n);  // entries of this batch that have their rows
+    while (true) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            x[u].clear();
-            if (j + u < b) x[u].load_wide(dout, int64_t(e[u].y) * p.ld_dout);
-        }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (j + u >= b) break;
+            if (j + u >= b || j + u >= known) break;
+            if (j + u < a) continue;
             if (e[u].x != now) {
                 if (now != 0xffffffffu) { leave(open_left, false); open_left = false; }
                 now = e[u].x;
@@ -330,6 +326,16 @@ __global__ void __launch_bounds__(256) embedding_sums_kernel(const GradParams p)
             x[u].get(f);
 #pragma unroll
             for (int k = 0; k < 4; ++k) sum[k] = add2(sum[k], f[k]);
+        }
+        j = min(j + kAhead, known);
+        known = b;
+        if (j >= b) break;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) e[u] = j + u < b ? ld_dependent_cg(p.sorted + j + u) : make_uint2(0u, 0u);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            x[u].clear();
+            if (j + u < b) x[u].load_wide(dout + uint64_t(e[u].y) * p.ld_dout, 0);
         }
     }
     leave(open_left, open_right);
@@ -343,18 +349,16 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const GradParams p)
     const int lane = int(threadIdx.x & 31), warp = int(threadIdx.x >> 5), group = lane & 7, way = int(threadIdx.x >> 3);
     const int c0 = int(blockIdx.y) * 64 + group * 8, dim = p.vectors * 8;
     griddep_wait();
-    const uint32_t count = ld_dependent_u32(p.long_count + blockIdx.x);
+    const uint32_t count = ld_dependent_u32(p.long_count + blockIdx.x), slice_at = ld_dependent_u32(p.start + blockIdx.x * p.slice);
     if (count == 0) return;
-    const uint32_t* longs = p.longs + ld_dependent_u32(p.start + blockIdx.x * p.slice) / p.longest + blockIdx.x;
     for (uint32_t k = 0; k < count; ++k) {
-        const uint32_t id = ld_dependent_u32(longs + k);
-        const uint32_t begin = ld_dependent_u32(p.start + id), end = ld_dependent_u32(p.start + id + 1);
-        const uint32_t first = begin / p.span, last = (end - 1) / p.span;
+        const uint4 entry = ld_dependent_cg(p.longs + slice_at / p.longest + blockIdx.x + k);
+        const uint32_t id = entry.x, first = entry.y / p.span, last = (entry.z - 1) / p.span;
         f32x2 sum[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] = pk2(0.f, 0.f);
         if (c0 < dim) {
-#pragma unroll 4
+#pragma unroll 8
             for (uint32_t i = first + way; i <= last; i += 32) {
                 const float4* part = reinterpret_cast<const float4*>(p.parts + (int64_t(i) * 2 + (i == first ? 1 : 0)) * dim + c0);
                 const float4 x = ld_dependent_cg(part), y = ld_dependent_cg(part + 1);
@@ -390,8 +394,10 @@ bool type_ok(hq_dtype t) { return t == HQ_F32 || t == HQ_BF16; }
 hq_status check_rows(const void* x, int64_t ld, int64_t dim, hq_dtype dt) {
     if (x == nullptr) return HQ_ERR_INVALID_ARG;
     if (ld < dim) return HQ_ERR_SHAPE;
-    return aligned16(x) && (ld * (dt == HQ_BF16 ? 2 : 4)) % 16 == 0 ? HQ_OK : HQ_ERR_ALIGNMENT;
+    if (!aligned16(x) || (ld * (dt == HQ_BF16 ? 2 : 4)) % 16 != 0) return HQ_ERR_ALIGNMENT;
+    return ld < int64_t(1) << 30 ? HQ_OK : HQ_ERR_UNSUPPORTED;             // a pitch in bytes has 32 bits
 }
+uint32_t pitch_of(int64_t ld, hq_dtype dt) { return uint32_t(ld) * (dt == HQ_BF16 ? 2u : 4u); }
 hq_status check_call(int id_bytes, int64_t tokens, int64_t classes, int64_t dim, hq_dtype a, hq_dtype b, float scale) {
     if ((id_bytes != 4 && id_bytes != 8) || !type_ok(a) || !type_ok(b) || !(scale - scale == 0.f)) return HQ_ERR_INVALID_ARG;
     if (tokens < 0 || classes <= 0 || dim <= 0) return HQ_ERR_SHAPE;
@@ -415,21 +421,25 @@ Plan plan_of(int64_t tokens, int64_t classes, int64_t dim) {
     a.sorted = up(size_t(tokens) * sizeof(uint2));             // behind the tokens as found
     a.start = a.sorted + up(size_t(tokens) * sizeof(uint2));
     a.longs = a.start + up((size_t(classes) + 1) * sizeof(uint32_t));
-    a.long_count = a.longs + up((size_t(tokens) / a.longest + a.slices + 1) * sizeof(uint32_t));
+    a.long_count = a.longs + up((size_t(tokens) / a.longest + a.slices + 1) * sizeof(uint4));
     a.parts = a.long_count + up(size_t(a.slices) * sizeof(uint32_t));
     a.bytes = a.parts + size_t(a.spans) * 2 * size_t(dim) * sizeof(float);
     return a;
 }
 
 template <typename T, typename U>
-cudaError_t launch_lookup(const LookupParams& p, int id_bytes, dim3 grid, cudaStream_t st) {
-    if (id_bytes == 4) embedding_kernel<int32_t, T, U><<<grid, 256, 0, st>>>(p);
-    else embedding_kernel<int64_t, T, U><<<grid, 256, 0, st>>>(p);
+cudaError_t launch_lookup(const LookupParams& p, int id_bytes, cudaStream_t st) {
+    const Spread s = spread(p.vectors);
+    const uint32_t per = uint32_t(s.slots * kTogether<T>);
+    const dim3 grid((p.tokens + per - 1) / per, s.slices);
+    if (id_bytes == 4) embedding_kernel<int32_t, T, U><<<grid, s.threads, 0, st>>>(p);
+    else embedding_kernel<int64_t, T, U><<<grid, s.threads, 0, st>>>(p);
     return cudaGetLastError();
 }
 template <typename T, typename U>
-cudaError_t launch_sums(const GradParams& p, dim3 grid, cudaStream_t st) {
-    return launch_dependent(embedding_sums_kernel<T, U>, grid, 256, 0, st, true, p);
+cudaError_t launch_sums(const GradParams& p, cudaStream_t st) {
+    const Spread s = spread(p.vectors);
+    return launch_dependent(embedding_sums_kernel<T, U>, dim3((p.spans + s.slots - 1) / s.slots, s.slices), s.threads, 0, st, true, p);
 }
 
 }  // namespace
@@ -444,13 +454,11 @@ extern "C" hq_status hq_embedding(const void* ids, int id_bytes, int64_t tokens,
     if (ids == nullptr) return HQ_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(ids) % uintptr_t(id_bytes) != 0) return HQ_ERR_ALIGNMENT;
     if ((e = check_rows(table, ld_table, dim, tdt)) != HQ_OK || (e = check_rows(out, ld_out, dim, odt)) != HQ_OK) return e;
-    const LookupParams p{ids, table, out, classes, ld_table, ld_out, uint32_t(tokens), int(dim / 8), scale};
-    const int64_t slots = p.vectors > 256 ? 1 : 256 / p.vectors, ctas = (tokens + slots - 1) / slots, most = int64_t(sm_count()) * 4;
-    const dim3 grid(unsigned(ctas < most ? ctas : most), unsigned((p.vectors + 255) / 256));
+    const LookupParams p{ids, table, out, pitch_of(ld_table, tdt), pitch_of(ld_out, odt), uint32_t(classes), uint32_t(tokens), int(dim / 8), scale};
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t c;
-    if (tdt == HQ_BF16) c = odt == HQ_BF16 ? launch_lookup<__nv_bfloat16, __nv_bfloat16>(p, id_bytes, grid, st) : launch_lookup<__nv_bfloat16, float>(p, id_bytes, grid, st);
-    else c = odt == HQ_BF16 ? launch_lookup<float, __nv_bfloat16>(p, id_bytes, grid, st) : launch_lookup<float, float>(p, id_bytes, grid, st);
+    if (tdt == HQ_BF16) c = odt == HQ_BF16 ? launch_lookup<__nv_bfloat16, __nv_bfloat16>(p, id_bytes, st) : launch_lookup<__nv_bfloat16, float>(p, id_bytes, st);
+    else c = odt == HQ_BF16 ? launch_lookup<float, __nv_bfloat16>(p, id_bytes, st) : launch_lookup<float, float>(p, id_bytes, st);
     return c == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }
 
@@ -480,11 +488,12 @@ extern "C" hq_status hq_embedding_bwd(const void* ids, int id_bytes, int64_t tok
     char* ws = static_cast<char*>(workspace);
     auto words = [&](size_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
     GradParams p{};
-    p.ids = ids; p.dout = dout; p.base = base; p.dtable = dtable; p.ld_dout = ld_dout; p.ld_base = ld_base; p.ld_dtable = ld_dtable; p.classes = classes;
+    p.ids = ids; p.dout = dout; p.base = base; p.dtable = dtable; p.classes = uint32_t(classes);
+    p.ld_dout = tokens > 0 ? pitch_of(ld_dout, ddt) : 0; p.ld_base = base != nullptr ? pitch_of(ld_base, gdt) : 0; p.ld_dtable = pitch_of(ld_dtable, gdt);
     p.tokens = uint32_t(tokens); p.slice = a.slice; p.span = a.span; p.longest = a.longest; p.spans = a.spans; p.vectors = int(dim / 8); p.half = gdt == HQ_BF16;
     p.in_place = base == dtable; p.fill_first = tokens < classes; p.scale = scale;
     p.found = reinterpret_cast<uint2*>(ws); p.sorted = reinterpret_cast<uint2*>(ws + a.sorted);
-    p.start = words(a.start); p.longs = words(a.longs); p.long_count = words(a.long_count); p.parts = reinterpret_cast<float*>(ws + a.parts);
+    p.start = words(a.start); p.longs = reinterpret_cast<uint4*>(ws + a.longs); p.long_count = words(a.long_count); p.parts = reinterpret_cast<float*>(ws + a.parts);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const size_t smem = size_t(kOrderWarps) * a.slice * sizeof(uint32_t);
     void (*order)(GradParams) = id_bytes == 4 ? embedding_order_kernel<int32_t> : embedding_order_kernel<int64_t>;
@@ -492,11 +501,9 @@ extern "C" hq_status hq_embedding_bwd(const void* ids, int id_bytes, int64_t tok
     order<<<a.slices, kOrderThreads, smem, st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return HQ_ERR_CUDA;
     if (tokens == 0) return HQ_OK;
-    const int slots = p.vectors > 256 ? 1 : 256 / p.vectors;
-    const dim3 grid((a.spans + slots - 1) / slots, unsigned((p.vectors + 255) / 256));
     cudaError_t c;
-    if (ddt == HQ_BF16) c = gdt == HQ_BF16 ? launch_sums<__nv_bfloat16, __nv_bfloat16>(p, grid, st) : launch_sums<__nv_bfloat16, float>(p, grid, st);
-    else c = gdt == HQ_BF16 ? launch_sums<float, __nv_bfloat16>(p, grid, st) : launch_sums<float, float>(p, grid, st);
+    if (ddt == HQ_BF16) c = gdt == HQ_BF16 ? launch_sums<__nv_bfloat16, __nv_bfloat16>(p, st) : launch_sums<__nv_bfloat16, float>(p, st);
+    else c = gdt == HQ_BF16 ? launch_sums<float, __nv_bfloat16>(p, st) : launch_sums<float, float>(p, st);
     if (c != cudaSuccess) return HQ_ERR_CUDA;
     if (tokens <= int64_t(p.longest)) return HQ_OK;            // no id has more tokens than one span takes
     const dim3 join(a.slices, unsigned((dim + 63) / 64));

@@ -11,7 +11,7 @@
 //   dgate[n] = sum d t,  dweight[n] = sum dy xh,  dbias[n] = sum dy,  dpost_weight = sum gate d hh over all rows
 //
 // Memory-bound: every row is read and written once, the vectors come from the caches once for a run of rows.  A team of ceil(cols / 256)
-// warps takes a run of rows, 8 columns a thread.  Rows are copied ahead into shared memory, by each thread for itself (no barrier stands
+// warps, a CTA of its own, takes a run of rows, 8 columns a thread.  Rows are copied ahead into shared memory, by each thread for itself (no barrier stands
 // between the copy and its use, and no register holds what is on the way); two rows are computed together, so that their sums share the
 // shuffles; sums over rows stay in the registers of the thread that owns the columns.
 #include "hq_common.cuh"
@@ -76,7 +76,7 @@ struct Walk {
 };
 
 // ---- a team, and its exchange of sums: two buffers in turn, so that one barrier stands between the writes and the reads of an exchange and
-// none behind it.  Teams of several warps are CTAs of their own, teams of one warp need no barrier. ----
+// none behind it. ----
 struct Team {
     int lane, warp, warps, c0, cols;
     bool col;                                      // the thread has columns
@@ -88,7 +88,7 @@ __device__ __forceinline__ Team team_of(const GateNormParams& p, float2* room) {
     Team t;
     t.lane = int(threadIdx.x & 31);
     t.warps = p.warps;
-    t.warp = p.warps == 1 ? 0 : int(threadIdx.x >> 5);
+    t.warp = int(threadIdx.x >> 5);
     t.c0 = (t.warp * 32 + t.lane) * 8;
     t.cols = p.cols;
     t.col = t.c0 < p.cols;
@@ -98,9 +98,6 @@ __device__ __forceinline__ Team team_of(const GateNormParams& p, float2* room) {
     t.room = room;
     t.turn = 0;
     return t;
-}
-__device__ __forceinline__ uint32_t team_index(const GateNormParams& p) {
-    return p.warps == 1 ? blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
 }
 __device__ __forceinline__ float sum8(const f32x2 (&v)[4]) { return pair_sum(add2(add2(v[0], v[1]), add2(v[2], v[3]))); }
 __device__ __forceinline__ float xor_add(float x, int off) { return x + __shfl_xor_sync(0xffffffffu, x, off); }
@@ -214,7 +211,7 @@ __device__ __forceinline__ void send(uint32_t at, const char* from, uint32_t ld,
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
         const bool live = i < b.live;
-        const char* row = from + row_at(live ? b.row + i : b.row, ld);
+        const char* row = from + row_at(b.row, ld) + (live ? uint32_t(i) * uint64_t(ld) : 0u);
         if constexpr (sizeof(T) == 2) {
             copy_ahead(at + uint32_t(i) * plane + threadIdx.x * 16u, t.col ? row : row - t.c0 * 2, live && t.col);
         } else {
@@ -256,9 +253,18 @@ __device__ __forceinline__ void clear_dead(const Walk& b, f32x2 (&v)[kRows][4]) 
 }
 template <typename T>
 __device__ __forceinline__ void put(char* to, uint32_t ld, const Walk& b, const Team& t, const f32x2 (&v)[kRows][4]) {
-    if (!t.col) return;
-    Vec8<T>::store_wide(to + row_at(b.row, ld), 0, v[0]);      // a batch has a row
-    if (b.n > 1) Vec8<T>::store_wide(to + row_at(b.row + 1, ld), 0, v[1]);
+    char* row = to + row_at(b.row, ld);            // a batch has a row
+    if (t.col) Vec8<T>::store_wide(row, 0, v[0]);
+    if (t.col && b.n > 1) Vec8<T>::store_wide(row + ld, 0, v[1]);
+}
+
+template <typename T>
+__device__ __forceinline__ void put_zeros(char* to, const MatrixOut& m, const Walk& b, const Team& t) {
+    if (m.p == nullptr) return;
+    f32x2 v[kRows][4];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) fill(v[i], 0.f);
+    put<T>(to, m.ld, b, t, v);
 }
 
 // Batches on their way: what keeps about 40 KB an SM in flight at 15 warps and more.
@@ -274,8 +280,7 @@ __global__ void __maxnreg__(96) gate_norm_kernel(const GateNormParams p) {
     __shared__ float2 room[2 * 32];
     constexpr int kStages = kForwardStages;
     Team t = team_of(p, room);
-    const uint32_t r0 = team_index(p) * p.chunk, r1 = min(r0 + p.chunk, p.rows);
-    if (r0 >= r1) return;
+    const uint32_t r0 = blockIdx.x * p.chunk, r1 = min(r0 + p.chunk, p.rows);
     const uint32_t plane = blockDim.x * 16u, batch = plane * kForwardPlanes<S, B>, h_at = plane * kRows * kPlanes<S>;
     const uint32_t base = smem_u32(ring);
     const bool branch = p.h.p != nullptr, normed = p.y.p != nullptr;
@@ -309,6 +314,15 @@ __global__ void __maxnreg__(96) gate_norm_kernel(const GateNormParams p) {
             loaded = b.g;
         }
         copies_wait<kStages - 2>();
+        if (b.live == 0) {                         // nothing but zeros to write
+            put_zeros<S>(x_out, p.x_out, b, t);
+            put_zeros<B>(y, p.y, b, t);
+            if (p.stats != nullptr && threadIdx.x < unsigned(b.n)) reinterpret_cast<float4*>(p.stats)[b.row + threadIdx.x] = make_float4(0.f, 0.f, 0.f, 0.f);
+            send_next();
+            at = at == base + (kStages - 1) * batch ? base : at + batch;
+            b.next(p, r1);
+            continue;
+        }
         f32x2 v[kRows][4];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) take<S>(v[i], at, i);
@@ -364,9 +378,8 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
     extern __shared__ uint4 ring[];
     __shared__ float2 room[2 * 32];
     Team t = team_of(p, room);
-    const uint32_t team = team_index(p), r0 = team * p.chunk, r1 = min(r0 + p.chunk, p.rows);
+    const uint32_t team = blockIdx.x, r0 = team * p.chunk, r1 = min(r0 + p.chunk, p.rows);
     griddep_launch();                              // all teams are at work at once: the joining kernel takes no place of theirs
-    if (r0 >= r1) return;
     const uint32_t plane = blockDim.x * 16u, batch = plane * kGradPlanes<S, B>, s_size = plane * kRows * kPlanes<S>, b_size = plane * kRows * kPlanes<B>;
     const uint32_t base = smem_u32(ring), y_at = s_size, d_at = s_size + b_size, h_at = 2 * s_size + b_size;
     const bool normed = p.dy.p != nullptr, gated = p.dgate.p != nullptr, later = p.dx_out.p != nullptr, branch = POST || gated;       // h itself is read
@@ -408,102 +421,107 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
         __syncwarp();                              // no lane of the warp still reads the batch before this one
         send_next();                               // into its place
         copies_wait<kStages - 1>();
-        f32x2 d[kRows][4];
-        if (normed) {
-            f32x2 xh[kRows][4];
-            float2 s[kRows];
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                const f32x2 less = pk2(-stats[i].x, -stats[i].x), inv = pk2(stats[i].y, stats[i].y);
-                f32x2 a = pk2(0.f, 0.f), c = pk2(0.f, 0.f);
-                take<S>(xh[i], at, i);
-                take<B>(d[i], at + y_at, i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    xh[i][e] = mul2(add2(xh[i][e], less), inv);
-                    dbias[e] = add2(dbias[e], d[i][e]);
-                    dweight[e] = fma2(d[i][e], xh[i][e], dweight[e]);
-                    d[i][e] = mul2(d[i][e], weight[e]);
-                    a = add2(a, d[i][e]);
-                    c = fma2(d[i][e], xh[i][e], c);
-                }
-                s[i] = t.col ? make_float2(pair_sum(a), pair_sum(c)) : make_float2(0.f, 0.f);
-            }
-            team_sums(t, s[0], s[1]);
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                const float mg = p.layer ? -s[i].x * t.per_row : 0.f, mx = -s[i].y * t.per_row;
-                const f32x2 inv = pk2(stats[i].y, stats[i].y), g2 = pk2(mg, mg), x2 = pk2(mx, mx);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) d[i][e] = mul2(inv, fma2(xh[i][e], x2, add2(d[i][e], g2)));
-            }
+        if (b.live == 0) {                         // nothing but zeros to write
+            put_zeros<S>(dx, p.dx, b, t);
+            put_zeros<B>(dh, p.dh, b, t);
         } else {
+            f32x2 d[kRows][4];
+            if (normed) {
+                f32x2 xh[kRows][4];
+                float2 s[kRows];
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) fill(d[i], 0.f);
-        }
-        if (later) {
+                for (int i = 0; i < kRows; ++i) {
+                    const f32x2 less = pk2(-stats[i].x, -stats[i].x), inv = pk2(stats[i].y, stats[i].y);
+                    f32x2 a = pk2(0.f, 0.f), c = pk2(0.f, 0.f);
+                    take<S>(xh[i], at, i);
+                    take<B>(d[i], at + y_at, i);
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                f32x2 o[4];
-                take<S>(o, at + d_at, i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) d[i][e] = add2(d[i][e], o[e]);
-            }
-        }
-        if (p.dx.p != nullptr) {
-            const f32x2 residual = pk2(p.residual, p.residual);
-            f32x2 o[kRows][4];
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[i][e] = mul2(residual, d[i][e]);
-            }
-            clear_dead(b, o);
-            put<S>(dx, p.dx.ld, b, t, o);
-        }
-        if (POST) {
-            f32x2 hh[kRows][4];
-            float2 s[kRows];
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                const f32x2 less = pk2(-stats[i].z, -stats[i].z), inv = pk2(stats[i].w, stats[i].w);
-                f32x2 a = pk2(0.f, 0.f), c = pk2(0.f, 0.f);
-                take<B>(hh[i], at + h_at, i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    hh[i][e] = mul2(add2(hh[i][e], less), inv);
-                    dgate[e] = fma2(d[i][e], hh[i][e], dgate[e]);              // both sums' part: dgate is post_weight times it, dpost gate times it
-                    d[i][e] = mul2(mul2(d[i][e], gate[e]), post_weight[e]);
-                    a = add2(a, d[i][e]);
-                    c = fma2(d[i][e], hh[i][e], c);
+                    for (int e = 0; e < 4; ++e) {
+                        xh[i][e] = mul2(add2(xh[i][e], less), inv);
+                        dbias[e] = add2(dbias[e], d[i][e]);
+                        dweight[e] = fma2(d[i][e], xh[i][e], dweight[e]);
+                        d[i][e] = mul2(d[i][e], weight[e]);
+                        a = add2(a, d[i][e]);
+                        c = fma2(d[i][e], xh[i][e], c);
+                    }
+                    s[i] = t.col ? make_float2(pair_sum(a), pair_sum(c)) : make_float2(0.f, 0.f);
                 }
-                s[i] = t.col ? make_float2(pair_sum(a), pair_sum(c)) : make_float2(0.f, 0.f);
-            }
-            if (p.dh.p != nullptr) {
                 team_sums(t, s[0], s[1]);
 #pragma unroll
                 for (int i = 0; i < kRows; ++i) {
-                    const float mg = p.post_layer ? -s[i].x * t.per_row : 0.f, mx = -s[i].y * t.per_row;
-                    const f32x2 inv = pk2(stats[i].w, stats[i].w), g2 = pk2(mg, mg), x2 = pk2(mx, mx);
+                    const float mg = p.layer ? -s[i].x * t.per_row : 0.f, mx = -s[i].y * t.per_row;
+                    const f32x2 inv = pk2(stats[i].y, stats[i].y), g2 = pk2(mg, mg), x2 = pk2(mx, mx);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) d[i][e] = mul2(inv, fma2(hh[i][e], x2, add2(d[i][e], g2)));
+                    for (int e = 0; e < 4; ++e) d[i][e] = mul2(inv, fma2(xh[i][e], x2, add2(d[i][e], g2)));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) fill(d[i], 0.f);
+            }
+            if (later) {
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    f32x2 o[4];
+                    take<S>(o, at + d_at, i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) d[i][e] = add2(d[i][e], o[e]);
                 }
             }
-        } else {
+            if (p.dx.p != nullptr) {
+                const f32x2 residual = pk2(p.residual, p.residual);
+                f32x2 o[kRows][4];
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                f32x2 o[4];
-                if (gated) take<B>(o, at + h_at, i);
+                for (int i = 0; i < kRows; ++i) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (gated) dgate[e] = fma2(d[i][e], o[e], dgate[e]);
-                    d[i][e] = mul2(d[i][e], gate[e]);
+                    for (int e = 0; e < 4; ++e) o[i][e] = mul2(residual, d[i][e]);
+                }
+                clear_dead(b, o);
+                put<S>(dx, p.dx.ld, b, t, o);
+            }
+            if (POST) {
+                f32x2 hh[kRows][4];
+                float2 s[kRows];
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    const f32x2 less = pk2(-stats[i].z, -stats[i].z), inv = pk2(stats[i].w, stats[i].w);
+                    f32x2 a = pk2(0.f, 0.f), c = pk2(0.f, 0.f);
+                    take<B>(hh[i], at + h_at, i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        hh[i][e] = mul2(add2(hh[i][e], less), inv);
+                        dgate[e] = fma2(d[i][e], hh[i][e], dgate[e]);              // both sums' part: dgate is post_weight times it, dpost gate times it
+                        d[i][e] = mul2(mul2(d[i][e], gate[e]), post_weight[e]);
+                        a = add2(a, d[i][e]);
+                        c = fma2(d[i][e], hh[i][e], c);
+                    }
+                    s[i] = t.col ? make_float2(pair_sum(a), pair_sum(c)) : make_float2(0.f, 0.f);
+                }
+                if (p.dh.p != nullptr) {
+                    team_sums(t, s[0], s[1]);
+#pragma unroll
+                    for (int i = 0; i < kRows; ++i) {
+                        const float mg = p.post_layer ? -s[i].x * t.per_row : 0.f, mx = -s[i].y * t.per_row;
+                        const f32x2 inv = pk2(stats[i].w, stats[i].w), g2 = pk2(mg, mg), x2 = pk2(mx, mx);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) d[i][e] = mul2(inv, fma2(hh[i][e], x2, add2(d[i][e], g2)));
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    f32x2 o[4];
+                    if (gated) take<B>(o, at + h_at, i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (gated) dgate[e] = fma2(d[i][e], o[e], dgate[e]);
+                        d[i][e] = mul2(d[i][e], gate[e]);
+                    }
                 }
             }
-        }
-        if (p.dh.p != nullptr) {
-            clear_dead(b, d);
-            put<B>(dh, p.dh.ld, b, t, d);
+            if (p.dh.p != nullptr) {
+                clear_dead(b, d);
+                put<B>(dh, p.dh.ld, b, t, d);
+            }
         }
         at = at == base + (kStages - 1) * batch ? base : at + batch;
         const uint32_t g = b.g, done = b.row + uint32_t(b.n);
@@ -536,58 +554,50 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
     if (POST && p.dpost != nullptr && t.col) Vec8<float>::store_wide(p.post_parts, int64_t(team) * p.cols + t.c0, dpost);
 }
 
-// The parts of groups that several teams took, joined in order, and dpost_weight's.  blockIdx.x: `wide` columns; y: a group, or, where there
-// are more groups than teams, the group at a border of two teams' rows, which the first border inside it takes; the last y: dpost_weight.
-// Thread = (4 columns, every 1024 / wide'th part).
-__global__ void __launch_bounds__(256) gate_norm_sums_kernel(const GateNormParams p, uint32_t teams, int group_wide, int post_wide, int by_group, uint32_t heads) {
+// The parts of groups that several teams took, joined in order, and dpost_weight's.  blockIdx.x: heads x `wide` columns of a group (head: the
+// group itself, or, where there are more groups than teams, the group at a border of two teams' rows, which the first border inside it takes),
+// then the columns of dpost_weight.  Thread = (4 columns, every 1024 / wide'th part).
+struct Joins { uint32_t teams, heads, group_ctas, post_ctas; int wide, post_wide, by_group; };         // CTAs: of a head, of dpost_weight
+__device__ __forceinline__ float4 plus(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+__global__ void __launch_bounds__(256) gate_norm_sums_kernel(const GateNormParams p, const Joins j) {
     __shared__ float4 sums[3][256];
-    const bool post = blockIdx.y == heads;
-    const int wide = post ? post_wide : group_wide, lanes = wide / 4, ways = 256 / lanes, way = int(threadIdx.x) / lanes, mine = int(threadIdx.x) - way * lanes;
-    const int c = int(blockIdx.x) * wide + mine * 4;
-    if (int(blockIdx.x) * wide >= p.cols) return;
-    uint32_t g = 0, from = 0, to = teams - 1;
+    const uint32_t head = blockIdx.x / j.group_ctas;
+    const bool post = head >= j.heads;
+    const int wide = post ? j.post_wide : j.wide, lanes = wide / 4, ways = 256 / lanes, way = int(threadIdx.x) / lanes, mine = int(threadIdx.x) - way * lanes;
+    const int c = int(blockIdx.x - (post ? j.heads : head) * j.group_ctas) * wide + mine * 4;
+    uint32_t g = 0, from = 0, to = j.teams - 1;
     bool second = false;
     if (!post) {
-        g = by_group ? blockIdx.y : (blockIdx.y + 1) * p.chunk / p.group;
+        g = j.by_group ? head : (head + 1) * p.chunk / p.group;
         const uint32_t first = g * p.group, last = (p.rows - first > p.group ? first + p.group : p.rows) - 1;
         from = first / p.chunk;
         to = last / p.chunk;
-        if (from == to || (!by_group && from != blockIdx.y)) return;
+        if (from == to || (!j.by_group && from != head)) return;
         second = first != from * p.chunk;          // the group is not the one of that team's first row
     }
-    const bool want[3] = {post || p.dweight.p != nullptr, !post && p.dbias.p != nullptr, !post && p.dgate.p != nullptr};
-    float4 sum[3];
-#pragma unroll
-    for (int k = 0; k < 3; ++k) sum[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    const bool want0 = post || p.dweight.p != nullptr, want1 = !post && p.dbias.p != nullptr, want2 = !post && p.dgate.p != nullptr;
+    float4 sum0 = make_float4(0.f, 0.f, 0.f, 0.f), sum1 = sum0, sum2 = sum0;
     griddep_wait();                                // the parts; no CTA that writes ends before the kernel in front has
     if (c < p.cols) {
         const float* parts = post ? p.post_parts + c : p.parts + c;
         const int64_t step = post ? p.cols : int64_t(6) * p.cols;
 #pragma unroll 4
         for (uint32_t i = from + way; i <= to; i += ways) {
-            const float* part = parts + i * step + (second && i == from ? 3 * p.cols : 0);
-#pragma unroll
-            for (int k = 0; k < 3; ++k)
-                if (want[k]) {
-                    const float4 v = ld_dependent_cg(reinterpret_cast<const float4*>(part + k * p.cols));
-                    sum[k].x += v.x; sum[k].y += v.y; sum[k].z += v.z; sum[k].w += v.w;
-                }
+            const float4* part = reinterpret_cast<const float4*>(parts + i * step + (second && i == from ? 3 * p.cols : 0));
+            if (want0) sum0 = plus(sum0, ld_dependent_cg(part));
+            if (want1) sum1 = plus(sum1, ld_dependent_cg(part + p.cols / 4));
+            if (want2) sum2 = plus(sum2, ld_dependent_cg(part + p.cols / 2));
         }
     }
-#pragma unroll
-    for (int k = 0; k < 3; ++k) sums[k][threadIdx.x] = sum[k];
+    sums[0][threadIdx.x] = sum0; sums[1][threadIdx.x] = sum1; sums[2][threadIdx.x] = sum2;
     __syncthreads();
-    if (way >= 3) return;                          // thread = (4 columns, sum): the ways in order
-    for (int k = way; k < 3; k += ways) {
-        if (!want[k] || c >= p.cols) continue;
+    for (int k = way; k < 3; k += ways) {          // thread = (4 columns, sum): the ways in order
+        if (c >= p.cols || !(k == 0 ? want0 : k == 1 ? want1 : want2)) continue;
         float4 s = sums[k][mine];
-        for (int w = 1; w < ways; ++w) {
-            const float4 v = sums[k][w * lanes + mine];
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
+        for (int w = 1; w < ways; ++w) s = plus(s, sums[k][w * lanes + mine]);
         if (k == 2 && p.post_weight != nullptr) {
             const float4 v = *reinterpret_cast<const float4*>(p.post_weight + c);
-            s.x *= v.x; s.y *= v.y; s.z *= v.z; s.w *= v.w;
+            s = make_float4(s.x * v.x, s.y * v.y, s.z * v.z, s.w * v.w);
         }
         float* out = post ? p.dpost : k == 0 ? p.dweight.p + g * p.dweight.ld : k == 1 ? p.dbias.p + g * p.dbias.ld : p.dgate.p + g * p.dgate.ld;
         *reinterpret_cast<float4*>(out + c) = s;
@@ -602,13 +612,6 @@ int64_t grad_chunk(int64_t rows, int64_t cols) {
     const int64_t teams = kGradWarps / team_warps(cols), chunk = (rows + teams - 1) / teams;
     return chunk < 2 * kRows ? 2 * kRows : chunk;
 }
-// CTAs and their size for this many teams: teams of one warp share a CTA.
-struct Launch { unsigned grid, threads; };
-Launch launch_of(int64_t teams, int warps) {
-    if (warps > 1) return Launch{unsigned(teams), unsigned(warps * 32)};
-    return Launch{unsigned((teams + 7) / 8), 256u};
-}
-
 hq_status check_matrix(const void* x, int64_t ld, int64_t cols, hq_dtype dt) {
     if (x == nullptr) return HQ_ERR_INVALID_ARG;
     if (ld < cols) return HQ_ERR_SHAPE;
@@ -639,6 +642,7 @@ hq_status check_sizes(hq_dtype xdt, hq_dtype hdt, int64_t rows, int64_t cols, in
     return HQ_OK;
 }
 
+struct Launch { unsigned grid, threads; };
 cudaError_t launch_kernel(void (*kern)(GateNormParams), const GateNormParams& p, Launch l, int planes, int stages, cudaStream_t st) {
     const size_t smem = size_t(planes) * stages * l.threads * 16;
     const cudaError_t e = smem <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
@@ -694,7 +698,7 @@ extern "C" hq_status hq_gate_norm(const void* x, int64_t ldx, hq_dtype xdt, cons
     const int64_t fit = int64_t(kMostShared / (size_t(planes) * kForwardStages * p.warps * 32 * 16)), by_warps = 20 / p.warps;
     const int64_t most = int64_t(sm_count()) * (fit < by_warps ? fit : by_warps), chunk = (rows + most - 1) / most;
     p.chunk = uint32_t(chunk < kRows ? kRows : chunk);
-    const Launch l = launch_of((rows + p.chunk - 1) / p.chunk, p.warps);
+    const Launch l{unsigned((rows + p.chunk - 1) / p.chunk), unsigned(p.warps * 32)};
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool after = post != HQ_NORM_NONE;
     cudaError_t c;
@@ -770,18 +774,21 @@ extern "C" hq_status hq_gate_norm_bwd(const void* x_out, int64_t ldx_out, hq_dty
     p.dpost = dpost_weight;
     p.parts = split ? static_cast<float*>(workspace) : nullptr;
     p.post_parts = static_cast<float*>(workspace) + size_t(teams) * 6 * cols;
-    const Launch l = launch_of(teams, p.warps);
+    const Launch l{unsigned(teams), unsigned(p.warps * 32)};
     cudaError_t c;
     if (xdt == HQ_BF16) c = hdt == HQ_BF16 ? launch_grad<__nv_bfloat16, __nv_bfloat16>(p, after, l, st) : launch_grad<__nv_bfloat16, float>(p, after, l, st);
     else c = hdt == HQ_BF16 ? launch_grad<float, __nv_bfloat16>(p, after, l, st) : launch_grad<float, float>(p, after, l, st);
     if (c != cudaSuccess) return HQ_ERR_CUDA;
     if (!split && dpost_weight == nullptr) return HQ_OK;
-    const int by_group = groups < teams;
-    const uint32_t heads = !split ? 0u : uint32_t(by_group ? groups : teams - 1);
+    Joins j{};
+    j.teams = uint32_t(teams);
+    j.by_group = groups < teams;
+    j.heads = !split ? 0u : uint32_t(j.by_group ? groups : teams - 1);
     // columns a CTA: as many as leave a thread two parts or more
     auto wide_for = [](int64_t parts) { int wide = 1024; while (wide > 32 && parts > 1024 / wide * 2) wide /= 2; return wide; };
-    const int wide = wide_for(p.group / p.chunk + 2), post_wide = wide_for(teams), least = dpost_weight != nullptr && post_wide < wide ? post_wide : wide;
-    const dim3 few(unsigned((cols + least - 1) / least), heads + (dpost_weight != nullptr ? 1u : 0u));
-    return launch_dependent(gate_norm_sums_kernel, few, 256, 0, st, true, p, uint32_t(teams), wide, post_wide, by_group, heads) == cudaSuccess
-               ? HQ_OK : HQ_ERR_CUDA;
+    j.wide = wide_for(p.group / p.chunk + 2);
+    j.post_wide = wide_for(teams);
+    j.group_ctas = uint32_t((cols + j.wide - 1) / j.wide);
+    j.post_ctas = dpost_weight != nullptr ? uint32_t((cols + j.post_wide - 1) / j.post_wide) : 0u;
+    return launch_dependent(gate_norm_sums_kernel, dim3(j.heads * j.group_ctas + j.post_ctas), 256, 0, st, true, p, j) == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }
