@@ -6,8 +6,8 @@
 // Memory-bound: the lookup reads ids and rows and writes rows; the gradient reads every token's row once and writes every row of the table once.
 //
 // The gradient has three kernels.  (1) order: CTA b owns a slice of the ids, reads all ids once, keeps the tokens of its slice in their order
-// and counts those of smaller ids (where its part of the sorted order begins), then sorts its tokens by id with one stable counting sort:
-// no atomics, so the order is the same on every run.  It writes its slice's rows of the table that have no tokens, too: all of them in front of
+// and counts those of smaller ids (where its part of the sorted order begins), then sorts its tokens by id with one stable counting sort, a
+// warp's run of tokens after the other's: no atomics, so the order is the same on every run.  It writes its slice's rows of the table that have no tokens, too: all of them in front of
 // the rest, while the memory is idle, where the tokens are fewer than the ids.  (2) sums: the sorted tokens are cut into spans of equal length,
 // whatever ids they hold (most tokens may be of one id); a team of threads adds up a span's rows with several rows in flight and writes a row of
 // the table whenever the id changes.  An id of up to `longest` tokens belongs to the span of its first one; the sums of a longer one go to the
@@ -80,18 +80,19 @@ __global__ void __launch_bounds__(256) embedding_kernel(const LookupParams p) {
 constexpr int kOrderThreads = 1024;
 constexpr int kOrderWarps = kOrderThreads / 32;
 constexpr int kSlice = kOrderThreads;              // ids a CTA of the order at most: a thread each in the scan, 128 KB of counters
+constexpr int kKept = 768;                         // tokens of its slice that a warp keeps in shared memory at most (16 bits of id, 32 of token)
 
 struct GradParams {
     const void* ids;
     const void *dout, *base;
     void* dtable;
     uint32_t ld_dout, ld_base, ld_dtable;          // pitches in bytes
-    uint32_t classes, tokens, slice;               // slice: ids of an order CTA
+    uint32_t classes, tokens, slice, kept;         // slice: ids of an order CTA; kept: tokens that each of its warps has room for
     uint32_t span, longest, spans;                 // positions of a span; tokens of the longest id that one span takes whole
     int vectors, half;                             // half: dtable is bf16
     bool in_place, fill_first;
     float scale;
-    uint2 *found, *sorted;                         // [tokens] (id in the slice, token) as found; (id, token) by id
+    uint2* sorted;                                 // [tokens] (id, token) by id
     uint32_t* start;                               // [classes + 1] first position of each id
     uint4* longs;                                  // (id, first position, end) of ids of more than `longest` tokens: slice s has
     uint32_t* long_count;                          // long_count[s] from its first position / longest + s on
@@ -100,9 +101,7 @@ struct GradParams {
 
 __device__ __forceinline__ uint32_t lanes_below() { uint32_t m; asm("mov.u32 %0, %%lanemask_lt;" : "=r"(m)); return m; }
 
-__device__ __forceinline__ uint32_t from_lane0(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
-
-// Exclusive sum of x over the CTA's threads; *total is the whole.  One barrier in front of its use of `room` and one behind.
+// Exclusive sum of x over the CTA's threads; *total is the whole.  One barrier in front of its use of `room` and one before it is read.
 __device__ __forceinline__ uint32_t exclusive_sum(uint32_t x, uint32_t* room, uint32_t* total) {
     const int lane = int(threadIdx.x & 31), warp = int(threadIdx.x >> 5);
     uint32_t sum = x;
@@ -141,105 +140,160 @@ __device__ __forceinline__ void fill_rows(const GradParams& p, uint32_t v0, uint
     }
 }
 
+// Four ids from token t on, of a run that ends at `end`; `wide`: 16-byte loads.
+template <typename I>
+__device__ __forceinline__ void four_ids(uint32_t (&id)[4], const void* ids, uint32_t t, uint32_t end, bool wide) {
+    if (sizeof(I) == 4 && wide && t + 4 <= end) {
+        const int4 v = __ldg(reinterpret_cast<const int4*>(static_cast<const int32_t*>(ids) + t));
+        id[0] = uint32_t(v.x); id[1] = uint32_t(v.y); id[2] = uint32_t(v.z); id[3] = uint32_t(v.w);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) id[k] = t + k < end ? id_at<I>(ids, t + k) : 0xffffffffu;
+    }
+}
+
+// The same with zeros for every row, by bulk copies of the zeros in shared memory, beside what the warps do (as stores they stand in the way of
+// the ids' loads: 32768 x 768 rows of bf16 6 us).  The issuing lanes wait for them before the CTA ends.
+constexpr uint32_t kZeros = 4096;                  // bytes
+__device__ __forceinline__ void zero_rows(const GradParams& p, uint32_t v0, uint32_t size, const uint4* zeros) {
+    const uint32_t row_bytes = uint32_t(p.vectors) * (p.half ? 16u : 32u);
+    char* first = static_cast<char*>(p.dtable) + uint64_t(v0) * p.ld_dtable;
+    // rows without gaps are one line
+    const uint64_t line = p.ld_dtable == row_bytes ? uint64_t(size) * row_bytes : row_bytes;
+    const uint32_t lines = p.ld_dtable == row_bytes ? 1u : size, pieces = uint32_t((line + kZeros - 1) / kZeros);
+    for (uint32_t i = threadIdx.x & 31; i < lines * pieces; i += 32) {
+        const uint32_t r = i / pieces;
+        const uint64_t at = uint64_t(i - r * pieces) * kZeros;
+        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
+                     ::"l"(first + uint64_t(r) * p.ld_dtable + at), "r"(smem_u32(zeros)), "r"(uint32_t(min(line - at, uint64_t(kZeros)))) : "memory");
+    }
+    bulk_commit_group();
+}
+
 template <typename I>
 __global__ void __launch_bounds__(kOrderThreads) embedding_order_kernel(const GradParams p) {
-    extern __shared__ uint32_t counts[];           // [warp][id of the slice]
+    extern __shared__ uint32_t counts[];           // [warp][id of the slice], then [warp][kept] tokens and [warp][kept] ids in the slice
     __shared__ uint32_t room[kOrderWarps], offset[kSlice];
-    constexpr int kAhead = 8;
+    __shared__ __align__(128) uint4 zeros[kZeros / 16];
     const int lane = int(threadIdx.x & 31), warp = int(threadIdx.x >> 5);
     const uint32_t v0 = blockIdx.x * p.slice, v1 = min(v0 + p.slice, p.classes), size = v1 - v0;
+    uint32_t* count = counts + uint32_t(warp) * size;
+    uint32_t* kept = counts + kOrderWarps * p.slice + uint32_t(warp) * p.kept;
+    uint16_t* kept_id = reinterpret_cast<uint16_t*>(counts + kOrderWarps * (p.slice + p.kept)) + uint32_t(warp) * p.kept;
     griddep_launch();                              // the sums' CTAs find room as these end
-    if (!p.in_place && p.fill_first) fill_rows(p, v0, size, nullptr);
-    // a warp's run of ids, read twice: how many are of the slice and how many smaller; then where they go
-    const uint32_t run = (p.tokens + kOrderThreads - 1) / kOrderThreads * 32, from = min(uint32_t(warp) * run, p.tokens), to = min(from + run, p.tokens);
-    uint32_t mine = 0, less = 0;
-    for (uint32_t t0 = from + lane; t0 < to; t0 += 32 * kAhead) {
-        uint32_t id[kAhead];
+    const bool zeroing = p.base == nullptr && p.fill_first;
+    if (zeroing) {
+        if (threadIdx.x < kZeros / 16) zeros[threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
+        fence_proxy_async_smem();
+        __syncthreads();
+        if (warp == 0) zero_rows(p, v0, size, zeros);
+    } else if (!p.in_place && p.fill_first) {
+        fill_rows(p, v0, size, nullptr);
+    }
+    for (uint32_t i = lane; i < size; i += 32) count[i] = 0;
+    // a warp's run of ids: how many are smaller than the slice's, how many are of it, and which, as far as there is room
+    const uint32_t run = (p.tokens + 32 * 128 - 1) / (32 * 128) * 128, from = min(uint32_t(warp) * run, p.tokens), to = min(from + run, p.tokens);
+    const bool wide = (reinterpret_cast<uintptr_t>(p.ids) & 15u) == 0;
+    uint32_t less = 0, mine = 0;                   // mine: the warp's, the same in every lane
+    constexpr int kAhead = 4;
+    for (uint32_t t0 = from + lane * 4; t0 < to + lane * 4; t0 += 128 * kAhead) {              // the same number of steps in every lane
+        uint32_t id[kAhead][4];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) id[u] = t0 + 32 * u < to ? id_at<I>(p.ids, t0 + 32 * u) : 0xffffffffu;
+        for (int u = 0; u < kAhead; ++u) four_ids<I>(id[u], p.ids, t0 + 128 * u, to, wide);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            less += id[u] < v0;
-            mine += id[u] - v0 < size;
-        }
-    }
-    uint32_t n, first;
-    (void)exclusive_sum(less, room, &first);       // the slice's first position
-    const uint32_t at = exclusive_sum(mine, room, &n);
-    uint32_t to_here = from_lane0(at);             // the warp's
-    if (from_lane0(__reduce_add_sync(0xffffffffu, mine)) > 0) {
-        for (uint32_t t0 = from; t0 < to; t0 += 32 * kAhead) {
-            uint32_t id[kAhead];
+            bool here[4];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) id[u] = t0 + 32 * u + lane < to ? id_at<I>(p.ids, t0 + 32 * u + lane) : 0xffffffffu;
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const bool here = id[u] - v0 < size;
-                const uint32_t who = __ballot_sync(0xffffffffu, here);
-                if (here) p.found[first + to_here + __popc(who & lanes_below())] = make_uint2(id[u] - v0, t0 + 32 * u + lane);
-                to_here += __popc(who);
+            for (int k = 0; k < 4; ++k) {
+                less += id[u][k] < v0;
+                here[k] = id[u][k] - v0 < size;
             }
+            if (!__any_sync(0xffffffffu, here[0] || here[1] || here[2] || here[3])) continue;
+            uint32_t at = mine, of_all = 0;        // tokens in front of this lane's first, of the step
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t who = __ballot_sync(0xffffffffu, here[k]);
+                at += __popc(who & lanes_below());
+                of_all += __popc(who);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (here[k] && at < p.kept) { kept[at] = t0 + 128 * u + k; kept_id[at] = uint16_t(id[u][k] - v0); }
+                at += here[k];
+            }
+            mine += of_all;
         }
     }
-    // the slice's tokens, a run for each warp: counted by id, then placed
-    const uint32_t part = (n + kOrderThreads - 1) / kOrderThreads * 32, begin = min(uint32_t(warp) * part, n), end = min(begin + part, n);
-    const uint32_t busy = part > 0 ? (n + part - 1) / part : 0;                // warps with tokens
-    for (uint32_t i = threadIdx.x; i < busy * size; i += kOrderThreads) counts[i] = 0;
-    __syncthreads();
-    const uint2* list = p.found + first;
-    uint32_t* count = counts + uint32_t(warp) * size;
-    constexpr int kBatch = 4;
-    for (uint32_t j0 = begin; j0 < end; j0 += 32 * kBatch) {
-        uint32_t key[kBatch];
+    __syncwarp();
+    // the warp's tokens of the slice, 32 at a time: f(id in the slice or 2^32 - 1, token, lanes of the same id).  Where they were too many, from
+    // the ids again.
+    auto each = [&](auto f) {
+        constexpr int kBatch = 4;
+        const bool again = mine > p.kept;
+        const uint32_t begin = again ? from : 0u, end = again ? to : mine;
+        for (uint32_t j0 = begin + lane; j0 < end + lane; j0 += 32 * kBatch) {
+            uint32_t key[kBatch], token[kBatch], same[kBatch];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) key[u] = j0 + 32 * u + lane < end ? list[j0 + 32 * u + lane].x : 0xffffffffu;
+            for (int u = 0; u < kBatch; ++u) {
+                const uint32_t j = j0 + 32 * u;
+                key[u] = 0xffffffffu;
+                token[u] = j;
+                if (j < end) {
+                    if (again) {
+                        const uint32_t id = id_at<I>(p.ids, j) - v0;
+                        if (id < size) key[u] = id;
+                    } else {
+                        key[u] = kept_id[j];
+                        token[u] = kept[j];
+                    }
+                }
+            }
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const uint32_t same = __match_any_sync(0xffffffffu, key[u]);
-            if (key[u] != 0xffffffffu && (same & lanes_below()) == 0) count[key[u]] += __popc(same);
-            __syncwarp();
+            for (int u = 0; u < kBatch; ++u) same[u] = __match_any_sync(0xffffffffu, key[u]);
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) f(key[u], token[u], same[u]);
         }
-    }
-    __syncthreads();
+    };
+    each([&](uint32_t key, uint32_t, uint32_t same) {
+        if (key != 0xffffffffu && (same & lanes_below()) == 0) count[key] += __popc(same);
+        __syncwarp();
+    });
+    uint32_t first, n, longs;
+    (void)exclusive_sum(less, room, &first);       // the slice's first position; the warps' counts are complete behind its barriers
     uint32_t sum = 0;
     if (threadIdx.x < size) {
-        for (uint32_t w = 0; w < busy; ++w) {
-            const uint32_t c = counts[w * size + threadIdx.x];
-            counts[w * size + threadIdx.x] = sum;
+#pragma unroll 8
+        for (int w = 0; w < kOrderWarps; ++w) {
+            const uint32_t c = counts[uint32_t(w) * size + threadIdx.x];
+            counts[uint32_t(w) * size + threadIdx.x] = sum;
             sum += c;
         }
     }
-    uint32_t all;
-    const uint32_t begins = exclusive_sum(sum, room, &all);
+    const uint32_t begins = first + exclusive_sum(sum, room, &n);
     if (threadIdx.x < size) {
         offset[threadIdx.x] = begins;
-        p.start[v0 + threadIdx.x] = first + begins;
+        p.start[v0 + threadIdx.x] = begins;
     }
     if (v1 == p.classes && threadIdx.x == 0) p.start[p.classes] = first + n;
     const bool is_long = sum > p.longest;
-    uint32_t longs;
     const uint32_t nth = exclusive_sum(is_long ? 1u : 0u, room, &longs);       // (its barriers stand in front of the use of `offset`, too)
-    if (is_long) p.longs[first / p.longest + blockIdx.x + nth] = make_uint4(v0 + threadIdx.x, first + begins, first + begins + sum, 0u);
+    if (is_long) p.longs[first / p.longest + blockIdx.x + nth] = make_uint4(v0 + threadIdx.x, begins, begins + sum, 0u);
     if (threadIdx.x == 0) p.long_count[blockIdx.x] = longs;
-    for (uint32_t j0 = begin; j0 < end; j0 += 32 * kBatch) {
-        uint2 e[kBatch];
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) e[u] = j0 + 32 * u + lane < end ? list[j0 + 32 * u + lane] : make_uint2(0xffffffffu, 0u);
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const uint32_t same = __match_any_sync(0xffffffffu, e[u].x), rank = __popc(same & lanes_below());
-            if (e[u].x != 0xffffffffu) p.sorted[first + offset[e[u].x] + count[e[u].x] + rank] = make_uint2(v0 + e[u].x, e[u].y);
-            __syncwarp();
-            if (e[u].x != 0xffffffffu && rank == 0) count[e[u].x] += __popc(same);
-            __syncwarp();
-        }
-    }
+    each([&](uint32_t key, uint32_t token, uint32_t same) {
+        const uint32_t rank = __popc(same & lanes_below());
+        const bool there = key != 0xffffffffu;
+        if (there) p.sorted[offset[key] + count[key] + rank] = make_uint2(v0 + key, token);
+        __syncwarp();
+        if (there && rank == 0) count[key] += __popc(same);
+        __syncwarp();
+    });
     if (!p.in_place && !p.fill_first) {
         __syncthreads();
         if (threadIdx.x < size) offset[threadIdx.x] = sum;
         __syncthreads();
         fill_rows(p, v0, size, offset);
     }
+    if (zeroing && warp == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
 
 __device__ __forceinline__ uint32_t ld_dependent_u32(const uint32_t* p) {
@@ -268,8 +322,8 @@ __device__ __forceinline__ void write_row(const GradParams& p, uint32_t v, int c
 
 // Span blockIdx.x * slots + slot.  The first rows are asked for before it is known whether they are this span's.
 template <typename T, typename U>
-__global__ void __launch_bounds__(256) embedding_sums_kernel(const GradParams p) {
-    constexpr int kAhead = 8;
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 3) embedding_sums_kernel(const GradParams p) {
+    constexpr int kAhead = sizeof(T) == 2 ? 8 : 4;
     const Place at = place_of(p.vectors);
     const uint32_t s = blockIdx.x * uint32_t(at.slots) + uint32_t(at.slot);
     if (at.slot >= at.slots || s >= p.spans) return;
@@ -341,6 +395,19 @@ __global__ void __launch_bounds__(256) embedding_sums_kernel(const GradParams p)
     leave(open_left, open_right);
 }
 
+// 8 values of each of four parts in one statement: as loads of their own the compiler put each part's sum behind its load, and an id of 690
+// parts, 22 a thread, took 10 us of waits.
+__device__ __forceinline__ void ld_four_parts(float (&x)[4][8], const float* const (&from)[4]) {
+#define HQ_OUT8(u) "=f"(x[u][0]), "=f"(x[u][1]), "=f"(x[u][2]), "=f"(x[u][3]), "=f"(x[u][4]), "=f"(x[u][5]), "=f"(x[u][6]), "=f"(x[u][7])
+    asm volatile(
+        "ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%32];\n\tld.global.cg.v4.f32 {%4, %5, %6, %7}, [%32 + 16];\n\t"
+        "ld.global.cg.v4.f32 {%8, %9, %10, %11}, [%33];\n\tld.global.cg.v4.f32 {%12, %13, %14, %15}, [%33 + 16];\n\t"
+        "ld.global.cg.v4.f32 {%16, %17, %18, %19}, [%34];\n\tld.global.cg.v4.f32 {%20, %21, %22, %23}, [%34 + 16];\n\t"
+        "ld.global.cg.v4.f32 {%24, %25, %26, %27}, [%35];\n\tld.global.cg.v4.f32 {%28, %29, %30, %31}, [%35 + 16];"
+        : HQ_OUT8(0), HQ_OUT8(1), HQ_OUT8(2), HQ_OUT8(3) : "l"(from[0]), "l"(from[1]), "l"(from[2]), "l"(from[3]) : "memory");
+#undef HQ_OUT8
+}
+
 // Ids that lie in several spans.  blockIdx.x: a slice of the order, whose long ids are taken one after the other; y: 64 channels.
 // Thread = (8 channels, every 32nd part).
 template <typename U>
@@ -358,12 +425,21 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const GradParams p)
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] = pk2(0.f, 0.f);
         if (c0 < dim) {
-#pragma unroll 8
-            for (uint32_t i = first + way; i <= last; i += 32) {
-                const float4* part = reinterpret_cast<const float4*>(p.parts + (int64_t(i) * 2 + (i == first ? 1 : 0)) * dim + c0);
-                const float4 x = ld_dependent_cg(part), y = ld_dependent_cg(part + 1);
-                sum[0] = add2(sum[0], pk2(x.x, x.y)); sum[1] = add2(sum[1], pk2(x.z, x.w));
-                sum[2] = add2(sum[2], pk2(y.x, y.y)); sum[3] = add2(sum[3], pk2(y.z, y.w));
+            for (uint32_t i0 = first + way; i0 <= last; i0 += 32 * 4) {
+                const float* part[4];              // of a part behind the last: the last one's, which is not added
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const uint32_t i = min(i0 + 32 * u, last);
+                    part[u] = p.parts + (int64_t(i) * 2 + (i == first ? 1 : 0)) * dim + c0;
+                }
+                float x[4][8];
+                ld_four_parts(x, part);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (i0 + 32 * u > last) break;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[e] = add2(sum[e], pk2(x[u][2 * e], x[u][2 * e + 1]));
+                }
             }
         }
         // four ways of a warp, then the warps in order
@@ -405,7 +481,7 @@ hq_status check_call(int id_bytes, int64_t tokens, int64_t classes, int64_t dim,
     return HQ_OK;
 }
 
-struct Plan { uint32_t slice, slices, span, spans, longest; size_t sorted, start, longs, long_count, parts, bytes; };
+struct Plan { uint32_t slice, slices, span, spans, longest; size_t start, longs, long_count, parts, bytes; };
 Plan plan_of(int64_t tokens, int64_t classes, int64_t dim) {
     Plan a{};
     const int64_t slice = (classes + 147) / 148;
@@ -418,8 +494,7 @@ Plan plan_of(int64_t tokens, int64_t classes, int64_t dim) {
     a.spans = uint32_t((tokens + span - 1) / span);
     a.longest = uint32_t(span * 4 > 64 ? span * 4 : 64);
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    a.sorted = up(size_t(tokens) * sizeof(uint2));             // behind the tokens as found
-    a.start = a.sorted + up(size_t(tokens) * sizeof(uint2));
+    a.start = up(size_t(tokens) * sizeof(uint2));  // behind the sorted tokens
     a.longs = a.start + up((size_t(classes) + 1) * sizeof(uint32_t));
     a.long_count = a.longs + up((size_t(tokens) / a.longest + a.slices + 1) * sizeof(uint4));
     a.parts = a.long_count + up(size_t(a.slices) * sizeof(uint32_t));
@@ -492,10 +567,15 @@ extern "C" hq_status hq_embedding_bwd(const void* ids, int id_bytes, int64_t tok
     p.ld_dout = tokens > 0 ? pitch_of(ld_dout, ddt) : 0; p.ld_base = base != nullptr ? pitch_of(ld_base, gdt) : 0; p.ld_dtable = pitch_of(ld_dtable, gdt);
     p.tokens = uint32_t(tokens); p.slice = a.slice; p.span = a.span; p.longest = a.longest; p.spans = a.spans; p.vectors = int(dim / 8); p.half = gdt == HQ_BF16;
     p.in_place = base == dtable; p.fill_first = tokens < classes; p.scale = scale;
-    p.found = reinterpret_cast<uint2*>(ws); p.sorted = reinterpret_cast<uint2*>(ws + a.sorted);
+    p.sorted = reinterpret_cast<uint2*>(ws);
     p.start = words(a.start); p.longs = reinterpret_cast<uint4*>(ws + a.longs); p.long_count = words(a.long_count); p.parts = reinterpret_cast<float*>(ws + a.parts);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const size_t smem = size_t(kOrderWarps) * a.slice * sizeof(uint32_t);
+    // room for every token of a warp's run, as far as shared memory goes
+    const size_t counters = size_t(kOrderWarps) * a.slice * sizeof(uint32_t), each = kOrderWarps * (sizeof(uint32_t) + sizeof(uint16_t));
+    const size_t run = size_t(tokens + 32 * 128 - 1) / (32 * 128) * 128, fit = (208 * 1024 - counters) / each / 2 * 2;
+    p.kept = uint32_t(run < fit ? run : fit);
+    if (p.kept > kKept) p.kept = kKept;
+    const size_t smem = counters + p.kept * each;
     void (*order)(GradParams) = id_bytes == 4 ? embedding_order_kernel<int32_t> : embedding_order_kernel<int64_t>;
     if (smem > 40 * 1024) HQ_CUDA_OK(cudaFuncSetAttribute(order, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
     order<<<a.slices, kOrderThreads, smem, st>>>(p);

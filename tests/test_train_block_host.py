@@ -130,7 +130,7 @@ def test_clipping_refuses(hq, change, want):
 
 def test_workspace_sizes(hq):
     assert hq.hq_gate_norm_bwd_workspace_size(1, 8, 0) >= 7 * 8 * 4 and hq.hq_gate_norm_bwd_workspace_size(0, 8, 0) == 0
-    assert hq.hq_embedding_bwd_workspace_size(100, 10, 64) >= 100 * 16 + 11 * 4
+    assert hq.hq_embedding_bwd_workspace_size(100, 10, 64) >= 100 * 8 + 11 * 4
     assert hq.hq_embedding_bwd_workspace_size(0, 10, 64) >= 11 * 4
     for bad in ((-1, 8, 0), (1, 4104, 0), (1, 12, 0), (1, 8, -1)):
         with pytest.raises(hq.HqError):
