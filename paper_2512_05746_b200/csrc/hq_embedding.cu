@@ -8,7 +8,7 @@
 // The gradient has three kernels.  (1) order: CTA b owns a slice of the ids, reads all ids once, keeps the tokens of its slice in their order
 // and counts those of smaller ids (where its part of the sorted order begins), then sorts its tokens by id with one stable counting sort, a
 // warp's run of tokens after the other's: no atomics, so the order is the same on every run.  It writes its slice's rows of the table that have no tokens, too: all of them in front of
-// the rest, while the memory is idle, where the tokens are fewer than the ids.  (2) sums: the sorted tokens are cut into spans of equal length,
+// the rest, while the memory is idle, where the tokens are fewer than the ids (or an fp32 base is added to).  (2) sums: the sorted tokens are cut into spans of equal length,
 // whatever ids they hold (most tokens may be of one id); a team of threads adds up a span's rows with several rows in flight and writes a row of
 // the table whenever the id changes.  An id of up to `longest` tokens belongs to the span of its first one; the sums of a longer one go to the
 // workspace, one for each span, and (3) join adds them up in order.
@@ -302,11 +302,27 @@ __device__ __forceinline__ uint32_t ld_dependent_u32(const uint32_t* p) {
     return v;
 }
 
+// An fp32 row with a base holds it already (in place, or copied by the order kernel): each value is added to once, without a wait for it.
+__device__ __forceinline__ void add_to(float* to, float4 x) {
+    asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(to), "f"(x.x), "f"(x.y), "f"(x.z), "f"(x.w) : "memory");
+}
+
 // Row v of the table from the sum of its tokens' rows.
 template <typename U>
 __device__ __forceinline__ void write_row(const GradParams& p, uint32_t v, int c0, const f32x2 (&sum)[4]) {
     const f32x2 s = pk2(p.scale, p.scale);
     f32x2 f[4];
+    if (sizeof(U) == 4 && p.base != nullptr) {
+        float* to = reinterpret_cast<float*>(static_cast<char*>(p.dtable) + uint64_t(v) * p.ld_dtable) + c0;
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+            float4 x;
+            upk2(mul2(sum[e], s), x.x, x.y);
+            upk2(mul2(sum[e + 1], s), x.z, x.w);
+            add_to(to + 2 * e, x);
+        }
+        return;
+    }
     if (p.base != nullptr) {
         Vec8<U> b;
         b.load_wide(static_cast<const char*>(p.base) + uint64_t(v) * p.ld_base, c0);
@@ -320,76 +336,118 @@ __device__ __forceinline__ void write_row(const GradParams& p, uint32_t v, int c
     Vec8<U>::store_wide(static_cast<char*>(p.dtable) + uint64_t(v) * p.ld_dtable, c0, f);
 }
 
-// Span blockIdx.x * slots + slot.  The first rows are asked for before it is known whether they are this span's.
-template <typename T, typename U>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 3) embedding_sums_kernel(const GradParams p) {
-    constexpr int kAhead = sizeof(T) == 2 ? 8 : 4;
-    const Place at = place_of(p.vectors);
-    const uint32_t s = blockIdx.x * uint32_t(at.slots) + uint32_t(at.slot);
-    if (at.slot >= at.slots || s >= p.spans) return;
-    const int c0 = at.c0;
-    const char* dout = static_cast<const char*>(p.dout) + c0 * int(sizeof(T));
-    uint32_t a = s * p.span, b = min(a + p.span, p.tokens), j = a;             // span >= kAhead: the first entries are inside
-    uint2 e[kAhead];
-    Vec8<T> x[kAhead];
+// 16 bytes of a row that a thread adds up (8 channels of bf16, 4 of fp32), and rows on their way to each thread: 64 KB a CTA.
+template <typename T> constexpr int kPiece = 16 / int(sizeof(T));
+constexpr int kFlight = 16;
+constexpr int kEntries = 2048;                     // sorted tokens of a CTA's spans
+
+// Row v of the table, N channels from c0 on, from the sum of its tokens' rows.
+template <typename U, int N>
+__device__ __forceinline__ void write_channels(const GradParams& p, uint32_t v, int c0, const f32x2 (&sum)[N / 2]) {
+    if constexpr (N == 8) {
+        write_row<U>(p, v, c0, sum);
+    } else {
+        const U* base = reinterpret_cast<const U*>(static_cast<const char*>(p.base) + uint64_t(v) * p.ld_base) + c0;
+        U* to = reinterpret_cast<U*>(static_cast<char*>(p.dtable) + uint64_t(v) * p.ld_dtable) + c0;
+        float f[4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) upk2(sum[e], f[2 * e], f[2 * e + 1]);
+        if constexpr (sizeof(U) == 4) {
+            const float4 x = make_float4(f[0] * p.scale, f[1] * p.scale, f[2] * p.scale, f[3] * p.scale);
+            if (p.base != nullptr) add_to(to, x);
+            else *reinterpret_cast<float4*>(to) = x;
+        } else {
+            uint2 o = make_uint2(0u, 0u);
+            if (p.base != nullptr) o = *reinterpret_cast<const uint2*>(base);
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(fmaf(f[0], p.scale, __uint_as_float(o.x << 16)), fmaf(f[1], p.scale, __uint_as_float(o.x & 0xFFFF0000u)));
+            const __nv_bfloat162 hi = __floats2bfloat162_rn(fmaf(f[2], p.scale, __uint_as_float(o.y << 16)), fmaf(f[3], p.scale, __uint_as_float(o.y & 0xFFFF0000u)));
+            *reinterpret_cast<uint2*>(to) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        }
+    }
+}
+
+// Span blockIdx.x * slots + slot of blockDim.x / slots threads.  The CTA's sorted tokens are in shared memory; each thread copies its piece of
+// kFlight rows ahead there, for itself, so that few teams keep the memory busy and the spans may be long.  BASED: a bf16 base, whose rows are
+// asked for as far ahead.
+template <typename T, typename U, bool BASED>
+__global__ void __launch_bounds__(256) embedding_sums_kernel(const GradParams p) {
+    extern __shared__ uint4 rows[];                // [kFlight][threads]
+    __shared__ uint2 entries[kEntries];
+    constexpr int kN = kPiece<T>;
+    const int pieces = p.vectors * 8 / kN;
+    const Place at = place_of(pieces);
+    const int c0 = at.c0 / 8 * kN;
     griddep_wait();
     griddep_launch();                              // the joining kernel's CTAs find room as these end
-    const uint32_t n = ld_dependent_u32(p.start + p.classes);
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) e[u] = j + u < b ? ld_dependent_cg(p.sorted + j + u) : make_uint2(0u, 0u);
-    b = min(b, n);
-    if (a >= b) return;
-    const uint32_t id0 = e[0].x, id1 = ld_dependent_cg(p.sorted + b - 1).x;
-    const uint32_t begin0 = ld_dependent_u32(p.start + id0), end0 = ld_dependent_u32(p.start + id0 + 1);
-    const uint32_t begin1 = ld_dependent_u32(p.start + id1), end1 = ld_dependent_u32(p.start + id1 + 1);
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-        x[u].clear();
-        if (j + u < b) x[u].load_wide(dout + uint64_t(e[u].y) * p.ld_dout, 0);
-    }
+    const uint32_t n = ld_dependent_u32(p.start + p.classes), from = blockIdx.x * uint32_t(at.slots) * p.span;
+    if (from >= n) return;
+    const uint32_t known = min(n - from, uint32_t(at.slots) * p.span + p.longest);
+    for (uint32_t i = threadIdx.x; i < known; i += blockDim.x) entries[i] = ld_dependent_cg(p.sorted + from + i);
+    __syncthreads();
+    const uint32_t s = blockIdx.x * uint32_t(at.slots) + uint32_t(at.slot);
+    uint32_t a = uint32_t(at.slot) * p.span, b = min(a + p.span, n - from);    // places in `entries`
+    if (at.slot >= at.slots || a >= b) return;
     // an id of at most `longest` tokens belongs to the span of its first one, whole; a longer one to every span that it lies in
     bool open_left = false, open_right = false;
-    if (begin0 < a) {
-        if (end0 - begin0 <= p.longest) a = end0;
-        else open_left = true;
-    }
-    if (a >= b) return;
-    if (end1 - begin1 > p.longest) open_right = end1 > b;
-    else b = end1;
-    f32x2 sum[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) sum[k] = pk2(0.f, 0.f);
-    uint32_t now = 0xffffffffu;
-    auto leave = [&](bool left, bool right) {
-        if (!left && !right) { write_row<U>(p, now, c0, sum); return; }
-        Vec8<float>::store_wide(p.parts, (int64_t(s) * 2 + (left ? 0 : 1)) * p.vectors * 8 + c0, sum);
-    };
-    uint32_t known = min(s * p.span + p.span, n);  // entries of this batch that have their rows
-    while (true) {
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (j + u >= b || j + u >= known) break;
-            if (j + u < a) continue;
-            if (e[u].x != now) {
-                if (now != 0xffffffffu) { leave(open_left, false); open_left = false; }
-                now = e[u].x;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) sum[k] = pk2(0.f, 0.f);
-            }
-            f32x2 f[4];
-            x[u].get(f);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) sum[k] = add2(sum[k], f[k]);
+    {
+        const uint32_t id0 = entries[a].x, id1 = entries[b - 1].x;
+        const uint32_t begin0 = ld_dependent_u32(p.start + id0), end0 = ld_dependent_u32(p.start + id0 + 1);
+        const uint32_t begin1 = ld_dependent_u32(p.start + id1), end1 = ld_dependent_u32(p.start + id1 + 1);
+        if (begin0 < from + a) {
+            if (end0 - begin0 <= p.longest) a = end0 - from;
+            else open_left = true;
         }
-        j = min(j + kAhead, known);
-        known = b;
-        if (j >= b) break;
+        if (a >= b) return;
+        if (end1 - begin1 > p.longest) open_right = end1 > from + b;
+        else b = end1 - from;
+    }
+    const char* dout = static_cast<const char*>(p.dout) + c0 * int(sizeof(T));
+    const uint32_t ring = smem_u32(rows) + threadIdx.x * 16u, step = blockDim.x * 16u;
+    auto send = [&](uint32_t j) {
+        if (j < b) {
+            if (BASED && (j == a || entries[j].x != entries[j - 1].x))
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const char*>(p.base) + uint64_t(entries[j].x) * p.ld_base + c0 * 2));
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                         ::"r"(ring + (j % kFlight) * step), "l"(dout + uint64_t(entries[j].y) * p.ld_dout) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    f32x2 sum[kN / 2];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) e[u] = j + u < b ? ld_dependent_cg(p.sorted + j + u) : make_uint2(0u, 0u);
+    for (int k = 0; k < kN / 2; ++k) sum[k] = pk2(0.f, 0.f);
+    uint32_t now = entries[a].x;
+    auto leave = [&](bool left, bool right) {
+        if (!left && !right) { write_channels<U, kN>(p, now, c0, sum); return; }
+        float* part = p.parts + (int64_t(s) * 2 + (left ? 0 : 1)) * p.vectors * 8 + c0;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            x[u].clear();
-            if (j + u < b) x[u].load_wide(dout + uint64_t(e[u].y) * p.ld_dout, 0);
+        for (int k = 0; k < kN / 2; k += 2) {
+            float4 v;
+            upk2(sum[k], v.x, v.y);
+            upk2(sum[k + 1], v.z, v.w);
+            *reinterpret_cast<float4*>(part + 2 * k) = v;
+        }
+    };
+#pragma unroll 1
+    for (uint32_t k = 0; k < kFlight - 1; ++k) send(a + k);
+#pragma unroll 2
+    for (uint32_t j = a; j < b; ++j) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kFlight - 2) : "memory");
+        uint4 x;
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(ring + (j % kFlight) * step) : "memory");
+        send(j + kFlight - 1);                     // into the place of the row before this one
+        const uint32_t id = entries[j].x;
+        if (id != now) {
+            leave(open_left, false);
+            open_left = false;
+            now = id;
+#pragma unroll
+            for (int k = 0; k < kN / 2; ++k) sum[k] = pk2(0.f, 0.f);
+        }
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int k = 0; k < kN / 2; ++k) {
+            if constexpr (kN == 8) sum[k] = add2(sum[k], pk2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xFFFF0000u)));
+            else sum[k] = add2(sum[k], pk2(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1])));
         }
     }
     leave(open_left, open_right);
@@ -482,17 +540,19 @@ hq_status check_call(int id_bytes, int64_t tokens, int64_t classes, int64_t dim,
 }
 
 struct Plan { uint32_t slice, slices, span, spans, longest; size_t start, longs, long_count, parts, bytes; };
-Plan plan_of(int64_t tokens, int64_t classes, int64_t dim) {
+Plan plan_of(int64_t tokens, int64_t classes, int64_t dim, int piece) {
     Plan a{};
     const int64_t slice = (classes + 147) / 148;
     a.slice = uint32_t(slice < kSlice ? slice : kSlice);
     a.slices = uint32_t((classes + a.slice - 1) / a.slice);
-    // spans that keep a thousand threads an SM busy, of 8 to 64 tokens
-    int64_t span = 8;
-    while (span < 64 && tokens * (dim / 8) > span * 148 * 1024) span *= 2;
+    // spans for two CTAs an SM, of up to 64 tokens, and no more tokens in a CTA than its room for entries
+    const int pieces = int(dim / piece), slots = 256 / (pieces < 256 ? pieces : 256);
+    int64_t span = 1;
+    while (span < 64 && tokens * pieces > span * 148 * 2 * 256) span *= 2;
+    a.longest = 64;
+    while (span > 1 && slots * span + a.longest > kEntries) span /= 2;
     a.span = uint32_t(span);
     a.spans = uint32_t((tokens + span - 1) / span);
-    a.longest = uint32_t(span * 4 > 64 ? span * 4 : 64);
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     a.start = up(size_t(tokens) * sizeof(uint2));  // behind the sorted tokens
     a.longs = a.start + up((size_t(classes) + 1) * sizeof(uint32_t));
@@ -513,8 +573,16 @@ cudaError_t launch_lookup(const LookupParams& p, int id_bytes, cudaStream_t st) 
 }
 template <typename T, typename U>
 cudaError_t launch_sums(const GradParams& p, cudaStream_t st) {
-    const Spread s = spread(p.vectors);
-    return launch_dependent(embedding_sums_kernel<T, U>, dim3((p.spans + s.slots - 1) / s.slots, s.slices), s.threads, 0, st, true, p);
+    const Spread s = spread(p.vectors * 8 / kPiece<T>);
+    const size_t smem = size_t(kFlight) * s.threads * 16;
+    void (*kern)(GradParams) = embedding_sums_kernel<T, U, false>;
+    if constexpr (sizeof(U) == 2)
+        if (p.base != nullptr) kern = embedding_sums_kernel<T, U, true>;
+    if (smem > 24 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+        if (e != cudaSuccess) { (void)cudaGetLastError(); return e; }
+    }
+    return launch_dependent(kern, dim3((p.spans + s.slots - 1) / s.slots, s.slices), s.threads, smem, st, true, p);
 }
 
 }  // namespace
@@ -542,7 +610,8 @@ extern "C" hq_status hq_embedding_bwd_workspace_size(int64_t tokens, int64_t cla
     if (bytes == nullptr) return HQ_ERR_INVALID_ARG;
     const hq_status e = check_call(4, tokens, classes, dim, HQ_F32, HQ_F32, 1.f);
     if (e != HQ_OK) return e;
-    *bytes = plan_of(tokens, classes, dim).bytes;
+    const size_t half = plan_of(tokens, classes, dim, kPiece<__nv_bfloat16>).bytes, full = plan_of(tokens, classes, dim, kPiece<float>).bytes;
+    *bytes = half > full ? half : full;            // of either type of dout
     return HQ_OK;
 }
 
@@ -558,7 +627,7 @@ extern "C" hq_status hq_embedding_bwd(const void* ids, int id_bytes, int64_t tok
         (base != nullptr && (e = check_rows(base, ld_base, dim, gdt)) != HQ_OK))
         return e;
     if (base == dtable && ld_base != ld_dtable) return HQ_ERR_SHAPE;
-    const Plan a = plan_of(tokens, classes, dim);
+    const Plan a = plan_of(tokens, classes, dim, ddt == HQ_BF16 ? kPiece<__nv_bfloat16> : kPiece<float>);
     if (ws_bytes < a.bytes) return HQ_ERR_WORKSPACE;
     char* ws = static_cast<char*>(workspace);
     auto words = [&](size_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
@@ -566,7 +635,7 @@ extern "C" hq_status hq_embedding_bwd(const void* ids, int id_bytes, int64_t tok
     p.ids = ids; p.dout = dout; p.base = base; p.dtable = dtable; p.classes = uint32_t(classes);
     p.ld_dout = tokens > 0 ? pitch_of(ld_dout, ddt) : 0; p.ld_base = base != nullptr ? pitch_of(ld_base, gdt) : 0; p.ld_dtable = pitch_of(ld_dtable, gdt);
     p.tokens = uint32_t(tokens); p.slice = a.slice; p.span = a.span; p.longest = a.longest; p.spans = a.spans; p.vectors = int(dim / 8); p.half = gdt == HQ_BF16;
-    p.in_place = base == dtable; p.fill_first = tokens < classes; p.scale = scale;
+    p.in_place = base == dtable; p.fill_first = tokens < classes || (base != nullptr && gdt == HQ_F32); p.scale = scale;
     p.sorted = reinterpret_cast<uint2*>(ws);
     p.start = words(a.start); p.longs = reinterpret_cast<uint4*>(ws + a.longs); p.long_count = words(a.long_count); p.parts = reinterpret_cast<float*>(ws + a.parts);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -585,7 +654,7 @@ extern "C" hq_status hq_embedding_bwd(const void* ids, int id_bytes, int64_t tok
     if (ddt == HQ_BF16) c = gdt == HQ_BF16 ? launch_sums<__nv_bfloat16, __nv_bfloat16>(p, st) : launch_sums<__nv_bfloat16, float>(p, st);
     else c = gdt == HQ_BF16 ? launch_sums<float, __nv_bfloat16>(p, st) : launch_sums<float, float>(p, st);
     if (c != cudaSuccess) return HQ_ERR_CUDA;
-    if (tokens <= int64_t(p.longest)) return HQ_OK;            // no id has more tokens than one span takes
+    if (tokens <= int64_t(p.longest)) return HQ_OK;            // no id has more tokens than a span takes whole
     const dim3 join(a.slices, unsigned((dim + 63) / 64));
     c = gdt == HQ_BF16 ? launch_dependent(embedding_join_kernel<__nv_bfloat16>, join, 256, 0, st, true, p) : launch_dependent(embedding_join_kernel<float>, join, 256, 0, st, true, p);
     return c == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
