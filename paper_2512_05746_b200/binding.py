@@ -546,7 +546,7 @@ def _stream_and_device(stream):
         _hqcall.bind_attention(torch.float32, torch.bfloat16, torch.int32, *(C.cast(getattr(lib, n), C.c_void_p).value for n in (
             "hq_qk_norm_rope", "hq_qk_norm_rope_bwd", "hq_attention_fwd", "hq_attention_bwd")))
         _hqcall.bind_block(torch.int64, *(C.cast(getattr(lib, n), C.c_void_p).value for n in ("hq_gate_norm", "hq_gate_norm_bwd", "hq_embedding",
-                                                                                            "hq_embedding_bwd")))
+                                                                                            "hq_embedding_bwd", "hq_grad_norm", "hq_grad_clip")))
         if not torch.cuda.is_available():
             return 0, -2
         _device_now = torch._C._cuda_getDevice
@@ -692,6 +692,7 @@ class GradList:
         self.grads, self.outs, self.n = grads, outs, len(grads)
         self.device = grads[0].get_device() if grads else None
         self.table = (_GradTensor * max(1, self.n))()
+        self.address = C.addressof(self.table)
         spans = []                                 # (first byte, end, written, gradient)
         for i, g in enumerate(grads):
             o = g if outs is None else outs[i]
@@ -717,27 +718,12 @@ class GradList:
             written = max(written, (end, i), key=lambda e: e[0]) if write else written
 
 
-def _grad_list(grads, what: str):
+def _grad_call(grads, max_norm, eps, norm, coef, workspace, stream, what: str) -> None:
     grads = grads if isinstance(grads, GradList) else GradList(grads)
-    at, device = _stream_and_device(None)
+    at, device = _stream_and_device(stream)
     if grads.n and device != grads.device:
         raise ValueError(f"{what}: the gradients are on CUDA device {grads.device}, the current one is {device}")
-    return grads, device
-
-
-def _scalar(t, name: str, what: str, device):
-    if t is None:
-        return None
-    import torch
-    if t.dtype != torch.float32 or t.numel() != 1 or t.get_device() != device:
-        raise ValueError(f"{what}: {name} is one fp32 value on the current CUDA device")
-    return t.data_ptr()
-
-
-def _bytes(workspace, what: str, device):
-    if not workspace.is_contiguous() or workspace.get_device() != device:
-        raise ValueError(f"{what}: workspace is a dense tensor on the current CUDA device")
-    return workspace.data_ptr(), workspace.nbytes
+    _check(_hqcall.grad_clip(grads.address, grads.n, max_norm, eps, norm, coef, workspace, at, device), what)
 
 
 def hq_grad_workspace_size() -> int:
@@ -749,17 +735,13 @@ def hq_grad_workspace_size() -> int:
 def hq_grad_norm(grads, norm, workspace, stream=None) -> None:
     """norm (one fp32 value on the device) = the norm of all gradients: a GradList, or the tensors themselves.  workspace:
     hq_grad_workspace_size bytes."""
-    grads, device = _grad_list(grads, "hq_grad_norm")
-    _check(lib.hq_grad_norm(grads.table, grads.n, _scalar(norm, "norm", "hq_grad_norm", device), *_bytes(workspace, "hq_grad_norm", device),
-                            _stream(stream)), "hq_grad_norm")
+    _grad_call(grads, None, 0.0, norm, None, workspace, stream, "hq_grad_norm")
 
 
 def hq_grad_clip(grads, max_norm: float, norm, workspace, eps: float = 1e-6, coef=None, stream=None) -> None:
     """norm as hq_grad_norm; every gradient times coef = min(1, max_norm / (norm + eps)), in place or into the list's outs.  norm, coef (or
     None): one fp32 value each on the device."""
-    grads, device = _grad_list(grads, "hq_grad_clip")
-    _check(lib.hq_grad_clip(grads.table, grads.n, max_norm, eps, _scalar(norm, "norm", "hq_grad_clip", device), _scalar(coef, "coef", "hq_grad_clip", device),
-                            *_bytes(workspace, "hq_grad_clip", device), _stream(stream)), "hq_grad_clip")
+    _grad_call(grads, max_norm, eps, norm, coef, workspace, stream, "hq_grad_clip")
 
 
 def hq_qlinear_fused(x, pw: PreparedWeight, bias, a_bits: int, y, static_scale=None, dev_status=None, stream=None) -> None:

@@ -3,8 +3,8 @@
 //   norm = sqrt(sum over tensors and elements of g^2),   c = min(1, max_norm / (norm + eps)),   out = c g
 //
 // Memory-bound: one pass that reads every gradient, one that reads and writes it.  The tensors are one line of chunks of equal size, laid
-// out in the kernel's parameters (address, count and first chunk of each), so that a call of hundreds of tensors is two launches without a
-// table in memory; a CTA takes a run of chunks and finds the tensor of its first one by bisection.  The second pass takes the chunks from the
+// out in the kernel's parameters (address, count and first chunk of each, and each CTA's first tensor), so that a call of hundreds of tensors is
+// two launches without a table in memory; a CTA takes a run of chunks.  The second pass takes the chunks from the
 // last one down: what the first pass read last is still in L2.
 //
 // A thread's squares are summed in fp32 over 8 elements at a time and these in fp64; a group of 8 whose squares leave fp32's range is
@@ -20,7 +20,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kNormBlocks = 148 * 6, kScaleBlocks = 148 * 5;                       // resident at once; on every device: one order of the sums
 constexpr int64_t kUnit = kThreads * 8;            // elements a CTA takes at a time
-constexpr int kMost = 1100;                        // tensors of a launch: 28 bytes each of 32 KB of parameters
+constexpr int kMost = 1088;                        // tensors of a launch: 28 bytes each of 32 KB of parameters, 2 for each CTA
 constexpr int kParts = 4096;                       // sums of CTAs of all launches of a call
 
 // N tensors; first[n] is the first chunk behind them.
@@ -29,6 +29,7 @@ template <int N> struct Tensors {
     void* out[N];
     int64_t count[N];                              // elements, and the two types in bits 62 (in) and 61 (out): 1 bf16
     uint32_t first[N + 1];
+    uint16_t at[kNormBlocks];                      // the tensor of a CTA's first chunk; second pass: of its last one
     int n;
     int64_t chunk;                                 // elements, a multiple of kUnit
     double* parts;                                 // a sum of each CTA of the norm's launches: this launch's, for the second pass all
@@ -39,22 +40,13 @@ template <int N> struct Tensors {
 };
 constexpr int64_t kInBf16 = int64_t(1) << 62, kOutBf16 = int64_t(1) << 61, kCount = kOutBf16 - 1;
 
-template <int N>
-__device__ __forceinline__ int tensor_of(const Tensors<N>& p, uint32_t chunk) {
-    int lo = 0, hi = p.n - 1;                      // the last tensor whose first chunk is not behind `chunk`
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (p.first[mid] <= chunk) lo = mid; else hi = mid - 1;
-    }
-    return lo;
-}
-
 template <typename T> __device__ __forceinline__ float element(const void* p, int64_t i);
 template <> __device__ __forceinline__ float element<float>(const void* p, int64_t i) { return static_cast<const float*>(p)[i]; }
 template <> __device__ __forceinline__ float element<__nv_bfloat16>(const void* p, int64_t i) { return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]); }
 
 // Squares of 8 values.  A square below fp32's range is off by 2^-150 at most: a sum above 2^-120 by 2^-27 of itself for all 8, less than a
-// rounding.  Smaller sums, and those near or behind the range's other end, are taken in fp64; NaN stays NaN.
+// rounding.  Smaller sums, and those near or behind the range's other end, are taken in fp64; NaN stays NaN.  (32 values to one fp64 addition
+// hold 24 registers more: 100 M of bf16 42 us, not 29.)
 __device__ __forceinline__ double squares(const f32x2 (&f)[4]) {
     f32x2 s = mul2(f[0], f[0]);
 #pragma unroll
@@ -117,11 +109,12 @@ template <typename T> __device__ __forceinline__ int shift_of(const void* p) { r
 template <int N>
 __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_constant__ Tensors<N> p) {
     __shared__ double sums[kThreads / 32];
+    griddep_launch();                              // the second pass finds room as CTAs end, and waits for all of them
     uint32_t c, end;
     my_chunks(p.first[p.n], c, end);
     double sum = 0.0;
     if (c < end) {
-        for (int k = tensor_of(p, c); c < end; ++k) {          // this CTA's part of each tensor
+        for (int k = p.at[blockIdx.x]; c < end; ++k) {         // this CTA's part of each tensor
             const uint32_t stop = min(end, p.first[k + 1]);
             const int64_t count = p.count[k] & kCount, from = int64_t(c - p.first[k]) * p.chunk, to = min(int64_t(stop - p.first[k]) * p.chunk, count);
             if (p.count[k] & kInBf16) sum += sum_squares<__nv_bfloat16>(p.in[k], from, to, shift_of<__nv_bfloat16>(p.in[k]));
@@ -212,7 +205,7 @@ __global__ void __launch_bounds__(kThreads) grad_scale_kernel(const __grid_const
     uint32_t from_chunk, c1;
     my_chunks(p.first[p.n], from_chunk, c1);
     if (from_chunk >= c1) return;
-    for (int k = tensor_of(p, c1 - 1); c1 > from_chunk; --k) {
+    for (int k = p.at[blockIdx.x]; c1 > from_chunk; --k) {
         const uint32_t start = max(from_chunk, p.first[k]);
         const void* in = p.in[k];
         void* out = p.out[k];
@@ -233,18 +226,27 @@ __global__ void __launch_bounds__(kThreads) grad_scale_kernel(const __grid_const
     }
 }
 
-struct Call { const hq_grad_tensor* t; int64_t n; bool clip; float max_norm, eps; float *norm, *coef; double* parts; int64_t chunk; unsigned most; cudaStream_t st; };
+struct Call {
+    const hq_grad_tensor* t;
+    int64_t n;
+    bool clip;
+    float max_norm, eps;
+    float *norm, *coef;
+    double* parts;
+    int64_t chunk;
+    unsigned most;                                 // CTAs of a launch of the norm
+    cudaStream_t st;
+};
 
-// Tensors [from, to) in one launch of each kernel.
+// Tensors [from, to) laid out for both kernels; the number of their chunks.
 template <int N>
-hq_status launch(const Call& c, int64_t from, int64_t to, bool norms, int part0, int parts, int* blocks, bool last) {
-    Tensors<N> p;
+uint32_t lay_out(Tensors<N>& p, const Call& c, int64_t from, int64_t to) {
     p.n = int(to - from);
     uint32_t chunks = 0;
     for (int k = 0; k < p.n; ++k) {
         const hq_grad_tensor& t = c.t[from + k];
         p.in[k] = t.grad;
-        p.out[k] = t.out != nullptr ? t.out : const_cast<void*>(static_cast<const void*>(t.grad));
+        p.out[k] = t.out != nullptr ? t.out : const_cast<void*>(t.grad);
         const int32_t odt = t.out != nullptr ? t.out_dtype : t.dtype;
         p.count[k] = t.count | (t.dtype == HQ_BF16 ? kInBf16 : 0) | (odt == HQ_BF16 ? kOutBf16 : 0);
         p.first[k] = chunks;
@@ -252,23 +254,62 @@ hq_status launch(const Call& c, int64_t from, int64_t to, bool norms, int part0,
     }
     p.first[p.n] = chunks;
     p.chunk = c.chunk;
-    p.parts = c.parts + (norms ? part0 : 0);
-    p.parts_n = parts;
-    p.norm = c.norm; p.coef = c.coef; p.max_norm = c.max_norm; p.eps = c.eps; p.clip = c.clip; p.write_norm = last;
-    const unsigned most = norms ? c.most : unsigned(kScaleBlocks), grid = chunks < 1 ? 1u : chunks < most ? chunks : most;
-    *blocks = int(grid);
-    if (norms) {
-        grad_norm_kernel<N><<<grid, kThreads, 0, c.st>>>(p);
-        return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
-    }
-    const unsigned few = c.clip ? grid : 1u;
-    return launch_dependent(grad_scale_kernel<N>, few, kThreads, 0, c.st, dependent_launch(few), p) == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+    p.norm = c.norm; p.coef = c.coef; p.max_norm = c.max_norm; p.eps = c.eps; p.clip = c.clip;
+    return chunks;
 }
-hq_status launch_any(const Call& c, int64_t from, int64_t to, bool norms, int part0, int parts, int* blocks, bool last) {
-    const int64_t n = to - from;
-    if (n <= 32) return launch<32>(c, from, to, norms, part0, parts, blocks, last);
-    if (n <= 256) return launch<256>(c, from, to, norms, part0, parts, blocks, last);
-    return launch<kMost>(c, from, to, norms, part0, parts, blocks, last);
+// The tensor each CTA begins with.
+template <int N>
+unsigned give_out(Tensors<N>& p, uint32_t chunks, unsigned most, bool last_first) {
+    const unsigned grid = chunks < 1 ? 1u : chunks < most ? chunks : most;
+    const uint32_t per = (chunks + grid - 1) / grid;           // as in my_chunks
+    for (unsigned b = 0, k = 0; b < grid; ++b) {
+        const uint64_t begin = uint64_t(b) * per, end = begin + per < chunks ? begin + per : chunks;
+        if (begin >= chunks) { p.at[b] = 0; continue; }
+        const uint64_t chunk = last_first ? end - 1 : begin;
+        while (p.first[k + 1] <= chunk) ++k;
+        p.at[b] = uint16_t(k);
+    }
+    return grid;
+}
+template <int N>
+hq_status launch_norm(Tensors<N>& p, const Call& c, uint32_t chunks, int part, int* blocks) {
+    const unsigned grid = give_out(p, chunks, c.most, false);
+    p.parts = c.parts + part;
+    *blocks = int(grid);
+    grad_norm_kernel<N><<<grid, kThreads, 0, c.st>>>(p);
+    return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+}
+template <int N>
+hq_status launch_scale(Tensors<N>& p, const Call& c, uint32_t chunks, int parts, bool last) {
+    const unsigned grid = c.clip ? give_out(p, chunks, kScaleBlocks, true) : 1u;
+    p.parts = c.parts;
+    p.parts_n = parts;
+    p.write_norm = last;
+    return launch_dependent(grad_scale_kernel<N>, grid, kThreads, 0, c.st, true, p) == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+}
+// All tensors in one launch of each kernel.
+template <int N>
+hq_status run_once(const Call& c) {
+    Tensors<N> p;
+    const uint32_t chunks = lay_out(p, c, 0, c.n);
+    int blocks = 0;
+    const hq_status e = launch_norm(p, c, chunks, 0, &blocks);
+    return e != HQ_OK ? e : launch_scale(p, c, chunks, blocks, true);
+}
+hq_status run_many(const Call& c) {
+    Tensors<kMost> p;
+    int part = 0, blocks = 0;
+    for (int64_t from = 0; from < c.n; from += kMost) {        // the norms' parts of all tensors, then the outputs, the last tensors first
+        const int64_t to = c.n - from > kMost ? from + kMost : c.n;
+        const hq_status e = launch_norm(p, c, lay_out(p, c, from, to), part, &blocks);
+        if (e != HQ_OK) return e;
+        part += blocks;
+    }
+    for (int64_t from = (c.n - 1) / kMost * kMost, to = c.n; from >= 0; to = from, from -= kMost) {
+        const hq_status e = launch_scale(p, c, lay_out(p, c, from, to), part, to == c.n);
+        if (e != HQ_OK || !c.clip) return e;
+    }
+    return HQ_OK;
 }
 
 hq_status run(const hq_grad_tensor* t, int64_t n, bool clip, float max_norm, float eps, float* norm, float* coef, void* workspace, size_t ws_bytes,
@@ -279,7 +320,7 @@ hq_status run(const hq_grad_tensor* t, int64_t n, bool clip, float max_norm, flo
     if (((reinterpret_cast<uintptr_t>(norm) | reinterpret_cast<uintptr_t>(coef)) & 3u) != 0 || (reinterpret_cast<uintptr_t>(workspace) & 7u) != 0) return HQ_ERR_ALIGNMENT;
     if (n > int64_t(kParts) * kMost) return HQ_ERR_UNSUPPORTED;
     if (ws_bytes < kParts * sizeof(double)) return HQ_ERR_WORKSPACE;
-    int64_t total = 0, largest = 0;
+    int64_t total = 0;
     for (int64_t k = 0; k < n; ++k) {
         if (t[k].count < 0) return HQ_ERR_SHAPE;
         if (t[k].count == 0) continue;
@@ -290,7 +331,6 @@ hq_status run(const hq_grad_tensor* t, int64_t n, bool clip, float max_norm, flo
             return HQ_ERR_ALIGNMENT;
         if (t[k].count > int64_t(1) << 40) return HQ_ERR_UNSUPPORTED;
         total += t[k].count;
-        if (t[k].count > largest) largest = t[k].count;
     }
     Call c{t, n, clip, max_norm, eps, norm, coef, static_cast<double*>(workspace), kUnit, unsigned(kNormBlocks), static_cast<cudaStream_t>(stream)};
     const int64_t launches = (n + kMost - 1) / kMost;
@@ -298,23 +338,11 @@ hq_status run(const hq_grad_tensor* t, int64_t n, bool clip, float max_norm, flo
     // chunks of one step of a CTA while these are fewer than the CTAs; larger ones keep a CTA's steps together
     while (total / c.chunk > kNormBlocks * 4 && c.chunk < kUnit * 16) c.chunk *= 2;
     while (total / c.chunk > INT_MAX / 2) c.chunk *= 2;
-    int part = 0, blocks = 0;
-    int64_t from = 0;
-    do {                                           // the norms' parts of all tensors, then the outputs
-        const int64_t to = n - from > kMost ? from + kMost : n;
-        const hq_status e = launch_any(c, from, to, true, part, 0, &blocks, false);
-        if (e != HQ_OK) return e;
-        part += blocks;
-        from = to;
-    } while (from < n);
-    if (!clip) return launch_any(c, 0, 0, false, 0, part, &blocks, true);
-    while (from > 0) {                             // the last tensors first
-        const int64_t at = (from - 1) / kMost * kMost;
-        const hq_status e = launch_any(c, at, from, false, 0, part, &blocks, from == n);
-        if (e != HQ_OK) return e;
-        from = at;
-    }
-    return n == 0 ? launch_any(c, 0, 0, false, 0, part, &blocks, true) : HQ_OK;
+    // the parameters of a launch are copied three times on the host: no more of them than the tensors need
+    if (n <= 32) return run_once<32>(c);
+    if (n <= 128) return run_once<128>(c);
+    if (n <= 384) return run_once<384>(c);
+    return n <= kMost ? run_once<kMost>(c) : run_many(c);
 }
 
 }  // namespace

@@ -654,14 +654,56 @@ static PyObject* py_embedding_bwd(PyObject* self, PyObject* const* a, Py_ssize_t
     return PyLong_FromLong(r);
 }
 
-/* bind_block(int64, gate_norm, gate_norm_bwd, embedding, embedding_bwd), behind bind_attention */
+typedef hq_status (*grad_norm_fn)(const hq_grad_tensor*, int64_t, float*, void*, size_t, void*);
+typedef hq_status (*grad_clip_fn)(const hq_grad_tensor*, int64_t, float, float, float*, float*, void*, size_t, void*);
+static grad_norm_fn f_grad_norm;
+static grad_clip_fn f_grad_clip;
+/* one value, of no dimension or one */
+static int one_value(const char* name, PyObject* t, int64_t device, void** p) {
+    int64_t dim[1];
+    *p = NULL;
+    if (t == Py_None) return 0;
+    PyObject* s = PyObject_GetAttr(t, s_shape);
+    if (s == NULL) return -1;
+    const Py_ssize_t n = PyObject_Length(s);
+    Py_DECREF(s);
+    if (n < 0 || (n == 1 && shape(t, 1, dim)) || is_type(name, t, dt_f32)) return -1;
+    if (n > 1 || (n == 1 && dim[0] != 1)) {
+        PyErr_Format(PyExc_ValueError, "%s: one value", name);
+        return -1;
+    }
+    return here(name, t, device) || address(t, p) ? -1 : 0;
+}
+/* grad_clip(table's address, tensors, max_norm (None: the norm alone), eps, norm, coef, workspace, stream, device) */
+static PyObject* py_grad_clip(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    (void)self;
+    int64_t table, tensors, stream, dev;
+    float max_norm = 0.f, eps = 0.f;
+    void *norm, *coef, *ws;
+    size_t ws_bytes;
+    if (arguments(n, 9, f_grad_clip) || integer(a[0], &table) || integer(a[1], &tensors) || (a[2] != Py_None && (real(a[2], &max_norm) || real(a[3], &eps))) ||
+        integer(a[7], &stream) || integer(a[8], &dev) || one_value("norm", a[4], dev, &norm) || one_value("coef", a[5], dev, &coef) ||
+        workspace_of(a[6], dev, &ws, &ws_bytes))
+        return NULL;
+    hq_status r;
+    Py_BEGIN_ALLOW_THREADS
+    const hq_grad_tensor* t = (const hq_grad_tensor*)(intptr_t)table;
+    r = a[2] == Py_None ? f_grad_norm(t, tensors, norm, ws, ws_bytes, (void*)(intptr_t)stream)
+                        : f_grad_clip(t, tensors, max_norm, eps, norm, coef, ws, ws_bytes, (void*)(intptr_t)stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(r);
+}
+
+/* bind_block(int64, gate_norm, gate_norm_bwd, embedding, embedding_bwd, grad_norm, grad_clip), behind bind_attention */
 static PyObject* py_bind_block(PyObject* self, PyObject* args) {
     (void)self;
     PyObject* d;
-    unsigned long long p[4];
-    if (!PyArg_ParseTuple(args, "OKKKK", &d, &p[0], &p[1], &p[2], &p[3])) return NULL;
+    unsigned long long p[6];
+    if (!PyArg_ParseTuple(args, "OKKKKKK", &d, &p[0], &p[1], &p[2], &p[3], &p[4], &p[5])) return NULL;
     Py_INCREF(d);
     Py_XSETREF(dt_i64, d);
+    f_grad_norm = (grad_norm_fn)(uintptr_t)p[4];
+    f_grad_clip = (grad_clip_fn)(uintptr_t)p[5];
     f_gate_norm = (gate_norm_fn)(uintptr_t)p[0];
     f_gate_norm_bwd = (gate_norm_bwd_fn)(uintptr_t)p[1];
     f_embedding = (embedding_fn)(uintptr_t)p[2];
@@ -695,6 +737,7 @@ static PyMethodDef methods[] = {
     {"bind_block", py_bind_block, METH_VARARGS, NULL},
     {"gate_norm", (PyCFunction)(void (*)(void))py_gate_norm, METH_FASTCALL, NULL},
     {"gate_norm_bwd", (PyCFunction)(void (*)(void))py_gate_norm_bwd, METH_FASTCALL, NULL},
+    {"grad_clip", (PyCFunction)(void (*)(void))py_grad_clip, METH_FASTCALL, NULL},
     {"embedding", (PyCFunction)(void (*)(void))py_embedding, METH_FASTCALL, NULL},
     {"embedding_bwd", (PyCFunction)(void (*)(void))py_embedding_bwd, METH_FASTCALL, NULL},
     {"bind", py_bind, METH_VARARGS, NULL},

@@ -70,7 +70,7 @@ def test_against_64_bits(hq, ws, sizes, dtypes, offset):
                 assert all(bool((t[:o] == 7).all()) for t in r)
 
 
-@pytest.mark.parametrize("n", [31, 32, 33, 256, 257, 1099, 1100, 1101, 2300, 6001])
+@pytest.mark.parametrize("n", [31, 32, 33, 256, 257, 1087, 1088, 1089, 1099, 1100, 1101, 2300, 6001])
 def test_numbers_of_tensors(hq, ws, n):
     gen = torch.Generator(device="cuda").manual_seed(n)
     flat = torch.randn(n * 40, generator=gen, device="cuda")
