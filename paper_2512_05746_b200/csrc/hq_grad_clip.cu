@@ -152,6 +152,37 @@ __device__ __forceinline__ double all_parts(const double* parts, int n, double* 
     return sum;
 }
 
+// 8 values that nothing reads from L2 again, and 8 that are written once: they give way to what is still to be read.
+template <typename T> __device__ __forceinline__ void load_last(Vec8<T>& v, const void* base, int64_t at) {
+    if constexpr (sizeof(T) == 2) {
+        asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(v.w.x), "=r"(v.w.y), "=r"(v.w.z), "=r"(v.w.w) : "l"(static_cast<const T*>(base) + at));
+    } else {
+        asm volatile("ld.global.L1::no_allocate.L2::evict_first.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(v.a.x), "=f"(v.a.y), "=f"(v.a.z), "=f"(v.a.w), "=f"(v.b.x), "=f"(v.b.y), "=f"(v.b.z), "=f"(v.b.w) : "l"(static_cast<const T*>(base) + at));
+    }
+}
+template <typename U> __device__ __forceinline__ void store_once(void* base, int64_t at, const f32x2 (&f)[4]) {
+    U* p = static_cast<U*>(base) + at;
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) upk2(f[e], x[2 * e], x[2 * e + 1]);
+    if constexpr (sizeof(U) == 2) {
+        uint32_t u[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
+            u[e] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        asm volatile("st.global.cs.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]) : "memory");
+    } else if ((reinterpret_cast<uintptr_t>(p) & 31u) == 0) {
+        asm volatile("st.global.L1::no_allocate.L2::evict_first.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
+    } else {
+        Vec8<U>::store(base, at, f);
+    }
+}
+
 // out = c in, elements [from, to).
 template <typename T, typename U>
 __device__ __forceinline__ void scale(const void* in, void* out, int64_t from, int64_t to, int shift, bool wide_out, float c) {
@@ -164,7 +195,7 @@ __device__ __forceinline__ void scale(const void* in, void* out, int64_t from, i
         for (int u = 0; u < kAhead; ++u) {
             const int64_t i = base + u * kUnit;
             v[u].clear();
-            if (i >= from && i + 8 <= to) v[u].load_wide(in, i);
+            if (i >= from && i + 8 <= to) load_last(v[u], in, i);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -174,7 +205,7 @@ __device__ __forceinline__ void scale(const void* in, void* out, int64_t from, i
             v[u].get(f);
 #pragma unroll
             for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], c2);
-            if (i >= from && i + 8 <= to && wide_out) { Vec8<U>::store_wide(out, i, f); continue; }
+            if (i >= from && i + 8 <= to && wide_out) { store_once<U>(out, i, f); continue; }
             const bool whole = i >= from && i + 8 <= to;
             float e[8];
 #pragma unroll
