@@ -19,7 +19,7 @@ namespace hq {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kNormBlocks = 148 * 6, kScaleBlocks = 148 * 5;                       // resident at once; on every device: one order of the sums
+constexpr int kNormBlocks = 148 * 6, kScaleBlocks = 148 * 4;                       // resident at once; on every device: one order of the sums
 constexpr int64_t kUnit = kThreads * 8;            // elements a CTA takes at a time
 constexpr int kMost = 1088;                        // tensors of a launch: 28 bytes each of 32 KB of parameters, 2 for each CTA
 constexpr int kParts = 4096;                       // sums of CTAs of all launches of a call
@@ -198,26 +198,26 @@ template <typename U> __device__ __forceinline__ void store_once(void* base, int
 template <typename T, typename U>
 __device__ __forceinline__ void scale(const void* in, void* out, int64_t from, int64_t to, int shift, bool wide_out, float c) {
     constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;
-    const int64_t v0 = (from + shift) / 8 * 8 - shift;
     const f32x2 c2 = pk2(c, c);
-    for (int64_t base = v0 + int64_t(threadIdx.x) * 8; base < to; base += kUnit * kAhead) {
-        Vec8<T> v[kAhead];
+    auto request = [&](Vec8<T> (&v)[kAhead], int64_t base) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int64_t i = base + u * kUnit;
             v[u].clear();
             if (i >= from && i + 8 <= to) load_last(v[u], in, i);
         }
+    };
+    auto write = [&](const Vec8<T> (&v)[kAhead], int64_t base) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int64_t i = base + u * kUnit;
             if (i >= to) break;
+            const bool whole = i >= from && i + 8 <= to;
             f32x2 f[4];
             v[u].get(f);
 #pragma unroll
             for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], c2);
-            if (i >= from && i + 8 <= to && wide_out) { store_once<U>(out, i, f); continue; }
-            const bool whole = i >= from && i + 8 <= to;
+            if (whole && wide_out) { store_once<U>(out, i, f); continue; }
             float e[8];
 #pragma unroll
             for (int k = 0; k < 4; ++k) upk2(f[k], e[2 * k], e[2 * k + 1]);
@@ -229,6 +229,20 @@ __device__ __forceinline__ void scale(const void* in, void* out, int64_t from, i
                 else static_cast<float*>(out)[i + k] = x;
             }
         }
+    };
+    // two groups of vectors in turn: loads are on their way while the other group is written
+    constexpr int64_t kStep = kUnit * kAhead;
+    Vec8<T> a[kAhead], b[kAhead];
+    int64_t base = (from + shift) / 8 * 8 - shift + int64_t(threadIdx.x) * 8;
+    request(a, base);
+    while (base < to) {
+        request(b, base + kStep);
+        write(a, base);
+        base += kStep;
+        if (base >= to) break;
+        request(a, base + kStep);
+        write(b, base);
+        base += kStep;
     }
 }
 
