@@ -95,7 +95,7 @@ def test_against_64_bits(hq, rows, cols, per, norm, post, xt, ht):
 
 
 @pytest.mark.parametrize("rows,cols,per", [(3, 16, 1), (1000, 64, 1), (33, 256, 7), (513, 248, 100), (129, 768, 129), (300, 1000, 77), (40, 4096, 13),
-                                           (9, 4088, 2), (2000, 320, 1999), (5000, 512, 0), (7, 1280, 1000000)])
+                                           (9, 4088, 2), (2000, 320, 1999), (5000, 512, 0), (7, 1280, 1000000), (77, 72, 10), (500, 128, 6), (41, 8, 3)])
 def test_shapes(hq, rows, cols, per):
     run(hq, rows, cols, per, pad=8)
     run(hq, rows, cols, per, "rms", "rms", F, BF, pad=16)
@@ -108,7 +108,7 @@ def test_many_rows(hq):
 
 
 @pytest.mark.parametrize("norm,post", [("layer", "none"), ("rms", "rms")])
-@pytest.mark.parametrize("rows,cols,per", [(154, 256, 77), (1000, 1152, 77), (33, 64, 4), (64, 2304, 16)])
+@pytest.mark.parametrize("rows,cols,per", [(154, 256, 77), (1000, 1152, 77), (33, 64, 4), (64, 2304, 16), (100, 128, 11), (90, 56, 7), (70, 120, 64)])
 def test_lengths(hq, rows, cols, per, norm, post):
     groups = -(-rows // per)
     lens = torch.tensor([(i * 5) % (per + 3) - 1 for i in range(groups)], dtype=torch.int32, device="cuda")     # none, negative, all, too many
