@@ -13,6 +13,7 @@ template <typename S, typename B, bool POST, int L, int kStages>
 __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
     extern __shared__ uint4 ring[];
     __shared__ float2 room[2 * 32];
+    __shared__ float4 moments_in[kStages][kMaxWarps][Team<L>::kBatch];         // the statistics on their way: each warp copies its own
     Team<L> t = team_of<L>(p, room);
     constexpr int kSide = Team<L>::kSide;
     const uint32_t team = blockIdx.x, r0 = team * p.chunk, r1 = min(r0 + p.chunk, p.rows);
@@ -26,13 +27,17 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
     b.start(p, r0, r1);
     ahead = b;
     uint32_t to = base, at = base;
+    int slot = 0, now = 0;                         // of the statistics: to send to, to take from
     auto send_next = [&]() {
         if (ahead.n > 0) {
             if (normed) { send<S>(to, x, p.x.ld, ahead, t); send<B>(to + y_at, dy, p.dy.ld, ahead, t); }
             if (later) send<S>(to + d_at, dx_out, p.dx_out.ld, ahead, t);
             if (branch) send<B>(to + h_at, h, p.h.ld, ahead, t);
+            if ((normed || POST) && t.lane < Team<L>::kBatch)
+                copy_ahead(smem_u32(&moments_in[slot][t.warp][t.lane]), p.stats + 4 * (int64_t(ahead.row) + (t.lane < ahead.live ? t.lane : 0)), t.lane < ahead.live);
             ahead.next(p, r1);
         }
+        slot = slot == kStages - 1 ? 0 : slot + 1;
         copies_sent();
         to = to == base + (kStages - 1) * batch ? base : to + batch;
     };
@@ -49,16 +54,13 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
             fill(dweight, 0.f); fill(dbias, 0.f); fill(dgate, 0.f);
             fresh = false;
         }
-        float4 stats[kRows];
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            stats[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            const int r = i * kSide + t.side;
-            if (r < b.live && (normed || POST)) stats[i] = reinterpret_cast<const float4*>(p.stats)[b.row + r];
-        }
         __syncwarp();                              // no lane of the warp still reads the batch before this one
         send_next();                               // into its place
         copies_wait<kStages - 1>();
+        float4 stats[kRows];                       // zeros for rows that are not there
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) stats[i] = normed || POST ? moments_in[now][t.warp][i * kSide + t.side] : make_float4(0.f, 0.f, 0.f, 0.f);
+        now = now == kStages - 1 ? 0 : now + 1;
         if (b.live == 0) {                         // nothing but zeros to write
             put_zeros<S>(dx, p.dx, b, t);
             put_zeros<B>(dh, p.dh, b, t);
@@ -201,6 +203,14 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
 // group itself, or, where there are more groups than teams, the group at a border of two teams' rows, which the first border inside it takes),
 // then the columns of dpost_weight.  Thread = (4 columns, every 1024 / wide'th part).
 struct Joins { uint32_t teams, heads, group_ctas, post_ctas; int wide, post_wide, by_group; };         // CTAs: of a head, of dpost_weight
+// One value of each of four parts in one statement: as loads of their own the compiler puts each sum behind its load.
+__device__ __forceinline__ void ld_four(float4 (&x)[4], const float4* const (&from)[4]) {
+#define HQ_OUT4(u) "=f"(x[u].x), "=f"(x[u].y), "=f"(x[u].z), "=f"(x[u].w)
+    asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%16];\n\tld.global.cg.v4.f32 {%4, %5, %6, %7}, [%17];\n\t"
+                 "ld.global.cg.v4.f32 {%8, %9, %10, %11}, [%18];\n\tld.global.cg.v4.f32 {%12, %13, %14, %15}, [%19];"
+                 : HQ_OUT4(0), HQ_OUT4(1), HQ_OUT4(2), HQ_OUT4(3) : "l"(from[0]), "l"(from[1]), "l"(from[2]), "l"(from[3]) : "memory");
+#undef HQ_OUT4
+}
 __device__ __forceinline__ float4 plus(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 __global__ void __launch_bounds__(256) gate_norm_sums_kernel(const GateNormParams p, const Joins j) {
     __shared__ float4 sums[3][256];
@@ -224,12 +234,25 @@ __global__ void __launch_bounds__(256) gate_norm_sums_kernel(const GateNormParam
     if (c < p.cols) {
         const float* parts = post ? p.post_parts + c : p.parts + c;
         const int64_t step = post ? p.cols : int64_t(6) * p.cols;
-#pragma unroll 4
-        for (uint32_t i = from + way; i <= to; i += ways) {
-            const float4* part = reinterpret_cast<const float4*>(parts + i * step + (second && i == from ? 3 * p.cols : 0));
-            if (want0) sum0 = plus(sum0, ld_dependent_cg(part));
-            if (want1) sum1 = plus(sum1, ld_dependent_cg(part + p.cols / 4));
-            if (want2) sum2 = plus(sum2, ld_dependent_cg(part + p.cols / 2));
+        if (post) {                                // many parts: four at a time; of one behind the last the last one is read and not added
+            for (uint32_t i = from + way; i <= to; i += 4 * ways) {
+                const float4* part[4];
+                float4 x[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) part[u] = reinterpret_cast<const float4*>(parts + min(i + u * ways, to) * step);
+                ld_four(x, part);
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (i + u * ways <= to) sum0 = plus(sum0, x[u]);
+            }
+        } else {
+#pragma unroll 2
+            for (uint32_t i = from + way; i <= to; i += ways) {
+                const float4* part = reinterpret_cast<const float4*>(parts + i * step + (second && i == from ? 3 * p.cols : 0));
+                if (want0) sum0 = plus(sum0, ld_dependent_cg(part));
+                if (want1) sum1 = plus(sum1, ld_dependent_cg(part + p.cols / 4));
+                if (want2) sum2 = plus(sum2, ld_dependent_cg(part + p.cols / 2));
+            }
         }
     }
     sums[0][threadIdx.x] = sum0; sums[1][threadIdx.x] = sum1; sums[2][threadIdx.x] = sum2;
@@ -350,8 +373,8 @@ extern "C" hq_status hq_gate_norm_bwd(const void* x_out, int64_t ldx_out, hq_dty
     j.teams = uint32_t(teams);
     j.by_group = groups < teams;
     j.heads = !split ? 0u : uint32_t(j.by_group ? groups : teams - 1);
-    // columns a CTA: as many as leave a thread two parts or more
-    auto wide_for = [](int64_t parts) { int wide = 1024; while (wide > 32 && parts > 1024 / wide * 2) wide /= 2; return wide; };
+    // columns a CTA: as many as leave a thread two parts or more (one group of all rows, dpost_weight: 64 threads a column's parts)
+    auto wide_for = [](int64_t parts) { int wide = 1024; while (wide > 16 && parts > 1024 / wide * 2) wide /= 2; return wide; };
     j.wide = wide_for(p.group / p.chunk + 2);
     j.post_wide = wide_for(teams);
     j.group_ctas = uint32_t((cols + j.wide - 1) / j.wide);
