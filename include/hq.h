@@ -439,8 +439,8 @@ hq_status hq_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ld
 
 /* ---- What a training step of a transformer block needs around its linears and its attention: the gated residual with the norms before and
  * after a block, the embedding lookup, both with their gradients, and the norm of all gradients with clipping (no counterpart in the paper's
- * equations).  Matrices [rows][ld] with contiguous columns, base pointers 16-byte aligned, pitches multiples of 16 bytes, numbers of columns
- * multiples of 8.  Outputs may not overlap inputs, except where said.  Every sum runs in a fixed order: the same inputs give the same
+ * equations).  Matrices [rows][ld] with contiguous columns, base pointers 16-byte aligned, pitches multiples of 16 bytes and below 2^30
+ * elements, numbers of columns multiples of 8, at most 2^31 - 1 rows.  Outputs may not overlap inputs, except where said.  Every sum runs in a fixed order: the same inputs give the same
  * bits. -----
  *
  * hq_gate_norm: the end of one block and the norm in front of the next.  Per row r, with the vectors of its group n = r / rows_per_group (a
@@ -484,7 +484,7 @@ hq_status hq_gate_norm_bwd(const void* x_out, int64_t ldx_out, hq_dtype xdt, con
  *   ids        device int32 or int64 (id_bytes 4 or 8) [tokens].  table [classes], out [tokens] rows of dim values, fp32 or bf16 each.
  * hq_embedding_bwd: dtable[v] = base[v] + scale * sum of dout[t] over the tokens t of id v, in ascending order, in fp32; ids outside the
  *   table have no part.  base: rows of dtable's type, or NULL (zeros: every row of dtable is written); base may be dtable (the gradient of an
- *   earlier micro-batch: rows without tokens are not touched).  With scale 1 it is the gradient of hq_class_embed_add's table, too.
+ *   earlier micro-batch: rows without tokens are not touched; an addition to an fp32 base takes values below 2^-126 as zero).  With scale 1 it is the gradient of hq_class_embed_add's table, too.
  *   workspace  hq_embedding_bwd_workspace_size bytes, 16-byte aligned; as above.  dim <= 65536. */
 hq_status hq_embedding(const void* ids, int id_bytes, int64_t tokens, const void* table, hq_dtype tdt, int64_t classes, int64_t dim,
                        int64_t ld_table, float scale, void* out, hq_dtype odt, int64_t ld_out, void* stream);

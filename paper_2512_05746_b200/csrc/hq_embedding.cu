@@ -134,8 +134,15 @@ __device__ __forceinline__ void fill_rows(const GradParams& p, uint32_t v0, uint
             for (int v = lane; v < pieces; v += 32) to[v] = make_uint4(0u, 0u, 0u, 0u);
         } else {
             const uint4* from = reinterpret_cast<const uint4*>(static_cast<const char*>(p.base) + uint64_t(v0 + r) * p.ld_base);
-#pragma unroll 4
-            for (int v = lane; v < pieces; v += 32) to[v] = from[v];
+            constexpr int kAhead = 5;
+            for (int v = lane; v < pieces; v += 32 * kAhead) {
+                uint4 x[kAhead];
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) x[u] = v + 32 * u < pieces ? from[v + 32 * u] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+                    if (v + 32 * u < pieces) to[v + 32 * u] = x[u];
+            }
         }
     }
 }
@@ -545,11 +552,14 @@ Plan plan_of(int64_t tokens, int64_t classes, int64_t dim, int piece) {
     const int64_t slice = (classes + 147) / 148;
     a.slice = uint32_t(slice < kSlice ? slice : kSlice);
     a.slices = uint32_t((classes + a.slice - 1) / a.slice);
-    // spans for two CTAs an SM, of up to 64 tokens, and no more tokens in a CTA than its room for entries
+    // spans for two CTAs an SM, of up to 64 tokens, and no more tokens in a CTA than its room for entries; where an id may lie in many of them
+    // no shorter than sqrt(tokens) / 6: adding up their sums takes as long as a span's rows then (3691 tokens of 64 channels, half of them of
+    // one id: spans of one token 29 us a call)
     const int pieces = int(dim / piece), slots = 256 / (pieces < 256 ? pieces : 256);
     int64_t span = 1;
     while (span < 64 && tokens * pieces > span * 148 * 2 * 256) span *= 2;
     a.longest = 64;
+    while (span < 64 && tokens > a.longest && 36 * span * span < tokens) span *= 2;
     while (span > 1 && slots * span + a.longest > kEntries) span /= 2;
     a.span = uint32_t(span);
     a.spans = uint32_t((tokens + span - 1) / span);

@@ -155,7 +155,7 @@ extern "C" hq_status hq_gate_norm(const void* x, int64_t ldx, hq_dtype xdt, cons
         return e;
     if (!aligned16(stats)) return HQ_ERR_ALIGNMENT;
     GateNormParams p{};
-    p.rows = uint32_t(rows); p.group = uint32_t(group < rows ? group : rows); p.cols = int(cols); p.warps = team_warps(cols); p.lens = lens;
+    p.rows = uint32_t(rows); p.group = uint32_t(group); p.cols = int(cols); p.warps = team_warps(cols); p.lens = lens;
     p.layer = norm == HQ_NORM_LAYER; p.post_layer = post == HQ_NORM_LAYER; p.post_weight = post_weight;
     p.gate = Vectors{gate, ld_gate}; p.weight = Vectors{weight, ld_weight}; p.bias = Vectors{bias, ld_bias};
     p.residual = residual_scale; p.plus = weight_plus; p.eps = eps; p.stats = stats;

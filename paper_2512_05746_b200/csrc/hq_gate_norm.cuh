@@ -327,7 +327,7 @@ inline hq_status check_sizes(hq_dtype xdt, hq_dtype hdt, int64_t rows, int64_t c
     if (!aligned16(post_weight)) return HQ_ERR_ALIGNMENT;
     if (!(residual - residual == 0.f)) return HQ_ERR_INVALID_ARG;
     if (h == nullptr && (post != HQ_NORM_NONE || gate != nullptr || residual != 1.f)) return HQ_ERR_INVALID_ARG;
-    *group = rows_per_group > 0 ? rows_per_group : rows > 0 ? rows : 1;
+    *group = rows_per_group > 0 && rows_per_group < rows ? rows_per_group : rows > 0 ? rows : 1;        // one group: at most all rows
     return HQ_OK;
 }
 

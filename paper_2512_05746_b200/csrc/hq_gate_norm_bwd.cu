@@ -341,7 +341,7 @@ extern "C" hq_status hq_gate_norm_bwd(const void* x_out, int64_t ldx_out, hq_dty
     if ((normed || after) && stats == nullptr) return HQ_ERR_INVALID_ARG;
     if (!aligned16(stats) || !aligned16(dpost_weight)) return HQ_ERR_ALIGNMENT;
     GateNormParams p{};
-    p.rows = uint32_t(rows); p.group = uint32_t(group < rows ? group : rows); p.cols = int(cols); p.warps = team_warps(cols); p.lens = lens;
+    p.rows = uint32_t(rows); p.group = uint32_t(group); p.cols = int(cols); p.warps = team_warps(cols); p.lens = lens;
     p.chunk = uint32_t(grad_chunk(rows, cols));
     const int64_t teams = (rows + p.chunk - 1) / p.chunk;
     const bool sums = dgate != nullptr || dweight != nullptr || dbias != nullptr;

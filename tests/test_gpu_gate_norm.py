@@ -101,6 +101,17 @@ def test_shapes(hq, rows, cols, per):
     run(hq, rows, cols, per, "rms", "rms", F, BF, pad=16)
 
 
+@pytest.mark.parametrize("rows,cols,per", [(33, 4096, 0), (21, 3848, 4), (9, 3584, 1)])
+def test_widest_rows_of_fp32(hq, rows, cols, per):
+    run(hq, rows, cols, per, xt=F, ht=F)
+    run(hq, rows, cols, per, "rms", "layer", F, F, gated=False)
+
+
+def test_groups_larger_than_all_rows(hq):
+    a, b = run(hq, 50, 128, (1 << 63) - 1), run(hq, 50, 128, 50)
+    assert all(torch.equal(s, t) for s, t in zip(a, b))
+
+
 def test_many_rows(hq):
     run(hq, 20011, 1152, 256)
     run(hq, 70001, 64, 0, "rms", "layer", F, F)

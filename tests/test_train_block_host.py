@@ -49,7 +49,7 @@ def norm_bwd(hq, **change):
     (dict(post=RMS, post_weight=ODD), ALIGNMENT), (dict(residual=NAN), INVALID), (dict(residual=INF), INVALID), (dict(plus=NAN), INVALID),
     (dict(h=None), INVALID), (dict(h=None, gate=None, residual=0.5), INVALID), (dict(h=None, gate=None, post=RMS), INVALID),
     (dict(x=None), INVALID), (dict(x=HALF), ALIGNMENT), (dict(h=HALF), ALIGNMENT), (dict(ldx=56), SHAPE), (dict(ldh=60), SHAPE), (dict(ldx=68), ALIGNMENT),
-    (dict(xdt=0, ldx=66), ALIGNMENT), (dict(gate=HALF), ALIGNMENT), (dict(ld_gate=60), SHAPE), (dict(ld_gate=66), ALIGNMENT),
+    (dict(xdt=0, ldx=66), ALIGNMENT), (dict(ldx=1 << 30), UNSUPPORTED), (dict(ldh=1 << 33), UNSUPPORTED), (dict(gate=HALF), ALIGNMENT), (dict(ld_gate=60), SHAPE), (dict(ld_gate=66), ALIGNMENT),
     (dict(weight=ODD), ALIGNMENT), (dict(ld_weight=0), SHAPE), (dict(stats=HALF), ALIGNMENT)])
 def test_gate_norm_refuses(hq, call, change, want):
     assert call(hq, **change) == want
@@ -95,7 +95,7 @@ def embed_bwd(hq, **change):
     (dict(tokens=1 << 31), UNSUPPORTED), (dict(classes=1 << 31), UNSUPPORTED), (dict(id_bytes=2), INVALID), (dict(tdt=2), INVALID), (dict(odt=7), INVALID),
     (dict(scale=NAN), INVALID), (dict(scale=INF), INVALID), (dict(ids=None), INVALID), (dict(table=None), INVALID), (dict(out=None), INVALID),
     (dict(ids=C.c_void_p(0x1002)), ALIGNMENT), (dict(id_bytes=8, ids=ODD), ALIGNMENT), (dict(table=HALF), ALIGNMENT), (dict(out=HALF), ALIGNMENT),
-    (dict(ld=56), SHAPE), (dict(ldo=0), SHAPE), (dict(ldo=68), ALIGNMENT)])
+    (dict(ld=56), SHAPE), (dict(ldo=0), SHAPE), (dict(ldo=68), ALIGNMENT), (dict(ld=1 << 30), UNSUPPORTED), (dict(ldo=1 << 32), UNSUPPORTED)])
 def test_embedding_refuses(hq, call, change, want):
     assert call(hq, **change) == want
 
