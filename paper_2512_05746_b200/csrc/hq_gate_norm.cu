@@ -28,10 +28,12 @@ __global__ void __maxnreg__(96) gate_norm_kernel(const GateNormParams p) {
     Team<L> t = team_of<L>(p, room);
     constexpr int kSide = Team<L>::kSide;
     const uint32_t r0 = blockIdx.x * p.chunk, r1 = min(r0 + p.chunk, p.rows);
-    const uint32_t plane = blockDim.x * 16u, batch = plane * kForwardPlanes<S, B>, h_at = plane * kRows * kPlanes<S>;
-    const uint32_t base = smem_u32(ring);
+    constexpr uint32_t batch = kPlane * kForwardPlanes<S, B>, h_at = kPlane * kRows * kPlanes<S>;
+    const uint32_t base = smem_u32(ring) + uint32_t(t.warp) * kStages * batch, lane = uint32_t(t.lane) * 16u;
+    const Pieces<S, L> wide(t);
+    const Pieces<B, L> narrow(t);
     const bool branch = p.h.p != nullptr, normed = p.y.p != nullptr;
-    const char *x = copied<S>(p.x, t), *h = copied<B>(p.h, t);
+    const char *x = copied(p.x, wide.first), *h = copied(p.h, narrow.first);
     char *x_out = columns<S>(p.x_out, t), *y = columns<B>(p.y, t);
     typename Team<L>::Walk b, ahead;
     b.start(p, r0, r1);
@@ -39,8 +41,8 @@ __global__ void __maxnreg__(96) gate_norm_kernel(const GateNormParams p) {
     uint32_t to = base;
     auto send_next = [&]() {
         if (ahead.n > 0) {
-            send<S>(to, x, p.x.ld, ahead, t);
-            if (branch) send<B>(to + h_at, h, p.h.ld, ahead, t);
+            send(to, x, p.x.ld, ahead, t, wide);
+            if (branch) send(to + h_at, h, p.h.ld, ahead, t, narrow);
             ahead.next(p, r1);
         }
         copies_sent();
@@ -48,12 +50,12 @@ __global__ void __maxnreg__(96) gate_norm_kernel(const GateNormParams p) {
     };
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) send_next();
-    f32x2 gate[4], weight[4], bias[4], post_weight[4];
-    if (POST) load_vector(post_weight, Vectors{p.post_weight, 0}, 0, t, 0.f, 1.f);
+    f32x2 gate[4], weight[4], bias[4];             // gate: times post_weight
     uint32_t loaded = 0xffffffffu, at = base;
     while (b.n > 0) {
         if (b.g != loaded) {
             load_vector(gate, p.gate, b.g, t, 0.f, 1.f);
+            if (POST) times_vector(gate, p.post_weight, t);
             if (normed) {
                 load_vector(weight, p.weight, b.g, t, p.plus, 1.f);
                 load_vector(bias, p.bias, b.g, t, 0.f, 0.f);
@@ -72,12 +74,12 @@ __global__ void __maxnreg__(96) gate_norm_kernel(const GateNormParams p) {
         }
         f32x2 v[kRows][4];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) take<S>(v[i], at, i);
+        for (int i = 0; i < kRows; ++i) take<S>(v[i], at + lane, i);
         float mean[kRows] = {0.f, 0.f}, inv[kRows] = {1.f, 1.f}, post_mean[kRows] = {0.f, 0.f}, post_inv[kRows] = {1.f, 1.f};
         if (branch) {
             f32x2 u[kRows][4];
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) take<B>(u[i], at + h_at, i);
+            for (int i = 0; i < kRows; ++i) take<B>(u[i], at + h_at + lane, i);
             if (POST) moments(t, u, p.post_layer, p.eps, post_mean, post_inv);
             const f32x2 residual = pk2(p.residual, p.residual);
 #pragma unroll
@@ -85,7 +87,7 @@ __global__ void __maxnreg__(96) gate_norm_kernel(const GateNormParams p) {
                 const f32x2 less = pk2(-post_mean[i], -post_mean[i]), s = pk2(post_inv[i], post_inv[i]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if (POST) u[i][e] = mul2(mul2(add2(u[i][e], less), s), post_weight[e]);
+                    if (POST) u[i][e] = mul2(add2(u[i][e], less), s);
                     v[i][e] = fma2(residual, v[i][e], mul2(gate[e], u[i][e]));
                 }
             }

@@ -202,11 +202,21 @@ __device__ __forceinline__ void load_vector(f32x2 (&v)[4], const Vectors& from, 
     v[0] = pk2(a.x + add, a.y + add); v[1] = pk2(a.z + add, a.w + add); v[2] = pk2(b.x + add, b.y + add); v[3] = pk2(b.z + add, b.w + add);
 }
 
-// ---- rows on their way through shared memory: a thread's 16 or 32 bytes of a row, in planes of 16 bytes a thread.  Neighbouring lanes copy
-// neighbouring 16 bytes; of fp32 they are another lane's of the warp (copied by their own lane, half of every sector would be asked for twice) ----
+template <int L>
+__device__ __forceinline__ void times_vector(f32x2 (&v)[4], const float* by, const Team<L>& t) {
+    f32x2 w[4];
+    load_vector(w, Vectors{by, 0}, 0, t, 0.f, 1.f);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = mul2(v[e], w[e]);
+}
+
+// ---- rows on their way through shared memory: a thread's 16 or 32 bytes of a row, in planes of 16 bytes a lane, 512 bytes a plane; each warp
+// copies its own.  Neighbouring lanes copy neighbouring 16 bytes; of fp32 they are another lane's of the warp (copied by their own lane, half of
+// every sector would be asked for twice) ----
 template <typename T> constexpr int kPlanes = int(sizeof(T)) * 8 / 16;
-__device__ __forceinline__ void copy_ahead(uint32_t to, const void* from, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+constexpr uint32_t kPlane = 512;
+__device__ __forceinline__ void copy_bytes(uint32_t to, const void* from, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copies_sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() {
@@ -214,31 +224,40 @@ template <int N> __device__ __forceinline__ void copies_wait() {
     __syncwarp();
 }
 __device__ __forceinline__ uint64_t row_at(uint32_t row, uint32_t ld) { return uint64_t(row) * ld; }
-// Where this thread's copies of a row begin, and its own columns' place in an output.
-template <typename T, int L> __device__ __forceinline__ const char* copied(const Matrix& m, const Team<L>& t) {
-    return static_cast<const char*>(m.p) + (sizeof(T) == 2 ? t.c0 * 2 : (t.warp * 256 + t.place * 4) * 4);
-}
-template <typename T, int L> __device__ __forceinline__ char* columns(const MatrixOut& m, const Team<L>& t) { return static_cast<char*>(m.p) + t.c0 * int(sizeof(T)); }
-// `at`: the batch's first plane; zeros for rows that are not there.
+
+// What a thread copies of a row of T: pieces of 16 bytes (two of fp32: number k * L + place of the row's 2 L in this warp, that of lane piece / 2,
+// plane piece % 2), with their bytes (0 behind the last column) and places.
+template <typename T, int L> struct Pieces {
+    uint32_t to, bytes[kPlanes<T>], apart;         // apart: from the first to the second in the row (0 where that has no columns)
+    int first;                                     // bytes from the row's beginning (0 behind the last column)
+    __device__ __forceinline__ explicit Pieces(const Team<L>& t) {
+        if constexpr (sizeof(T) == 2) {
+            to = uint32_t(t.lane) * 16u;
+            bytes[0] = t.col ? 16u : 0u;
+            first = t.col ? t.c0 * 2 : 0;
+            apart = 0;
+        } else {
+            const int c = t.warp * 256 + t.place * 4;
+            to = uint32_t(t.lane & 1) * kPlane + uint32_t((t.lane & ~(L - 1)) + t.place / 2) * 16u;
+            bytes[0] = c < t.cols ? 16u : 0u;
+            bytes[1] = c + L * 4 < t.cols ? 16u : 0u;
+            first = c < t.cols ? c * 4 : 0;
+            apart = c + L * 4 < t.cols ? uint32_t(L) * 16u : 0u;
+        }
+    }
+};
+// `at`: the warp's first plane of the matrix; from: the matrix's first row, at this thread's first piece; zeros for rows that are not there.
 template <typename T, int L>
-__device__ __forceinline__ void send(uint32_t at, const char* from, uint32_t ld, const typename Team<L>::Walk& b, const Team<L>& t) {
-    const uint32_t plane = blockDim.x * 16u;
+__device__ __forceinline__ void send(uint32_t at, const char* from, uint32_t ld, const typename Team<L>::Walk& b, const Team<L>& t, const Pieces<T, L>& mine) {
+    const char* base = from + row_at(b.row, ld);
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-        const int r = i * Team<L>::kSide + t.side;
-        const bool live = r < b.live;
-        const char* row = from + row_at(b.row, ld) + (live ? uint32_t(r) * uint64_t(ld) : 0u);
-        if constexpr (sizeof(T) == 2) {
-            copy_ahead(at + uint32_t(i) * plane + threadIdx.x * 16u, t.col ? row : row - t.c0 * 2, live && t.col);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {          // piece k * L + place of the row's (the warp's) 2 L: of lane piece / 2, plane piece % 2
-                const int c = t.warp * 256 + (k * L + t.place) * 4;
-                const bool col = c < t.cols;
-                copy_ahead(at + (uint32_t(i) * 2u + (t.lane & 1u)) * plane + ((threadIdx.x & ~uint32_t(L - 1)) + uint32_t(k * (L / 2) + t.place / 2)) * 16u,
-                           col ? row + k * L * 16 : row - (t.warp * 256 + t.place * 4) * 4, live && col);
-            }
-        }
+        const uint32_t r = uint32_t(i * Team<L>::kSide + t.side);
+        const bool live = int(r) < b.live;
+        const char* row = L == 32 && i == 0 ? base : base + (live ? r * uint64_t(ld) : 0u);
+        copy_bytes(at + mine.to + uint32_t(i * kPlanes<T>) * kPlane, row, live ? mine.bytes[0] : 0u);
+        if constexpr (sizeof(T) == 4)
+            copy_bytes(at + mine.to + uint32_t(i * 2) * kPlane + uint32_t(L) * 8u, row + mine.apart, live ? mine.bytes[1] : 0u);
     }
 }
 __device__ __forceinline__ uint4 plane_at(uint32_t at) {
@@ -246,20 +265,22 @@ __device__ __forceinline__ uint4 plane_at(uint32_t at) {
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
 }
-// This thread's columns of row i of the batch whose first plane is `at`.
+// This lane's columns of row i; `at`: the lane's place in the matrix's first plane.
 template <typename T>
 __device__ __forceinline__ void take(f32x2 (&v)[4], uint32_t at, int i) {
-    const uint32_t plane = blockDim.x * 16u, mine = at + threadIdx.x * 16u;
     Vec8<T> raw;
     if constexpr (sizeof(T) == 2) {
-        raw.w = plane_at(mine + uint32_t(i) * plane);
+        raw.w = plane_at(at + uint32_t(i) * kPlane);
     } else {
-        const uint4 a = plane_at(mine + uint32_t(2 * i) * plane), b = plane_at(mine + uint32_t(2 * i + 1) * plane);
+        const uint4 a = plane_at(at + uint32_t(2 * i) * kPlane), b = plane_at(at + uint32_t(2 * i + 1) * kPlane);
         raw.a = make_float4(__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w));
         raw.b = make_float4(__uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w));
     }
     raw.get(v);
 }
+template <typename T, int L> __device__ __forceinline__ char* columns(const MatrixOut& m, const Team<L>& t) { return static_cast<char*>(m.p) + t.c0 * int(sizeof(T)); }
+__device__ __forceinline__ const char* copied(const Matrix& m, int first) { return static_cast<const char*>(m.p) + first; }
+
 // Rows that are not there leave as zeros.
 template <int L>
 __device__ __forceinline__ void clear_dead(const typename Team<L>::Walk& b, const Team<L>& t, f32x2 (&v)[kRows][4]) {

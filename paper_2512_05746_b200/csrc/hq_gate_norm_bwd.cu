@@ -18,10 +18,13 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
     constexpr int kSide = Team<L>::kSide;
     const uint32_t team = blockIdx.x, r0 = team * p.chunk, r1 = min(r0 + p.chunk, p.rows);
     griddep_launch();                              // all teams are at work at once: the joining kernel takes no place of theirs
-    const uint32_t plane = blockDim.x * 16u, batch = plane * kGradPlanes<S, B>, s_size = plane * kRows * kPlanes<S>, b_size = plane * kRows * kPlanes<B>;
-    const uint32_t base = smem_u32(ring), y_at = s_size, d_at = s_size + b_size, h_at = 2 * s_size + b_size;
+    constexpr uint32_t batch = kPlane * kGradPlanes<S, B>, s_size = kPlane * kRows * kPlanes<S>, b_size = kPlane * kRows * kPlanes<B>;
+    constexpr uint32_t y_at = s_size, d_at = s_size + b_size, h_at = 2 * s_size + b_size;
+    const uint32_t base = smem_u32(ring) + uint32_t(t.warp) * kStages * batch, lane = uint32_t(t.lane) * 16u;
+    const Pieces<S, L> wide(t);
+    const Pieces<B, L> narrow(t);
     const bool normed = p.dy.p != nullptr, gated = p.dgate.p != nullptr, later = p.dx_out.p != nullptr, branch = POST || gated;       // h itself is read
-    const char *x = copied<S>(p.x, t), *dy = copied<B>(p.dy, t), *dx_out = copied<S>(p.dx_out, t), *h = copied<B>(p.h, t);
+    const char *x = copied(p.x, wide.first), *dy = copied(p.dy, narrow.first), *dx_out = copied(p.dx_out, wide.first), *h = copied(p.h, narrow.first);
     char *dx = columns<S>(p.dx, t), *dh = columns<B>(p.dh, t);
     typename Team<L>::Walk b, ahead;
     b.start(p, r0, r1);
@@ -30,11 +33,11 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
     int slot = 0, now = 0;                         // of the statistics: to send to, to take from
     auto send_next = [&]() {
         if (ahead.n > 0) {
-            if (normed) { send<S>(to, x, p.x.ld, ahead, t); send<B>(to + y_at, dy, p.dy.ld, ahead, t); }
-            if (later) send<S>(to + d_at, dx_out, p.dx_out.ld, ahead, t);
-            if (branch) send<B>(to + h_at, h, p.h.ld, ahead, t);
+            if (normed) { send(to, x, p.x.ld, ahead, t, wide); send(to + y_at, dy, p.dy.ld, ahead, t, narrow); }
+            if (later) send(to + d_at, dx_out, p.dx_out.ld, ahead, t, wide);
+            if (branch) send(to + h_at, h, p.h.ld, ahead, t, narrow);
             if ((normed || POST) && t.lane < Team<L>::kBatch)
-                copy_ahead(smem_u32(&moments_in[slot][t.warp][t.lane]), p.stats + 4 * (int64_t(ahead.row) + (t.lane < ahead.live ? t.lane : 0)), t.lane < ahead.live);
+                copy_bytes(smem_u32(&moments_in[slot][t.warp][t.lane]), p.stats + 4 * (int64_t(ahead.row) + (t.lane < ahead.live ? t.lane : 0)), t.lane < ahead.live ? 16u : 0u);
             ahead.next(p, r1);
         }
         slot = slot == kStages - 1 ? 0 : slot + 1;
@@ -43,13 +46,13 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
     };
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) send_next();
-    f32x2 post_weight[4], dpost[4], gate[4], weight[4], dweight[4], dbias[4], dgate[4];
+    f32x2 dpost[4], gate[4], weight[4], dweight[4], dbias[4], dgate[4];
     fill(dpost, 0.f);
-    if (POST) load_vector(post_weight, Vectors{p.post_weight, 0}, 0, t, 0.f, 1.f);
     bool fresh = true, begun = b.g * p.group == r0;            // begun: the group's first row is this team's
     while (b.n > 0) {
         if (fresh) {
-            load_vector(gate, p.gate, b.g, t, 0.f, 1.f);
+            load_vector(gate, p.gate, b.g, t, 0.f, 1.f);       // with a norm behind the block: times post_weight
+            if (POST) times_vector(gate, p.post_weight, t);
             load_vector(weight, p.weight, b.g, t, p.plus, 1.f);
             fill(dweight, 0.f); fill(dbias, 0.f); fill(dgate, 0.f);
             fresh = false;
@@ -73,8 +76,8 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
                 for (int i = 0; i < kRows; ++i) {
                     const f32x2 less = pk2(-stats[i].x, -stats[i].x), inv = pk2(stats[i].y, stats[i].y);
                     f32x2 a = pk2(0.f, 0.f), c = pk2(0.f, 0.f);
-                    take<S>(xh[i], at, i);
-                    take<B>(d[i], at + y_at, i);
+                    take<S>(xh[i], at + lane, i);
+                    take<B>(d[i], at + y_at + lane, i);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         xh[i][e] = mul2(add2(xh[i][e], less), inv);
@@ -102,7 +105,7 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
 #pragma unroll
                 for (int i = 0; i < kRows; ++i) {
                     f32x2 o[4];
-                    take<S>(o, at + d_at, i);
+                    take<S>(o, at + d_at + lane, i);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) d[i][e] = add2(d[i][e], o[e]);
                 }
@@ -125,12 +128,12 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
                 for (int i = 0; i < kRows; ++i) {
                     const f32x2 less = pk2(-stats[i].z, -stats[i].z), inv = pk2(stats[i].w, stats[i].w);
                     f32x2 a = pk2(0.f, 0.f), c = pk2(0.f, 0.f);
-                    take<B>(hh[i], at + h_at, i);
+                    take<B>(hh[i], at + h_at + lane, i);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         hh[i][e] = mul2(add2(hh[i][e], less), inv);
                         dgate[e] = fma2(d[i][e], hh[i][e], dgate[e]);              // both sums' part: dgate is post_weight times it, dpost gate times it
-                        d[i][e] = mul2(mul2(d[i][e], gate[e]), post_weight[e]);
+                        d[i][e] = mul2(d[i][e], gate[e]);
                         a = add2(a, d[i][e]);
                         c = fma2(d[i][e], hh[i][e], c);
                     }
@@ -150,7 +153,7 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
 #pragma unroll
                 for (int i = 0; i < kRows; ++i) {
                     f32x2 o[4];
-                    if (gated) take<B>(o, at + h_at, i);
+                    if (gated) take<B>(o, at + h_at + lane, i);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         if (gated) dgate[e] = fma2(d[i][e], o[e], dgate[e]);
@@ -178,14 +181,12 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
         }
         if (!t.col || t.side > 0) continue;
         if (POST) {
+            load_vector(gate, p.gate, g, t, 0.f, 1.f);
 #pragma unroll
             for (int e = 0; e < 4; ++e) dpost[e] = fma2(gate[e], dgate[e], dpost[e]);
         }
         if (whole) {
-            if (POST && gated) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) dgate[e] = mul2(dgate[e], post_weight[e]);
-            }
+            if (POST && gated) times_vector(dgate, p.post_weight, t);
             if (p.dweight.p != nullptr) Vec8<float>::store_wide(p.dweight.p, int64_t(g) * p.dweight.ld + t.c0, dweight);
             if (p.dbias.p != nullptr) Vec8<float>::store_wide(p.dbias.p, int64_t(g) * p.dbias.ld + t.c0, dbias);
             if (gated) Vec8<float>::store_wide(p.dgate.p, int64_t(g) * p.dgate.ld + t.c0, dgate);
