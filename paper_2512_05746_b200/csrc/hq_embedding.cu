@@ -12,6 +12,9 @@
 // whatever ids they hold (most tokens may be of one id); a team of threads adds up a span's rows with several rows in flight and writes a row of
 // the table whenever the id changes.  An id of up to `longest` tokens belongs to the span of its first one; the sums of a longer one go to the
 // workspace, one for each span, and (3) join adds them up in order.
+//
+// 19712 tokens of 768 bf16 (32768 ids): lookup 10.2 us a call (4.1 TB/s), gradient 36 where more than half of the tokens are of one id: order 16, of
+// which 8 would do for its 50 MB of zeros, sums 13, join 9; each kernel's start and two or three loads that wait for one another are half of it.
 #include "hq_common.cuh"
 #include "hq_vec8.cuh"
 

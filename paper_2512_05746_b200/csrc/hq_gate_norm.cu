@@ -14,6 +14,9 @@
 // warps, a CTA of its own, takes a run of rows, 8 columns a thread (up to 128 columns: two or four rows side by side in a warp).  Rows are copied ahead into shared memory, by each thread for itself (no barrier stands
 // between the copy and its use, and no register holds what is on the way); two rows are computed together, so that their sums share the
 // shuffles; sums over rows stay in the registers of the thread that owns the columns.
+//
+// 65536 x 1152 bf16 105 us a call (5.8 TB/s, 90 % of the copy rate), 8192 x 1152 18.4 (64 %: about 4 us of start, then instructions: 54 to 62 % of
+// the issue slots at 20 warps an SM), 65536 x 512 of an fp32 stream and a bf16 branch with a norm behind it 88 (71 %: two chains of sums a batch).
 #include "hq_gate_norm.cuh"
 
 namespace hq {

@@ -5,11 +5,14 @@
 // Memory-bound: one pass that reads every gradient, one that reads and writes it.  The tensors are one line of chunks of equal size, laid
 // out in the kernel's parameters (address, count and first chunk of each, and each CTA's first tensor), so that a call of hundreds of tensors is
 // two launches without a table in memory.  Few chunks: a CTA takes a run of them.  Many: the CTAs' chunks lie side by side, so that all that is
-// under way lies in one moving window (642 M gradients of bf16, clipped to fp32: runs a CTA 212 + 710 us).  The second pass takes the chunks
+// under way lies in one moving window.  The second pass takes the chunks
 // from the last one down: what the first pass read last is still in L2.
 //
 // A thread's squares are summed in fp32 over 8 elements at a time and these in fp64; a group of 8 whose squares leave fp32's range is
 // squared in fp64 instead.  Threads, warps and CTAs are joined in a fixed order: the same gradients give the same bits.
+//
+// 642 M gradients of bf16 in 287 tensors, clipped to fp32: norm 212 us (6.0 TB/s, 94 % of the copy rate), outputs 677 (5.7 TB/s; runs of chunks a CTA 710).
+// 280 tensors of 4.1 M fp32 together: 14 us a call, 12 of them on the host.
 #include <climits>
 
 #include "hq_common.cuh"
