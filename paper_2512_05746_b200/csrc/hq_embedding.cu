@@ -11,7 +11,7 @@
 // the rest, while the memory is idle, where the tokens are fewer than the ids (or an fp32 base is added to).  (2) sums: the sorted tokens are cut into spans of equal length,
 // whatever ids they hold (most tokens may be of one id); a team of threads adds up a span's rows with several rows in flight and writes a row of
 // the table whenever the id changes.  An id of up to `longest` tokens belongs to the span of its first one; the sums of a longer one go to the
-// workspace, one for each span, and (3) join adds them up in order.
+// workspace, one for each span, and (3) join adds them up in order.  Up to 128 tokens are added up by the first kernel alone.
 //
 // 19712 tokens of 768 bf16 (32768 ids): lookup 10.2 us a call (4.1 TB/s), gradient 36 where more than half of the tokens are of one id: order 16, of
 // which 8 would do for its 50 MB of zeros, sums 13, join 9; each kernel's start and two or three loads that wait for one another are half of it.
@@ -180,17 +180,139 @@ __device__ __forceinline__ void zero_rows(const GradParams& p, uint32_t v0, uint
     bulk_commit_group();
 }
 
-template <typename I>
+__device__ __forceinline__ uint32_t ld_dependent_u32(const uint32_t* p) {
+    uint32_t v;
+    asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+
+// HELD: an fp32 row with a base holds it already (in place, or copied by the order kernel): each value is added to once, without a wait for it.
+__device__ __forceinline__ void add_to(float* to, float4 x) {
+    asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(to), "f"(x.x), "f"(x.y), "f"(x.z), "f"(x.w) : "memory");
+}
+
+// Row v of the table from the sum of its tokens' rows.
+template <typename U, bool HELD = true>
+__device__ __forceinline__ void write_row(const GradParams& p, uint32_t v, int c0, const f32x2 (&sum)[4]) {
+    const f32x2 s = pk2(p.scale, p.scale);
+    f32x2 f[4];
+    if (HELD && sizeof(U) == 4 && p.base != nullptr) {
+        float* to = reinterpret_cast<float*>(static_cast<char*>(p.dtable) + uint64_t(v) * p.ld_dtable) + c0;
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+            float4 x;
+            upk2(mul2(sum[e], s), x.x, x.y);
+            upk2(mul2(sum[e + 1], s), x.z, x.w);
+            add_to(to + 2 * e, x);
+        }
+        return;
+    }
+    if (p.base != nullptr) {
+        Vec8<U> b;
+        b.load_wide(static_cast<const char*>(p.base) + uint64_t(v) * p.ld_base, c0);
+        b.get(f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = fma2(sum[e], s, f[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = mul2(sum[e], s);
+    }
+    Vec8<U>::store_wide(static_cast<char*>(p.dtable) + uint64_t(v) * p.ld_dtable, c0, f);
+}
+
+// 16 bytes of a row that a thread adds up (8 channels of bf16, 4 of fp32), and rows on their way to each thread: 64 KB a CTA.
+template <typename T> constexpr int kPiece = 16 / int(sizeof(T));
+constexpr int kFlight = 16;
+constexpr int kEntries = 2048;                     // sorted tokens of a CTA's spans
+
+// Row v of the table, N channels from c0 on, from the sum of its tokens' rows.
+template <typename U, int N, bool HELD = true>
+__device__ __forceinline__ void write_channels(const GradParams& p, uint32_t v, int c0, const f32x2 (&sum)[N / 2]) {
+    if constexpr (N == 8) {
+        write_row<U, HELD>(p, v, c0, sum);
+    } else {
+        const U* base = reinterpret_cast<const U*>(static_cast<const char*>(p.base) + uint64_t(v) * p.ld_base) + c0;
+        U* to = reinterpret_cast<U*>(static_cast<char*>(p.dtable) + uint64_t(v) * p.ld_dtable) + c0;
+        float f[4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) upk2(sum[e], f[2 * e], f[2 * e + 1]);
+        if constexpr (sizeof(U) == 4) {
+            const float4 x = make_float4(f[0] * p.scale, f[1] * p.scale, f[2] * p.scale, f[3] * p.scale);
+            if (p.base == nullptr) {
+                *reinterpret_cast<float4*>(to) = x;
+            } else if (HELD) {
+                add_to(to, x);
+            } else {
+                const float4 o = *reinterpret_cast<const float4*>(base);
+                *reinterpret_cast<float4*>(to) = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
+            }
+        } else {
+            uint2 o = make_uint2(0u, 0u);
+            if (p.base != nullptr) o = *reinterpret_cast<const uint2*>(base);
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(fmaf(f[0], p.scale, __uint_as_float(o.x << 16)), fmaf(f[1], p.scale, __uint_as_float(o.x & 0xFFFF0000u)));
+            const __nv_bfloat162 hi = __floats2bfloat162_rn(fmaf(f[2], p.scale, __uint_as_float(o.y << 16)), fmaf(f[3], p.scale, __uint_as_float(o.y & 0xFFFF0000u)));
+            *reinterpret_cast<uint2*>(to) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        }
+    }
+}
+
+// A thread's piece added to its sums.
+template <int N> __device__ __forceinline__ void add_piece(f32x2 (&sum)[N / 2], const uint4& x) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) {
+        if constexpr (N == 8) sum[k] = add2(sum[k], pk2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xFFFF0000u)));
+        else sum[k] = add2(sum[k], pk2(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1])));
+    }
+}
+
+// The rows of a slice whose tokens are few: places[r] .. places[r + 1] of `tokens` are row r's (n behind the last).  As many threads as a row has
+// pieces take a row.
+template <typename T, typename U>
+__device__ __forceinline__ void sum_rows(const GradParams& p, uint32_t v0, uint32_t size, uint32_t n, const uint32_t* places, const uint32_t* tokens) {
+    constexpr int kAhead = 8, kN = kPiece<T>;
+    const int pieces = p.vectors * 8 / kN, across = min(pieces, kOrderThreads), teams = kOrderThreads / across, team = int(threadIdx.x) / across;
+    if (team >= teams) return;
+    const char* dout = static_cast<const char*>(p.dout);
+    for (uint32_t r = uint32_t(team); r < size; r += uint32_t(teams)) {
+        const uint32_t begin = places[r], end = r + 1 < size ? places[r + 1] : n;
+        if (begin == end) continue;
+        for (int v = int(threadIdx.x) - team * across; v < pieces; v += across) {
+            f32x2 sum[kN / 2];
+#pragma unroll
+            for (int k = 0; k < kN / 2; ++k) sum[k] = pk2(0.f, 0.f);
+            for (uint32_t j = begin; j < end; j += kAhead) {
+                uint4 x[kAhead];
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    x[u] = make_uint4(0u, 0u, 0u, 0u);
+                    if (j + u < end) x[u] = *reinterpret_cast<const uint4*>(dout + uint64_t(tokens[j + u]) * p.ld_dout + v * 16);
+                }
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    if (j + u >= end) break;
+                    add_piece<kN>(sum, x[u]);
+                }
+            }
+            write_channels<U, kN, false>(p, v0 + r, v * kN, sum);
+        }
+    }
+}
+
+// HERE: at most kHere tokens, whose rows are added up here as well (64 labels into 1001 x 1152: the kernel of the sums and its start took 4 of 10 us).
+constexpr int kHere = 128;
+template <typename I, typename T, typename U, bool HERE>
 __global__ void __launch_bounds__(kOrderThreads) embedding_order_kernel(const GradParams p) {
     extern __shared__ uint32_t counts[];           // [warp][id of the slice], then [warp][kept] tokens and [warp][kept] ids in the slice
     __shared__ uint32_t room[kOrderWarps], offset[kSlice];
     __shared__ __align__(128) uint4 zeros[kZeros / 16];
+    __shared__ uint32_t chosen[HERE ? kHere : 1];  // the slice's tokens by id
     const int lane = int(threadIdx.x & 31), warp = int(threadIdx.x >> 5);
     const uint32_t v0 = blockIdx.x * p.slice, v1 = min(v0 + p.slice, p.classes), size = v1 - v0;
     uint32_t* count = counts + uint32_t(warp) * size;
     uint32_t* kept = counts + kOrderWarps * p.slice + uint32_t(warp) * p.kept;
     uint16_t* kept_id = reinterpret_cast<uint16_t*>(counts + kOrderWarps * (p.slice + p.kept)) + uint32_t(warp) * p.kept;
-    griddep_launch();                              // the sums' CTAs find room as these end
+    if (!HERE) griddep_launch();                   // the sums' CTAs find room as these end
     const bool zeroing = p.base == nullptr && p.fill_first;
     if (zeroing) {
         if (threadIdx.x < kZeros / 16) zeros[threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
@@ -292,11 +414,22 @@ __global__ void __launch_bounds__(kOrderThreads) embedding_order_kernel(const Gr
     each([&](uint32_t key, uint32_t token, uint32_t same) {
         const uint32_t rank = __popc(same & lanes_below());
         const bool there = key != 0xffffffffu;
-        if (there) p.sorted[offset[key] + count[key] + rank] = make_uint2(v0 + key, token);
+        if (there) {
+            const uint32_t at = offset[key] + count[key] + rank;
+            if (HERE) chosen[at - first] = token;
+            else p.sorted[at] = make_uint2(v0 + key, token);
+        }
         __syncwarp();
         if (there && rank == 0) count[key] += __popc(same);
         __syncwarp();
     });
+    if constexpr (HERE) {
+        if (zeroing && warp == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");        // behind the zeros
+        __syncthreads();                           // every warp has placed its tokens
+        if (threadIdx.x < size) offset[threadIdx.x] -= first;
+        __syncthreads();
+        sum_rows<T, U>(p, v0, size, n, offset, chosen);
+    }
     if (!p.in_place && !p.fill_first) {
         __syncthreads();
         if (threadIdx.x < size) offset[threadIdx.x] = sum;
@@ -304,76 +437,6 @@ __global__ void __launch_bounds__(kOrderThreads) embedding_order_kernel(const Gr
         fill_rows(p, v0, size, offset);
     }
     if (zeroing && warp == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-}
-
-__device__ __forceinline__ uint32_t ld_dependent_u32(const uint32_t* p) {
-    uint32_t v;
-    asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-    return v;
-}
-
-// An fp32 row with a base holds it already (in place, or copied by the order kernel): each value is added to once, without a wait for it.
-__device__ __forceinline__ void add_to(float* to, float4 x) {
-    asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(to), "f"(x.x), "f"(x.y), "f"(x.z), "f"(x.w) : "memory");
-}
-
-// Row v of the table from the sum of its tokens' rows.
-template <typename U>
-__device__ __forceinline__ void write_row(const GradParams& p, uint32_t v, int c0, const f32x2 (&sum)[4]) {
-    const f32x2 s = pk2(p.scale, p.scale);
-    f32x2 f[4];
-    if (sizeof(U) == 4 && p.base != nullptr) {
-        float* to = reinterpret_cast<float*>(static_cast<char*>(p.dtable) + uint64_t(v) * p.ld_dtable) + c0;
-#pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-            float4 x;
-            upk2(mul2(sum[e], s), x.x, x.y);
-            upk2(mul2(sum[e + 1], s), x.z, x.w);
-            add_to(to + 2 * e, x);
-        }
-        return;
-    }
-    if (p.base != nullptr) {
-        Vec8<U> b;
-        b.load_wide(static_cast<const char*>(p.base) + uint64_t(v) * p.ld_base, c0);
-        b.get(f);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = fma2(sum[e], s, f[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = mul2(sum[e], s);
-    }
-    Vec8<U>::store_wide(static_cast<char*>(p.dtable) + uint64_t(v) * p.ld_dtable, c0, f);
-}
-
-// 16 bytes of a row that a thread adds up (8 channels of bf16, 4 of fp32), and rows on their way to each thread: 64 KB a CTA.
-template <typename T> constexpr int kPiece = 16 / int(sizeof(T));
-constexpr int kFlight = 16;
-constexpr int kEntries = 2048;                     // sorted tokens of a CTA's spans
-
-// Row v of the table, N channels from c0 on, from the sum of its tokens' rows.
-template <typename U, int N>
-__device__ __forceinline__ void write_channels(const GradParams& p, uint32_t v, int c0, const f32x2 (&sum)[N / 2]) {
-    if constexpr (N == 8) {
-        write_row<U>(p, v, c0, sum);
-    } else {
-        const U* base = reinterpret_cast<const U*>(static_cast<const char*>(p.base) + uint64_t(v) * p.ld_base) + c0;
-        U* to = reinterpret_cast<U*>(static_cast<char*>(p.dtable) + uint64_t(v) * p.ld_dtable) + c0;
-        float f[4];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) upk2(sum[e], f[2 * e], f[2 * e + 1]);
-        if constexpr (sizeof(U) == 4) {
-            const float4 x = make_float4(f[0] * p.scale, f[1] * p.scale, f[2] * p.scale, f[3] * p.scale);
-            if (p.base != nullptr) add_to(to, x);
-            else *reinterpret_cast<float4*>(to) = x;
-        } else {
-            uint2 o = make_uint2(0u, 0u);
-            if (p.base != nullptr) o = *reinterpret_cast<const uint2*>(base);
-            const __nv_bfloat162 lo = __floats2bfloat162_rn(fmaf(f[0], p.scale, __uint_as_float(o.x << 16)), fmaf(f[1], p.scale, __uint_as_float(o.x & 0xFFFF0000u)));
-            const __nv_bfloat162 hi = __floats2bfloat162_rn(fmaf(f[2], p.scale, __uint_as_float(o.y << 16)), fmaf(f[3], p.scale, __uint_as_float(o.y & 0xFFFF0000u)));
-            *reinterpret_cast<uint2*>(to) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-        }
-    }
 }
 
 // Span blockIdx.x * slots + slot of blockDim.x / slots threads.  The CTA's sorted tokens are in shared memory; each thread copies its piece of
@@ -453,12 +516,7 @@ __global__ void __launch_bounds__(256) embedding_sums_kernel(const GradParams p)
 #pragma unroll
             for (int k = 0; k < kN / 2; ++k) sum[k] = pk2(0.f, 0.f);
         }
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int k = 0; k < kN / 2; ++k) {
-            if constexpr (kN == 8) sum[k] = add2(sum[k], pk2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xFFFF0000u)));
-            else sum[k] = add2(sum[k], pk2(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1])));
-        }
+        add_piece<kN>(sum, x);
     }
     leave(open_left, open_right);
 }
@@ -562,7 +620,7 @@ Plan plan_of(int64_t tokens, int64_t classes, int64_t dim, int piece) {
     int64_t span = 1;
     while (span < 64 && tokens * pieces > span * 148 * 2 * 256) span *= 2;
     a.longest = 64;
-    while (span < 64 && tokens > a.longest && 36 * span * span < tokens) span *= 2;
+    while (span < 64 && 36 * span * span < tokens) span *= 2;
     while (span > 1 && slots * span + a.longest > kEntries) span /= 2;
     a.span = uint32_t(span);
     a.spans = uint32_t((tokens + span - 1) / span);
@@ -583,6 +641,10 @@ cudaError_t launch_lookup(const LookupParams& p, int id_bytes, cudaStream_t st) 
     if (id_bytes == 4) embedding_kernel<int32_t, T, U><<<grid, s.threads, 0, st>>>(p);
     else embedding_kernel<int64_t, T, U><<<grid, s.threads, 0, st>>>(p);
     return cudaGetLastError();
+}
+template <typename I> auto order_here(hq_dtype ddt, hq_dtype gdt) -> void (*)(GradParams) {
+    if (ddt == HQ_BF16) return gdt == HQ_BF16 ? embedding_order_kernel<I, __nv_bfloat16, __nv_bfloat16, true> : embedding_order_kernel<I, __nv_bfloat16, float, true>;
+    return gdt == HQ_BF16 ? embedding_order_kernel<I, float, __nv_bfloat16, true> : embedding_order_kernel<I, float, float, true>;
 }
 template <typename T, typename U>
 cudaError_t launch_sums(const GradParams& p, cudaStream_t st) {
@@ -658,16 +720,18 @@ extern "C" hq_status hq_embedding_bwd(const void* ids, int id_bytes, int64_t tok
     p.kept = uint32_t(run < fit ? run : fit);
     if (p.kept > kKept) p.kept = kKept;
     const size_t smem = counters + p.kept * each;
-    void (*order)(GradParams) = id_bytes == 4 ? embedding_order_kernel<int32_t> : embedding_order_kernel<int64_t>;
+    const bool here = tokens <= kHere;
+    if (here) p.fill_first = tokens < classes;     // behind the fill and a barrier the sums are written as they are
+    void (*order)(GradParams) = !here ? (id_bytes == 4 ? embedding_order_kernel<int32_t, float, float, false> : embedding_order_kernel<int64_t, float, float, false>)
+                                : id_bytes == 4 ? order_here<int32_t>(ddt, gdt) : order_here<int64_t>(ddt, gdt);
     if (smem > 40 * 1024) HQ_CUDA_OK(cudaFuncSetAttribute(order, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
     order<<<a.slices, kOrderThreads, smem, st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return HQ_ERR_CUDA;
-    if (tokens == 0) return HQ_OK;
+    if (here) return HQ_OK;
     cudaError_t c;
     if (ddt == HQ_BF16) c = gdt == HQ_BF16 ? launch_sums<__nv_bfloat16, __nv_bfloat16>(p, st) : launch_sums<__nv_bfloat16, float>(p, st);
     else c = gdt == HQ_BF16 ? launch_sums<float, __nv_bfloat16>(p, st) : launch_sums<float, float>(p, st);
     if (c != cudaSuccess) return HQ_ERR_CUDA;
-    if (tokens <= int64_t(p.longest)) return HQ_OK;            // no id has more tokens than a span takes whole
     const dim3 join(a.slices, unsigned((dim + 63) / 64));
     c = gdt == HQ_BF16 ? launch_dependent(embedding_join_kernel<__nv_bfloat16>, join, 256, 0, st, true, p) : launch_dependent(embedding_join_kernel<float>, join, 256, 0, st, true, p);
     return c == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;

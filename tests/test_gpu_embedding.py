@@ -78,7 +78,7 @@ def check(hq, T, V, dim, how, dt, gt, dtype=torch.int32, with_base=False, seed=0
 
 @pytest.mark.parametrize("dt,gt", [(BF, BF), (F, BF), (BF, F), (F, F)])
 @pytest.mark.parametrize("how", ["all", "half", "one", "runs", "outside"])
-@pytest.mark.parametrize("T,V,dim", [(1, 1, 8), (64, 1001, 1152), (1000, 50, 64), (3000, 7, 2056), (2500, 300000, 16), (33, 2, 5000)])
+@pytest.mark.parametrize("T,V,dim", [(1, 1, 8), (64, 1001, 1152), (1000, 50, 64), (3000, 7, 2056), (2500, 300000, 16), (33, 2, 5000), (128, 40, 320), (129, 40, 320), (100, 9, 16384)])
 def test_gradient(hq, T, V, dim, how, dt, gt):
     check(hq, T, V, dim, how, dt, gt)
     check(hq, T, V, dim, how, dt, gt, torch.int64, with_base=True)
