@@ -3,7 +3,7 @@
 // One pass over x', h and the gradients of both outputs, 12 bytes an element of bf16; sums over rows in registers, a part for each team that
 // took rows of a group, joined by a second kernel in a fixed order.
 //
-// 65536 x 1152 bf16 154 us a call (5.9 TB/s, 92 % of the copy rate), 8192 x 1152 28 (62 %: 24 here at 15 warps an SM and 55 % of the issue slots, the
+// 65536 x 1152 bf16 154 to 161 us a call (5.7 to 5.9 TB/s, 88 to 92 % of the copy rate), 8192 x 1152 28 (62 %: 24 here at 15 warps an SM and 55 % of the issue slots, the
 // rest the join of 14 parts a group).
 #include "hq_gate_norm.cuh"
 
@@ -52,6 +52,7 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
     f32x2 dpost[4], gate[4], weight[4], dweight[4], dbias[4], dgate[4];
     fill(dpost, 0.f);
     bool fresh = true, begun = b.g * p.group == r0;            // begun: the group's first row is this team's
+    bool lived = false;                            // the group has rows here: the vectors of one without any may hold anything
     while (b.n > 0) {
         if (fresh) {
             load_vector(gate, p.gate, b.g, t, 0.f, 1.f);       // with a norm behind the block: times post_weight
@@ -71,6 +72,7 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
             put_zeros<S>(dx, p.dx, b, t);
             put_zeros<B>(dh, p.dh, b, t);
         } else {
+            lived = true;
             f32x2 d[kRows][4];
             if (normed) {
                 f32x2 xh[kRows][4];
@@ -177,13 +179,15 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
         fresh = true;                              // the group's sums leave
         const bool whole = begun && over, first = g * p.group <= r0;
         begun = true;
+        const bool counts = lived;
+        lived = false;
         if constexpr (L < 32) {                    // of the rows side by side
             side_sums<L>(dweight);
             side_sums<L>(dbias);
             side_sums<L>(dgate);
         }
         if (!t.col || t.side > 0) continue;
-        if (POST) {
+        if (POST && counts) {
             load_vector(gate, p.gate, g, t, 0.f, 1.f);
 #pragma unroll
             for (int e = 0; e < 4; ++e) dpost[e] = fma2(gate[e], dgate[e], dpost[e]);

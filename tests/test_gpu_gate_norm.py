@@ -127,6 +127,26 @@ def test_lengths(hq, rows, cols, per, norm, post):
     run(hq, rows, cols, per, norm, post, lens=torch.zeros_like(lens))
 
 
+@pytest.mark.parametrize("cols", [64, 1152])
+def test_vectors_of_empty_groups_hold_anything(hq, cols):
+    rows, per = 200, 20
+    lens = torch.tensor([0, 20, 3, 0, 0, 7, 20, 0, 1, 0], dtype=torch.int32, device="cuda")
+    x, h, rand, mod = inputs(rows, cols, per, F, BF, lens=lens)
+    pw, dxo, dy = 1 + 0.3 * rand(cols), rand(rows, cols), rand(rows, cols).to(BF)
+    results = []
+    for fill in (0.0, math.nan, math.inf):
+        gate, bias, weight = (torch.where((lens == 0)[:, None], torch.full_like(m, fill), m) for m in mod)
+        x_out, y, stats, dx, dh = torch.empty_like(x), torch.empty_like(h), torch.empty((rows, 4), device="cuda"), torch.empty_like(x), torch.empty_like(h)
+        kw = dict(rows_per_group=per, lens=lens, post=1, post_weight=pw, weight_plus=1.0)
+        hq.hq_gate_norm(x, h, gate, weight, bias, x_out, y, stats, **kw)
+        sums = [torch.empty((10, cols), device="cuda") for _ in range(3)] + [torch.empty(cols, device="cuda")]
+        ws = torch.empty((hq.hq_gate_norm_bwd_workspace_size(rows, cols, per),), dtype=torch.uint8, device="cuda")
+        hq.hq_gate_norm_bwd(x_out, h, stats, gate, weight, dxo, dy, dx, dh, *sums[:3], ws, dpost_weight=sums[3], **kw)
+        results.append([x_out, y, stats, dx, dh] + sums)
+        assert all(bool(t.isfinite().all()) for t in results[-1]) and all(bool((s[lens == 0] == 0).all()) for s in sums[:3])
+    assert all(torch.equal(a, b) for r in results[1:] for a, b in zip(results[0], r))
+
+
 def test_parts_of_the_operator(hq):
     run(hq, 130, 640, 32, norm="none")             # the residual alone
     run(hq, 130, 640, 32, norm="none", post="layer", xt=F, gated=False)
