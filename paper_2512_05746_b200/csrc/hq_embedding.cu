@@ -46,7 +46,7 @@ __device__ __forceinline__ Place place_of(int vectors) {
 
 struct LookupParams { const void *ids, *table; void* out; uint32_t ld_table, ld_out, classes, tokens; int vectors; float scale; };       // pitches in bytes
 
-// A thread takes 8 channels of kTogether tokens: the ids, then the rows, then the stores.
+// A thread takes 8 channels of kTogether tokens (three to eight are level): the ids, then the rows, then the stores.
 template <typename T> constexpr int kTogether = sizeof(T) == 2 ? 6 : 4;
 template <typename I, typename T, typename U>
 __global__ void __launch_bounds__(256) embedding_kernel(const LookupParams p) {
