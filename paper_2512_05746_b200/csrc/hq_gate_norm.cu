@@ -46,7 +46,13 @@ __global__ void __maxnreg__(96) gate_norm_kernel(const GateNormParams p) {
         if (ahead.n > 0) {
             send(to, x, p.x.ld, ahead, t, wide);
             if (branch) send(to + h_at, h, p.h.ld, ahead, t, narrow);
+            const uint32_t g = ahead.g;
             ahead.next(p, r1);
+            if (ahead.g != g && ahead.n > 0) {
+                ask_for_vector(p.gate, ahead.g, t);
+                ask_for_vector(p.weight, ahead.g, t);
+                ask_for_vector(p.bias, ahead.g, t);
+            }
         }
         copies_sent();
         to = to == base + (kStages - 1) * batch ? base : to + batch;

@@ -41,7 +41,12 @@ __global__ void __maxnreg__(128) gate_norm_grad_kernel(const GateNormParams p) {
             if (branch) send(to + h_at, h, p.h.ld, ahead, t, narrow);
             if ((normed || POST) && t.lane < Team<L>::kBatch)
                 copy_bytes(smem_u32(&moments_in[slot][t.warp][t.lane]), p.stats + 4 * (int64_t(ahead.row) + (t.lane < ahead.live ? t.lane : 0)), t.lane < ahead.live ? 16u : 0u);
+            const uint32_t g = ahead.g;
             ahead.next(p, r1);
+            if (ahead.g != g && ahead.n > 0) {
+                ask_for_vector(p.gate, ahead.g, t);
+                ask_for_vector(p.weight, ahead.g, t);
+            }
         }
         slot = slot == kStages - 1 ? 0 : slot + 1;
         copies_sent();
