@@ -653,7 +653,7 @@ cudaError_t launch_sums(const GradParams& p, cudaStream_t st) {
     void (*kern)(GradParams) = embedding_sums_kernel<T, U, false>;
     if constexpr (sizeof(U) == 2)
         if (p.base != nullptr) kern = embedding_sums_kernel<T, U, true>;
-    if (smem > 24 * 1024) {
+    if (smem > 24 * 1024) {                        // 48 KB without asking, less the entries' 16
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
         if (e != cudaSuccess) { (void)cudaGetLastError(); return e; }
     }
@@ -724,7 +724,8 @@ extern "C" hq_status hq_embedding_bwd(const void* ids, int id_bytes, int64_t tok
     if (here) p.fill_first = tokens < classes;     // behind the fill and a barrier the sums are written as they are
     void (*order)(GradParams) = !here ? (id_bytes == 4 ? embedding_order_kernel<int32_t, float, float, false> : embedding_order_kernel<int64_t, float, float, false>)
                                 : id_bytes == 4 ? order_here<int32_t>(ddt, gdt) : order_here<int64_t>(ddt, gdt);
-    if (smem > 40 * 1024) HQ_CUDA_OK(cudaFuncSetAttribute(order, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+    // 48 KB without asking, less the kernel's own 9
+    if (smem > 32 * 1024) HQ_CUDA_OK(cudaFuncSetAttribute(order, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
     order<<<a.slices, kOrderThreads, smem, st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return HQ_ERR_CUDA;
     if (here) return HQ_OK;

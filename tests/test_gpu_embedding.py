@@ -91,6 +91,16 @@ def test_gradient_of_many_tokens(hq, T, V, dim, how):
     check(hq, T, V, dim, how, BF, F, torch.int64, with_base=True)
 
 
+@pytest.mark.parametrize("T", [1, 100, 1000, 4096, 4097, 9000])
+def test_every_size_of_the_counters(hq, T):
+    """Slices of the ids of every size up to the largest: shared memory on both sides of what a kernel has without asking."""
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    dout = torch.randint(-4, 5, (T, 8), generator=gen, device="cuda").to(BF)
+    for slice_of in list(range(1, 256, 3)) + list(range(256, 1030, 51)):
+        ids = torch.randint(0, 148 * slice_of, (T,), generator=gen, device="cuda").to(torch.int32)
+        assert torch.equal(grad(hq, ids, dout, 148 * slice_of, F, scale=1.0).double(), embedding_grad(ids, dout, 148 * slice_of, 1.0)[0])
+
+
 @pytest.mark.parametrize("n", list(range(1, 80, 3)) + [127, 128, 129, 1023, 1024, 1025])
 def test_runs_at_the_borders_of_spans(hq, n):
     """Ids of n tokens each, and one of n between others: sums that end, begin and go on at every place of a span."""
