@@ -43,7 +43,7 @@ template <int BATCH> struct Walk {
     int left, alive, n, live;
     __device__ __forceinline__ void enter(const GateNormParams& p, uint32_t behind) {        // behind: rows of the group in front of `row`
         left = int(min(p.group - behind, p.rows - row));
-        alive = p.lens != nullptr && left > 0 ? min(p.lens[g] - int(behind), left) : left;
+        alive = p.lens != nullptr && left > 0 ? min(max(p.lens[g], 0) - int(behind), left) : left;       // below zero by a group's rows at most
     }
     __device__ __forceinline__ void count(uint32_t end) {
         n = min(min(BATCH, left), int(end - row));
