@@ -364,7 +364,8 @@ inline int row_lanes(int64_t cols) { return cols <= 64 ? 8 : cols <= 128 ? 16 : 
 struct Launch { unsigned grid, threads; };
 inline cudaError_t launch_kernel(void (*kern)(GateNormParams), const GateNormParams& p, Launch l, int planes, int stages, cudaStream_t st) {
     const size_t smem = size_t(planes) * stages * l.threads * 16;
-    const cudaError_t e = smem <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    // one value whatever the call needs: another host thread's call of the same kernel may set it between these two
+    const cudaError_t e = smem <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMostShared));
     if (e != cudaSuccess) { (void)cudaGetLastError(); return e; }
     kern<<<l.grid, l.threads, smem, st>>>(p);
     return cudaGetLastError();

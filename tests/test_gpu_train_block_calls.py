@@ -1,10 +1,14 @@
-"""Calls of the operators around a transformer block's linears that their documentation allows and that come seldom: lengths of any value."""
+"""Calls of the operators around a transformer block's linears that their documentation allows and that come seldom: lengths of any value, host
+threads beside one another."""
+import threading
+
 import pytest
 import torch
 
 from test_gpu_gate_norm import run
 
 pytestmark = pytest.mark.gpu
+BF, F = torch.bfloat16, torch.float32
 LEAST, MOST = -2 ** 31, 2 ** 31 - 1
 
 
@@ -22,3 +26,61 @@ def test_lengths_of_any_value(hq, rows, cols, per, norm, post):
     for values in ((LEAST, MOST), (LEAST + 1, 0, LEAST + per // 2), (LEAST + per, MOST - 1, -1, LEAST + per - 1)):
         lens = torch.tensor([values[i % len(values)] for i in range(groups)], dtype=torch.int32, device="cuda")
         run(hq, rows, cols, per, norm, post, lens=lens)
+
+
+def side_by_side(calls, times):
+    """Every call `times` over in a host thread and on a stream of its own; what the first that failed raised."""
+    failed, start = [], threading.Barrier(len(calls))
+
+    def work(call):
+        try:
+            stream = torch.cuda.Stream()
+            start.wait(60)
+            for i in range(times):
+                call(stream)
+                if i % 64 == 63:
+                    stream.synchronize()
+            stream.synchronize()
+        except Exception as e:                     # shown by the test's own thread
+            failed.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=(c,)) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    if failed:
+        raise failed[0]
+
+
+def gate_norm_calls(hq, cols, xt, ht):
+    """Forward and gradient on buffers of their own, and the results."""
+    rows, per = 64, 16
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    x, h, mod = rand(rows, cols).to(xt), rand(rows, cols).to(ht), 0.3 * rand(4, 3 * cols)
+    gate, weight, bias = mod[:, :cols], mod[:, cols: 2 * cols], mod[:, 2 * cols:]
+    x_out, y, stats, dx, dh = torch.empty_like(x), torch.empty_like(h), torch.empty((rows, 4), device="cuda"), torch.empty_like(x), torch.empty_like(h)
+    dxo, dy, dmod = rand(rows, cols).to(xt), rand(rows, cols).to(ht), torch.empty_like(mod)
+    ws = torch.empty((hq.hq_gate_norm_bwd_workspace_size(rows, cols, per),), dtype=torch.uint8, device="cuda")
+    kw = dict(rows_per_group=per, weight_plus=1.0)
+
+    def call(stream):
+        hq.hq_gate_norm(x, h, gate, weight, bias, x_out, y, stats, stream=stream, **kw)
+        hq.hq_gate_norm_bwd(x_out, h, stats, gate, weight, dxo, dy, dx, dh, dmod[:, :cols], dmod[:, cols: 2 * cols], dmod[:, 2 * cols:], ws, stream=stream, **kw)
+    return call, (x_out, y, stats, dx, dh, dmod)
+
+
+@pytest.mark.parametrize("xt,ht,widths", [(BF, BF, (4096, 2048, 3000)), (F, F, (2048, 1024, 3584)), (F, BF, (4096, 1536, 2304))])
+def test_gate_norm_in_host_threads(hq, xt, ht, widths):
+    """Other widths of one type in other threads: none takes from a launch of another the shared memory that it asked for."""
+    made = [gate_norm_calls(hq, c, xt, ht) for c in widths]
+    alone = []
+    for call, out in made:
+        call(None)
+        torch.cuda.synchronize()
+        alone.append([t.clone() for t in out])
+    side_by_side([call for call, _ in made], 1500)
+    assert all(torch.equal(a, b) for (_, out), want in zip(made, alone) for a, b in zip(out, want))
