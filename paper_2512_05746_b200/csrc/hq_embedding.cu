@@ -83,6 +83,7 @@ __global__ void __launch_bounds__(256) embedding_kernel(const LookupParams p) {
 constexpr int kOrderThreads = 1024;
 constexpr int kOrderWarps = kOrderThreads / 32;
 constexpr int kSlice = kOrderThreads;              // ids a CTA of the order at most: a thread each in the scan, 128 KB of counters
+constexpr size_t kOrderShared = 208 * 1024;        // counters and kept tokens of an order CTA at most, beside the kernel's own 9 KB
 constexpr int kKept = 768;                         // tokens of its slice that a warp keeps in shared memory at most (16 bits of id, 32 of token)
 
 struct GradParams {
@@ -653,8 +654,8 @@ cudaError_t launch_sums(const GradParams& p, cudaStream_t st) {
     void (*kern)(GradParams) = embedding_sums_kernel<T, U, false>;
     if constexpr (sizeof(U) == 2)
         if (p.base != nullptr) kern = embedding_sums_kernel<T, U, true>;
-    if (smem > 24 * 1024) {                        // 48 KB without asking, less the entries' 16
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    if (smem > 24 * 1024) {                        // 48 KB without asking, less the entries' 16; one value for every call, as another host thread's may come between
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kFlight * 256 * 16);
         if (e != cudaSuccess) { (void)cudaGetLastError(); return e; }
     }
     return launch_dependent(kern, dim3((p.spans + s.slots - 1) / s.slots, s.slices), s.threads, smem, st, true, p);
@@ -716,7 +717,7 @@ extern "C" hq_status hq_embedding_bwd(const void* ids, int id_bytes, int64_t tok
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     // room for every token of a warp's run, as far as shared memory goes
     const size_t counters = size_t(kOrderWarps) * a.slice * sizeof(uint32_t), each = kOrderWarps * (sizeof(uint32_t) + sizeof(uint16_t));
-    const size_t run = size_t(tokens + 32 * 128 - 1) / (32 * 128) * 128, fit = (208 * 1024 - counters) / each / 2 * 2;
+    const size_t run = size_t(tokens + 32 * 128 - 1) / (32 * 128) * 128, fit = (kOrderShared - counters) / each / 2 * 2;
     p.kept = uint32_t(run < fit ? run : fit);
     if (p.kept > kKept) p.kept = kKept;
     const size_t smem = counters + p.kept * each;
@@ -724,8 +725,8 @@ extern "C" hq_status hq_embedding_bwd(const void* ids, int id_bytes, int64_t tok
     if (here) p.fill_first = tokens < classes;     // behind the fill and a barrier the sums are written as they are
     void (*order)(GradParams) = !here ? (id_bytes == 4 ? embedding_order_kernel<int32_t, float, float, false> : embedding_order_kernel<int64_t, float, float, false>)
                                 : id_bytes == 4 ? order_here<int32_t>(ddt, gdt) : order_here<int64_t>(ddt, gdt);
-    // 48 KB without asking, less the kernel's own 9
-    if (smem > 32 * 1024) HQ_CUDA_OK(cudaFuncSetAttribute(order, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+    // 48 KB without asking, less the kernel's own 9; one value for every call, as another host thread's may come between
+    if (smem > 32 * 1024) HQ_CUDA_OK(cudaFuncSetAttribute(order, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kOrderShared)));
     order<<<a.slices, kOrderThreads, smem, st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return HQ_ERR_CUDA;
     if (here) return HQ_OK;

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from test_gpu_gate_norm import run
+from train_block_reference import embedding_grad
 
 pytestmark = pytest.mark.gpu
 BF, F = torch.bfloat16, torch.float32
@@ -84,3 +85,18 @@ def test_gate_norm_in_host_threads(hq, xt, ht, widths):
         alone.append([t.clone() for t in out])
     side_by_side([call for call, _ in made], 1500)
     assert all(torch.equal(a, b) for (_, out), want in zip(made, alone) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("sizes", [((300, 100, 2048), (300, 100, 1152), (300, 100, 1664)), ((200, 150000, 8), (200, 40000, 8), (5000, 90000, 8)),
+                                   ((100, 150000, 8), (128, 40000, 8), (3, 90000, 8))])
+def test_embedding_in_host_threads(hq, sizes):
+    made = []
+    for tokens, classes, dim in sizes:
+        gen = torch.Generator(device="cuda").manual_seed(classes + dim)
+        ids = torch.randint(0, classes, (tokens,), generator=gen, device="cuda").to(torch.int32)
+        dout = torch.randint(-4, 5, (tokens, dim), generator=gen, device="cuda").to(BF)
+        dtable = torch.empty((classes, dim), device="cuda")
+        ws = torch.empty((hq.hq_embedding_bwd_workspace_size(tokens, classes, dim),), dtype=torch.uint8, device="cuda")
+        made.append((lambda stream, a=(ids, dout, dtable, ws): hq.hq_embedding_bwd(*a, stream=stream), dtable, embedding_grad(ids, dout, classes, 1.0)[0]))
+    side_by_side([call for call, _, _ in made], 1500)
+    assert all(torch.equal(got.double(), want) for _, got, want in made)
