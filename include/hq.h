@@ -464,8 +464,9 @@ hq_status hq_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ld
  *   dx, dh     NULL: not wanted.  dx may be dx_out, dh may be dy or h.  Rows behind lens: zeros.
  *   dgate, dweight, dbias   device fp32 [groups] with pitches of their own, 16-byte aligned, NULL: not wanted; dpost_weight fp32 [cols].
  *              h is read where dgate is wanted or a post norm was taken.
- *   workspace  hq_gate_norm_bwd_workspace_size bytes, 16-byte aligned (NULL where none of the four is wanted); it need not be cleared, and
- *              calls that may overlap on the GPU (other streams, captured graphs that run side by side) need one each. */
+ *   workspace  hq_gate_norm_bwd_workspace_size bytes, 16-byte aligned (NULL where none of the four is wanted); those of the most rows of so
+ *              many columns do for fewer.  It need not be cleared, and calls that may overlap on the GPU (other streams, captured
+ *              graphs that run side by side) need one each. */
 typedef enum { HQ_NORM_LAYER = 0, HQ_NORM_RMS = 1, HQ_NORM_NONE = 2 } hq_norm;
 hq_status hq_gate_norm(const void* x, int64_t ldx, hq_dtype xdt, const void* h, int64_t ldh, hq_dtype hdt, int64_t rows, int64_t cols,
                        int64_t rows_per_group, const int32_t* lens, hq_norm post, const float* post_weight, const float* gate,

@@ -284,10 +284,18 @@ __global__ void __launch_bounds__(256) gate_norm_sums_kernel(const GateNormParam
 }
 
 constexpr int kGradWarps = 148 * 15;               // warps at a time, on every device: gradients are summed in one order
+int64_t least_chunk(int64_t cols) { return 2 * kRows * (32 / row_lanes(cols)); }
 int64_t grad_chunk(int64_t rows, int64_t cols) {
-    const int64_t teams = kGradWarps / team_warps(cols), chunk = (rows + teams - 1) / teams, least = 2 * kRows * (32 / row_lanes(cols));
+    const int64_t teams = kGradWarps / team_warps(cols), chunk = (rows + teams - 1) / teams, least = least_chunk(cols);
     return chunk < least ? least : chunk;
 }
+// Teams of a call of at most so many rows: fewer rows may make more teams, as a chunk is a whole number of rows (of 1152 columns 8192 rows make
+// 432, 7992 rows 444).
+int64_t most_teams(int64_t rows, int64_t cols) {
+    const int64_t teams = kGradWarps / team_warps(cols), least = least_chunk(cols), few = (rows + least - 1) / least;
+    return few < teams ? few : teams;
+}
+size_t parts_bytes(int64_t teams, int64_t cols) { return size_t(teams) * 7 * size_t(cols) * sizeof(float); }
 template <typename S, typename B, int L>
 cudaError_t launch_grad(const GateNormParams& p, bool post, Launch l, cudaStream_t st) {
     if constexpr (sizeof(S) + sizeof(B) == 8 && L == 32) {     // the widest rows of fp32 on both sides: 256 KB in two stages
@@ -315,8 +323,7 @@ extern "C" hq_status hq_gate_norm_bwd_workspace_size(int64_t rows, int64_t cols,
     int64_t group = 0;
     const hq_status e = check_sizes(HQ_BF16, HQ_BF16, rows, cols, rows_per_group, nullptr, HQ_NORM_NONE, nullptr, HQ_NORM_NONE, nullptr, nullptr, 1.f, &group);
     if (e != HQ_OK) return e;
-    const int64_t chunk = grad_chunk(rows, cols), teams = (rows + chunk - 1) / chunk;
-    *bytes = size_t(teams) * 7 * size_t(cols) * sizeof(float);
+    *bytes = parts_bytes(most_teams(rows, cols), cols);
     return HQ_OK;
 }
 
@@ -361,11 +368,9 @@ extern "C" hq_status hq_gate_norm_bwd(const void* x_out, int64_t ldx_out, hq_dty
     // parts are for groups that several teams took; without a sum over rows, or where every group is one team's, there are none
     const bool split = sums && p.chunk % p.group != 0 && teams > 1;
     if (split || dpost_weight != nullptr) {
-        size_t need = 0;
         if (workspace == nullptr) return HQ_ERR_INVALID_ARG;
         if (!aligned16(workspace)) return HQ_ERR_ALIGNMENT;
-        hq_gate_norm_bwd_workspace_size(rows, cols, rows_per_group, &need);
-        if (ws_bytes < need) return HQ_ERR_WORKSPACE;
+        if (ws_bytes < parts_bytes(teams, cols)) return HQ_ERR_WORKSPACE;
     }
     p.layer = norm == HQ_NORM_LAYER; p.post_layer = post == HQ_NORM_LAYER; p.post_weight = post_weight;
     p.gate = Vectors{gate, ld_gate}; p.weight = Vectors{weight, ld_weight};

@@ -1,5 +1,5 @@
 """Calls of the operators around a transformer block's linears that their documentation allows and that come seldom: lengths of any value, host
-threads beside one another."""
+threads beside one another, workspaces of a larger batch."""
 import threading
 
 import pytest
@@ -100,3 +100,19 @@ def test_embedding_in_host_threads(hq, sizes):
         made.append((lambda stream, a=(ids, dout, dtable, ws): hq.hq_embedding_bwd(*a, stream=stream), dtable, embedding_grad(ids, dout, classes, 1.0)[0]))
     side_by_side([call for call, _, _ in made], 1500)
     assert all(torch.equal(got.double(), want) for _, got, want in made)
+
+
+def test_gate_norm_in_the_workspace_of_a_larger_batch(hq):
+    """Of 1152 columns 7992 rows make more parts than 8192."""
+    cols, per = 1152, 256
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    x, dy, stats, weight = rand(8192, cols).to(BF), rand(8192, cols).to(BF), rand(8192, 4), rand(32, cols)
+    largest = torch.empty((hq.hq_gate_norm_bwd_workspace_size(8192, cols, per),), dtype=torch.uint8, device="cuda")
+    for rows in (8192, 7992, 7991, 5000, 33):
+        groups, results = -(-rows // per), []
+        for ws in (largest, torch.empty((hq.hq_gate_norm_bwd_workspace_size(rows, cols, per),), dtype=torch.uint8, device="cuda")):
+            dx, dw, db = torch.empty_like(x[:rows]), torch.empty((groups, cols), device="cuda"), torch.empty((groups, cols), device="cuda")
+            hq.hq_gate_norm_bwd(x[:rows], None, stats[:rows], None, weight[:groups], None, dy[:rows], dx, None, None, dw, db, ws, rows_per_group=per)
+            results.append((dx, dw, db))
+        assert all(torch.equal(a, b) for a, b in zip(*results))
