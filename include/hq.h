@@ -486,7 +486,8 @@ hq_status hq_gate_norm_bwd(const void* x_out, int64_t ldx_out, hq_dtype xdt, con
  * hq_embedding_bwd: dtable[v] = base[v] + scale * sum of dout[t] over the tokens t of id v, in ascending order, in fp32; ids outside the
  *   table have no part.  base: rows of dtable's type, or NULL (zeros: every row of dtable is written); base may be dtable (the gradient of an
  *   earlier micro-batch: rows without tokens are not touched; an addition to an fp32 base takes values below 2^-126 as zero).  With scale 1 it is the gradient of hq_class_embed_add's table, too.
- *   workspace  hq_embedding_bwd_workspace_size bytes, 16-byte aligned; as above.  dim <= 65536. */
+ *   workspace  hq_embedding_bwd_workspace_size bytes, 16-byte aligned; those of the most tokens do for fewer (of the same table); as above.
+ *              dim <= 65536. */
 hq_status hq_embedding(const void* ids, int id_bytes, int64_t tokens, const void* table, hq_dtype tdt, int64_t classes, int64_t dim,
                        int64_t ld_table, float scale, void* out, hq_dtype odt, int64_t ld_out, void* stream);
 hq_status hq_embedding_bwd_workspace_size(int64_t tokens, int64_t classes, int64_t dim, size_t* bytes);

@@ -609,20 +609,24 @@ hq_status check_call(int id_bytes, int64_t tokens, int64_t classes, int64_t dim,
 }
 
 struct Plan { uint32_t slice, slices, span, spans, longest; size_t start, longs, long_count, parts, bytes; };
+constexpr int64_t kLongestSpan = 64, kSumsThreads = 148 * 2 * 256;         // threads: of two CTAs an SM
+// Tokens of which a span of `span` (or fewer) is enough: spans for two CTAs an SM, and where an id may lie in many of them no shorter than
+// sqrt(tokens) / 6: adding up their sums takes as long as a span's rows then (3691 tokens of 64 channels, half of them of one id: spans of one
+// token 29 us a call).
+int64_t tokens_of_span(int64_t span, int64_t pieces) {
+    const int64_t resident = span * kSumsThreads / pieces, joined = 36 * span * span;
+    return resident < joined ? resident : joined;
+}
 Plan plan_of(int64_t tokens, int64_t classes, int64_t dim, int piece) {
     Plan a{};
     const int64_t slice = (classes + 147) / 148;
     a.slice = uint32_t(slice < kSlice ? slice : kSlice);
     a.slices = uint32_t((classes + a.slice - 1) / a.slice);
-    // spans for two CTAs an SM, of up to 64 tokens, and no more tokens in a CTA than its room for entries; where an id may lie in many of them
-    // no shorter than sqrt(tokens) / 6: adding up their sums takes as long as a span's rows then (3691 tokens of 64 channels, half of them of
-    // one id: spans of one token 29 us a call)
-    const int pieces = int(dim / piece), slots = 256 / (pieces < 256 ? pieces : 256);
+    const int64_t pieces = dim / piece, slots = 256 / (pieces < 256 ? pieces : 256);
+    a.longest = kLongestSpan;
     int64_t span = 1;
-    while (span < 64 && tokens * pieces > span * 148 * 2 * 256) span *= 2;
-    a.longest = 64;
-    while (span < 64 && 36 * span * span < tokens) span *= 2;
-    while (span > 1 && slots * span + a.longest > kEntries) span /= 2;
+    while (span < kLongestSpan && tokens > tokens_of_span(span, pieces)) span *= 2;
+    while (span > 1 && slots * span + a.longest > kEntries) span /= 2;         // no more tokens in a CTA than its room for entries
     a.span = uint32_t(span);
     a.spans = uint32_t((tokens + span - 1) / span);
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -632,6 +636,16 @@ Plan plan_of(int64_t tokens, int64_t classes, int64_t dim, int piece) {
     a.parts = a.long_count + up(size_t(a.slices) * sizeof(uint32_t));
     a.bytes = a.parts + size_t(a.spans) * 2 * size_t(dim) * sizeof(float);
     return a;
+}
+// Bytes for at most so many tokens: the spans get longer with the tokens, and there are most of them where they are about to.
+size_t most_bytes(int64_t tokens, int64_t classes, int64_t dim, int piece) {
+    const Plan a = plan_of(tokens, classes, dim, piece);
+    int64_t spans = a.spans;
+    for (int64_t span = 1; span < a.span; span *= 2) {
+        const int64_t most = tokens_of_span(span, dim / piece), n = ((most < tokens ? most : tokens) + span - 1) / span;
+        if (n > spans) spans = n;
+    }
+    return a.parts + size_t(spans) * 2 * size_t(dim) * sizeof(float);
 }
 
 template <typename T, typename U>
@@ -686,7 +700,7 @@ extern "C" hq_status hq_embedding_bwd_workspace_size(int64_t tokens, int64_t cla
     if (bytes == nullptr) return HQ_ERR_INVALID_ARG;
     const hq_status e = check_call(4, tokens, classes, dim, HQ_F32, HQ_F32, 1.f);
     if (e != HQ_OK) return e;
-    const size_t half = plan_of(tokens, classes, dim, kPiece<__nv_bfloat16>).bytes, full = plan_of(tokens, classes, dim, kPiece<float>).bytes;
+    const size_t half = most_bytes(tokens, classes, dim, kPiece<__nv_bfloat16>), full = most_bytes(tokens, classes, dim, kPiece<float>);
     *bytes = half > full ? half : full;            // of either type of dout
     return HQ_OK;
 }

@@ -116,3 +116,18 @@ def test_gate_norm_in_the_workspace_of_a_larger_batch(hq):
             hq.hq_gate_norm_bwd(x[:rows], None, stats[:rows], None, weight[:groups], None, dy[:rows], dx, None, None, dw, db, ws, rows_per_group=per)
             results.append((dx, dw, db))
         assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("dt", [BF, F])
+def test_embedding_in_the_workspace_of_a_larger_batch(hq, dt):
+    """Of 768 channels 8400 tokens make more spans than 16000."""
+    classes, dim = 32768, 768
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    ids = torch.randint(0, classes, (16000,), generator=gen, device="cuda").to(torch.int32)
+    ids[torch.rand(16000, generator=gen, device="cuda") < 0.5] = 5
+    dout = torch.randint(-4, 5, (16000, dim), generator=gen, device="cuda").to(dt)
+    largest = torch.empty((hq.hq_embedding_bwd_workspace_size(16000, classes, dim),), dtype=torch.uint8, device="cuda")
+    for tokens in (16000, 8400, 4927, 1500, 129, 100):
+        dtable = torch.empty((classes, dim), device="cuda")
+        hq.hq_embedding_bwd(ids[:tokens], dout[:tokens], dtable, largest)
+        assert torch.equal(dtable.double(), embedding_grad(ids[:tokens], dout[:tokens], classes, 1.0)[0])

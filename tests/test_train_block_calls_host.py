@@ -25,3 +25,9 @@ def test_a_workspace_of_the_gated_residual_does_for_fewer_rows(hq, cols):
     for per in (0, 1, 77):
         sizes = [hq.hq_gate_norm_bwd_workspace_size(rows, cols, per) for rows in sizes_up_to(600_000)]
         assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+
+@pytest.mark.parametrize("classes,dim", [(2, 8), (7, 64), (1001, 64), (50, 320), (1001, 1152), (32768, 768), (300, 2048), (300, 2056), (9, 16384), (11, 65536)])
+def test_a_workspace_of_the_embedding_does_for_fewer_tokens(hq, classes, dim):
+    sizes = [hq.hq_embedding_bwd_workspace_size(tokens, classes, dim) for tokens in sizes_up_to(600_000)]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:]))
