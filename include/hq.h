@@ -485,7 +485,9 @@ hq_status hq_gate_norm_bwd(const void* x_out, int64_t ldx_out, hq_dtype xdt, con
  *   ids        device int32 or int64 (id_bytes 4 or 8) [tokens].  table [classes], out [tokens] rows of dim values, fp32 or bf16 each.
  * hq_embedding_bwd: dtable[v] = base[v] + scale * sum of dout[t] over the tokens t of id v, in ascending order, in fp32; ids outside the
  *   table have no part.  base: rows of dtable's type, or NULL (zeros: every row of dtable is written); base may be dtable (the gradient of an
- *   earlier micro-batch: rows without tokens are not touched; an addition to an fp32 base takes values below 2^-126 as zero).  With scale 1 it is the gradient of hq_class_embed_add's table, too.
+ *   earlier micro-batch: rows without tokens are not touched; an addition to an fp32 base takes values below 2^-126 as zero).  With scale 1 and ids
+ *   inside the table it is the gradient of hq_class_embed_add's table, too; of a label outside that call adds the first or the last class, so
+ *   its labels are clamped before they come here.
  *   workspace  hq_embedding_bwd_workspace_size bytes, 16-byte aligned; those of the most tokens do for fewer (of the same table); as above.
  *              dim <= 65536. */
 hq_status hq_embedding(const void* ids, int id_bytes, int64_t tokens, const void* table, hq_dtype tdt, int64_t classes, int64_t dim,

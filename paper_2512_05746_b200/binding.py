@@ -655,8 +655,9 @@ def hq_embedding_bwd_workspace_size(tokens: int, classes: int, dim: int) -> int:
 
 
 def hq_embedding_bwd(ids, dout, dtable, workspace, scale: float = 1.0, base=None, stream=None) -> None:
-    """dtable [classes, dim] = base + scale * the sums of dout's rows by id (ids and dout as ids and out of hq_embedding; base: a table of
-    dtable's type, dtable itself to add to what it holds, or None for zeros).  workspace: hq_embedding_bwd_workspace_size bytes."""
+    """dtable [classes, dim] = base + scale * the sums of dout's rows by id (ids and dout as ids and out of hq_embedding, ids outside the table
+    have no part; base: a table of dtable's type, dtable itself to add to what it holds, or None for zeros).  workspace:
+    hq_embedding_bwd_workspace_size bytes.  For the table of hq_class_embed_add labels are clamped to 0 .. classes - 1 first, as that call does."""
     at, device = _stream_and_device(stream)
     if ids.dim() != 1 or dout.dim() != 2:
         if tuple(dout.shape[:-1]) != tuple(ids.shape):

@@ -1,5 +1,6 @@
 """Calls of the operators around a transformer block's linears that their documentation allows and that come seldom: lengths of any value, host
-threads beside one another, workspaces of a larger batch."""
+threads beside one another, workspaces of a larger batch, labels outside
+their table."""
 import threading
 
 import pytest
@@ -131,3 +132,22 @@ def test_embedding_in_the_workspace_of_a_larger_batch(hq, dt):
         dtable = torch.empty((classes, dim), device="cuda")
         hq.hq_embedding_bwd(ids[:tokens], dout[:tokens], dtable, largest)
         assert torch.equal(dtable.double(), embedding_grad(ids[:tokens], dout[:tokens], classes, 1.0)[0])
+
+
+def test_gradient_of_the_class_table_with_labels_outside(hq):
+    """hq_class_embed_add takes them for the first or last class: its table's gradient is that of the clamped labels; as ids they have no part."""
+    classes = 11
+    labels = torch.tensor([3, -1, 0, 11, 10, 3, LEAST, MOST], dtype=torch.int32, device="cuda")
+    weights = torch.arange(1, 9, device="cuda").view(8, 1).expand(8, 64).to(BF).contiguous()
+    ws = torch.empty((hq.hq_embedding_bwd_workspace_size(8, classes, 64),), dtype=torch.uint8, device="cuda")
+    clamped, dropped = torch.empty((classes, 64), device="cuda"), torch.empty((classes, 64), device="cuda")
+    hq.hq_embedding_bwd(labels.clamp(0, classes - 1), weights, clamped, ws)
+    hq.hq_embedding_bwd(labels, weights, dropped, ws)
+    table = torch.zeros((classes, 64), dtype=BF, device="cuda")
+    for v in range(classes):
+        table.zero_()
+        table[v] = 1
+        emb = torch.zeros((8, 64), dtype=BF, device="cuda")
+        hq.hq_class_embed_add(emb, table, labels)
+        assert torch.equal((emb.float() * weights.float()).sum(0), clamped[v])
+    assert torch.equal(dropped.double(), embedding_grad(labels, weights, classes, 1.0)[0]) and not torch.equal(dropped, clamped)
