@@ -450,7 +450,8 @@ hq_status hq_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ld
  *     y = norm(x_out) * (weight_plus + weight[n]) + bias[n]     (norm: its kind; of x_out before it is rounded to xdt)
  *   HQ_NORM_LAYER: (v - mean(v)) / sqrt(var(v) + eps), biased variance; HQ_NORM_RMS: v / sqrt(mean(v^2) + eps); over the row's cols values.
  *   eps >= 0; a row without variance has no norm where it is 0 (NaN).  With weight_plus 1 a modulation's scale and shift are passed as they are.
- *   x, x_out   fp32 or bf16 (xdt); h, y of hdt, the same or the other.  cols <= 4096.  x_out may be x; y may be h.  x_out NULL: not wanted.
+ *   x, x_out   fp32 or bf16 (xdt); h, y of hdt, the same or the other.  cols <= 4096.  x_out may be x and y may be h (of one
+ *              pitch).  x_out NULL: not wanted.
  *   h          NULL: x_out = x (gate NULL, post NONE, residual_scale 1), a norm alone.  y NULL with norm HQ_NORM_NONE: the residual alone,
  *              in front of a call that normalises on its own (hq_ln_qlinear).
  *   gate, weight, bias   device fp32 [groups] with pitches of their own (slices of one modulation), 16-byte aligned, or NULL (1, 1, 0: without
@@ -461,7 +462,7 @@ hq_status hq_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ld
  *              (0, 1) for a norm that is not taken, mean 0 for HQ_NORM_RMS.
  * hq_gate_norm_bwd: the gradients of the same call from those of its outputs (dx_out, dy; dx_out NULL: nothing else uses x_out; dy NULL with
  *   HQ_NORM_NONE), its results x_out and stats and its input h.  A norm alone: x_out is its input x.  x_out is read where a norm is taken.
- *   dx, dh     NULL: not wanted.  dx may be dx_out, dh may be dy or h.  Rows behind lens: zeros.
+ *   dx, dh     NULL: not wanted.  dx may be dx_out, dh may be dy or h (of one pitch).  Rows behind lens: zeros.
  *   dgate, dweight, dbias   device fp32 [groups] with pitches of their own, 16-byte aligned, NULL: not wanted; dpost_weight fp32 [cols].
  *              h is read where dgate is wanted or a post norm was taken.
  *   workspace  hq_gate_norm_bwd_workspace_size bytes, 16-byte aligned (NULL where none of the four is wanted); those of the most rows of so

@@ -164,6 +164,7 @@ extern "C" hq_status hq_gate_norm(const void* x, int64_t ldx, hq_dtype xdt, cons
         (e = check_vectors(gate, ld_gate, groups, cols)) != HQ_OK || (e = check_vectors(weight, ld_weight, groups, cols)) != HQ_OK ||
         (e = check_vectors(bias, ld_bias, groups, cols)) != HQ_OK)
         return e;
+    if (in_place_apart(x_out, ldx_out, x, ldx, rows) || in_place_apart(y, ldy, h, ldh, rows)) return HQ_ERR_SHAPE;
     if (!aligned16(stats)) return HQ_ERR_ALIGNMENT;
     GateNormParams p{};
     p.rows = uint32_t(rows); p.group = uint32_t(group); p.cols = int(cols); p.warps = team_warps(cols); p.lens = lens;

@@ -335,6 +335,10 @@ inline hq_status check_matrix(const void* x, int64_t ld, int64_t cols, hq_dtype 
     if (!aligned16(x) || (ld * (dt == HQ_BF16 ? 2 : 4)) % 16 != 0) return HQ_ERR_ALIGNMENT;
     return ld < int64_t(1) << 30 ? HQ_OK : HQ_ERR_UNSUPPORTED;             // a pitch in bytes has 32 bits
 }
+// In place: rows at other places than the input's are rows that are still to be read.
+inline bool in_place_apart(const void* out, int64_t ld_out, const void* in, int64_t ld_in, int64_t rows) {
+    return out != nullptr && out == in && ld_out != ld_in && rows > 1;
+}
 inline Matrix matrix(const void* p, int64_t ld, hq_dtype dt) { return Matrix{p, p != nullptr ? uint32_t(ld) * (dt == HQ_BF16 ? 2u : 4u) : 0u}; }
 inline MatrixOut matrix_out(void* p, int64_t ld, hq_dtype dt) { return MatrixOut{p, p != nullptr ? uint32_t(ld) * (dt == HQ_BF16 ? 2u : 4u) : 0u}; }
 inline hq_status check_vectors(const float* v, int64_t ld, int64_t groups, int64_t cols) {

@@ -358,6 +358,7 @@ extern "C" hq_status hq_gate_norm_bwd(const void* x_out, int64_t ldx_out, hq_dty
         (e = check_vectors(dgate, ld_dgate, groups, cols)) != HQ_OK || (e = check_vectors(dweight, ld_dweight, groups, cols)) != HQ_OK ||
         (e = check_vectors(dbias, ld_dbias, groups, cols)) != HQ_OK)
         return e;
+    if (in_place_apart(dx, lddx, dx_out, lddx_out, rows) || in_place_apart(dh, lddh, dy, lddy, rows) || in_place_apart(dh, lddh, h, ldh, rows)) return HQ_ERR_SHAPE;
     if ((normed || after) && stats == nullptr) return HQ_ERR_INVALID_ARG;
     if (!aligned16(stats) || !aligned16(dpost_weight)) return HQ_ERR_ALIGNMENT;
     GateNormParams p{};

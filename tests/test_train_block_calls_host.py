@@ -1,5 +1,8 @@
-"""What the calls around a transformer block's linears promise of their arguments, where no GPU is needed: workspaces of a larger batch."""
+"""What the calls around a transformer block's linears promise of their arguments, where no GPU is needed: workspaces of a larger batch,
+outputs in place."""
 import pytest
+
+from test_train_block_host import ALIGNMENT, HALF, SHAPE, C, norm, norm_bwd
 
 
 @pytest.fixture(scope="module")
@@ -31,3 +34,22 @@ def test_a_workspace_of_the_gated_residual_does_for_fewer_rows(hq, cols):
 def test_a_workspace_of_the_embedding_does_for_fewer_tokens(hq, classes, dim):
     sizes = [hq.hq_embedding_bwd_workspace_size(tokens, classes, dim) for tokens in sizes_up_to(600_000)]
     assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+
+AT = [C.c_void_p(0x100000 * (i + 1)) for i in range(8)]        # never read: every call is refused, the last check's of `stats` where no other does
+
+
+def test_in_place_with_another_pitch(hq):
+    """Rows written at other places than they are read from lie on rows that another thread block still has to read."""
+    apart = dict(x=AT[0], h=AT[1], x_out=AT[2], y=AT[3], stats=HALF)
+    assert norm(hq, **apart, ldx_out=72, ldy=72) == norm(hq, **dict(apart, x_out=AT[0], y=AT[1])) == ALIGNMENT
+    for change in (dict(x_out=AT[0], ldx_out=72), dict(x_out=AT[0], ldx=72), dict(y=AT[1], ldy=128), dict(y=AT[1], ldh=80)):
+        assert norm(hq, **dict(apart, **change)) == SHAPE, change
+        assert norm(hq, **dict(apart, rows=1, per=1, **change)) == ALIGNMENT, change
+    apart = dict(x=AT[0], h=AT[1], dx_out=AT[2], dy=AT[3], dx=AT[4], dh=AT[5], stats=HALF)
+    assert norm_bwd(hq, **apart, lddx=72, lddh=72) == ALIGNMENT
+    for same in (dict(dx=AT[2]), dict(dh=AT[3]), dict(dh=AT[1])):
+        assert norm_bwd(hq, **dict(apart, **same)) == ALIGNMENT
+    for change in (dict(dx=AT[2], lddx=72), dict(dh=AT[3], lddh=72), dict(dh=AT[1], ldh=72), dict(dh=AT[3], lddy=128)):
+        assert norm_bwd(hq, **dict(apart, **change)) == SHAPE, change
+        assert norm_bwd(hq, **dict(apart, rows=1, per=1, **change)) == ALIGNMENT, change
