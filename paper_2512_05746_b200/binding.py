@@ -672,6 +672,8 @@ class _GradTensor(C.Structure):
 
 def _is_dense(t) -> bool:
     """Whether a tensor's elements fill one run of memory, in whatever order of its dimensions."""
+    if t.numel() == 0:
+        return True
     size = 1
     for stride, n in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
         if stride != size:

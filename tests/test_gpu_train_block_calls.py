@@ -1,6 +1,6 @@
 """Calls of the operators around a transformer block's linears that their documentation allows and that come seldom: lengths of any value, host
 threads beside one another, workspaces of a larger batch, labels outside
-their table."""
+their table, gradients without elements."""
 import threading
 
 import pytest
@@ -151,3 +151,14 @@ def test_gradient_of_the_class_table_with_labels_outside(hq):
         hq.hq_class_embed_add(emb, table, labels)
         assert torch.equal((emb.float() * weights.float()).sum(0), clamped[v])
     assert torch.equal(dropped.double(), embedding_grad(labels, weights, classes, 1.0)[0]) and not torch.equal(dropped, clamped)
+
+
+def test_gradients_without_elements(hq):
+    ws, norm = torch.empty((hq.hq_grad_workspace_size(),), dtype=torch.uint8, device="cuda"), torch.empty(1, device="cuda")
+    g = torch.full((9,), 2.0, device="cuda")
+    empty = [torch.empty(s, device="cuda") for s in ((5, 0), (2, 0, 3), (0,))]
+    hq.hq_grad_clip([empty[0], g, empty[1], empty[2]], 3.0, norm, ws, eps=0.0)
+    assert float(norm) == 6.0 and bool((g == 1.0).all())
+    out = torch.empty(9, device="cuda")
+    hq.hq_grad_clip(hq.GradList([empty[0], g], [torch.empty((5, 0), device="cuda"), out]), 1.5, norm, ws, eps=0.0)
+    assert float(norm) == 3.0 and bool((out == 0.5).all()) and bool((g == 1.0).all())

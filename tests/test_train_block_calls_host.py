@@ -1,6 +1,7 @@
 """What the calls around a transformer block's linears promise of their arguments, where no GPU is needed: workspaces of a larger batch,
-outputs in place."""
+outputs in place, gradients without elements."""
 import pytest
+import torch
 
 from test_train_block_host import ALIGNMENT, HALF, SHAPE, C, norm, norm_bwd
 
@@ -53,3 +54,12 @@ def test_in_place_with_another_pitch(hq):
     for change in (dict(dx=AT[2], lddx=72), dict(dh=AT[3], lddh=72), dict(dh=AT[1], ldh=72), dict(dh=AT[3], lddy=128)):
         assert norm_bwd(hq, **dict(apart, **change)) == SHAPE, change
         assert norm_bwd(hq, **dict(apart, rows=1, per=1, **change)) == ALIGNMENT, change
+
+
+def test_layouts_of_gradients(hq):
+    """A tensor without elements has a dense layout whatever its strides; others by their strides."""
+    for shape in ((0,), (0, 5), (5, 0), (2, 0, 3), (3, 2, 0, 4)):
+        assert hq._is_dense(torch.empty(shape)) and hq._is_dense(torch.empty(shape).transpose(0, -1)), shape
+    t = torch.empty((4, 6, 5))
+    assert hq._is_dense(t) and hq._is_dense(t.permute(2, 0, 1)) and hq._is_dense(t[1:3]) and hq._is_dense(t[:0]) and hq._is_dense(t[:, :1][:1])
+    assert not any(hq._is_dense(v) for v in (t[::2], t[:, 1:], t[..., :4], t[:1].expand(4, 6, 5)))
