@@ -743,7 +743,9 @@ def hq_grad_norm(grads, norm, workspace, stream=None) -> None:
 
 def hq_grad_clip(grads, max_norm: float, norm, workspace, eps: float = 1e-6, coef=None, stream=None) -> None:
     """norm as hq_grad_norm; every gradient times coef = min(1, max_norm / (norm + eps)), in place or into the list's outs.  norm, coef (or
-    None): one fp32 value each on the device."""
+    None): one fp32 value each on the device.  (max_norm math.inf: nothing is clipped.)"""
+    if max_norm is None:
+        raise TypeError("hq_grad_clip: max_norm is None")
     _grad_call(grads, max_norm, eps, norm, coef, workspace, stream, "hq_grad_clip")
 
 

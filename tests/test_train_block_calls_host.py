@@ -1,5 +1,6 @@
 """What the calls around a transformer block's linears promise of their arguments, where no GPU is needed: workspaces of a larger batch,
-outputs in place, gradients without elements."""
+outputs in place, gradients without elements,
+clipping without a norm."""
 import pytest
 import torch
 
@@ -63,3 +64,10 @@ def test_layouts_of_gradients(hq):
     t = torch.empty((4, 6, 5))
     assert hq._is_dense(t) and hq._is_dense(t.permute(2, 0, 1)) and hq._is_dense(t[1:3]) and hq._is_dense(t[:0]) and hq._is_dense(t[:, :1][:1])
     assert not any(hq._is_dense(v) for v in (t[::2], t[:, 1:], t[..., :4], t[:1].expand(4, 6, 5)))
+
+
+def test_clipping_by_no_norm(hq):
+    """None, an option that was not set, is refused: it would leave the gradients as they are."""
+    norm, ws = torch.zeros(1), torch.zeros(hq.hq_grad_workspace_size(), dtype=torch.uint8)
+    with pytest.raises(TypeError):
+        hq.hq_grad_clip([], None, norm, ws)
