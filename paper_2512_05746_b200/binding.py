@@ -9,6 +9,8 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import warnings
+import weakref
 
 import numpy as np
 
@@ -685,9 +687,14 @@ def _is_dense(t) -> bool:
 class GradList:
     """The gradients of a step (and, where they are written elsewhere, the tensors `outs` of the same shapes and strides, fp32 / bf16) as
     hq_grad_norm and hq_grad_clip take them: checked and laid out once for tensors that stay where they are, which it keeps alive.
-    Gradients that get new memory (set to None between steps) need a new list."""
+    Gradients that get new memory (set to None between steps) need a new list, which takes 5 to 7 us a tensor on the host; a call with a
+    list of gradients that their parameters hold no more warns: it is an earlier step's."""
 
     def __init__(self, grads, outs=None):
+        grads = list(grads)
+        # those that a parameter (or another owner than Python's variables) holds now, noted in `gone` when it lets go of them
+        self.gone = []
+        self.watch = [weakref.ref(g, self.gone.append) for g in grads if getattr(g, "_use_count", int)() > 1]
         grads = [g.detach() for g in grads]
         outs = None if outs is None else [o.detach() for o in outs]
         if outs is not None and len(outs) != len(grads):
@@ -723,6 +730,9 @@ class GradList:
 
 def _grad_call(grads, max_norm, eps, norm, coef, workspace, stream, what: str) -> None:
     grads = grads if isinstance(grads, GradList) else GradList(grads)
+    if grads.gone:
+        warnings.warn(f"{what}: {len(grads.gone)} of the list's gradients are no parameter's any more (set to None since?); a new list takes the new ones",
+                      RuntimeWarning, stacklevel=3)
     at, device = _stream_and_device(stream)
     if grads.n and device != grads.device:
         raise ValueError(f"{what}: the gradients are on CUDA device {grads.device}, the current one is {device}")

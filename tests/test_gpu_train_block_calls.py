@@ -1,7 +1,8 @@
 """Calls of the operators around a transformer block's linears that their documentation allows and that come seldom: lengths of any value, host
 threads beside one another, workspaces of a larger batch, labels outside
-their table, gradients without elements."""
+their table, gradients without elements, lists of gradients that were let go."""
 import threading
+import warnings
 
 import pytest
 import torch
@@ -162,3 +163,41 @@ def test_gradients_without_elements(hq):
     out = torch.empty(9, device="cuda")
     hq.hq_grad_clip(hq.GradList([empty[0], g], [torch.empty((5, 0), device="cuda"), out]), 1.5, norm, ws, eps=0.0)
     assert float(norm) == 3.0 and bool((out == 0.5).all()) and bool((g == 1.0).all())
+
+
+def test_a_list_of_gradients_that_were_let_go(hq):
+    """Gradients of an earlier step in a list that was kept: the call says so.  Gradients that stay, views and copies in the list alone do not."""
+    ws, norm = torch.empty((hq.hq_grad_workspace_size(),), dtype=torch.uint8, device="cuda"), torch.empty(1, device="cuda")
+    params = [torch.nn.Parameter(torch.randn(50, device="cuda")) for _ in range(3)]
+    optimizer = torch.optim.SGD(params, lr=0.1)
+
+    def backward():
+        sum((p * p).sum() for p in params).backward()
+
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        backward()
+        kept = hq.GradList([p.grad for p in params])
+        for _ in range(3):
+            hq.hq_grad_norm(kept, norm, ws)
+            hq.hq_grad_clip(kept, 1.0, norm, ws)
+            optimizer.zero_grad(set_to_none=False)
+            backward()
+        for grads in ([p.grad.view(5, 10) for p in params], [p.grad.clone() for p in params], [p.grad.detach() for p in params]):
+            other = hq.GradList(grads)
+            del grads
+            hq.hq_grad_clip(other, 1.0, norm, ws)
+        hq.hq_grad_clip([p.grad for p in params], 1.0, norm, ws)
+    optimizer.zero_grad()
+    backward()
+    for call in (lambda: hq.hq_grad_norm(kept, norm, ws), lambda: hq.hq_grad_clip(kept, 1.0, norm, ws)):
+        with pytest.warns(RuntimeWarning, match="3 of the list's gradients"):
+            call()
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        hq.hq_grad_clip(hq.GradList([p.grad for p in params]), 1.0, norm, ws)
+    params[1].grad = torch.ones(50, device="cuda")
+    before = hq.GradList([p.grad for p in params])
+    params[1].grad = None
+    with pytest.warns(RuntimeWarning, match="1 of the list's gradients"):
+        hq.hq_grad_clip(before, 1.0, norm, ws)
