@@ -1,6 +1,7 @@
 """Calls of the operators around a transformer block's linears that their documentation allows and that come seldom: lengths of any value, host
 threads beside one another, workspaces of a larger batch, labels outside
-their table, gradients without elements, lists of gradients that were let go."""
+their table, gradients without elements, lists of gradients that were
+let go, very many groups."""
 import threading
 import warnings
 
@@ -201,3 +202,13 @@ def test_a_list_of_gradients_that_were_let_go(hq):
     params[1].grad = None
     with pytest.warns(RuntimeWarning, match="1 of the list's gradients"):
         hq.hq_grad_clip(before, 1.0, norm, ws)
+
+
+@pytest.mark.parametrize("rows,cols,per", [(500_003, 64, 3), (300_007, 128, 1), (400_001, 72, 2)])
+def test_very_many_groups(hq, rows, cols, per):
+    """More groups than teams by far: most are one team's, and the join takes those at the borders of two."""
+    run(hq, rows, cols, per, "layer", "none")
+    run(hq, rows, cols, per, "rms", "layer", F, BF)
+    groups = -(-rows // per)
+    lens = torch.arange(groups, dtype=torch.int32, device="cuda") % (per + 2)
+    run(hq, rows, cols, per, "layer", "rms", lens=lens)
