@@ -54,6 +54,13 @@ ProductPlan plan_product(int limbs, int64_t out_rows, int tile_rows, int64_t n_p
 
 #ifdef __CUDACC__
 
+// The shared memory that launches of a kernel may take beside up to 1 KB of its own.  The limit is the kernel's, for all host threads: set to
+// what a call needs, it could fall below that again, by a smaller call, before the launch.  So every call sets the same.
+constexpr size_t kDynamicShared = 226 * 1024;
+template <typename... Params> inline cudaError_t allow_shared(void (*kern)(Params...)) {
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kDynamicShared));
+}
+
 template <typename... Params, typename... Args>
 cudaError_t launch_dependent(void (*kern)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, bool dependent, Args... args) {
     cudaLaunchConfig_t cfg = {};

@@ -603,7 +603,7 @@ extern "C" hq_status hq_conv2d_direct(const void* x, hq_dtype xdt, const float* 
         if (!aligned16(y)) return HQ_ERR_ALIGNMENT;
         if (same3x3 && (C == 3 || C == 4) && (Cout <= 256 || Cout % 256 == 0)) {
 #define HQ_CIN_CASE(T, N)                                                                                           \
-            HQ_CUDA_OK(cudaFuncSetAttribute(conv3x3_small_cin_kernel<T, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem))); \
+            HQ_CUDA_OK(allow_shared(conv3x3_small_cin_kernel<T, N>)); \
             conv3x3_small_cin_kernel<T, N><<<grid8, 256, smem, st>>>(static_cast<const T*>(x), w, bias,              \
                 static_cast<__nv_bfloat16*>(y), int(Nb), int(H), int(W), int(Cout));
             if (xdt == HQ_F32) { if (C == 3) { HQ_CIN_CASE(float, 3) } else { HQ_CIN_CASE(float, 4) } }
@@ -612,11 +612,11 @@ extern "C" hq_status hq_conv2d_direct(const void* x, hq_dtype xdt, const float* 
             return cudaGetLastError() == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
         }
         if (xdt == HQ_F32) {
-            HQ_CUDA_OK(cudaFuncSetAttribute(conv_small_cin_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+            HQ_CUDA_OK(allow_shared(conv_small_cin_kernel<float>));
             conv_small_cin_kernel<float><<<grid, 256, smem, st>>>(static_cast<const float*>(x), w, bias,
                 static_cast<__nv_bfloat16*>(y), int(Nb), int(H), int(W), int(C), int(Cout), R, stride, pad, int(Ho), int(Wo));
         } else {
-            HQ_CUDA_OK(cudaFuncSetAttribute(conv_small_cin_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+            HQ_CUDA_OK(allow_shared(conv_small_cin_kernel<__nv_bfloat16>));
             conv_small_cin_kernel<__nv_bfloat16><<<grid, 256, smem, st>>>(static_cast<const __nv_bfloat16*>(x), w, bias,
                 static_cast<__nv_bfloat16*>(y), int(Nb), int(H), int(W), int(C), int(Cout), R, stride, pad, int(Ho), int(Wo));
         }
@@ -627,7 +627,7 @@ extern "C" hq_status hq_conv2d_direct(const void* x, hq_dtype xdt, const float* 
         if (same3x3 && (C <= 256 || C % 256 == 0)) {
 #define HQ_COUT3_CASE(N)                                                                                            \
             case N:                                                                                                 \
-                HQ_CUDA_OK(cudaFuncSetAttribute(conv3x3_small_cout_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem))); \
+                HQ_CUDA_OK(allow_shared(conv3x3_small_cout_kernel<N>)); \
                 conv3x3_small_cout_kernel<N><<<grid, 256, smem, st>>>(static_cast<const __nv_bfloat16*>(x), w, bias, \
                     static_cast<float*>(y), int(Nb), int(H), int(W), int(C));                                       \
                 break;
@@ -640,7 +640,7 @@ extern "C" hq_status hq_conv2d_direct(const void* x, hq_dtype xdt, const float* 
         }
 #define HQ_COUT_CASE(N)                                                                                             \
         case N:                                                                                                     \
-            HQ_CUDA_OK(cudaFuncSetAttribute(conv_small_cout_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem))); \
+            HQ_CUDA_OK(allow_shared(conv_small_cout_kernel<N>)); \
             conv_small_cout_kernel<N><<<grid, 256, smem, st>>>(static_cast<const __nv_bfloat16*>(x), w, bias,       \
                 static_cast<float*>(y), int(Nb), int(H), int(W), int(C), R, stride, pad, int(Ho), int(Wo));         \
             break;
