@@ -986,7 +986,7 @@ cudaError_t launch_fast(const QuantParams& p, bool int8_out, int grid, int threa
     const bool stat = p.static_scale != nullptr;
     auto go = [&](auto kern) -> cudaError_t {
         if (smem > 48 * 1024) {
-            cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+            cudaError_t e = allow_shared(kern);
             if (e != cudaSuccess) return e;
         }
         // with statistics a dependent of the statistics kernel: its rows are on their way before it waits for them (1-2 us)
@@ -1169,13 +1169,11 @@ static hq_status launch_quant_impl(const void* x, hq_dtype xdt, int64_t rows, in
     cudaError_t e;
     if (xdt == HQ_F32) {
         if (smem > 48 * 1024)
-            HQ_CUDA_OK(cudaFuncSetAttribute(fwht_quant_generic<float>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                            int(smem)));
+            HQ_CUDA_OK(allow_shared(fwht_quant_generic<float>));
         fwht_quant_generic<float><<<grid, 256, smem, st>>>(p, n, cont == HQ_CODES_INT8);
     } else {
         if (smem > 48 * 1024)
-            HQ_CUDA_OK(cudaFuncSetAttribute(fwht_quant_generic<__nv_bfloat16>,
-                                            cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+            HQ_CUDA_OK(allow_shared(fwht_quant_generic<__nv_bfloat16>));
         fwht_quant_generic<__nv_bfloat16><<<grid, 256, smem, st>>>(p, n, cont == HQ_CODES_INT8);
     }
     e = cudaGetLastError();

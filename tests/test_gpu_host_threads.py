@@ -39,3 +39,15 @@ def test_direct_convolution(hq, shapes, xt, yt, R, pad):
         w, y = torch.randn((Cout, R, R, C), generator=gen, device="cuda"), torch.empty((1, 6, 6, Cout), dtype=yt, device="cuda")
         made.append((lambda stream, x=x, w=w, y=y: hq.hq_conv2d_direct(x, w, None, R, 1, pad, y, stream=stream), (y,)))
     check(made)
+
+
+@pytest.mark.parametrize("had_block,widths", [(4096, (16384, 12288, 4096)), (2048, (16384, 14336, 2048)), (32, (16384, 24576, 49152))])
+@pytest.mark.parametrize("xt", [F, BF])
+def test_quantization(hq, had_block, widths, xt):
+    made = []
+    for cols in widths:
+        gen = torch.Generator(device="cuda").manual_seed(cols)
+        x = torch.randn((20, cols), generator=gen, device="cuda").to(xt)
+        codes, scales = torch.empty((20, cols), dtype=torch.uint8, device="cuda"), torch.empty((20,), device="cuda")
+        made.append((lambda stream, a=(x, had_block, 4, codes, hq.HQ_CODES_INT8, scales): hq.hq_hadamard_quant(*a, stream=stream), (codes, scales)))
+    check(made)
