@@ -218,7 +218,7 @@ cudaError_t launch_small(const SmallParams& p, int limbs, cudaStream_t st) {
     const dim3 grid(unsigned((p.N + kSmCols - 1) / kSmCols), unsigned((p.M + kSmRows - 1) / kSmRows));
     auto go = [&](auto kern) -> cudaError_t {
         if (smem > 48 * 1024) {
-            const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+            const cudaError_t e = allow_shared(kern);
             if (e != cudaSuccess) return e;
         }
         return launch_dependent(kern, grid, unsigned(kSmRows * p.K / 32), smem, st, true, p);

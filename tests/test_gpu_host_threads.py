@@ -3,6 +3,7 @@ memory that it asked for, and each has the results of the call alone."""
 import pytest
 import torch
 
+from paper_2512_05746_b200 import inputs
 from test_gpu_train_block_calls import side_by_side
 
 pytestmark = pytest.mark.gpu
@@ -50,4 +51,16 @@ def test_quantization(hq, had_block, widths, xt):
         x = torch.randn((20, cols), generator=gen, device="cuda").to(xt)
         codes, scales = torch.empty((20, cols), dtype=torch.uint8, device="cuda"), torch.empty((20,), device="cuda")
         made.append((lambda stream, a=(x, had_block, 4, codes, hq.HQ_CODES_INT8, scales): hq.hq_hadamard_quant(*a, stream=stream), (codes, scales)))
+    check(made)
+
+
+@pytest.mark.parametrize("mode,xt", [("folded", F), ("double", BF)])
+def test_small_linear(hq, mode, xt):
+    made = []
+    for K in (1024, 768, 512):
+        gen = torch.Generator(device="cuda").manual_seed(K)
+        x = torch.randn((16, K), generator=gen, device="cuda").to(xt)
+        pw = hq.hq_weight_prepare(inputs.weights((64, K), seed=K), 4, 256, hq.WEIGHT_MODES[mode], hq.HQ_CODES_INT8).to_device()
+        y, ws = torch.empty((16, 64), dtype=BF, device="cuda"), torch.empty((hq.hq_layer_workspace_size(pw, 4, 16),), dtype=torch.uint8, device="cuda")
+        made.append((lambda stream, a=(x, pw, None, 4, y, ws): hq.hq_qlinear(*a, stream=stream), (y,)))
     check(made)
