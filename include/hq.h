@@ -422,8 +422,8 @@ hq_status hq_qk_norm_rope_bwd(const void* q, int64_t ldq, const void* k, int64_t
  *   of two roundings.
  *   Every sum runs in a fixed order: the same inputs give the same bits.  Rows behind the lengths, and of queries that see no key: zeros.
  *   dq, dk, dv  device bf16, laid out as q, k, v with pitches of their own.
- *   workspace  hq_attention_bwd_workspace_size bytes (asked with the device current that the call runs on: its number of SMs counts),
- *              16-byte aligned; it need not be cleared, and calls that may overlap on the GPU
+ *   workspace  hq_attention_bwd_workspace_size bytes (asked with the device current that the call runs on: its number of SMs counts;
+ *              a smaller shape may need more: one for several takes the most of them), 16-byte aligned; it need not be cleared, and calls that may overlap on the GPU
  *              (other streams, captured graphs that run side by side) need one each. */
 hq_status hq_attention_fwd_workspace_size(int64_t Nb, int64_t Lq, int64_t Lk, int heads, int kv_heads, int dh, size_t* bytes);
 hq_status hq_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int64_t Nb, int64_t Lq,

@@ -176,9 +176,12 @@ extern "C" hq_status hq_gate_norm(const void* x, int64_t ldx, hq_dtype xdt, cons
     const int planes = kRows * ((xdt == HQ_BF16 ? 1 : 2) + (hdt == HQ_BF16 ? 1 : 2)), side = 32 / row_lanes(cols);
     const int64_t fit = int64_t(kMostShared / (size_t(planes) * kForwardStages * p.warps * 32 * 16)), by_warps = 20 / p.warps;
     const int64_t most = int64_t(sm_count()) * (fit < by_warps ? fit : by_warps);
-    // runs of a dozen rows, in up to four turns of all teams: what is under way lies closer together than in one turn of long runs (65536 rows
-    // of 1152 bf16 120 -> 106 us, of 512 fp32 / bf16 with a second norm 95 -> 86); one where two norms with means bound a run by its
-    // instructions, and each run's start is felt (29491 x 1280: one turn 69 us, two 72, four 78)
+    // runs of a dozen rows, in up to four turns of all teams: what is under way lies closer together than in one turn of long runs (one, two and
+    // four turns, LayerNorm in front alone: 65536 rows of 1152 bf16 115, 107 and 111 us, 131072 of 256 57, 52 and 49, 300000 of 128 fp32 109, 106
+    // and 97; RMS on both sides, 65536 of 512 fp32 97, 90 and 89).  One turn where both norms take means: a run is bound by its instructions, and
+    // each run's start is felt (29491 x 1280 bf16 64, 68 and 74, 16384 x 2304 72, 73 and 76; not narrow rows: 300000 x 128 68, 62 and 63).
+    // The rule is a coarse one: a LayerNorm beside an RMS norm in bf16 would be better off with one turn from 512 columns on, too (29491 x 1280
+    // 60, 64 and 68; 65536 x 512 54, 59 and 59).
     const int64_t one = (rows + most - 1) / most, turns = one / (12 * side), limit = norm == HQ_NORM_LAYER && post == HQ_NORM_LAYER ? 1 : 4;
     const int64_t teams = most * (turns < 1 ? 1 : turns > limit ? limit : turns), chunk = (rows + teams - 1) / teams;
     p.chunk = uint32_t(chunk < kRows * side ? kRows * side : chunk);
