@@ -3,7 +3,7 @@
 // One pass over x', h and the gradients of both outputs, 12 bytes an element of bf16; sums over rows in registers, a part for each team that
 // took rows of a group, joined by a second kernel in a fixed order.
 //
-// 65536 x 1152 bf16 154 to 161 us a call (5.7 to 5.9 TB/s, 88 to 92 % of the copy rate), 8192 x 1152 28 (62 %: 24 here at 15 warps an SM and 55 % of the issue slots, the
+// 65536 x 1152 bf16 152 to 165 us a call (5.5 to 6.0 TB/s, 86 to 93 % of the copy rate), 8192 x 1152 28 (62 %: 24 here at 15 warps an SM and 55 % of the issue slots, the
 // rest the join of 14 parts a group).
 #include "hq_gate_norm.cuh"
 
