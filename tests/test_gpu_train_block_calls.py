@@ -1,7 +1,6 @@
-"""Calls of the operators around a transformer block's linears that their documentation allows and that come seldom: lengths of any value, host
-threads beside one another, workspaces of a larger batch, labels outside
-their table, gradients without elements, lists of gradients that were
-let go, very many groups."""
+"""Calls of the operators around a transformer block's linears that their documentation allows and that are seldom made: lengths of any value,
+host threads beside one another, workspaces of a larger batch, labels outside their table, gradients without elements, lists of gradients
+that were let go, very many groups."""
 import threading
 import warnings
 

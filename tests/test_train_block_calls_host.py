@@ -1,6 +1,5 @@
-"""What the calls around a transformer block's linears promise of their arguments, where no GPU is needed: workspaces of a larger batch,
-outputs in place, gradients without elements,
-clipping without a norm."""
+"""What the calls around a transformer block's linears promise of their arguments, where no GPU is needed: workspaces of a larger batch, outputs
+in place, gradients without elements, clipping without a norm."""
 import pytest
 import torch
 
